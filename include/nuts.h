@@ -32,6 +32,12 @@ enum { NUTS_OK = 0, NUTS_E_INVALID_ARG = -1, NUTS_E_ALLOC = -2, NUTS_E_DEVICE = 
  * log-weights and U-turn dot products are binary64 in both cases. */
 enum { NUTS_F32 = 0, NUTS_F64 = 1 };
 
+/* The categorical operators (last section) take NUTS_F32 and these two: bfloat16, binary16. */
+enum { NUTS_BF16 = 2, NUTS_F16 = 3 };
+
+/* Type of an array of classes. */
+enum { NUTS_I32 = 0, NUTS_I64 = 1 };
+
 /* Target families (the paper's two test problems, Section 4, plus the two
  * element-wise Gaussians of the benchmark configurations). */
 enum {
@@ -242,6 +248,114 @@ typedef struct {
 } nuts_tile_layout;
 int nuts_tile_pack(const double* X, const double* y, int64_t n, int64_t d, nuts_tile_layout* layout, double* operands,
                    int64_t capacity);
+
+/* ---- Categorical models -------------------------------------------------------------------------------------------
+ *
+ * The logistic regression above has two classes, y in {0, 1}.  These operators are its parts for observations of one of
+ * many classes (a word of a vocabulary, a group, a choice), for programs that put a log density of such a model and its
+ * gradient together, or ask a fitted one for its answers: rows of a table by class and the gradient of that, the
+ * log-probabilities of given classes, and their gradient.
+ *
+ * All pointers but the descriptors are DEVICE pointers.  The calls are enqueued on the stream of nuts_set_stream and
+ * return; nothing is allocated, copied or kept, so they can be captured into a graph.  Sums, maxima and statistics are
+ * binary32 whatever the element type, and each output is rounded once (the one exception is named at nuts_score_grad).  The order of
+ * every sum is fixed by the descriptor and the classes: a call repeated gives the same bits.  Strides are in elements; rows
+ * may begin at any address that suits an element, and outputs must not overlap inputs unless that is said.  A class
+ * outside [0, n_classes) is no error: such a row has no class (a pad, an observation that does not count).
+ * A workspace of the size that the *_workspace functions say may hold anything; it is the caller's again when the call's work
+ * is done.  Alignment: workspaces 256 bytes.  Sizes of zero are allowed (n_ids, n_rows): nothing is read then. */
+
+#define NUTS_CAT_MAX_TOP 64
+
+typedef struct {
+    int32_t dtype;        /* NUTS_F32, NUTS_BF16 or NUTS_F16: table, its gradient, rows                    */
+    int32_t id_type;      /* NUTS_I32 or NUTS_I64                                                          */
+    int64_t n_ids;        /* 0 .. 2^31 - 2                                                                 */
+    int64_t n_classes;    /* rows of the table, 1 .. 2^31 - 2                                              */
+    int64_t dim;          /* numbers in a row, 1 .. 2^24                                                   */
+    int64_t table_stride; /* from one row of the table (or of its gradient) to the next, >= dim            */
+    int64_t row_stride;   /* the same of the n_ids rows                                                    */
+    double scale;         /* finite                                                                        */
+    int32_t accumulate;   /* nuts_lookup_grad: 0 writes all of the gradient, 1 adds to what is there       */
+    int32_t reserved;
+} nuts_lookup_desc;
+
+/* rows[i, :] = scale * table[ids[i], :]; zeros where ids[i] is no class. */
+int nuts_lookup(const nuts_lookup_desc* desc, const void* table, const void* ids, void* rows);
+
+/* grad_table[v, :] = scale * sum of grad_rows[i, :] over the i with ids[i] = v, zeros for a class that does not come
+ * (accumulate: such rows are not touched, the others' sums are added to them and rounded once). */
+int nuts_lookup_grad_workspace(const nuts_lookup_desc* desc, int64_t* bytes);
+int nuts_lookup_grad(const nuts_lookup_desc* desc, const void* grad_rows, const void* ids, void* grad_table,
+                     void* workspace, int64_t workspace_bytes);
+
+typedef struct {
+    int32_t dtype;          /* of the logits and their gradient                                            */
+    int32_t id_type;        /* of the targets                                                              */
+    int64_t n_rows;         /* 0 .. 2^31 - 2                                                               */
+    int64_t n_classes;      /* 1 .. 2^31 - 2^16 - 1                                                        */
+    int64_t row_stride;     /* of the logits, >= n_classes                                                 */
+    int64_t allowed_stride; /* 32-bit words from one row of `allowed` to the next; 0: one row for all      */
+    double scale;           /* z = scale * logits; finite, > 0 (a temperature is 1 / scale)                */
+    int32_t n_top;          /* alternatives, 0 .. NUTS_CAT_MAX_TOP                                         */
+    int32_t reserved;
+} nuts_logits_desc;
+
+/* For each row of z = scale * logits:
+ *   lse = log sum_v e^(z_v);   logprob = z_target - lse, 0 if the row has no target (or `targets` is NULL);
+ *   entropy = lse - sum_v p_v z_v, p = e^(z - lse);
+ *   top_ids / top_logprobs [n_rows][n_top]: the n_top largest z in falling order, of equal ones the lower class first.
+ * `allowed` (or NULL): class v may come if bit v % 32 of word v / 32 of the row is set; the others count as z = -infinity whatever
+ * is there (NaN, too), and are no alternatives.  Where fewer classes than n_top may come, the rest is -1 and -infinity.
+ * A row in which every z is -infinity has lse = -infinity, logprob = -infinity, entropy 0 and alternatives of
+ * logprob -infinity.  A row with a NaN or +infinity that may come has NaN for all but its top_ids; NaN ranks above
+ * everything.  Any output may be NULL. */
+int nuts_logprobs_workspace(const nuts_logits_desc* desc, int64_t* bytes);
+int nuts_logprobs(const nuts_logits_desc* desc, const void* logits, const void* targets, const uint32_t* allowed,
+                  float* logprob, float* lse, float* entropy, int32_t* top_ids, float* top_logprobs,
+                  void* workspace, int64_t workspace_bytes);
+
+/* Gradient with respect to the logits of sum_rows grad_logprob * logprob + grad_lse * lse + grad_entropy * entropy (each
+ * [n_rows] or NULL), from the forward pass's lse and entropy (entropy only with grad_entropy):
+ *   scale * (grad_logprob ([v = target] - p_v) + grad_lse p_v - grad_entropy p_v (log p_v + entropy)),
+ * where a row without a target has no grad_logprob; 0 for classes that may not come, and where p_v is 0 but for the target.
+ * A row in which every z is -infinity has gradient 0.  Rows of grad_logits are grad_stride apart. */
+int nuts_logprobs_grad(const nuts_logits_desc* desc, const void* logits, const void* targets, const uint32_t* allowed,
+                       const float* lse, const float* entropy, const float* grad_logprob, const float* grad_lse,
+                       const float* grad_entropy, void* grad_logits, int64_t grad_stride);
+
+typedef struct {
+    int32_t dtype;         /* NUTS_F32 or NUTS_BF16: x, weight and their gradients                         */
+    int32_t id_type;       /* of the targets                                                               */
+    int64_t n_rows;        /* 0 .. 2^24                                                                    */
+    int64_t n_classes;     /* 1 .. 2^24                                                                    */
+    int64_t dim;           /* 1 .. 2^20                                                                    */
+    int64_t x_stride;      /* from row to row, >= dim; and so on                                           */
+    int64_t weight_stride;
+    int64_t logits_stride; /* >= n_classes                                                                 */
+    int64_t grad_x_stride, grad_weight_stride;
+    double scale;          /* z = scale * x weight'; finite, > 0                                           */
+} nuts_score_desc;
+
+/* nuts_logprobs of z = scale * x weight' [n_rows][n_classes], from the features x [n_rows][dim] and the classes' weights
+ * [n_classes][dim]: the products are made tile by tile and reduced where they are made.  `logits`, if not NULL, receives z
+ * itself in binary32 (for nuts_score_grad, or for nuts_logprobs with scale 1 to name alternatives).  Any output may
+ * be NULL.  x and weight begin at multiples of 16 bytes (here and in nuts_score_grad); rows whose stride or length is none are
+ * copied to the workspace first. */
+int nuts_score_workspace(const nuts_score_desc* desc, int64_t* bytes);
+int nuts_score(const nuts_score_desc* desc, const void* x, const void* weight, const void* targets, float* logprob,
+               float* lse, float* entropy, float* logits, void* workspace, int64_t workspace_bytes);
+
+/* Gradients of sum_rows grad_logprob * logprob + grad_lse * lse + grad_entropy * entropy:
+ *   grad_x = dz weight, grad_weight = dz' x, dz as in nuts_logprobs_grad.
+ * `logits`: what nuts_score stored, or NULL, when z is computed again.  Either gradient may be NULL.  With bfloat16 features dz is
+ * rounded to bfloat16, for the matrix instructions multiply nothing wider; the products' sums are binary32.  The
+ * workspace's size is that for the larger of both ways. */
+int nuts_score_grad_workspace(const nuts_score_desc* desc, int64_t* bytes);
+int nuts_score_grad(const nuts_score_desc* desc, const void* x, const void* weight, const void* targets,
+                    const float* logits, const float* lse, const float* entropy, const float* grad_logprob,
+                    const float* grad_lse, const float* grad_entropy, void* grad_x, void* grad_weight, void* workspace,
+                    int64_t workspace_bytes);
 
 #ifdef __cplusplus
 }

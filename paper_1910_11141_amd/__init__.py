@@ -11,4 +11,5 @@ def __getattr__(name):
     if name.startswith("__"):
         raise AttributeError(name)
     binding = importlib.import_module(__name__ + ".binding")
-    return getattr(binding, name)
+    categorical = importlib.import_module(__name__ + ".categorical")
+    return getattr(categorical if name in categorical.__all__ else binding, name)

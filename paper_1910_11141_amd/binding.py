@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 
 import numpy as np
 
@@ -16,6 +17,9 @@ LIB_PATH = os.path.join(_HERE, "libnuts_hip.so")
 
 NUTS_OK, NUTS_E_INVALID_ARG, NUTS_E_ALLOC, NUTS_E_DEVICE, NUTS_E_UNSUPPORTED = 0, -1, -2, -3, -4
 NUTS_F32, NUTS_F64 = 0, 1
+NUTS_BF16, NUTS_F16 = 2, 3
+NUTS_I32, NUTS_I64 = 0, 1
+NUTS_CAT_MAX_TOP = 64
 NUTS_TARGET_STD_NORMAL, NUTS_TARGET_GAUSS_DENSE_PRECISION, NUTS_TARGET_GAUSS_DIAG, NUTS_TARGET_LOGISTIC_REGRESSION = 0, 1, 2, 3
 NUTS_VARIANT_AUTO, NUTS_VARIANT_WAVE, NUTS_VARIANT_TILE, NUTS_VARIANT_ELEM, NUTS_VARIANT_GRID = 0, 1, 2, 3, 4
 NUTS_VARIANT_DENSE, NUTS_VARIANT_QUAD = 5, 6
@@ -23,7 +27,10 @@ NUTS_SCHEDULE_FREE, NUTS_SCHEDULE_TRAJECTORY = 0, 1
 NUTS_SAMPLER_MULTINOMIAL, NUTS_SAMPLER_SLICE = 0, 1
 
 EXPORTS = ("nuts_create_target", "nuts_destroy_target", "nuts_sample", "nuts_sample_ex", "nuts_get_stats",
-           "nuts_sample_static", "nuts_set_stream", "nuts_tile_pack", "nuts_last_error")
+           "nuts_sample_static", "nuts_set_stream", "nuts_tile_pack",
+           "nuts_lookup", "nuts_lookup_grad", "nuts_lookup_grad_workspace", "nuts_logprobs", "nuts_logprobs_workspace",
+           "nuts_logprobs_grad", "nuts_score", "nuts_score_workspace", "nuts_score_grad", "nuts_score_grad_workspace",
+           "nuts_last_error")
 NUTS_STATIC_SCRATCH_BYTES = 64 << 20
 
 
@@ -42,6 +49,24 @@ class nuts_stats(C.Structure):
 class nuts_sample_options(C.Structure):
     _fields_ = [("init_states", C.c_void_p), ("first_chain", C.c_int64), ("variant", C.c_int32),
                 ("leaf_steps", C.c_int32), ("schedule", C.c_int32), ("sampler", C.c_int32)]
+
+
+class nuts_lookup_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("id_type", C.c_int32), ("n_ids", C.c_int64), ("n_classes", C.c_int64), ("dim", C.c_int64),
+                ("table_stride", C.c_int64), ("row_stride", C.c_int64), ("scale", C.c_double), ("accumulate", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class nuts_logits_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("id_type", C.c_int32), ("n_rows", C.c_int64), ("n_classes", C.c_int64),
+                ("row_stride", C.c_int64), ("allowed_stride", C.c_int64), ("scale", C.c_double), ("n_top", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class nuts_score_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("id_type", C.c_int32), ("n_rows", C.c_int64), ("n_classes", C.c_int64), ("dim", C.c_int64),
+                ("x_stride", C.c_int64), ("weight_stride", C.c_int64), ("logits_stride", C.c_int64),
+                ("grad_x_stride", C.c_int64), ("grad_weight_stride", C.c_int64), ("scale", C.c_double)]
 
 
 class NutsError(RuntimeError):
@@ -72,6 +97,18 @@ def lib() -> C.CDLL:
         L.nuts_sample_static.argtypes = L.nuts_sample_ex.argtypes
         L.nuts_get_stats.argtypes = [C.c_void_p, C.POINTER(nuts_stats)]
         L.nuts_set_stream.argtypes = [C.c_void_p]
+        ptr, size, bytes_out = C.c_void_p, C.c_int64, C.POINTER(C.c_int64)
+        lookup, logits, score = C.POINTER(nuts_lookup_desc), C.POINTER(nuts_logits_desc), C.POINTER(nuts_score_desc)
+        L.nuts_lookup.argtypes = [lookup, ptr, ptr, ptr]
+        L.nuts_lookup_grad.argtypes = [lookup, ptr, ptr, ptr, ptr, size]
+        L.nuts_lookup_grad_workspace.argtypes = [lookup, bytes_out]
+        L.nuts_logprobs.argtypes = [logits] + [ptr] * 9 + [size]
+        L.nuts_logprobs_workspace.argtypes = [logits, bytes_out]
+        L.nuts_logprobs_grad.argtypes = [logits] + [ptr] * 9 + [size]
+        L.nuts_score.argtypes = [score] + [ptr] * 8 + [size]
+        L.nuts_score_workspace.argtypes = [score, bytes_out]
+        L.nuts_score_grad.argtypes = [score] + [ptr] * 12 + [size]
+        L.nuts_score_grad_workspace.argtypes = [score, bytes_out]
         L.nuts_last_error.argtypes = []
         L.nuts_last_error.restype = C.c_char_p
         for name in EXPORTS[:-1]:
@@ -160,10 +197,14 @@ class Target:
             pass
 
 
+_thread = threading.local()  # .stream: what nuts_set_stream was given on this thread
+
+
 def nuts_set_stream(stream) -> None:
     """`stream`: a torch.cuda.Stream, a raw hipStream_t integer, or None for the null stream."""
     raw = 0 if stream is None else int(getattr(stream, "cuda_stream", stream))
     _check(lib().nuts_set_stream(C.c_void_p(raw)))
+    _thread.stream = raw
 
 
 def nuts_sample(target: Target, n_chains: int, n_iters: int, step_size: float, max_tree_depth: int, seed: int, *,

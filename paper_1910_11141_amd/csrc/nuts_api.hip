@@ -20,6 +20,7 @@
 #include "nuts_dev.h"
 #include "nuts_band.h"
 #include "nuts_block.h"
+#include "nuts_cat.h"
 #include "nuts_chip.h"
 #include "nuts_dense.h"
 #include "nuts_elem.h"
@@ -1236,6 +1237,30 @@ int launch_chip(nuts_target* t, nuts::DevSample sa)
 }
 
 }  // namespace
+
+// What the categorical operators (nuts_cat.h) share with the sampler's entry points.
+namespace nuts {
+
+int api_fail(int code, const char* fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+hipStream_t api_stream() { return g_stream; }
+
+int api_have_device()
+{
+    int count = 0;
+    if (hipGetDeviceCount(&count) != hipSuccess || count < 1)
+        return fail(NUTS_E_DEVICE, "no HIP device available (this library has no CPU path)");
+    return NUTS_OK;
+}
+
+}  // namespace nuts
 
 extern "C" {
 

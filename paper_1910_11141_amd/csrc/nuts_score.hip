@@ -1,0 +1,558 @@
+// Log-probabilities of given classes from features and class weights, and the gradients of both.
+//
+//   z = s X W',  statistics of its rows as in nuts_softmax.h;   dX = dZ W,  dW = dZ' X,  dZ = s (g_lp ([v = y] - p) + ...)
+//
+// The work is matrix products (2 n V D operations forward, 4 n V D backward), which run on the matrix instructions
+// (nuts_product.h).  Forward, a workgroup reduces its tile of z to each row's maximum, sum and weighted sum in
+// registers and only those are stored; backward, dZ is made from binary32 z (kept, or computed again) and stored along both of its
+// axes, so that all three products have their contraction along rows.  A large batch goes in pieces that bound
+// the workspace: of rows forward, of classes backward.
+#include "nuts_product.h"
+
+#include <algorithm>
+
+namespace nuts {
+namespace {
+
+constexpr int kThreads = 256;
+
+// ---- small kernels --------------------------------------------------------------------------------------------------
+
+// Rows at any place copied to rows of `to_stride` elements, zeros behind their end.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void pack_rows_kernel(const T* from, long stride, long rows, int columns, T* to, long to_stride)
+{
+    for (long row = blockIdx.x; row < rows; row += gridDim.x)
+        for (int i = threadIdx.x; i < to_stride; i += kThreads) to[row * to_stride + i] = i < columns ? from[row * stride + i] : static_cast<T>(0.f);
+}
+
+constexpr int kSquare = 64;
+
+// to[column][row] = from[row][column]: squares through LDS, zeros for rows behind the last up to to_stride.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void transpose_kernel(const T* from, long stride, int rows, int columns, T* to, long to_stride)
+{
+    __shared__ T square[kSquare][kSquare + 4 / sizeof(T)];  // (a word more: columns are in different banks)
+    const int row0 = blockIdx.x * kSquare, column0 = blockIdx.y * kSquare;
+    const int x = threadIdx.x % 64, y = threadIdx.x / 64;
+    for (int i = y; i < kSquare; i += kThreads / 64) {
+        const int row = row0 + i, column = column0 + x;
+        square[i][x] = row < rows && column < columns ? from[(long)row * stride + column] : static_cast<T>(0.f);
+    }
+    __syncthreads();
+    for (int i = y; i < kSquare; i += kThreads / 64)
+        if (column0 + i < columns && row0 + x < to_stride) to[(long)(column0 + i) * to_stride + row0 + x] = square[x][i];
+}
+
+struct GradArgs {
+    const float* z;  // of the classes [first, first + classes)
+    const void* targets;
+    const float* lse;
+    const float* entropy;
+    const float* grad_logprob;
+    const float* grad_lse;
+    const float* grad_entropy;
+    void* dz;    // [rows][dz_stride] or NULL
+    void* dz_t;  // [classes][dz_t_stride] or NULL
+    long z_stride, dz_stride, dz_t_stride;
+    int n_rows, first, classes, n_classes, id_type;
+    float scale;
+};
+
+// dZ and its transpose, a square at a time; zeros beyond the matrix up to the strides.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void dz_kernel(GradArgs a)
+{
+    __shared__ T square[kSquare][kSquare + 4 / sizeof(T)];
+    const int row0 = blockIdx.x * kSquare, column0 = blockIdx.y * kSquare;
+    const int x = threadIdx.x % 64, y = threadIdx.x / 64;
+    T* dz = static_cast<T*>(a.dz);
+    T* dz_t = static_cast<T*>(a.dz_t);
+    for (int i = y; i < kSquare; i += kThreads / 64) {
+        const int row = row0 + i, column = column0 + x;
+        float g = 0.f;
+        if (row < a.n_rows && column < a.classes) {
+            const int target = a.targets ? class_at(a.targets, a.id_type, row, a.n_classes) : -1;
+            const float lse = a.lse[row], g_lp = a.grad_logprob && target >= 0 ? a.grad_logprob[row] : 0.f;
+            const float log_p = a.z[(long)row * a.z_stride + column] - lse, p = __builtin_amdgcn_exp2f(log_p * kLog2e);
+            g = (a.grad_lse ? a.grad_lse[row] : 0.f) - g_lp;
+            if (a.grad_entropy) g = __builtin_fmaf(-a.grad_entropy[row], fmaxf(log_p, kNothing) + a.entropy[row], g);
+            g *= p;
+            if (a.first + column == target) g += g_lp;
+            g = lse == -INFINITY ? 0.f : g * a.scale;
+        }
+        const T value = rounded<T>(g);
+        if (dz && row < a.n_rows && column < a.dz_stride) dz[(long)row * a.dz_stride + column] = value;
+        square[i][x] = value;
+    }
+    if (!dz_t) return;
+    __syncthreads();
+    for (int i = y; i < kSquare; i += kThreads / 64)
+        if (column0 + i < a.classes && row0 + x < a.dz_t_stride) dz_t[(long)(column0 + i) * a.dz_t_stride + row0 + x] = square[x][i];
+}
+
+// out[row][column] = scale * sum over the divisions of a contraction, in order.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void add_up_kernel(const float* sums, int splits, long rows, int columns, float scale, T* out, long stride)
+{
+    const long all = rows * columns;
+    for (long i = (long)blockIdx.x * kThreads + threadIdx.x; i < all; i += (long)gridDim.x * kThreads) {
+        float sum = sums[i];
+        for (int s = 1; s < splits; ++s) sum += sums[s * all + i];
+        out[i / columns * stride + i % columns] = rounded<T>(sum * scale);
+    }
+}
+
+struct JoinArgs {
+    const float4* stats;
+    const float* target_logit;
+    const void* targets;
+    float* logprob;
+    float* lse;
+    float* entropy;
+    long first_row, n_rows;  // of this piece of the batch
+    int parts, n_classes, id_type;
+};
+
+// A wave a row: the statistics of its tiles joined.
+__global__ __launch_bounds__(kThreads) void join_scores_kernel(JoinArgs a)
+{
+    const long row = (long)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+    const int lane = threadIdx.x % 64;
+    if (row >= a.n_rows) return;
+    Stats v{-INFINITY, 0.f, 0.f};
+    for (int p = lane; p < a.parts; p += 64) {
+        const float4 s = a.stats[row * a.parts + p];
+        v = join(v, Stats{s.x, s.y, s.z}, kLog2e);
+    }
+#pragma unroll
+    for (int step = 32; step >= 1; step /= 2) v = join(v, Stats{__shfl_xor(v.m, step), __shfl_xor(v.s, step), __shfl_xor(v.t, step)}, kLog2e);
+    if (lane != 0) return;
+    const Row r = finish(v, 1.f);
+    const long at = a.first_row + row;
+    if (a.lse) a.lse[at] = r.lse;
+    if (a.entropy) a.entropy[at] = r.entropy;
+    if (a.logprob) a.logprob[at] = a.targets && class_at(a.targets, a.id_type, at, a.n_classes) >= 0 ? logprob_of(r, a.target_logit[row], 1.f) : 0.f;
+}
+
+// ---- which tiles ------------------------------------------------------------------------------------------------------
+
+enum Tiles { kLarge, kMiddle, kSmall };
+struct TileShape {
+    int m, n, parts_n;     // parts_n: waves along the columns
+    int per_cu;            // workgroups that a compute unit holds
+    float step;            // time of a step when so many run, relative to the others'
+};
+constexpr TileShape kShapes[] = {{256, 256, 2, 1, 2.1f}, {128, 128, 2, 2, 1.7f}, {32, 64, 2, 3, 0.5f}};
+constexpr int kUnits = 256;        // compute units
+constexpr int kLeastSteps = 8;     // of a division of a contraction
+
+struct Choice {
+    Tiles tiles;
+    int tiles_m, tiles_n, splits, split_steps;
+    int64_t groups() const { return (int64_t)tiles_m * tiles_n * splits; }
+};
+
+int steps_of(int64_t k_bytes) { return (int)ceil_div(k_bytes, kStepBytes); }
+
+// The tiles, and the divisions of the contraction (1, unless it may be divided), that take least time by rounds of
+// workgroups over the chip.
+Choice choose(int64_t m, int64_t n, int64_t k_bytes, bool may_split)
+{
+    Choice best{};
+    float least = INFINITY;
+    const int steps = std::max(1, steps_of(k_bytes));
+    for (int t = kLarge; t <= kSmall; ++t) {
+        const TileShape& s = kShapes[t];
+        Choice c{(Tiles)t, (int)ceil_div(m, s.m), (int)ceil_div(n, s.n), 1, steps};
+        const int64_t tiles = (int64_t)c.tiles_m * c.tiles_n, slots = (int64_t)kUnits * s.per_cu;
+        if (may_split && tiles < slots) {
+            c.splits = (int)std::max<int64_t>(1, std::min<int64_t>(slots / tiles, steps / kLeastSteps));
+            c.split_steps = (int)ceil_div(steps, c.splits);
+            c.splits = (int)ceil_div(steps, c.split_steps);
+        }
+        const float time = (float)ceil_div(c.groups(), slots) * s.step * (c.split_steps + 8);
+        if (time < least) {
+            least = time;
+            best = c;
+        }
+    }
+    return best;
+}
+
+template <ProductKind kKind, typename T>
+void launch_product(const Choice& c, ProductArgs p, hipStream_t stream)
+{
+    p.tiles_m = c.tiles_m;
+    p.tiles_n = c.tiles_n;
+    p.splits = c.splits;
+    p.split_steps = c.split_steps;
+    const dim3 grid((unsigned)c.tiles_m * c.tiles_n, c.splits);
+    switch (c.tiles) {
+    case kLarge: hipLaunchKernelGGL((product_kernel<T, 256, 256, 4, 2, 2, kKind>), grid, dim3(512), 0, stream, p); break;
+    case kMiddle: hipLaunchKernelGGL((product_kernel<T, 128, 128, 2, 2, 2, kKind>), grid, dim3(256), 0, stream, p); break;
+    case kSmall: hipLaunchKernelGGL((product_kernel<T, 32, 64, 2, 2, 4, kKind>), grid, dim3(256), 0, stream, p); break;
+    }
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------------
+
+int check_score(const nuts_score_desc* d, const char* who)
+{
+    if (!d) return api_fail(NUTS_E_INVALID_ARG, "%s: desc must not be NULL", who);
+    if (d->dtype != NUTS_F32 && d->dtype != NUTS_BF16) return api_fail(NUTS_E_INVALID_ARG, "%s: dtype must be NUTS_F32 or NUTS_BF16", who);
+    if (d->id_type != NUTS_I32 && d->id_type != NUTS_I64) return api_fail(NUTS_E_INVALID_ARG, "%s: id_type must be NUTS_I32 or NUTS_I64", who);
+    if (d->n_rows < 0 || d->n_rows > (1 << 20)) return api_fail(NUTS_E_INVALID_ARG, "%s: n_rows must be in [0, 2^20]", who);
+    if (d->n_classes < 1 || d->n_classes > (1 << 24)) return api_fail(NUTS_E_INVALID_ARG, "%s: n_classes must be in [1, 2^24]", who);
+    if (d->dim < 1 || d->dim > (1 << 20)) return api_fail(NUTS_E_INVALID_ARG, "%s: dim must be in [1, 2^20]", who);
+    if (d->x_stride < d->dim || d->weight_stride < d->dim || d->grad_x_stride < d->dim || d->grad_weight_stride < d->dim || d->logits_stride < d->n_classes)
+        return api_fail(NUTS_E_INVALID_ARG, "%s: a stride is smaller than its rows", who);
+    const int64_t most = INT64_MAX / 8 / (1 << 24);
+    if (d->x_stride > most || d->weight_stride > most || d->grad_x_stride > most || d->grad_weight_stride > most || d->logits_stride > most)
+        return api_fail(NUTS_E_INVALID_ARG, "%s: a stride is too large", who);
+    const float scale = (float)d->scale;
+    if (!std::isfinite(scale) || !(scale > 0.f)) return api_fail(NUTS_E_INVALID_ARG, "%s: scale must be finite and > 0", who);
+    return NUTS_OK;
+}
+
+struct Space {
+    size_t bytes = 0;
+    size_t take(size_t n)
+    {
+        const size_t at = bytes;
+        bytes += (n + 255) & ~(size_t)255;
+        return at;
+    }
+};
+
+int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+
+// Whether rows can be read as they lie.
+bool rows_fit(int64_t stride, int64_t dim, size_t size)
+{
+    return stride * size % 16 == 0 && dim * size % 16 == 0 && stride * size <= (size_t)kMostBufferBytes / 256;
+}
+bool aligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+constexpr int64_t kMostStats = (int64_t)1 << 28;     // bytes of statistics of one piece of a batch
+constexpr int64_t kMostPiece = (int64_t)1 << 28;     // logits of one piece of the classes
+constexpr int64_t kSeparateGroups = 128;             // fewer workgroups than this, and the contraction is divided
+
+// Forward.  Where few tiles would have a long contraction each, the products are divided along it and z is stored; nuts_logprobs
+// then goes over it (it is small).
+struct ScorePlan {
+    int64_t dim_pad;  // of packed rows
+    bool separate;
+    Choice choice;
+    int64_t piece;    // rows of x at a time
+    int parts;
+    nuts_logits_desc logits;
+    size_t x, weight, stats, target_logit, sums, z, logprobs;
+    int64_t logprobs_bytes;
+    Space space;
+};
+
+ScorePlan plan_score(const nuts_score_desc* d)
+{
+    ScorePlan p{};
+    const size_t size = cat_size(d->dtype);
+    p.dim_pad = round_up(d->dim, 64);
+    const int64_t k_bytes = d->dim * size;
+    p.choice = choose(d->n_rows, d->n_classes, k_bytes, false);
+    p.separate = p.choice.groups() < kSeparateGroups && steps_of(k_bytes) >= 2 * kLeastSteps;
+    p.x = p.space.take(rows_fit(d->x_stride, d->dim, size) ? 0 : (size_t)d->n_rows * p.dim_pad * size);
+    p.weight = p.space.take(rows_fit(d->weight_stride, d->dim, size) ? 0 : (size_t)d->n_classes * p.dim_pad * size);
+    if (p.separate) {
+        p.choice = choose(d->n_rows, d->n_classes, k_bytes, true);
+        p.piece = d->n_rows;
+        p.logits = nuts_logits_desc{NUTS_F32, d->id_type, d->n_rows, d->n_classes, round_up(d->n_classes, 4), 0, 1.0, 0, 0};
+        p.sums = p.space.take((size_t)p.choice.splits * d->n_rows * d->n_classes * sizeof(float));
+        p.z = p.space.take((size_t)d->n_rows * p.logits.row_stride * sizeof(float));
+        nuts_logits_desc any = p.logits;  // (the caller's own logits may have any stride)
+        nuts_logprobs_workspace(&any, &p.logprobs_bytes);
+        p.logprobs = p.space.take((size_t)p.logprobs_bytes);
+    } else {
+        p.parts = p.choice.tiles_n * kShapes[p.choice.tiles].parts_n;
+        p.piece = std::max<int64_t>(256, kMostStats / ((int64_t)p.parts * sizeof(float4)) / 256 * 256);
+        p.piece = std::min(p.piece, d->n_rows);
+        p.stats = p.space.take((size_t)p.piece * p.parts * sizeof(float4));
+        p.target_logit = p.space.take((size_t)p.piece * sizeof(float));
+    }
+    return p;
+}
+
+template <typename T>
+void pack(const void* from, int64_t stride, int64_t rows, int64_t dim, void* to, int64_t to_stride, hipStream_t stream)
+{
+    hipLaunchKernelGGL(pack_rows_kernel<T>, dim3((unsigned)std::min<int64_t>(rows, 65536)), dim3(kThreads), 0, stream, static_cast<const T*>(from),
+                       (long)stride, (long)rows, (int)dim, static_cast<T*>(to), (long)to_stride);
+}
+
+template <typename T>
+void transpose(const void* from, int64_t stride, int64_t rows, int64_t columns, void* to, int64_t to_stride, hipStream_t stream)
+{
+    hipLaunchKernelGGL(transpose_kernel<T>, dim3((unsigned)ceil_div(to_stride, kSquare), (unsigned)ceil_div(columns, kSquare)), dim3(kThreads), 0, stream,
+                       static_cast<const T*>(from), (long)stride, (int)rows, (int)columns, static_cast<T*>(to), (long)to_stride);
+}
+
+template <typename T>
+void add_up(const float* sums, int splits, int64_t rows, int64_t columns, float scale, void* out, int64_t stride, hipStream_t stream)
+{
+    hipLaunchKernelGGL(add_up_kernel<T>, dim3((unsigned)std::min<int64_t>(ceil_div(rows * columns, kThreads), 16384)), dim3(kThreads), 0, stream, sums,
+                       splits, (long)rows, (int)columns, scale, static_cast<T*>(out), (long)stride);
+}
+
+template <typename T>
+int score(const nuts_score_desc* d, const ScorePlan& p, const void* x, const void* weight, const void* targets, float* logprob, float* lse,
+          float* entropy, float* logits, char* w)
+{
+    hipStream_t stream = api_stream();
+    const size_t size = sizeof(T);
+    int64_t x_stride = d->x_stride, weight_stride = d->weight_stride, dim = d->dim;
+    if (!rows_fit(x_stride, dim, size)) {
+        pack<T>(x, x_stride, d->n_rows, dim, w + p.x, p.dim_pad, stream);
+        x = w + p.x;
+        x_stride = p.dim_pad;
+    }
+    if (!rows_fit(weight_stride, dim, size)) {
+        pack<T>(weight, weight_stride, d->n_classes, dim, w + p.weight, p.dim_pad, stream);
+        weight = w + p.weight;
+        weight_stride = p.dim_pad;
+    }
+    // (packed rows are zero from dim to dim_pad: both then are, or both end where a piece does)
+    const int64_t k_bytes = round_up(dim * size, 16);
+    ProductArgs a{};
+    a.a = static_cast<const char*>(x);
+    a.b = static_cast<const char*>(weight);
+    a.a_stride = (long)(x_stride * size);
+    a.b_stride = (long)(weight_stride * size);
+    a.n = (int)d->n_classes;
+    a.k_bytes = (int)k_bytes;
+    if (p.separate) {
+        a.m = (int)d->n_rows;
+        a.sums = reinterpret_cast<float*>(w + p.sums);
+        launch_product<kSums, T>(p.choice, a, stream);
+        float* z = logits ? logits : reinterpret_cast<float*>(w + p.z);
+        nuts_logits_desc l = p.logits;
+        if (logits) l.row_stride = d->logits_stride;
+        add_up<float>(a.sums, p.choice.splits, d->n_rows, d->n_classes, (float)d->scale, z, l.row_stride, stream);
+        NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
+        return nuts_logprobs(&l, z, targets, nullptr, logprob, lse, entropy, nullptr, nullptr, w + p.logprobs, p.logprobs_bytes);
+    }
+    const bool wanted = logprob || lse || entropy;
+    for (int64_t row = 0; row < d->n_rows; row += p.piece) {
+        const int64_t rows = std::min(p.piece, d->n_rows - row);
+        a.a = static_cast<const char*>(x) + row * a.a_stride;
+        a.m = (int)rows;
+        a.c = logits ? logits + row * d->logits_stride : nullptr;
+        a.c_stride = (long)d->logits_stride;
+        a.scale = (float)d->scale;
+        a.targets = !targets ? nullptr : static_cast<const char*>(targets) + row * (d->id_type == NUTS_I64 ? 8 : 4);
+        a.id_type = d->id_type;
+        a.stats = wanted ? reinterpret_cast<float4*>(w + p.stats) : nullptr;
+        a.target_logit = reinterpret_cast<float*>(w + p.target_logit);
+        Choice c = p.choice;
+        c.tiles_m = (int)ceil_div(rows, kShapes[c.tiles].m);
+        launch_product<kScores, T>(c, a, stream);
+        if (wanted) {
+            const JoinArgs j{a.stats, a.target_logit, targets, logprob, lse, entropy, (long)row, (long)rows, p.parts, (int)d->n_classes, d->id_type};
+            hipLaunchKernelGGL(join_scores_kernel, dim3((unsigned)ceil_div(rows, kThreads / 64)), dim3(kThreads), 0, stream, j);
+        }
+    }
+    NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
+    return NUTS_OK;
+}
+
+// Backward: pieces of the classes.
+struct ScoreGradPlan {
+    int64_t dim_pad, rows_pad, piece, piece_pad, pieces;
+    Choice scores, grad_x, grad_weight;
+    size_t x, weight, x_t, weight_t, z, dz, dz_t, sums_x, sums_weight;
+    Space space;
+};
+
+ScoreGradPlan plan_score_grad(const nuts_score_desc* d)
+{
+    ScoreGradPlan p{};
+    const size_t size = cat_size(d->dtype);
+    p.dim_pad = round_up(d->dim, 64);
+    p.rows_pad = round_up(std::max<int64_t>(d->n_rows, 1), 64);
+    p.piece = std::clamp<int64_t>(kMostPiece / p.rows_pad / 256 * 256, 256, 1 << 20);
+    p.piece = std::min(p.piece, d->n_classes);
+    p.pieces = ceil_div(d->n_classes, p.piece);
+    p.piece_pad = round_up(p.piece, 64);
+    const int64_t some_rows = std::max<int64_t>(d->n_rows, 1);
+    p.scores = choose(some_rows, p.piece, d->dim * size, false);
+    p.grad_x = choose(some_rows, d->dim, p.piece_pad * size, true);
+    p.grad_weight = choose(p.piece, d->dim, p.rows_pad * size, true);
+    // (whether z is computed again is the call's)
+    p.x = p.space.take(rows_fit(d->x_stride, d->dim, size) ? 0 : (size_t)d->n_rows * p.dim_pad * size);
+    p.weight = p.space.take(rows_fit(d->weight_stride, d->dim, size) ? 0 : (size_t)p.piece * p.dim_pad * size);
+    p.z = p.space.take((size_t)d->n_rows * p.piece_pad * sizeof(float));
+    p.x_t = p.space.take((size_t)d->dim * p.rows_pad * size);
+    p.weight_t = p.space.take((size_t)d->dim * p.piece_pad * size);
+    p.dz = p.space.take((size_t)d->n_rows * p.piece_pad * size);
+    p.dz_t = p.space.take((size_t)p.piece * p.rows_pad * size);
+    p.sums_x = p.space.take(p.grad_x.splits > 1 || p.pieces > 1 ? (size_t)p.grad_x.splits * d->n_rows * d->dim * sizeof(float) : 0);
+    p.sums_weight = p.space.take(p.grad_weight.splits > 1 ? (size_t)p.grad_weight.splits * p.piece * d->dim * sizeof(float) : 0);
+    return p;
+}
+
+template <typename T>
+int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, const void* weight, const void* targets, const float* logits,
+               const float* lse, const float* entropy, const float* grad_logprob, const float* grad_lse, const float* grad_entropy,
+               void* grad_x, void* grad_weight, char* w)
+{
+    hipStream_t stream = api_stream();
+    const int64_t size = sizeof(T), n = d->n_rows, dim = d->dim;
+    const void* own_x = x;
+    int64_t x_stride = d->x_stride;
+    if (!logits && !rows_fit(x_stride, dim, size) && n > 0) {
+        pack<T>(x, x_stride, n, dim, w + p.x, p.dim_pad, stream);
+        own_x = w + p.x;
+        x_stride = p.dim_pad;
+    }
+    if (grad_weight && n > 0) transpose<T>(x, d->x_stride, n, dim, w + p.x_t, p.rows_pad, stream);
+    for (int64_t first = 0; first < d->n_classes; first += p.piece) {
+        const int64_t classes = std::min(p.piece, d->n_classes - first);
+        const char* own_weight = static_cast<const char*>(weight) + first * d->weight_stride * size;
+        const float* z = logits ? logits + first : nullptr;
+        int64_t z_stride = d->logits_stride;
+        if (!logits && n > 0) {
+            const char* rows = own_weight;
+            int64_t weight_stride = d->weight_stride;
+            if (!rows_fit(weight_stride, dim, size)) {
+                pack<T>(own_weight, weight_stride, classes, dim, w + p.weight, p.dim_pad, stream);
+                rows = w + p.weight;
+                weight_stride = p.dim_pad;
+            }
+            ProductArgs a{};
+            a.a = static_cast<const char*>(own_x);
+            a.b = rows;
+            a.a_stride = (long)(x_stride * size);
+            a.b_stride = (long)(weight_stride * size);
+            a.m = (int)n;
+            a.n = (int)classes;
+            a.k_bytes = (int)round_up(dim * size, 16);
+            a.c = w + p.z;
+            a.c_stride = (long)p.piece_pad;
+            a.scale = (float)d->scale;
+            Choice c = p.scores;
+            c.tiles_n = (int)ceil_div(classes, kShapes[c.tiles].n);
+            launch_product<kScores, T>(c, a, stream);
+            z = reinterpret_cast<const float*>(w + p.z);
+            z_stride = p.piece_pad;
+        }
+        if (n > 0) {
+            const GradArgs g{z, targets, lse, entropy, grad_logprob, grad_lse, grad_entropy, grad_x ? w + p.dz : nullptr, grad_weight ? w + p.dz_t : nullptr,
+                             (long)z_stride, (long)p.piece_pad, (long)p.rows_pad, (int)n, (int)first, (int)classes, (int)d->n_classes, d->id_type,
+                             (float)d->scale};
+            hipLaunchKernelGGL(dz_kernel<T>, dim3((unsigned)ceil_div(p.rows_pad, kSquare), (unsigned)ceil_div(p.piece_pad, kSquare)), dim3(kThreads), 0, stream, g);
+        }
+        if (grad_x && n > 0) {
+            transpose<T>(own_weight, d->weight_stride, classes, dim, w + p.weight_t, p.piece_pad, stream);
+            ProductArgs a{};
+            a.a = w + p.dz;
+            a.b = w + p.weight_t;
+            a.a_stride = a.b_stride = (long)(p.piece_pad * size);
+            a.m = (int)n;
+            a.n = (int)dim;
+            a.k_bytes = (int)(p.piece_pad * size);  // (zeros behind the last class)
+            a.sums = reinterpret_cast<float*>(w + p.sums_x);
+            a.add = first > 0;
+            a.c = grad_x;
+            a.c_stride = (long)d->grad_x_stride;
+            if (p.grad_x.splits > 1 || p.pieces > 1) launch_product<kSums, T>(p.grad_x, a, stream);
+            else launch_product<kOutput, T>(p.grad_x, a, stream);
+        }
+        if (grad_weight) {
+            ProductArgs a{};
+            a.a = w + p.dz_t;
+            a.b = w + p.x_t;
+            a.a_stride = a.b_stride = (long)(p.rows_pad * size);
+            a.m = (int)classes;
+            a.n = (int)dim;
+            a.k_bytes = n > 0 ? (int)(p.rows_pad * size) : 0;  // (zeros behind the last row)
+            a.sums = reinterpret_cast<float*>(w + p.sums_weight);
+            a.c = static_cast<char*>(grad_weight) + first * d->grad_weight_stride * size;
+            a.c_stride = (long)d->grad_weight_stride;
+            Choice c = p.grad_weight;
+            c.tiles_m = (int)ceil_div(classes, kShapes[c.tiles].m);
+            if (c.splits > 1) {
+                launch_product<kSums, T>(c, a, stream);
+                add_up<T>(a.sums, c.splits, classes, dim, 1.f, a.c, d->grad_weight_stride, stream);
+            } else {
+                launch_product<kOutput, T>(c, a, stream);
+            }
+        }
+    }
+    if (grad_x && n > 0 && (p.grad_x.splits > 1 || p.pieces > 1))
+        add_up<T>(reinterpret_cast<const float*>(w + p.sums_x), p.grad_x.splits, n, dim, 1.f, grad_x, d->grad_x_stride, stream);
+    NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
+    return NUTS_OK;
+}
+
+int check_workspace(const char* who, const void* workspace, int64_t given, size_t bytes)
+{
+    if (bytes > 0 && (!workspace || given < (int64_t)bytes)) return api_fail(NUTS_E_INVALID_ARG, "%s: needs a workspace of %zu bytes", who, bytes);
+    if (bytes > 0 && reinterpret_cast<uintptr_t>(workspace) % 256) return api_fail(NUTS_E_INVALID_ARG, "%s: workspace must be aligned to 256 bytes", who);
+    return NUTS_OK;
+}
+
+}  // namespace
+}  // namespace nuts
+
+using namespace nuts;
+
+extern "C" {
+
+int nuts_score_workspace(const nuts_score_desc* d, int64_t* bytes)
+{
+    if (int rc = check_score(d, "nuts_score_workspace")) return rc;
+    if (!bytes) return api_fail(NUTS_E_INVALID_ARG, "nuts_score_workspace: bytes must not be NULL");
+    *bytes = d->n_rows == 0 ? 0 : (int64_t)plan_score(d).space.bytes;
+    return NUTS_OK;
+}
+
+int nuts_score(const nuts_score_desc* d, const void* x, const void* weight, const void* targets, float* logprob, float* lse, float* entropy,
+               float* logits, void* workspace, int64_t workspace_bytes)
+{
+    if (int rc = check_score(d, "nuts_score")) return rc;
+    if (d->n_rows == 0) return NUTS_OK;
+    if (!x || !weight) return api_fail(NUTS_E_INVALID_ARG, "nuts_score: null pointer");
+    if (!aligned(x) || !aligned(weight)) return api_fail(NUTS_E_INVALID_ARG, "nuts_score: x and weight must begin at multiples of 16 bytes");
+    const ScorePlan p = plan_score(d);
+    if (int rc = check_workspace("nuts_score", workspace, workspace_bytes, p.space.bytes)) return rc;
+    if (int rc = api_have_device()) return rc;
+    char* w = static_cast<char*>(workspace);
+    return d->dtype == NUTS_F32 ? score<float>(d, p, x, weight, targets, logprob, lse, entropy, logits, w)
+                                : score<bf16>(d, p, x, weight, targets, logprob, lse, entropy, logits, w);
+}
+
+int nuts_score_grad_workspace(const nuts_score_desc* d, int64_t* bytes)
+{
+    if (int rc = check_score(d, "nuts_score_grad_workspace")) return rc;
+    if (!bytes) return api_fail(NUTS_E_INVALID_ARG, "nuts_score_grad_workspace: bytes must not be NULL");
+    *bytes = (int64_t)plan_score_grad(d).space.bytes;
+    return NUTS_OK;
+}
+
+int nuts_score_grad(const nuts_score_desc* d, const void* x, const void* weight, const void* targets, const float* logits, const float* lse,
+                    const float* entropy, const float* grad_logprob, const float* grad_lse, const float* grad_entropy, void* grad_x,
+                    void* grad_weight, void* workspace, int64_t workspace_bytes)
+{
+    if (int rc = check_score(d, "nuts_score_grad")) return rc;
+    if (d->n_rows > 0 && (!x || !weight || !lse)) return api_fail(NUTS_E_INVALID_ARG, "nuts_score_grad: null pointer");
+    if (!aligned(x) || !aligned(weight)) return api_fail(NUTS_E_INVALID_ARG, "nuts_score_grad: x and weight must begin at multiples of 16 bytes");
+    if (grad_entropy && !entropy) return api_fail(NUTS_E_INVALID_ARG, "nuts_score_grad: grad_entropy needs the entropy");
+    if (!grad_x && !grad_weight) return NUTS_OK;
+    const ScoreGradPlan p = plan_score_grad(d);
+    if (int rc = check_workspace("nuts_score_grad", workspace, workspace_bytes, p.space.bytes)) return rc;
+    if (int rc = api_have_device()) return rc;
+    char* w = static_cast<char*>(workspace);
+    return d->dtype == NUTS_F32
+               ? score_grad<float>(d, p, x, weight, targets, logits, lse, entropy, grad_logprob, grad_lse, grad_entropy, grad_x, grad_weight, w)
+               : score_grad<bf16>(d, p, x, weight, targets, logits, lse, entropy, grad_logprob, grad_lse, grad_entropy, grad_x, grad_weight, w);
+}
+
+}  // extern "C"

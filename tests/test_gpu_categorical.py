@@ -1,0 +1,565 @@
+"""The categorical operators against plain forms in 64 bits.
+
+Tolerances.  u = 2^-24.  Sums of rows: tests/categorical_ref.py.  Statistics of logits: with w = (x - m) s log2(e), a term 2^w
+has the relative error of w's two roundings (2 u |w|) and of the exponential (2 u); a row's sum weights these with the
+probabilities, for which |w| averages less than 30 (entropies here are below 20 bits, and terms with |w| > 126 are
+nothing), and adds, in chains of at most some hundreds of terms, (c - 1) u: in all below 60 u + 60 u + 512 u < 4e-5.  TOL is
+that, for ln S; the entropy's weighted sum has the same with another factor |w|.  Where z itself is large, its own rounding
+(u |z|) is added."""
+import math
+
+import pytest
+import torch
+
+import categorical_ref as R
+
+pytestmark = pytest.mark.gpu
+
+TOL = 4e-5
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def ops():
+    import paper_1910_11141_amd as nuts
+    return nuts
+
+
+# ---- lookup ---------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,classes,dim,id_dtype", [
+    (1, 1, 1, torch.int32), (0, 5, 7, torch.int64), (3, 10, 25, torch.int32), (64, 1000, 64, torch.int64), (1000, 77, 100, torch.int32),
+    (5, 3, 4097, torch.int64), (40000, 300, 65, torch.int32), (9000, 500, 2048, torch.int64)])
+def test_lookup(dtype, n, classes, dim, id_dtype):
+    nuts, g = ops(), gen(n + dim)
+    table = torch.randn(classes, dim, generator=g, device="cuda").to(dtype)
+    ids = torch.randint(-2, classes + 2, (n,), generator=g, device="cuda").to(id_dtype)
+    for scale in (1.0, -0.37):
+        got = nuts.nuts_lookup(table, ids, scale=scale)
+        known = (ids >= 0) & (ids < classes)
+        rows = table[torch.where(known, ids, 0).long()].float() * torch.tensor(scale, dtype=torch.float32)
+        want = torch.where(known[:, None], rows, torch.zeros_like(rows)).to(dtype)
+        assert got.shape == (n, dim) and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_lookup_strides_and_shapes(dtype):
+    nuts, g = ops(), gen(7)
+    big = torch.randn(50, 143, generator=g, device="cuda").to(dtype)
+    table = big[3:40, 1:130]                                     # rows begin at odd places
+    ids = torch.randint(0, 37, (4, 9), generator=g, device="cuda")
+    want = (table[ids].float() * 2.5).to(dtype)
+    assert torch.equal(nuts.nuts_lookup(table, ids, scale=2.5), want)
+    out = torch.full((36, 140), 7.0, dtype=dtype, device="cuda")
+    nuts.nuts_lookup(table, ids.view(-1), scale=2.5, out=out[:, 5:134])
+    assert torch.equal(out[:, 5:134], want.view(36, 129))
+    assert bool((out[:, :5] == 7).all()) and bool((out[:, 134:] == 7).all())   # nothing beside the rows is written
+    assert torch.equal(nuts.nuts_lookup(table, ids.t(), scale=1.0), table[ids.t()])  # ids that do not lie in order
+
+
+def test_lookup_beyond_32_bits():
+    nuts = ops()
+    classes, dim = (1 << 21) + 5, 2048                            # more than 2^32 elements
+    table = torch.zeros(classes, dim, dtype=torch.bfloat16, device="cuda")
+    ids = torch.tensor([0, classes - 1, (1 << 21) - 1, (1 << 20) + 3, classes], device="cuda")
+    table[ids[:4]] = torch.randn(4, dim, device="cuda").bfloat16()
+    got = nuts.nuts_lookup(table, ids)
+    assert torch.equal(got[:4], table[ids[:4]]) and not bool(got[4].any())
+    grad = torch.randn(5, dim, device="cuda").bfloat16()
+    nuts.nuts_lookup_grad(grad, ids, classes, out=table)
+    assert torch.equal(table[ids[:4]], grad[:4])
+    table[ids[:4]] = 0
+    assert not bool(table.view(-1, 1 << 11).any(1).any())
+
+
+# ---- gradient of lookup ----------------------------------------------------------------------------------------------
+
+def _ids(kind, n, classes, g):
+    if kind == "even":
+        return torch.randint(0, classes, (n,), generator=g, device="cuda")
+    if kind == "skewed":
+        return (torch.rand(n, generator=g, device="cuda") ** 6 * classes).long().clamp(max=classes - 1)
+    if kind == "one":
+        return torch.full((n,), classes // 2, device="cuda")
+    if kind == "none":
+        return torch.full((n,), -1, device="cuda")
+    if kind == "sorted":
+        return torch.randint(0, classes, (n,), generator=g, device="cuda").sort().values
+    return torch.randint(-classes, 2 * classes, (n,), generator=g, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kind", ["even", "skewed", "one", "none", "sorted", "outside"])
+@pytest.mark.parametrize("n,classes,dim", [(0, 3, 5), (1, 1, 1), (37, 9, 25), (1000, 5000, 100), (1024, 70, 520), (1025, 70, 33), (2049, 1, 8),
+                                           (5000, 2048, 64), (4100, 5000, 257), (20000, 300000, 24), (9000, 5, 1500)])
+def test_lookup_grad(dtype, kind, n, classes, dim):
+    nuts, g = ops(), gen(n + classes + dim)
+    grad = torch.randn(n, dim, generator=g, device="cuda").to(dtype)
+    ids = _ids(kind, n, classes, g).to(torch.int32 if dim % 2 else torch.int64)
+    got = nuts.nuts_lookup_grad(grad, ids, classes, scale=0.75)
+    want, bound = R.lookup_grad(grad, ids, classes, 0.75)
+    assert bool(((got.double() - want).abs() <= bound).all())
+    assert torch.equal(got, nuts.nuts_lookup_grad(grad, ids, classes, scale=0.75))   # the order of sums is fixed
+    old = torch.randn(classes, dim, generator=g, device="cuda").to(dtype)
+    into = old.clone()
+    nuts.nuts_lookup_grad(grad, ids, classes, scale=0.75, out=into, accumulate=True)
+    want, bound = R.lookup_grad(grad, ids, classes, 0.75, old)
+    assert bool(((into.double() - want).abs() <= bound).all())
+    absent = torch.ones(classes, dtype=torch.bool, device="cuda")
+    absent[ids[(ids >= 0) & (ids < classes)].long()] = False
+    assert torch.equal(into[absent], old[absent])
+
+
+@pytest.mark.parametrize("n", [700, 3000])
+def test_lookup_grad_strides_and_infinities(n):
+    nuts, g = ops(), gen(n)
+    wide = torch.randn(n, 90, generator=g, device="cuda").bfloat16()
+    grad = wide[:, 3:80]
+    ids = torch.randint(0, 40, (n,), generator=g, device="cuda")
+    grad[5, 4], grad[6, 5] = math.inf, math.nan                  # reach the rows and columns that they belong to, no others
+    out = torch.full((41, 99), 3.0, dtype=torch.bfloat16, device="cuda")
+    nuts.nuts_lookup_grad(grad, ids, 41, out=out[:, 7:84])
+    want, bound = R.lookup_grad(grad, ids, 41, 1.0)
+    got = out[:, 7:84].double()
+    bad = ~torch.isfinite(want)
+    assert int(bad.sum()) in (1, 2)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    assert bool(((got - want).abs() <= bound)[~bad].all())
+    assert bool((out[:, :7] == 3).all()) and bool((out[:, 84:] == 3).all())
+
+
+def test_lookup_grad_against_differences():
+    """d/dT of sum(G * lookup(T)) by differences of the operator itself: it is linear, so any step does."""
+    nuts, g = ops(), gen(3)
+    table = torch.randint(-8, 8, (50, 12), generator=g, device="cuda").float()
+    ids = torch.randint(0, 50, (2000,), generator=g, device="cuda")
+    weight = torch.randint(-3, 4, (2000, 12), generator=g, device="cuda").float()
+    value = lambda t: (weight.double() * nuts.nuts_lookup(t, ids, scale=0.5).double()).sum()
+    grad = nuts.nuts_lookup_grad(weight, ids, 50, scale=0.5)
+    for v, c in ((0, 0), (17, 5), (49, 11)):
+        up = table.clone()
+        up[v, c] += 4.0
+        assert float(grad[v, c]) == float((value(up) - value(table)) / 4.0)
+
+
+# ---- log-probabilities -----------------------------------------------------------------------------------------------
+
+def _check_logprobs(logits, targets, *, scale=1.0, allowed=None, n_top=0):
+    """The operator's outputs against the plain form's; `allowed` as booleans."""
+    nuts = ops()
+    classes = logits.shape[1]
+    packed = None if allowed is None else R.pack_bits(allowed)
+    got = nuts.nuts_logprobs(logits, targets, scale=scale, allowed=packed, n_top=n_top)
+    full = None if allowed is None else allowed.expand(logits.shape[0], classes)
+    z = logits.double() * torch.tensor(scale, dtype=torch.float32).double()
+    if full is not None:
+        z = torch.where(full, z, torch.full_like(z, -math.inf))
+    logprob, lse, entropy, p = R.logprobs(z, targets)
+    size = torch.where(torch.isfinite(lse), lse.abs(), torch.zeros_like(lse))
+
+    def near(a, b, bound):
+        a = a.double()
+        assert torch.equal(torch.isnan(a), torch.isnan(b)), (a, b)
+        fine = torch.isfinite(b)
+        assert torch.equal(a[~fine & ~torch.isnan(b)], b[~fine & ~torch.isnan(b)])
+        off = ((a - b).abs() - bound)[fine]
+        assert off.numel() == 0 or float(off.max()) <= 0, float(off.max())
+
+    near(got.lse, lse, TOL + 2 * R.U * size)
+    near(got.entropy, entropy, 30 * TOL)
+    if targets is not None:
+        far = torch.where(torch.isfinite(logprob), logprob.abs(), torch.zeros_like(logprob))
+        near(got.logprob, logprob, TOL + 2 * R.U * far)
+    if n_top:
+        ids = R.top(logits, full, n_top)
+        assert torch.equal(got.top_ids.cpu().long(), ids), (got.top_ids, ids)
+        at = ids.to(logits.device)
+        each = [R.logprobs(z, at[:, k].clamp(min=0))[0] for k in range(n_top)]
+        want = torch.where(at >= 0, torch.stack(each, 1), torch.full_like(at, -math.inf, dtype=torch.float64))
+        want = torch.where((torch.isinf(lse) & (lse < 0))[:, None], torch.full_like(want, -math.inf), want)
+        far = torch.where(torch.isfinite(want), want.abs(), torch.zeros_like(want))
+        near(got.top_logprobs, want, TOL + 2 * R.U * far)
+    return got
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,classes,n_top", [
+    (1, 1, 1), (1, 1, 0), (2, 7, 9), (5, 64, 64), (3, 255, 5), (4, 257, 3), (7, 1000, 64), (300, 511, 2), (1, 2048, 20), (2, 2049, 1),
+    (3, 9999, 64), (1100, 33, 4), (1030, 2500, 7), (5, 40003, 33), (1, 131072, 64), (0, 10, 3)])
+@pytest.mark.parametrize("masked", [False, True])
+def test_logprobs(dtype, n, classes, n_top, masked):
+    g = gen(n * 31 + classes)
+    logits = (torch.randn(n, classes, generator=g, device="cuda") * 3).to(dtype)
+    targets = torch.randint(-1, classes + 1, (n,), generator=g, device="cuda").to(torch.int32 if n % 2 else torch.int64)
+    allowed = torch.rand(n, classes, generator=g, device="cuda") < 0.7 if masked else None
+    _check_logprobs(logits, targets, scale=1.25, allowed=allowed, n_top=n_top)
+    _check_logprobs(logits, None, n_top=0, allowed=allowed)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("classes", [5, 300, 9001, 70001])
+@pytest.mark.parametrize("n_rows", [16, 1040])
+def test_logprobs_of_odd_rows(dtype, classes, n_rows):
+    """Rows that are constant, of the type's lowest value, empty, with infinities and NaN, in allowed and in other places."""
+    if n_rows * classes > 2e7:
+        classes = 12007
+    g = gen(classes)
+    lowest = torch.finfo(dtype).min
+    logits = (torch.randn(n_rows, classes, generator=g, device="cuda") * 2).to(dtype)
+    targets = torch.randint(0, classes, (n_rows,), generator=g, device="cuda")
+    allowed = torch.rand(n_rows, classes, generator=g, device="cuda") < 0.5
+    allowed[:, 0] = True
+    logits[0] = 1.5                                               # constant: all alternatives are equal
+    logits[1] = lowest
+    logits[2] = -math.inf
+    logits[3] = -math.inf
+    logits[3, classes // 2] = -3.0                                # one class alone
+    logits[4, 1:] = lowest
+    logits[5, 3] = math.nan
+    logits[6, 4] = math.inf
+    allowed[7] = False                                            # nothing may come
+    allowed[8], logits[8, 2] = True, math.nan
+    allowed[8, 2] = False                                         # NaN where nothing may come
+    allowed[9], logits[9, 2] = True, math.inf
+    allowed[9, 2] = False
+    allowed[10] = False
+    allowed[10, classes - 1] = True
+    allowed[11] = torch.arange(classes, device="cuda") % 3 == 0
+    logits[12] = 0.0
+    logits[12, ::2] = -0.0                                        # equal
+    logits[13] = torch.linspace(-5, 5, classes, device="cuda").to(dtype)   # rising: the last part holds all alternatives
+    logits[14] = torch.linspace(5, -5, classes, device="cuda").to(dtype)
+    logits[15] = -math.inf
+    logits[15, 1] = math.nan
+    for mask in (None, allowed):
+        got = _check_logprobs(logits[:16], targets[:16], allowed=None if mask is None else mask[:16], n_top=7)
+        whole = ops().nuts_logprobs(logits, targets, allowed=None if mask is None else R.pack_bits(mask), n_top=7)
+        # (rows divided over workgroups or not: the same alternatives; the sums' order may differ)
+        assert torch.equal(whole.top_ids[:16], got.top_ids)
+        assert torch.allclose(whole.lse[:16], got.lse, rtol=1e-6, atol=TOL, equal_nan=True)
+
+
+def test_logprobs_strides_and_shared_mask():
+    g = gen(11)
+    wide = torch.randn(9, 1500, generator=g, device="cuda").half()
+    logits = wide[:, 3:1204]
+    targets = torch.randint(0, 1201, (9,), generator=g, device="cuda")
+    allowed = torch.rand(1201, generator=g, device="cuda") < 0.3
+    _check_logprobs(logits, targets, allowed=allowed, n_top=12)
+    words = torch.zeros(9, 50, dtype=torch.int32, device="cuda")
+    each = torch.rand(9, 1201, generator=g, device="cuda") < 0.3
+    words[:, 4:42] = R.pack_bits(each)
+    a = ops().nuts_logprobs(logits, targets, allowed=words[:, 4:42], n_top=12)
+    b = ops().nuts_logprobs(logits, targets, allowed=R.pack_bits(each), n_top=12)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_logprobs_of_many_short_rows():
+    n = (1 << 22) + 5                                             # more workgroups than one launch has
+    logits = torch.randn(n, 3, generator=gen(2), device="cuda")
+    targets = torch.arange(n, device="cuda") % 3
+    got = ops().nuts_logprobs(logits, targets)
+    want, lse, entropy, _ = R.logprobs(logits.double(), targets)
+    assert float((got.logprob.double() - want).abs().max()) <= TOL + 1e-6
+    assert float((got.entropy.double() - entropy).abs().max()) <= TOL + 1e-6
+
+
+def test_logprobs_beyond_32_bits():
+    n, classes = 33000, 131072                                    # more than 2^32 logits
+    logits = torch.zeros(n, classes, dtype=torch.bfloat16, device="cuda")
+    rows = [0, 16385, 32768, n - 1]
+    logits[rows] = (torch.randn(4, classes, generator=gen(4), device="cuda") * 3).bfloat16()
+    targets = torch.full((n,), classes - 1, device="cuda")
+    got = ops().nuts_logprobs(logits, targets, n_top=3)
+    want, lse, _, _ = R.logprobs(logits[rows].double(), targets[rows])
+    assert float((got.logprob[rows].double() - want).abs().max()) <= TOL + 30 * R.U
+    assert torch.equal(got.top_ids[rows].cpu().long(), R.top(logits[rows], None, 3))
+    assert abs(float(got.lse[12345]) - math.log(classes)) <= TOL
+    grad = ops().nuts_logprobs_grad(logits, targets, got.lse, grad_logprob=torch.ones(n, device="cuda"))
+    exact = R.grad_logits(logits[rows].double(), targets[rows], None, 1.0, torch.ones(4, device="cuda"))
+    assert float((grad[rows].double() - exact).abs().max()) <= 2 * R.EPS[torch.bfloat16]
+    assert abs(float(grad[12345, classes - 1]) - (1 - 1 / classes)) <= 2 * R.EPS[torch.bfloat16]
+
+
+# ---- gradient of log-probabilities -------------------------------------------------------------------------------------
+
+def _grad_bound(want, z, targets, scale, parts, dtype):
+    """p has the relative error of lse (TOL, and u |z| twice) and of its exponential; log p + H adds its own; then the
+    output is rounded."""
+    _, lse, entropy, p = R.logprobs(z, targets)
+    size = torch.where(torch.isfinite(lse), lse.abs(), torch.zeros_like(lse))[:, None]
+    log_p = torch.where(p == 0, torch.zeros_like(p), torch.log(p.clamp(min=1e-300))).abs()
+    rel = 2 * TOL + 4 * R.U * (size + log_p)
+    total = sum(g.double().abs() if g is not None else 0 for g in parts[:2])
+    total = total[:, None] if torch.is_tensor(total) else 0
+    h = 0 if parts[2] is None else parts[2].double().abs()[:, None] * (log_p + entropy[:, None] + 60)
+    bound = (p * (total + h) * rel + R.U * 4 * total * (p > 0)) * scale + want.abs() * 4 * R.U
+    return torch.nan_to_num(bound) + (want.abs() + torch.nan_to_num(bound)) * R.EPS[dtype] * 1.01 + R.TINY[dtype] + 2.0 ** -126
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,classes", [(1, 1), (3, 7), (40, 1000), (5, 8193), (2, 33000), (700, 129)])
+@pytest.mark.parametrize("which", ["logprob", "lse", "entropy", "all", "all, masked"])
+def test_logprobs_grad(dtype, n, classes, which):
+    nuts, g = ops(), gen(n + classes)
+    logits = (torch.randn(n, classes + 3, generator=g, device="cuda") * 3).to(dtype)[:, 1:classes + 1]
+    targets = torch.randint(-1, classes + 1, (n,), generator=g, device="cuda")
+    allowed = torch.rand(n, classes, generator=g, device="cuda") < 0.6 if "masked" in which else None
+    packed = None if allowed is None else R.pack_bits(allowed)
+    give = lambda name: torch.randn(n, generator=g, device="cuda") if name in which or "all" in which else None
+    parts = [give("logprob"), give("lse"), give("entropy")]
+    fwd = nuts.nuts_logprobs(logits, targets, scale=0.8, allowed=packed)
+    got = nuts.nuts_logprobs_grad(logits, targets, fwd.lse, fwd.entropy, grad_logprob=parts[0], grad_lse=parts[1], grad_entropy=parts[2],
+                                  scale=0.8, allowed=packed)
+    s = torch.tensor(0.8, dtype=torch.float32).double().item()
+    z = logits.double() * s
+    if allowed is not None:
+        z = torch.where(allowed, z, torch.full_like(z, -math.inf))
+    want = R.grad_logits(z, targets, allowed, s, *parts)
+    off = (got.double() - want).abs() - _grad_bound(want, z, targets, s, parts, dtype)
+    assert float(off.max()) <= 0, float(off.max())
+    out = torch.full((n, classes + 9), 5.0, dtype=dtype, device="cuda")
+    nuts.nuts_logprobs_grad(logits, targets, fwd.lse, fwd.entropy, grad_logprob=parts[0], grad_lse=parts[1], grad_entropy=parts[2],
+                            scale=0.8, allowed=packed, out=out[:, 5:classes + 5])
+    assert torch.equal(out[:, 5:classes + 5], got) and bool((out[:, :5] == 5).all()) and bool((out[:, classes + 5:] == 5).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_logprobs_grad_of_odd_rows(dtype):
+    nuts, g = ops(), gen(5)
+    classes = 3000
+    logits = torch.randn(9, classes, generator=g, device="cuda").to(dtype)
+    targets = torch.randint(0, classes, (9,), generator=g, device="cuda")
+    allowed = torch.ones(9, classes, dtype=torch.bool, device="cuda")
+    logits[0] = torch.finfo(dtype).min                            # all equal, far below: an even distribution
+    logits[1] = -math.inf
+    allowed[2] = False
+    logits[3, 7], allowed[3, 7] = math.nan, False
+    logits[4, 8] = -math.inf
+    targets[4] = 8                                                # a target of probability 0
+    logits[5, 9], allowed[5, targets[5]] = -math.inf, False       # a target that may not come
+    logits[6, 1:] = torch.finfo(dtype).min
+    logits[7, 3] = math.nan
+    packed = R.pack_bits(allowed)
+    fwd = nuts.nuts_logprobs(logits, targets, allowed=packed)
+    parts = [torch.ones(9, device="cuda"), None, torch.full((9,), 0.5, device="cuda")]
+    got = nuts.nuts_logprobs_grad(logits, targets, fwd.lse, fwd.entropy, grad_logprob=parts[0], grad_entropy=parts[2], allowed=packed).double()
+    z = torch.where(allowed, logits.double(), torch.full((1, 1), -math.inf, dtype=torch.float64, device="cuda"))
+    want = R.grad_logits(z, targets, allowed, 1.0, *parts)
+    assert bool(torch.isnan(got[7]).all())
+    rows = [0, 1, 2, 3, 4, 5, 6, 8]
+    assert not bool(got[1].any()) and not bool(got[2].any()) and float(got[3, 7]) == 0 and float(got[5, targets[5]]) == 0
+    z[0] = 0.0  # (the bound's |z| is about rounding, of which an even row has none)
+    off = (got - want).abs()[rows] - _grad_bound(want, z, targets, 1.0, parts, dtype)[rows]
+    assert float(off.max()) <= 0, off.amax(1)
+
+
+def test_logprobs_grad_against_differences():
+    """Central differences of the plain form in 64 bits: an error of h^2 = 1e-10 and of 1e-16 / h."""
+    nuts, g = ops(), gen(9)
+    logits = torch.randn(4, 50, generator=g, device="cuda") * 2
+    targets = torch.tensor([3, -1, 49, 20], device="cuda")
+    g_lp, g_lse, g_h = (torch.randn(4, generator=g, device="cuda") for _ in range(3))
+
+    def value(x):
+        logprob, lse, entropy, _ = R.logprobs(x * 1.5, targets)
+        return (g_lp.double() * logprob + g_lse.double() * lse + g_h.double() * entropy).sum()
+
+    fwd = nuts.nuts_logprobs(logits, targets, scale=1.5)
+    grad = nuts.nuts_logprobs_grad(logits, targets, fwd.lse, fwd.entropy, grad_logprob=g_lp, grad_lse=g_lse, grad_entropy=g_h, scale=1.5)
+    for r in range(4):
+        for v in (0, 3, 20, 49):
+            up, down = logits.double().clone(), logits.double().clone()
+            up[r, v] += 1e-5
+            down[r, v] -= 1e-5
+            diff = float((value(up) - value(down)) / 2e-5)
+            assert abs(float(grad[r, v]) - diff) <= 1e-4
+
+
+# ---- scores ------------------------------------------------------------------------------------------------------------
+
+def _score_bounds(x, w, scale):
+    """z in 64 bits and what binary32 sums of products may be off by, (D + 2) u |x|'|w|."""
+    z = x.double() @ w.double().t() * scale
+    off = (x.double().abs() @ w.double().abs().t()) * scale * (x.shape[1] + 2) * R.U + z.abs() * 2 * R.U
+    return z, off
+
+
+SHAPES = [(1, 1, 1), (3, 5, 25), (2, 7, 8), (1000, 1000, 25), (100, 300, 100), (17, 1001, 72), (33, 4100, 64), (300, 513, 200), (257, 1030, 1000),
+          (1, 5000, 512), (8, 20001, 256), (130, 70, 4096), (520, 600, 130), (1500, 2100, 96)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,classes,dim", SHAPES)
+def test_score(dtype, n, classes, dim):
+    nuts, g = ops(), gen(n + classes + dim)
+    x = torch.randn(n, dim, generator=g, device="cuda").to(dtype)
+    w = (torch.randn(classes, dim, generator=g, device="cuda") * 2 / math.sqrt(dim)).to(dtype)
+    targets = torch.randint(-1, classes + 1, (n,), generator=g, device="cuda")
+    s = torch.tensor(1.3, dtype=torch.float32).double().item()
+    got = nuts.nuts_score(x, w, targets, scale=1.3, keep_logits=True)
+    z, off = _score_bounds(x, w, s)
+    assert bool(((got.logits.double() - z).abs() <= off).all())
+    logprob, lse, entropy, p = R.logprobs(z, targets)
+    worst = off.amax(1)
+    assert bool(((got.lse.double() - lse).abs() <= worst + TOL + 2 * R.U * lse.abs()).all())
+    assert bool(((got.logprob.double() - logprob).abs() <= 2 * worst + TOL + 2 * R.U * logprob.abs()).all())
+    # an entropy's terms p log p move with p, by twice the largest error of z, times |log p|
+    assert bool(((got.entropy.double() - entropy).abs() <= 30 * TOL + 60 * worst).all())
+    again = nuts.nuts_score(x, w, targets, scale=1.3)
+    assert again.logits is None and all(torch.equal(a, b) for a, b in zip(got[:3], again[:3]))
+    assert nuts.nuts_score(x, w).logprob is None
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,classes,dim", SHAPES + [(0, 10, 16)])
+@pytest.mark.parametrize("kept", [True, False])
+def test_score_grad(dtype, n, classes, dim, kept):
+    nuts, g = ops(), gen(n + classes + dim)
+    x = torch.randn(n, dim, generator=g, device="cuda").to(dtype)
+    w = (torch.randn(classes, dim, generator=g, device="cuda") * 2 / math.sqrt(dim)).to(dtype)
+    targets = torch.randint(-1, classes + 1, (n,), generator=g, device="cuda").int()
+    parts = [torch.randn(n, generator=g, device="cuda") for _ in range(3)]
+    s = torch.tensor(0.7, dtype=torch.float32).double().item()
+    fwd = nuts.nuts_score(x, w, targets, scale=0.7, keep_logits=kept)
+    args = dict(grad_logprob=parts[0], grad_lse=parts[1], grad_entropy=parts[2], scale=0.7, logits=fwd.logits)
+    grad_x, grad_w = nuts.nuts_score_grad(x, w, targets, fwd.lse, fwd.entropy, **args)
+    z, off = _score_bounds(x, w, s)
+    dz = R.grad_logits(z, targets, None, s, *parts)
+    if n:
+        # dz: as of logits, with z's own error on top (relative to p, times what multiplies p), then rounded to the inputs' type
+        _, lse, entropy, p = R.logprobs(z, targets)
+        log_p = torch.log(p.clamp(min=1e-300)).abs()
+        factor = (parts[0].double().abs() + parts[1].double().abs())[:, None] + parts[2].double().abs()[:, None] * (log_p + entropy[:, None] + 1)
+        dz_off = _grad_bound(dz, z, targets, s, parts, dtype) + 4 * p * factor * s * (off + off.amax(1, keepdim=True))
+    else:
+        dz_off = torch.zeros_like(dz)
+    want_x, want_w = dz @ w.double(), dz.t() @ x.double()
+    bound_x = dz_off @ w.double().abs() + (dz.abs() @ w.double().abs()) * (classes + 2) * R.U
+    bound_w = dz_off.t() @ x.double().abs() + (dz.abs().t() @ x.double().abs()) * (n + 2) * R.U
+    for got, want, bound in ((grad_x, want_x, bound_x), (grad_w, want_w, bound_w)):
+        bound = bound * 1.01 + (want.abs() + bound) * R.EPS[dtype] * 1.01 + 1e-30
+        assert got.shape == want.shape
+        assert bool(((got.double() - want).abs() <= bound).all()), float(((got.double() - want).abs() / bound).max())
+    only_x, none = nuts.nuts_score_grad(x, w, targets, fwd.lse, fwd.entropy, want_weight=False, **args)
+    assert none is None and torch.equal(only_x, grad_x)
+    none, only_w = nuts.nuts_score_grad(x, w, targets, fwd.lse, fwd.entropy, want_x=False, **args)
+    assert none is None and torch.equal(only_w, grad_w)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_score_strides_and_addresses(dtype):
+    nuts, g = ops(), gen(21)
+    wide_x, wide_w = (torch.randn(200, 333, generator=g, device="cuda").to(dtype) for _ in range(2))
+    for a, b in ((0, 64), (8, 200), (1, 65), (3, 330)):
+        x, w = wide_x[:, a:b], wide_w[:150, a:b]
+        targets = torch.arange(200, device="cuda") % 150
+        got = nuts.nuts_score(x, w, targets, keep_logits=True)
+        want = nuts.nuts_score(x.contiguous(), w.contiguous(), targets, keep_logits=True)
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+        ones = torch.ones(200, device="cuda")
+        for kept in (got.logits, None):
+            u = nuts.nuts_score_grad(x, w, targets, got.lse, grad_logprob=ones, logits=kept)
+            v = nuts.nuts_score_grad(x.contiguous(), w.contiguous(), targets, got.lse, grad_logprob=ones, logits=kept)
+            assert all(torch.equal(p, q) for p, q in zip(u, v))
+
+
+def test_score_grad_over_several_pieces():
+    """More logits than one piece of the classes holds: what is summed over pieces is the same gradient."""
+    nuts, g = ops(), gen(22)
+    n, classes, dim = 65536 + 40, 9000, 64                        # pieces of 3840 classes
+    x = torch.randn(n, dim, generator=g, device="cuda")
+    w = torch.randn(classes, dim, generator=g, device="cuda") * 0.25
+    targets = torch.randint(0, classes, (n,), generator=g, device="cuda")
+    fwd = nuts.nuts_score(x, w, targets, keep_logits=True)
+    ones = torch.full((n,), 1.0 / n, device="cuda")
+    for kept in (fwd.logits, None):
+        grad_x, grad_w = nuts.nuts_score_grad(x, w, targets, fwd.lse, grad_logprob=ones, logits=kept)
+        want_w = torch.zeros(classes, dim, dtype=torch.float64, device="cuda")
+        for r in range(0, n, 8192):
+            rows = slice(r, min(r + 8192, n))
+            z = x[rows].double() @ w.double().t()
+            dz = R.grad_logits(z, targets[rows], None, 1.0, ones[rows])
+            want_x = dz @ w.double()
+            assert float((grad_x[rows].double() - want_x).norm() / want_x.norm()) <= 1e-5
+            want_w += dz.t() @ x[rows].double()
+        assert float((grad_w.double() - want_w).norm() / want_w.norm()) <= 1e-5
+
+
+def test_score_of_features_that_are_not_finite():
+    nuts, g = ops(), gen(23)
+    x = torch.randn(70, 64, generator=g, device="cuda").bfloat16()
+    w = (torch.randn(500, 64, generator=g, device="cuda") * 0.2).bfloat16()
+    x[3, 5] = math.nan
+    targets = torch.arange(70, device="cuda")
+    got = nuts.nuts_score(x, w, targets, keep_logits=True)
+    rows = torch.arange(70, device="cuda") != 3
+    clean = nuts.nuts_score(torch.where(torch.isnan(x), torch.zeros_like(x), x), w, targets, keep_logits=True)
+    for a, b in zip(got, clean):
+        assert torch.equal(a[rows], b[rows]) and bool(torch.isnan(a[3]).all())
+
+
+# ---- streams, graphs, a model's step --------------------------------------------------------------------------------------
+
+def _all_calls(nuts, s):
+    rows = nuts.nuts_lookup(s["table"], s["ids"], scale=2.0)
+    fwd = nuts.nuts_score(rows, s["weight"], s["targets"], keep_logits=True)
+    alternatives = nuts.nuts_logprobs(fwd.logits, s["targets"], n_top=4)
+    grad_logits = nuts.nuts_logprobs_grad(fwd.logits, s["targets"], fwd.lse, grad_logprob=s["g"])
+    grad_rows, grad_weight = nuts.nuts_score_grad(rows, s["weight"], s["targets"], fwd.lse, grad_logprob=s["g"], logits=fwd.logits)
+    grad_table = nuts.nuts_lookup_grad(grad_rows, s["ids"], s["table"].shape[0], scale=2.0)
+    return [rows, *fwd, *alternatives, grad_logits, grad_rows, grad_weight, grad_table]
+
+
+def _model(seed, n, dtype=torch.bfloat16, classes=2100, dim=96):
+    g = gen(seed)
+    return {"table": torch.randn(classes, dim, generator=g, device="cuda").to(dtype), "ids": torch.randint(0, classes, (n,), generator=g, device="cuda"),
+            "weight": (torch.randn(classes, dim, generator=g, device="cuda") * 0.2).to(dtype),
+            "targets": torch.randint(0, classes, (n,), generator=g, device="cuda"), "g": torch.randn(n, generator=g, device="cuda")}
+
+
+@pytest.mark.parametrize("n", [50, 3000])
+def test_side_streams_and_the_librarys_stream(n):
+    nuts = ops()
+    s = _model(31, n)
+    want = _all_calls(nuts, s)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = _all_calls(nuts, s)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    nuts.nuts_set_stream(side)
+    try:
+        # inputs made on PyTorch's stream just before, outputs waited for by the caller
+        again = {k: v.clone() for k, v in s.items()}
+        rows = nuts.nuts_lookup(again["table"], again["ids"], scale=2.0)
+        fwd = nuts.nuts_score(rows, again["weight"], again["targets"])
+        side.synchronize()
+    finally:
+        nuts.nuts_set_stream(None)
+    assert torch.equal(rows, want[0]) and torch.equal(fwd.logprob, want[1])
+
+
+@pytest.mark.parametrize("n", [50, 3000])
+def test_graph_replays(n):
+    nuts = ops()
+    s = _model(32, n)
+    _all_calls(nuts, s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _all_calls(nuts, s)
+    for seed in (33, 34, 35, 33):
+        for k, v in _model(seed, n).items():
+            s[k].copy_(v)
+        want = _all_calls(nuts, s)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
