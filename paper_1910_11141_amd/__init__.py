@@ -12,4 +12,6 @@ def __getattr__(name):
         raise AttributeError(name)
     binding = importlib.import_module(__name__ + ".binding")
     categorical = importlib.import_module(__name__ + ".categorical")
-    return getattr(categorical if name in categorical.__all__ else binding, name)
+    if name in categorical.__all__:  # (calls of a few microseconds: found here from now on)
+        return globals().setdefault(name, getattr(categorical, name))
+    return getattr(binding, name)

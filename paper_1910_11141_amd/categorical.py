@@ -82,28 +82,28 @@ def _per_row(t, what, n):
 
 def _call(entry, desc, tensors, workspace_bytes=None, last=()):
     """`entry` on the library's stream; `tensors`: its pointers in order (None: NULL), then the workspace."""
-    device = None
+    device = tensors[0].device
+    args = [desc]
     for t in tensors:
-        if t is not None:
-            if device is None:
-                device = t.device
-            elif t.device != device:
-                raise ValueError(f"tensors are on {device} and {t.device}")
-    L = _b.lib()
+        if t is None:
+            args.append(None)
+        elif t.device == device:
+            args.append(t.data_ptr())
+        else:
+            raise ValueError(f"tensors are on {device} and {t.device}")
     if device.type != "cuda":
         if torch.cuda.is_available():
             raise ValueError(f"tensors must be on the GPU, not on {device}")
         # no device: the library says so itself
-        args = [None if t is None else t.data_ptr() for t in tensors]
-        _b._check(entry(desc, *args, *((256, 1 << 62) if workspace_bytes is not None else ()), *last))
+        _b._check(entry(*args, *((256, 1 << 62) if workspace_bytes is not None else ()), *last))
         return
     if device.index != torch.cuda.current_device():
         raise ValueError(f"tensors are on {device}, the current device is {torch.cuda.current_device()}")
-    args = [None if t is None else t.data_ptr() for t in tensors]
     if workspace_bytes is not None:
         workspace = torch.empty(workspace_bytes, dtype=torch.uint8, device=device) if workspace_bytes else None
-        args += [workspace.data_ptr() if workspace is not None else None, workspace_bytes]
+        args += (workspace.data_ptr() if workspace_bytes else None, workspace_bytes)
         tensors = (*tensors, workspace)
+    args += last
     current = torch._C._cuda_getCurrentRawStream(device.index)
     own = getattr(_b._thread, "stream", 0)
     if own and own != current:
@@ -113,13 +113,14 @@ def _call(entry, desc, tensors, workspace_bytes=None, last=()):
         for t in tensors:
             if t is not None:
                 t.record_stream(stream)
-        _b._check(entry(desc, *args, *last))
+        _b._check(entry(*args))
     elif own or not current:
-        _b._check(entry(desc, *args, *last))
+        _b._check(entry(*args))
     else:
+        L = _b.lib()
         L.nuts_set_stream(current)
         try:
-            _b._check(entry(desc, *args, *last))
+            _b._check(entry(*args))
         finally:
             L.nuts_set_stream(None)
 
@@ -130,7 +131,7 @@ def nuts_lookup(table, ids, *, scale=1.0, out=None):
     ids = _ids(ids, "ids")
     classes, dim = table.shape
     if out is None:
-        out = torch.empty((*ids.shape, dim), dtype=table.dtype, device=table.device)
+        out = table.new_empty((*ids.shape, dim))
     n = ids.numel()
     rows = out.view(n, dim) if out.dim() != 2 else out
     if rows.dtype != table.dtype:
@@ -151,7 +152,7 @@ def nuts_lookup_grad(grad, ids, n_classes, *, scale=1.0, out=None, accumulate=Fa
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = torch.empty((n_classes, dim), dtype=grad.dtype, device=grad.device)
+        out = grad.new_empty((n_classes, dim))
     elif out.dtype != grad.dtype:
         raise ValueError(f"out must be {grad.dtype}")
     _matrix(out, "out", shape=(n_classes, dim))
@@ -207,7 +208,7 @@ def nuts_logprobs_grad(logits, targets, lse, entropy=None, *, grad_logprob=None,
     allowed, allowed_stride = _mask(allowed, n, classes)
     desc, _ = _logits_desc(False, _DTYPES[logits.dtype], id_type, n, classes, _stride(logits), allowed_stride, float(scale), 0)
     if out is None:
-        out = torch.empty((n, classes), dtype=logits.dtype, device=logits.device)
+        out = logits.new_empty((n, classes))
     elif out.dtype != logits.dtype:
         raise ValueError(f"out must be {logits.dtype}")
     _matrix(out, "out", shape=(n, classes))
@@ -255,8 +256,8 @@ def nuts_score_grad(x, weight, targets, lse, entropy=None, *, grad_logprob=None,
     n, classes = x.shape[0], weight.shape[0]
     if logits is not None:
         _matrix(logits, "logits", {torch.float32: 0}, (n, classes))
-    grad_x = torch.empty((n, x.shape[1]), dtype=x.dtype, device=x.device) if want_x else None
-    grad_weight = torch.empty((classes, x.shape[1]), dtype=x.dtype, device=x.device) if want_weight else None
+    grad_x = x.new_empty((n, x.shape[1])) if want_x else None
+    grad_weight = x.new_empty((classes, x.shape[1])) if want_weight else None
     desc, size = _score_desc(True, *fields, _stride(logits) if logits is not None else classes, x.shape[1], x.shape[1], float(scale))
     _call(_b.lib().nuts_score_grad, desc,
           (x, weight, targets, logits, _per_row(lse, "lse", n), _per_row(entropy, "entropy", n), _per_row(grad_logprob, "grad_logprob", n),
