@@ -74,17 +74,15 @@ struct GradArgs {
     int id_type, accumulate, lane_bits;
 };
 
+// kN columns of a row, zeros where only `left` are left.
 template <typename T, int kN>
-__device__ __forceinline__ void load_columns(const T* p, int left, float (&x)[kN])
+__device__ __forceinline__ Pack<T, kN> load_part(const T* p, int left)
 {
-    if (left >= kN) {
-        const Pack<T, kN> in = load_pack<T, kN>(p);
+    if (left >= kN) return load_pack<T, kN>(p);
+    Pack<T, kN> x;
 #pragma unroll
-        for (int e = 0; e < kN; ++e) x[e] = to_float(in.v[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < kN; ++e) x[e] = e < left ? to_float(p[e]) : 0.f;
-    }
+    for (int e = 0; e < kN; ++e) x.v[e] = e < left ? p[e] : static_cast<T>(0.f);
+    return x;
 }
 
 // A class's finished sum to its row of the table's gradient.
@@ -124,81 +122,108 @@ __device__ __forceinline__ void zero_columns(T* p, int left)
 
 // ---- gradient of few rows: one launch --------------------------------------------------------------------------------
 
-constexpr int kFew = 1024;     // positions that a workgroup looks through by itself
-constexpr int kFewRows = 64;   // at most so many classes a workgroup (an occupancy mask is one word)
+constexpr int kFewEach = 4;                    // positions of a thread
+constexpr int kFew = kFewEach * kThreads;      // positions that a workgroup looks through by itself
+constexpr int kFewRows = 64;                   // at most so many classes a workgroup (an occupancy mask is one word)
 
 // A workgroup owns `classes` neighbouring rows of the table: it finds the positions of theirs among all n (few, from
-// cache), in ascending order, and adds them up.
+// cache) and adds them up.  What bounds it is the wait for memory, twice at least, and again for every 32 rows or so of
+// the class that comes most often.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int classes, long first_block)
 {
     constexpr int kN = 16 / sizeof(T);
+    constexpr int kFlight = 8;
     __shared__ int position[kFew];
     __shared__ unsigned char of_class[kFew];
-    __shared__ int found[kThreads / 64];
+    __shared__ int found[kFewEach][kThreads / 64];
     __shared__ unsigned occupied_half[2];
+    __shared__ int mine[kThreads / 64][64];    // a wave's class's among 64 positions
+    __shared__ float sums[kThreads / 64][kN][64];
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
     const long v0 = (first_block + blockIdx.x) * classes;
     const int own = (int)min((long)classes, a.n_classes - v0);
     if (threadIdx.x < 2) occupied_half[threadIdx.x] = 0u;
+    int id[kFewEach];
+    unsigned long long hits[kFewEach];
+#pragma unroll
+    for (int u = 0; u < kFewEach; ++u) {
+        const int i = u * kThreads + (int)threadIdx.x;
+        id[u] = i < a.n_ids ? class_at(a.ids, a.id_type, i, a.n_classes) : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kFewEach; ++u) {
+        hits[u] = __ballot(id[u] >= v0 && id[u] < v0 + own);
+        if (lane == 0) found[u][wave] = __popcll(hits[u]);
+    }
     __syncthreads();
     int count = 0;
-    for (int base = 0; base < a.n_ids; base += kThreads) {
-        const int i = base + threadIdx.x;
-        const int id = i < a.n_ids ? class_at(a.ids, a.id_type, i, a.n_classes) : -1;
-        const bool hit = id >= v0 && id < v0 + own;
-        const unsigned long long hits = __ballot(hit);
-        if (lane == 0) found[wave] = __popcll(hits);
-        __syncthreads();
-        int at = count;
+#pragma unroll
+    for (int u = 0; u < kFewEach; ++u)
+#pragma unroll
         for (int w = 0; w < kThreads / 64; ++w) {
-            if (w < wave) at += found[w];
-            count += found[w];
-        }
-        if (hit) {
-            at += __popcll(hits & ((1ull << lane) - 1));
-            position[at] = i;
-            of_class[at] = (unsigned char)(id - v0);
-            atomicOr(&occupied_half[(id - v0) >> 5], 1u << ((id - v0) & 31));
-        }
-        __syncthreads();
-    }
-    const unsigned long long occupied = occupied_half[0] | (unsigned long long)occupied_half[1] << 32;
-    const long packs = (a.dim + kN - 1) / kN;
-    T* table = static_cast<T*>(a.table);
-    const T* rows = static_cast<const T*>(a.rows);
-    // groups of 64 or of all threads go through the classes, a thread through its columns
-    const int lanes = 1 << a.lane_bits, group = threadIdx.x >> a.lane_bits;
-    for (int r = group; r < own; r += kThreads >> a.lane_bits) {
-        const bool any = occupied >> r & 1;
-        if (!any && a.accumulate) continue;
-        for (long p = threadIdx.x & (lanes - 1); p < packs; p += lanes) {
-            const long c = p * kN;
-            const int left = (int)min((long)kN, a.dim - c);
-            T* to = table + (v0 + r) * a.table_stride + c;
-            if (!any) {
-                zero_columns<T, kN>(to, left);
-                continue;
+            if (w == wave && (hits[u] >> lane & 1)) {
+                const int at = count + __popcll(hits[u] & ((1ull << lane) - 1)), c = (int)(id[u] - v0);
+                position[at] = u * kThreads + (int)threadIdx.x;
+                of_class[at] = (unsigned char)c;
+                atomicOr(&occupied_half[c >> 5], 1u << (c & 31));
             }
+            count += found[u][w];
+        }
+    __syncthreads();
+    const unsigned long long occupied = occupied_half[0] | (unsigned long long)occupied_half[1] << 32;
+    const int packs = (int)((a.dim + kN - 1) / kN);
+    T* table = static_cast<T*>(a.table) + v0 * a.table_stride;
+    const T* rows = static_cast<const T*>(a.rows);
+    if (!a.accumulate)
+        for (long i = threadIdx.x; i < (long)own * packs; i += kThreads) {
+            const int r = (int)(i / packs);
+            const long c = i % packs * kN;
+            if (!(occupied >> r & 1)) zero_columns<T, kN>(table + r * a.table_stride + c, (int)min((long)kN, a.dim - c));
+        }
+    // Each class is added up by the whole workgroup: a row is read by 2^lane_bits lanes of a wave (or by a wave in several
+    // turns), and every wave has a list of the class's positions for itself, of which its groups of lanes take turns.
+    const int lanes = 1 << a.lane_bits, workers = kThreads >> a.lane_bits, worker = threadIdx.x >> a.lane_bits;
+    for (unsigned long long rest = occupied; rest; rest &= rest - 1) {
+        const int r = __builtin_ctzll(rest);
+        for (int p = lane & (lanes - 1); p < ((packs + lanes - 1) & -lanes); p += lanes) {
+            const long c = (long)p * kN;
+            const int left = (int)max(0l, min((long)kN, a.dim - c));
             float sum[kN];
 #pragma unroll
             for (int e = 0; e < kN; ++e) sum[e] = 0.f;
-            for (int m = 0; m < count; m += 4) {  // four rows in flight
-                float x[4][kN];
-                bool mine[4];
+            for (int m = 0; m < count; m += 64) {
+                const bool hit = m + lane < count && of_class[m + lane] == r;
+                const unsigned long long all = __ballot(hit);
+                if (hit) mine[wave][__popcll(all & ((1ull << lane) - 1))] = position[m + lane];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                const int n = left > 0 ? __popcll(all) : 0;
+                for (int q = worker; q < n; q += workers * kFlight) {
+                    Pack<T, kN> x[kFlight];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    mine[u] = m + u < count && of_class[m + u] == r;
-                    if (mine[u]) load_columns<T, kN>(rows + (long)position[m + u] * a.row_stride + c, left, x[u]);
+                    for (int u = 0; u < kFlight; ++u)
+                        if (q + u * workers < n) x[u] = load_part<T, kN>(rows + (long)mine[wave][q + u * workers] * a.row_stride + c, left);
+#pragma unroll
+                    for (int u = 0; u < kFlight; ++u)
+                        if (q + u * workers < n) {
+#pragma unroll
+                            for (int e = 0; e < kN; ++e) sum[e] += to_float(x[u].v[e]);
+                        }
                 }
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (mine[u]) {
-#pragma unroll
-                        for (int e = 0; e < kN; ++e) sum[e] += x[u][e];
-                    }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
-            finish_columns<T, kN>(a, to, left, sum);
+            for (int step = lanes; step < 64; step *= 2)
+#pragma unroll
+                for (int e = 0; e < kN; ++e) sum[e] += __shfl_xor(sum[e], step);
+#pragma unroll
+            for (int e = 0; e < kN; ++e) sums[wave][e][lane] = sum[e];
+            __syncthreads();
+            if (wave == 0 && lane < lanes && left > 0) {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) sum[e] = (sums[0][e][lane] + sums[1][e][lane]) + (sums[2][e][lane] + sums[3][e][lane]);
+                finish_columns<T, kN>(a, table + r * a.table_stride + c, left, sum);
+            }
+            __syncthreads();
         }
     }
 }
@@ -211,6 +236,9 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int clas
 
 constexpr int kMaxDigitBits = 11;
 constexpr int kWaves = kThreads / 64;
+// rounds of a tile: short tiles while the counts of all of them are little work for one workgroup
+constexpr int kFewRounds = 4, kManyRounds = 16;
+constexpr long kManyIds = 1l << 17;
 
 struct SortArgs {
     const void* ids;          // first digit: the classes themselves; else keys_in, pos_in
@@ -241,7 +269,15 @@ __global__ __launch_bounds__(kThreads) void count_kernel(SortArgs a)
     for (int d = threadIdx.x; d < digits; d += kThreads) count[d] = 0;
     __syncthreads();
     const long begin = (long)blockIdx.x * a.tile, end = min(begin + a.tile, a.n_ids);
-    for (long i = begin + threadIdx.x; i < end; i += kThreads) atomicAdd(&count[key_at<kFirst>(a, i) >> a.shift & (digits - 1)], 1u);
+    for (long i = begin + threadIdx.x; i < end; i += 4 * kThreads) {
+        unsigned key[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + u * kThreads < end) key[u] = key_at<kFirst>(a, i + u * kThreads);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + u * kThreads < end) atomicAdd(&count[key[u] >> a.shift & (digits - 1)], 1u);
+    }
     __syncthreads();
     for (int d = threadIdx.x; d < digits; d += kThreads) a.counts[(long)blockIdx.x * digits + d] = count[d];
     if (kFirst && a.present) {  // nothing is present yet
@@ -258,12 +294,12 @@ __global__ __launch_bounds__(1024) void places_kernel(SortArgs a)
     for (int d = threadIdx.x; d < digits; d += 1024) {
         unsigned sum = 0;
         int t = 0;
-        for (; t + 8 <= a.tiles; t += 8) {  // eight reads in flight
-            unsigned c[8];
+        for (; t + 16 <= a.tiles; t += 16) {  // sixteen reads in flight
+            unsigned c[16];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) c[u] = a.counts[(long)(t + u) * digits + d];
+            for (int u = 0; u < 16; ++u) c[u] = a.counts[(long)(t + u) * digits + d];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < 16; ++u) {
                 a.counts[(long)(t + u) * digits + d] = sum;
                 sum += c[u];
             }
@@ -291,18 +327,26 @@ __global__ __launch_bounds__(1024) void places_kernel(SortArgs a)
     }
 }
 
-// A wave places its run of the tile 64 positions at a time: lanes that hold the same digit find each other by a ballot for each bit.
-template <bool kFirst>
+// A wave places its run of the tile, kRounds times 64 positions: lanes that hold the same digit find each other by a ballot for each bit.
+template <bool kFirst, int kRounds>
 __global__ __launch_bounds__(kThreads) void place_kernel(SortArgs a)
 {
     extern __shared__ unsigned next[];  // [wave][digit]
     const int digits = 1 << a.digit_bits, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const long begin = (long)blockIdx.x * a.tile + wave * kRounds * 64 + lane;
+    unsigned key[kRounds], pos[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+        if (begin + r * 64 < a.n_ids) {
+            key[r] = key_at<kFirst>(a, begin + r * 64);
+            pos[r] = kFirst ? (unsigned)(begin + r * 64) : a.pos_in[begin + r * 64];
+        }
     for (int d = threadIdx.x; d < kWaves * digits; d += kThreads) next[d] = 0;
     __syncthreads();
-    const long tile_begin = (long)blockIdx.x * a.tile, run = a.tile / kWaves;
-    const long begin = tile_begin + wave * run, end = min(begin + run, a.n_ids);
     unsigned* own = next + wave * digits;
-    for (long i = begin + lane; i < end; i += 64) atomicAdd(&own[key_at<kFirst>(a, i) >> a.shift & (digits - 1)], 1u);
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+        if (begin + r * 64 < a.n_ids) atomicAdd(&own[key[r] >> a.shift & (digits - 1)], 1u);
     __syncthreads();
     for (int d = threadIdx.x; d < digits; d += kThreads) {
         unsigned at = a.starts[d] + a.counts[(long)blockIdx.x * digits + d];
@@ -313,11 +357,10 @@ __global__ __launch_bounds__(kThreads) void place_kernel(SortArgs a)
         }
     }
     __syncthreads();
-    for (long base = begin; base < end; base += 64) {
-        const long i = base + lane;
-        const bool valid = i < end;
-        const unsigned key = valid ? key_at<kFirst>(a, i) : 0u;
-        const unsigned digit = key >> a.shift & (digits - 1);
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const bool valid = begin + r * 64 < a.n_ids;
+        const unsigned digit = valid ? key[r] >> a.shift & (digits - 1) : 0u;
         unsigned long long same = __ballot(valid);
         for (int b = 0; b < a.digit_bits; ++b) {
             const bool set = digit >> b & 1;
@@ -330,9 +373,9 @@ __global__ __launch_bounds__(kThreads) void place_kernel(SortArgs a)
         if (valid && before == 0) own[digit] = start + (unsigned)__popcll(same);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (valid) {
-            a.keys_out[start + before] = key;
-            a.pos_out[start + before] = kFirst ? (unsigned)i : a.pos_in[i];
-            if (kFirst && a.present && key < (unsigned long)a.n_classes) a.present[key] = 1;
+            a.keys_out[start + before] = key[r];
+            a.pos_out[start + before] = pos[r];
+            if (kFirst && a.present && key[r] < (unsigned long)a.n_classes) a.present[key[r]] = 1;
         }
     }
 }
@@ -344,10 +387,14 @@ struct SumArgs {
     const unsigned* keys;
     const unsigned* pos;
     const unsigned char* present;  // NULL: no rows to clear
-    float* part;                   // [chunk][2][dim]
-    long chunks, sum_blocks;       // (of the first column block)
+    float* part;                   // [chunk][2][part_stride]
+    long chunks, sum_blocks, part_stride;
     int chunk;                     // positions in a chunk
 };
+
+constexpr int kBatch = 32;         // positions whose keys are read at once; a chunk is a multiple
+constexpr int kClear = 16;         // neighbouring classes that a group looks at to clear them
+constexpr int kLeastLanes = 3;     // groups of 8 threads and more: at most 32 in a workgroup
 
 // A group of 2^lane_bits threads adds the rows of one chunk of the sorted positions, a thread 16 bytes of columns.  A class that
 // lies wholly in the chunk is finished; what belongs to one that began before goes to the chunk's part 0, to one that begins
@@ -357,107 +404,141 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a)
 {
     constexpr int kN = 16 / sizeof(T);
     constexpr int kFlight = 8;
-    const int lanes = 1 << a.g.lane_bits, groups = kThreads >> a.g.lane_bits;
+    __shared__ unsigned keys[kThreads >> kLeastLanes][kBatch], positions[kThreads >> kLeastLanes][kBatch];
+    const int lanes = 1 << a.g.lane_bits, groups = kThreads >> a.g.lane_bits, group = threadIdx.x >> a.g.lane_bits;
+    const int lane = threadIdx.x & (lanes - 1);
     T* table = static_cast<T*>(a.g.table);
-    const long c = ((long)blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * kN;
-    if (c >= a.g.dim) return;
-    const int left = (int)min((long)kN, a.g.dim - c);
+    const long c = ((long)blockIdx.y * lanes + lane) * kN;
+    const int left = (int)max(0l, min((long)kN, a.g.dim - c));
     if ((long)blockIdx.x >= a.sum_blocks) {
-        const long step = ((long)gridDim.x - a.sum_blocks) * groups;
-        for (long v = ((long)blockIdx.x - a.sum_blocks) * groups + (threadIdx.x >> a.g.lane_bits); v < a.g.n_classes; v += step)
-            if (!a.present[v]) zero_columns<T, kN>(table + v * a.g.table_stride + c, left);
+        const long step = ((long)gridDim.x - a.sum_blocks) * groups * kClear;
+        for (long v = (((long)blockIdx.x - a.sum_blocks) * groups + group) * kClear; v < a.g.n_classes; v += step) {
+            const uint4 flags = *reinterpret_cast<const uint4*>(a.present + v);  // (padded to whole words)
+            const unsigned word[4] = {flags.x, flags.y, flags.z, flags.w};
+#pragma unroll
+            for (int r = 0; r < kClear; ++r)
+                if (left > 0 && v + r < a.g.n_classes && !(word[r / 4] >> (r % 4 * 8) & 0xff)) zero_columns<T, kN>(table + (v + r) * a.g.table_stride + c, left);
+        }
         return;
     }
-    const long q = (long)blockIdx.x * groups + (threadIdx.x >> a.g.lane_bits);
-    if (q >= a.chunks) return;
-    const long begin = q * a.chunk, end = min(begin + a.chunk, a.g.n_ids);
-    const T* rows = static_cast<const T*>(a.g.rows);
+    const long q = (long)blockIdx.x * groups + group;
+    const long begin = min(q * a.chunk, a.g.n_ids), end = min(begin + a.chunk, a.g.n_ids);
+    const T* rows = static_cast<const T*>(a.g.rows) + c;
     const unsigned none = (unsigned)a.g.n_classes;
     const unsigned before = begin > 0 ? a.keys[begin - 1] : none, after = end < a.g.n_ids ? a.keys[end] : none;
     float sum[kN];
 #pragma unroll
     for (int e = 0; e < kN; ++e) sum[e] = 0.f;
-    unsigned current = a.keys[begin];
-    bool entered = current == before;  // the class began in an earlier chunk
+    unsigned current = none;
+    bool entered = false;  // the class began in an earlier chunk
     auto flush = [&](bool open) {
-        if (current == none) return;
-        if (entered || open) {
-            float* to = a.part + (q * 2 + (entered ? 0 : 1)) * a.g.dim + c;
+        if (current == none || left == 0) return;
+        if (entered || open) {  // (parts are padded to whole packs)
+            float* to = a.part + (q * 2 + (entered ? 0 : 1)) * a.part_stride + c;
 #pragma unroll
-            for (int e = 0; e < kN; ++e)
-                if (e < left) to[e] = sum[e];
+            for (int e = 0; e < kN; e += 4) *reinterpret_cast<float4*>(to + e) = float4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
         } else {
             finish_columns<T, kN>(a.g, table + current * a.g.table_stride + c, left, sum);
         }
     };
-    for (long i = begin; i < end; i += kFlight) {
-        unsigned key[kFlight];
-        float x[kFlight][kN];
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u) {
-            key[u] = i + u < end ? a.keys[i + u] : none;
-            if (key[u] != none) load_columns<T, kN>(rows + (long)a.pos[i + u] * a.g.row_stride + c, left, x[u]);
+    for (int batch = 0; batch < a.chunk; batch += kBatch) {
+        const long first = begin + batch;
+        for (int i = lane; i < kBatch; i += lanes) {
+            keys[group][i] = first + i < end ? a.keys[first + i] : none;
+            positions[group][i] = first + i < end ? a.pos[first + i] : 0u;
         }
+        __syncthreads();
+        if (batch == 0) {
+            current = keys[group][0];
+            entered = current == before;
+        }
+        for (int i = 0; i < kBatch && keys[group][i] != none; i += kFlight) {  // (no class: such keys are the last)
+            Pack<T, kN> x[kFlight];
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u) {
-            if (key[u] == none) continue;  // (no class: such keys are the last)
-            if (key[u] != current) {
-                flush(false);
-                current = key[u];
-                entered = false;
+            for (int u = 0; u < kFlight; ++u)
+                if (keys[group][i + u] != none && left > 0) x[u] = load_part<T, kN>(rows + (long)positions[group][i + u] * a.g.row_stride, left);
 #pragma unroll
-                for (int e = 0; e < kN; ++e) sum[e] = x[u][e];
-            } else {
+            for (int u = 0; u < kFlight; ++u) {
+                const unsigned key = keys[group][i + u];
+                if (key == none) break;
+                if (key != current) {
+                    flush(false);
+                    current = key;
+                    entered = false;
 #pragma unroll
-                for (int e = 0; e < kN; ++e) sum[e] += x[u][e];
+                    for (int e = 0; e < kN; ++e) sum[e] = 0.f;
+                }
+                if (left > 0) {
+#pragma unroll
+                    for (int e = 0; e < kN; ++e) sum[e] += to_float(x[u].v[e]);
+                }
             }
         }
+        __syncthreads();
     }
     flush(current == after);
 }
 
-// Classes that reach over chunks: the group of the chunk in which one begins joins its parts, in order.
+// Classes that reach over chunks: the workgroups of the chunk in which one begins join its parts.  Each of the four waves adds every
+// fourth part, in order, four columns a thread; then the waves' sums are added in order.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void join_kernel(SumArgs a)
 {
-    constexpr int kN = 16 / sizeof(T);
     constexpr int kFlight = 8;
-    const int lanes = 1 << a.g.lane_bits, groups = kThreads >> a.g.lane_bits;
-    const long c = ((long)blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * kN;
-    const long q = (long)blockIdx.x * groups + (threadIdx.x >> a.g.lane_bits);
-    if (c >= a.g.dim || q + 1 >= a.chunks) return;  // (the last chunk's classes end in it)
-    const int left = (int)min((long)kN, a.g.dim - c);
+    __shared__ int over[kThreads / 64];
+    __shared__ float4 sums[kThreads / 64][64];
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const long q = blockIdx.x, begin = q * a.chunk, end = begin + a.chunk;  // (the last chunk's classes end in it and have no workgroup)
     const unsigned none = (unsigned)a.g.n_classes;
-    const long begin = q * a.chunk, end = begin + a.chunk;
-    const unsigned key = a.keys[end - 1];
-    if (key == none || a.keys[end] != key) return;
-    if (begin > 0 && a.keys[begin - 1] == key) return;  // it began earlier
-    long low = end, high = a.g.n_ids;  // the first position behind the class: in (low, high]
-    while (high - low > 1) {
-        const long mid = (low + high) / 2;
-        (a.keys[mid] == key ? low : high) = mid;
+    const unsigned key = a.keys[end - 1], next = a.keys[end], before = begin > 0 ? a.keys[begin - 1] : none;
+    if (key == none || next != key || before == key) return;
+    // the chunks behind this one that the class goes on beyond: all of the first, and then none
+    long more = 0;
+    for (long first = q + 1;; first += kThreads) {
+        const long r = first + threadIdx.x;
+        const bool goes_on = (r + 1) * a.chunk < a.g.n_ids && a.keys[(r + 1) * a.chunk] == key;
+        const unsigned long long all = __ballot(goes_on);
+        if (lane == 0) over[wave] = __popcll(all);
+        __syncthreads();
+        int here = 0;
+        for (int w = 0; w < kThreads / 64; ++w) here += over[w];
+        __syncthreads();
+        more += here;
+        if (here < kThreads) break;
     }
-    const long last = low / a.chunk;
-    float sum[kN];
-    const float* part = a.part + c;
+    const long parts = more + 2;  // this chunk's, those of the chunks that it goes on beyond, that of the one where it ends
+    const long c = ((long)blockIdx.y * 64 + lane) * 4;
+    const bool inside = c < a.part_stride;
+    const float* part = a.part + q * 2 * a.part_stride + c;
+    float4 sum{0.f, 0.f, 0.f, 0.f};
+    for (long r = wave; r < parts; r += kThreads / 64 * kFlight) {
+        float4 x[kFlight];
 #pragma unroll
-    for (int e = 0; e < kN; ++e) sum[e] = e < left ? part[(q * 2 + 1) * a.g.dim + e] : 0.f;
-    for (long r = q + 1; r <= last; r += kFlight) {
-        float x[kFlight][kN];
+        for (int u = 0; u < kFlight; ++u) {
+            const long at = r + u * (kThreads / 64);
+            if (at < parts && inside) x[u] = *reinterpret_cast<const float4*>(part + (at * 2 + (at == 0 ? 1 : 0)) * a.part_stride);
+        }
 #pragma unroll
         for (int u = 0; u < kFlight; ++u)
-            if (r + u <= last) {
-#pragma unroll
-                for (int e = 0; e < kN; ++e) x[u][e] = e < left ? part[(r + u) * 2 * a.g.dim + e] : 0.f;
-            }
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u)
-            if (r + u <= last) {
-#pragma unroll
-                for (int e = 0; e < kN; ++e) sum[e] += x[u][e];
+            if (r + u * (kThreads / 64) < parts && inside) {
+                sum.x += x[u].x;
+                sum.y += x[u].y;
+                sum.z += x[u].z;
+                sum.w += x[u].w;
             }
     }
-    finish_columns<T, kN>(a.g, static_cast<T*>(a.g.table) + key * a.g.table_stride + c, left, sum);
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || c >= a.g.dim) return;
+    float total[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < kThreads / 64; ++w) {
+        const float4 x = sums[w][lane];
+        total[0] += x.x;
+        total[1] += x.y;
+        total[2] += x.z;
+        total[3] += x.w;
+    }
+    finish_columns<T, 4>(a.g, static_cast<T*>(a.g.table) + key * a.g.table_stride + c, (int)min(4l, a.g.dim - c), total);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
@@ -492,7 +573,7 @@ struct GradPlan {
     int few_classes;
     int digit_bits, passes, tile, tiles;
     int chunk;
-    long chunks;
+    long chunks, part_stride;
     // offsets into the workspace
     size_t counts, starts, keys[2], pos[2], present, part, bytes;
 };
@@ -510,11 +591,11 @@ GradPlan plan_grad(const nuts_lookup_desc* d)
     while (d->n_classes >> bits) ++bits;  // n_classes itself is a key
     p.passes = (bits + kMaxDigitBits - 1) / kMaxDigitBits;
     p.digit_bits = (bits + p.passes - 1) / p.passes;
-    p.tile = d->n_ids <= (1 << 17) ? 2048 : 8192;
+    p.tile = (d->n_ids <= kManyIds ? kFewRounds : kManyRounds) * kThreads;
     p.tiles = (int)ceil_div(d->n_ids, p.tile);
-    // chunks: short enough that there are thousands, long enough that a class over many of them is joined from few parts
-    p.chunk = 32;
-    while (d->n_ids / p.chunk > 4096) p.chunk *= 2;
+    // chunks: short enough that there are a thousand workgroups, long enough that a class over many of them is joined from few parts
+    p.chunk = kBatch;
+    while (d->n_ids / (p.chunk * 2) >= 1024 * (int64_t)(kThreads >> lane_bits_of(d->dim, d->dtype, kLeastLanes))) p.chunk *= 2;
     p.chunks = ceil_div(d->n_ids, p.chunk);
     auto take = [&](size_t bytes) {
         const size_t at = p.bytes;
@@ -527,8 +608,9 @@ GradPlan plan_grad(const nuts_lookup_desc* d)
         p.keys[s] = take(sizeof(unsigned) * d->n_ids);
         p.pos[s] = take(sizeof(unsigned) * d->n_ids);
     }
-    p.present = take((size_t)d->n_classes + 16);
-    p.part = take((size_t)p.chunks * 2 * d->dim * sizeof(float));
+    p.present = take((size_t)d->n_classes + kClear);
+    p.part_stride = (long)(ceil_div(d->dim, 8) * 8);
+    p.part = take((size_t)p.chunks * 2 * p.part_stride * sizeof(float));
     return p;
 }
 
@@ -583,7 +665,7 @@ int nuts_lookup_grad(const nuts_lookup_desc* d, const void* grad_rows, const voi
     a.g = GradArgs{grad_rows, ids, grad_table, (long)d->n_ids, (long)d->n_classes, (long)d->dim, (long)d->table_stride, (long)d->row_stride,
                    (float)d->scale, d->id_type, d->accumulate, 0};
     if (p.few) {
-        a.g.lane_bits = lane_bits_of(d->dim, d->dtype, 6) > 6 ? 8 : 6;
+        a.g.lane_bits = std::min(6, lane_bits_of(d->dim, d->dtype, 0));
         by_dtype(d->dtype, [&](auto t) {
             for (long first = 0, blocks = (long)ceil_div(d->n_classes, p.few_classes); first < blocks; first += kMaxBlocks)
                 hipLaunchKernelGGL(few_rows_kernel<decltype(t)>, dim3((unsigned)std::min(blocks - first, kMaxBlocks)), dim3(kThreads), 0, stream, a.g,
@@ -602,7 +684,9 @@ int nuts_lookup_grad(const nuts_lookup_desc* d, const void* grad_rows, const voi
         const size_t lds = (size_t)kWaves * sizeof(unsigned) << p.digit_bits;
         hipLaunchKernelGGL(k == 0 ? count_kernel<true> : count_kernel<false>, dim3(p.tiles), dim3(kThreads), 0, stream, s);
         hipLaunchKernelGGL(places_kernel, dim3(1), dim3(1024), 0, stream, s);
-        hipLaunchKernelGGL(k == 0 ? place_kernel<true> : place_kernel<false>, dim3(p.tiles), dim3(kThreads), lds, stream, s);
+        void (*place)(SortArgs) = d->n_ids <= kManyIds ? (k == 0 ? place_kernel<true, kFewRounds> : place_kernel<false, kFewRounds>)
+                                                       : (k == 0 ? place_kernel<true, kManyRounds> : place_kernel<false, kManyRounds>);
+        hipLaunchKernelGGL(place, dim3(p.tiles), dim3(kThreads), lds, stream, s);
     }
     a.keys = reinterpret_cast<unsigned*>(w + p.keys[(p.passes - 1) & 1]);
     a.pos = reinterpret_cast<unsigned*>(w + p.pos[(p.passes - 1) & 1]);
@@ -610,16 +694,18 @@ int nuts_lookup_grad(const nuts_lookup_desc* d, const void* grad_rows, const voi
     a.part = reinterpret_cast<float*>(w + p.part);
     a.chunks = p.chunks;
     a.chunk = p.chunk;
-    a.g.lane_bits = lane_bits_of(d->dim, d->dtype, 0);
+    a.part_stride = p.part_stride;
+    a.g.lane_bits = lane_bits_of(d->dim, d->dtype, kLeastLanes);
     const int groups = kThreads >> a.g.lane_bits;
     const int64_t columns = (int64_t)(16 / cat_size(d->dtype)) << a.g.lane_bits;
     a.sum_blocks = (long)ceil_div(p.chunks, groups);
-    const unsigned clear = present ? (unsigned)std::min<int64_t>(ceil_div(d->n_classes, groups), 4096) : 0u;
+    const unsigned clear = present ? (unsigned)std::min<int64_t>(ceil_div(d->n_classes, groups * kClear), 1 << 16) : 0u;
     const unsigned slices = (unsigned)ceil_div(d->dim, columns);
     by_dtype(d->dtype, [&](auto t) {
         using T = decltype(t);
         hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)a.sum_blocks + clear, slices), dim3(kThreads), 0, stream, a);
-        hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)a.sum_blocks, slices), dim3(kThreads), 0, stream, a);
+        if (p.chunks > 1)
+            hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)(p.chunks - 1), (unsigned)ceil_div(d->dim, 256)), dim3(kThreads), 0, stream, a);
     });
     NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
     return NUTS_OK;
