@@ -293,7 +293,7 @@ typedef struct {
     int32_t dtype;          /* of the logits and their gradient                                            */
     int32_t id_type;        /* of the targets                                                              */
     int64_t n_rows;         /* 0 .. 2^31 - 2                                                               */
-    int64_t n_classes;      /* 1 .. 2^31 - 2^16 - 1                                                        */
+    int64_t n_classes;      /* 1 .. 2^31 - 2^18 - 1                                                        */
     int64_t row_stride;     /* of the logits, >= n_classes                                                 */
     int64_t allowed_stride; /* 32-bit words from one row of `allowed` to the next; 0: one row for all      */
     double scale;           /* z = scale * logits; finite, > 0 (a temperature is 1 / scale)                */

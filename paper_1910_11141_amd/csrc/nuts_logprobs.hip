@@ -85,59 +85,62 @@ __device__ __forceinline__ unsigned load_logits(const T* row, const uint32_t* al
     return may;
 }
 
-// The n_top largest of the workgroup's keys, which `each` goes through (thread by thread, in any order): sorted[0 .. n_top - 1].
-// `best`: the largest logit of this thread's, NaNs aside.  The n_top-th largest of these is no larger than the n_top-th largest
-// logit, so what is below it need not be looked at twice: a few logits more than n_top are left and get their
-// rank by counting.  Rows with very many equal ones (or fewer finite ones than threads) leave too many: then the largest is
-// looked for n_top times.
-template <typename F>
-__device__ void select_top(int n_top, float best, bool has_nan, unsigned long long* sorted, F each)
+// The n_top largest of a workgroup's logits, sorted: `collect(least, see)` goes through those of them that are `least` or more (or
+// NaN) and `every(see)` through all, thread by thread, in any order.  `best`: the largest of this thread's, NaNs aside.
+// Four threads' best make a group's, of which there are 64, and the n_top-th largest of these is no larger than the n_top-th
+// largest logit: what is below it need not be looked at twice.  A few logits more than n_top are left and get
+// their ranks by counting.  Rows with very many equal ones (or fewer finite ones than groups) leave too many: then the largest
+// is looked for n_top times.
+template <typename Collect, typename Every>
+__device__ void select_top(int n_top, float best, unsigned long long* sorted, Collect collect, Every every)
 {
-    __shared__ unsigned long long candidate[kCandidates];
-    __shared__ float bests[kThreads];
+    __shared__ __attribute__((aligned(16))) unsigned long long candidate[kCandidates];
+    __shared__ __attribute__((aligned(16))) float bests[64];
     __shared__ unsigned long long most[kWaves];
-    __shared__ float threshold;
     __shared__ int count;
-    bests[threadIdx.x] = best;
+    float group = fmaxf(best, __shfl_xor(best, 1));
+    group = fmaxf(group, __shfl_xor(group, 2));
+    if (threadIdx.x % 4 == 0) bests[threadIdx.x / 4] = group;
     if (threadIdx.x == 0) count = 0;
     if (threadIdx.x < (unsigned)n_top) sorted[threadIdx.x] = 0;
     __syncthreads();
+    const int lane = threadIdx.x % 64;
+    const float own = bests[lane];
     int rank = 0;
-    for (int i = 0; i < kThreads; i += 4) {
+#pragma unroll
+    for (int i = 0; i < 64; i += 4) {
         const float4 other = *reinterpret_cast<const float4*>(&bests[i]);
-        rank += (other.x > best || (other.x == best && i < (int)threadIdx.x)) + (other.y > best || (other.y == best && i + 1 < (int)threadIdx.x)) +
-                (other.z > best || (other.z == best && i + 2 < (int)threadIdx.x)) + (other.w > best || (other.w == best && i + 3 < (int)threadIdx.x));
+        rank += (other.x > own || (other.x == own && i < lane)) + (other.y > own || (other.y == own && i + 1 < lane)) +
+                (other.z > own || (other.z == own && i + 2 < lane)) + (other.w > own || (other.w == own && i + 3 < lane));
     }
-    if (rank == n_top - 1) threshold = best;
-    __syncthreads();
-    const float least = threshold;
-    if (best >= least || has_nan)
-        each([&](float x, int v) {
-            if (x >= least || x != x) {
-                const int at = atomicAdd(&count, 1);
-                if (at < kCandidates) candidate[at] = key_of(x, v);
-            }
-        });
+    const float least = __shfl(own, __builtin_ctzll(__ballot(rank == n_top - 1)));
+    collect(least, [&](float x, int v) {
+        if (x >= least || x != x) {
+            const int at = atomicAdd(&count, 1);
+            if (at < kCandidates) candidate[at] = key_of(x, v);
+        }
+    });
     __syncthreads();
     const int n = count;
     if (n <= kCandidates) {
         for (int i = threadIdx.x; i < n; i += kThreads) {
-            const unsigned long long own = candidate[i];
+            const unsigned long long key = candidate[i];
             int r = 0;
-            for (int j = 0; j < n; ++j) r += candidate[j] > own;
-            if (r < n_top) sorted[r] = own;
+#pragma unroll 8
+            for (int k = 0; k < n; ++k) r += candidate[k] > key;
+            if (r < n_top) sorted[r] = key;
         }
     } else {
         unsigned long long last = ~0ull;
         for (int r = 0; r < n_top; ++r) {
             unsigned long long next = 0;
-            each([&](float x, int v) {
+            every([&](float x, int v) {
                 const unsigned long long key = key_of(x, v);
                 if (key < last && key > next) next = key;
             });
 #pragma unroll
             for (int step = 32; step >= 1; step /= 2) next = max(next, (unsigned long long)__shfl_xor(next, step));
-            if (threadIdx.x % 64 == 0) most[threadIdx.x / 64] = next;
+            if (lane == 0) most[threadIdx.x / 64] = next;
             __syncthreads();
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) next = max(next, most[w]);
@@ -158,20 +161,24 @@ __device__ __forceinline__ void write_top(const LogitsArgs& a, long row, const R
     if (a.top_logprobs) a.top_logprobs[row * a.n_top + threadIdx.x] = key ? logprob_of(r, logit_of(key), a.scale) : -INFINITY;
 }
 
-// Thread 0 reads the row's target (and its logit) before it reads the row, and writes the results.
+// Thread 0 asks for the row's target before the row is read, for its logit behind that, and writes the results.
 struct Target {
+    long id;
     int y;
     float x;
 };
-template <typename T>
-__device__ __forceinline__ Target target_of(const LogitsArgs& a, long row)
+__device__ __forceinline__ void ask_target(const LogitsArgs& a, long row, Target& t)
 {
-    Target t{-1, -INFINITY};
-    if (threadIdx.x != 0 || !a.targets || !a.logprob) return t;
-    t.y = class_at(a.targets, a.id_type, row, a.n_classes);
-    if (t.y >= 0 && may_come(a.allowed ? a.allowed + row * a.allowed_stride : nullptr, t.y))
-        t.x = to_float(static_cast<const T*>(a.logits)[row * a.row_stride + t.y]);
-    return t;
+    t = Target{-1, -1, -INFINITY};
+    if (threadIdx.x == 0 && a.targets && a.logprob)
+        t.id = a.id_type == NUTS_I64 ? static_cast<const int64_t*>(a.targets)[row] : static_cast<const int32_t*>(a.targets)[row];
+}
+template <typename T>
+__device__ __forceinline__ void ask_logit(const LogitsArgs& a, long row, Target& t)
+{
+    if (t.id < 0 || t.id >= a.n_classes) return;
+    t.y = (int)t.id;
+    if (may_come(a.allowed ? a.allowed + row * a.allowed_stride : nullptr, t.y)) t.x = to_float(static_cast<const T*>(a.logits)[row * a.row_stride + t.y]);
 }
 __device__ __forceinline__ void write_row(const LogitsArgs& a, long row, const Row& r, const Target& t)
 {
@@ -180,6 +187,28 @@ __device__ __forceinline__ void write_row(const LogitsArgs& a, long row, const R
     if (a.entropy) a.entropy[row] = r.entropy;
     if (a.logprob) a.logprob[row] = t.y >= 0 ? logprob_of(r, t.x, a.scale) : 0.f;
 }
+
+// kCount packs of a thread, kThreads packs apart, from `at` on; none behind `end`.
+template <typename T, int kN, bool kMask, int kCount>
+struct Packs {
+    float x[kCount * kN];
+    unsigned may[kCount];
+    __device__ __forceinline__ void load(const T* row, const uint32_t* allowed, int at, int end)
+    {
+#pragma unroll
+        for (int u = 0; u < kCount; ++u) {
+            const int v = at + u * kThreads * kN;
+            float(&to)[kN] = *reinterpret_cast<float(*)[kN]>(&x[u * kN]);
+            may[u] = 0;
+            if (v < end) {
+                may[u] = load_logits<T, kN, kMask>(row, allowed, v, end, to);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) to[e] = -INFINITY;
+            }
+        }
+    }
+};
 
 // One workgroup a row, or a part of one where there are few rows (kWhole = false: join_rows_kernel ends them).
 template <typename T, bool kMask, bool kTop, bool kWhole>
@@ -194,39 +223,87 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogitsArgs a)
     const T* x_row = static_cast<const T*>(a.logits) + row * a.row_stride;
     const uint32_t* allowed = kMask ? a.allowed + row * a.allowed_stride : nullptr;
     const float c = a.scale * kLog2e;
-    const Target target = kWhole ? target_of<T>(a, row) : Target{-1, 0.f};
+    Target target;
+    if (kWhole) ask_target(a, row, target);
     Stats v{-INFINITY, 0.f, 0.f};
-    // four packs of a thread at a time, all in flight before the first is used; the maximum is settled once for all of them
-    constexpr int kFlight = 4;
+    // Four packs of a thread at a time, the next four under way while these are added up; the maximum is settled once for all of them.
+    constexpr int kFlight = 4, kStep = kFlight * kThreads * kN;
     int at = begin + (int)threadIdx.x * kN;
-    for (; at < end - (kFlight - 1) * kThreads * kN - (kN - 1); at += kFlight * kThreads * kN) {
-        float x[kFlight][kN], all[kFlight * kN];
+    const int last = end - (kFlight - 1) * kThreads * kN - kN;  // where four whole packs still fit
+    if (at <= last) {
+        Pack<T, kN> next[kFlight];
+        unsigned may[kFlight];
+        auto fetch = [&](int from) {
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u) load_logits<T, kN, kMask>(x_row, allowed, at + u * kThreads * kN, end, x[u]);
+            for (int u = 0; u < kFlight; ++u) {
+                const int i = from + u * kThreads * kN;
+                next[u] = load_pack<T, kN>(x_row + i);
+                if (kMask) may[u] = reinterpret_cast<const unsigned char*>(allowed)[i >> 3] >> (i & 7);
+            }
+        };
+        fetch(at);
+        while (true) {
+            float x[kFlight * kN];
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u)
+            for (int u = 0; u < kFlight; ++u)
 #pragma unroll
-            for (int e = 0; e < kN; ++e) all[u * kN + e] = x[u][e];
-        add_logits<kFlight * kN>(v, all, c);
+                for (int e = 0; e < kN; ++e) x[u * kN + e] = kMask && !(may[u] >> e & 1) ? -INFINITY : to_float(next[u].v[e]);
+            at += kStep;
+            const bool more = at <= last;
+            if (more) fetch(at);
+            add_logits<kFlight * kN>(v, x, c);
+            if (!more) break;
+        }
     }
-    for (; at < end; at += kThreads * kN) {
-        float x[kN];
-        load_logits<T, kN, kMask>(x_row, allowed, at, end, x);
-        add_logits<kN>(v, x, c);
+    if (at < end) {
+        Packs<T, kN, kMask, kFlight> rest;
+        rest.load(x_row, allowed, at, end);
+        add_logits<kFlight * kN>(v, rest.x, c);
     }
+    if (kWhole) ask_logit<T>(a, row, target);
     const float best = v.m;
     const bool has_nan = v.s != v.s;
     const Stats all = join_block(v, c, shared);
-    if (kTop)
-        select_top(a.n_top, best, has_nan, sorted, [&](auto see) {
-            for (int i = begin + (int)threadIdx.x * kN; i < end; i += kThreads * kN) {
+    if (kTop) {
+        // all logits of the threads in `mine` (of this wave): each thread its own, or, where few are asked for, a thread's by the whole wave
+        auto look = [&](unsigned long long mine, auto see) {
+            const int each = (end - begin + kThreads * kN - 1) / (kThreads * kN);  // packs of a thread
+            const int lane = threadIdx.x % 64;
+            auto see_pack = [&](int i) {
                 float x[kN];
                 const unsigned may = load_logits<T, kN, kMask>(x_row, allowed, i, end, x);
 #pragma unroll
                 for (int e = 0; e < kN; ++e)
                     if (may >> e & 1) see(x[e], i + e);
+            };
+            if (__popcll(mine) * ((each + 63) / 64) <= (each + kFlight - 1) / kFlight) {
+                for (; mine; mine &= mine - 1) {
+                    const int thread = (int)(threadIdx.x & ~63u) + __builtin_ctzll(mine);
+                    for (int i = begin + (thread + lane * kThreads) * kN; i < end; i += 64 * kThreads * kN) see_pack(i);
+                }
+            } else if (mine >> lane & 1) {
+                for (int i = begin + (int)threadIdx.x * kN; i < end; i += kStep) {
+                    Packs<T, kN, kMask, kFlight> packs;
+                    packs.load(x_row, allowed, i, end);
+#pragma unroll
+                    for (int u = 0; u < kFlight; ++u)
+#pragma unroll
+                        for (int e = 0; e < kN; ++e)
+                            if (packs.may[u] >> e & 1) see(packs.x[u * kN + e], i + u * kThreads * kN + e);
+                }
             }
-        });
+        };
+        select_top(a.n_top, best, sorted, [&](float least, auto see) { look(__ballot(best >= least || has_nan), see); },
+                   [&](auto see) {
+                       for (int i = begin + (int)threadIdx.x * kN; i < end; i += kThreads * kN) {
+                           float x[kN];
+                           const unsigned may = load_logits<T, kN, kMask>(x_row, allowed, i, end, x);
+#pragma unroll
+                           for (int e = 0; e < kN; ++e)
+                               if (may >> e & 1) see(x[e], i + e);
+                       }
+                   });
+    }
     if (kWhole) {
         const Row r = finish(all, a.scale);
         write_row(a, row, r, target);
@@ -244,30 +321,34 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(LogitsArgs a)
     __shared__ unsigned long long sorted[NUTS_CAT_MAX_TOP];
     const long row = blockIdx.x;
     const float c = a.scale * kLog2e;
-    const Target target = target_of<T>(a, row);
+    Target target;
+    ask_target(a, row, target);
+    // (a thread's keys stay in registers)
+    constexpr int kKeys = kTop ? kJoinKeys / kThreads : 1;
+    unsigned long long keys[kKeys];
+    const int n = a.parts * a.n_top;
+#pragma unroll
+    for (int k = 0; k < kKeys; ++k) {
+        const int i = k * kThreads + (int)threadIdx.x;
+        keys[k] = kTop && i < n ? a.part_keys[row * n + i] : 0;
+    }
     Stats v{-INFINITY, 0.f, 0.f};
     for (int p = threadIdx.x; p < a.parts; p += kThreads) {
         const float4 s = a.part_stats[row * a.parts + p];
         v = join(v, Stats{s.x, s.y, s.z}, c);
     }
+    ask_logit<T>(a, row, target);
     const Row r = finish(join_block(v, c, shared), a.scale);
     write_row(a, row, r, target);
     if (kTop) {
-        const unsigned long long* keys = a.part_keys + row * a.parts * a.n_top;
-        const int n = a.parts * a.n_top;
         float best = -INFINITY;
-        bool has_nan = false;
-        auto each = [&](auto see) {
-            for (int i = threadIdx.x; i < n; i += kThreads) {
-                const unsigned long long key = keys[i];
-                if (key) see(logit_of(key), class_of(key));
-            }
+        auto every = [&](auto see) {
+#pragma unroll
+            for (int k = 0; k < kKeys; ++k)
+                if (keys[k]) see(logit_of(keys[k]), class_of(keys[k]));
         };
-        each([&](float x, int) {
-            best = fmaxf(best, x);
-            has_nan |= x != x;
-        });
-        select_top(a.n_top, best, has_nan, sorted, each);
+        every([&](float x, int) { best = fmaxf(best, x); });
+        select_top(a.n_top, best, sorted, [&](float, auto see) { every(see); }, every);
         write_top(a, row, r, sorted);
     }
 }
@@ -360,8 +441,8 @@ int check_logits(const nuts_logits_desc* d, const char* who)
     if (!cat_dtype_known(d->dtype)) return api_fail(NUTS_E_INVALID_ARG, "%s: dtype must be NUTS_F32, NUTS_BF16 or NUTS_F16", who);
     if (d->id_type != NUTS_I32 && d->id_type != NUTS_I64) return api_fail(NUTS_E_INVALID_ARG, "%s: id_type must be NUTS_I32 or NUTS_I64", who);
     if (d->n_rows < 0 || d->n_rows > INT32_MAX - 1) return api_fail(NUTS_E_INVALID_ARG, "%s: n_rows must be in [0, 2^31 - 2]", who);
-    // (indexes of classes are 32 bits, and a thread's next one may lie 16384 behind the last)
-    if (d->n_classes < 1 || d->n_classes > INT32_MAX - (1 << 16)) return api_fail(NUTS_E_INVALID_ARG, "%s: n_classes must be in [1, 2^31 - 2^16)", who);
+    // (indexes of classes are 32 bits, and the next that a thread would look at may lie 2^17 behind the last)
+    if (d->n_classes < 1 || d->n_classes > INT32_MAX - (1 << 18)) return api_fail(NUTS_E_INVALID_ARG, "%s: n_classes must be in [1, 2^31 - 2^18)", who);
     if (d->row_stride < d->n_classes) return api_fail(NUTS_E_INVALID_ARG, "%s: row_stride is smaller than n_classes", who);
     if (d->n_rows > 0 && d->row_stride > INT64_MAX / 8 / d->n_rows) return api_fail(NUTS_E_INVALID_ARG, "%s: row_stride is too large", who);
     if (d->allowed_stride < 0 || (d->allowed_stride > 0 && d->allowed_stride < ceil_div(d->n_classes, 32)))
