@@ -72,6 +72,20 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T, kN>& r)
     __builtin_memcpy(p, &r, sizeof(r));
 }
 
+// The same past the caches, for outputs that would push out of them what is still to be read (kStreamed).
+template <typename T, int kN>
+__device__ __forceinline__ void stream_pack(T* p, const Pack<T, kN>& r)
+{
+    static_assert(sizeof(r) == 16, "");
+    typedef __attribute__((ext_vector_type(4), aligned(2))) unsigned Words;
+    Words w;
+    __builtin_memcpy(&w, &r, sizeof(r));
+    __builtin_nontemporal_store(w, reinterpret_cast<Words*>(p));
+}
+
+// Outputs of this many bytes and more go past the caches: half the last-level cache (256 MB).
+constexpr int64_t kStreamed = (int64_t)1 << 27;
+
 // A class as the kernels hold it: the id, or -1 where it is outside [0, n_classes).
 __device__ __forceinline__ int class_at(const void* ids, int id_type, long i, long n_classes)
 {

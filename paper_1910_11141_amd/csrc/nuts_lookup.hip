@@ -23,7 +23,7 @@ struct LookupArgs {
     void* rows;
     long first_block, n_ids, n_classes, dim, table_stride, row_stride;
     float scale;
-    int id_type, lane_bits;
+    int id_type, lane_bits, streamed;
 };
 
 // A group of 2^lane_bits threads copies kRows rows, 16 bytes a thread at a time: kRows classes are read first and then as many
@@ -51,7 +51,8 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs a)
                 Pack<T, kN> out;
 #pragma unroll
                 for (int e = 0; e < kN; ++e) out.v[e] = rounded<T>(id[r] >= 0 ? to_float(in[r].v[e]) * a.scale : 0.f);
-                store_pack(rows + (first + r) * a.row_stride + c, out);
+                T* to = rows + (first + r) * a.row_stride + c;
+                a.streamed ? stream_pack(to, out) : store_pack(to, out);
             }
         } else {
             for (int r = 0; r < kRows; ++r) {
@@ -71,7 +72,7 @@ struct GradArgs {
     void* table;
     long n_ids, n_classes, dim, table_stride, row_stride;
     float scale;
-    int id_type, accumulate, lane_bits;
+    int id_type, accumulate, lane_bits, streamed;
 };
 
 // kN columns of a row, zeros where only `left` are left.
@@ -99,7 +100,8 @@ __device__ __forceinline__ void finish_columns(const GradArgs& a, T* p, int left
 #pragma unroll
             for (int e = 0; e < kN; ++e) out.v[e] = rounded<T>(a.scale * sum[e]);
         }
-        store_pack(p, out);
+        if (sizeof(out) == 16 && a.streamed) stream_pack(p, *reinterpret_cast<const Pack<T, 16 / sizeof(T)>*>(&out));
+        else store_pack(p, out);
     } else {
 #pragma unroll
         for (int e = 0; e < kN; ++e)
@@ -108,13 +110,13 @@ __device__ __forceinline__ void finish_columns(const GradArgs& a, T* p, int left
 }
 
 template <typename T, int kN>
-__device__ __forceinline__ void zero_columns(T* p, int left)
+__device__ __forceinline__ void zero_columns(const GradArgs& a, T* p, int left)
 {
     if (left >= kN) {
         Pack<T, kN> out;
 #pragma unroll
         for (int e = 0; e < kN; ++e) out.v[e] = static_cast<T>(0.f);
-        store_pack(p, out);
+        a.streamed ? stream_pack(p, out) : store_pack(p, out);
     } else {
         for (int e = 0; e < left; ++e) p[e] = static_cast<T>(0.f);
     }
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int clas
         for (long i = threadIdx.x; i < (long)own * packs; i += kThreads) {
             const int r = (int)(i / packs);
             const long c = i % packs * kN;
-            if (!(occupied >> r & 1)) zero_columns<T, kN>(table + r * a.table_stride + c, (int)min((long)kN, a.dim - c));
+            if (!(occupied >> r & 1)) zero_columns<T, kN>(a, table + r * a.table_stride + c, (int)min((long)kN, a.dim - c));
         }
     // Each class is added up by the whole workgroup: a row is read by 2^lane_bits lanes of a wave (or by a wave in several
     // turns), and every wave has a list of the class's positions for itself, of which its groups of lanes take turns.
@@ -417,7 +419,7 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a)
             const unsigned word[4] = {flags.x, flags.y, flags.z, flags.w};
 #pragma unroll
             for (int r = 0; r < kClear; ++r)
-                if (left > 0 && v + r < a.g.n_classes && !(word[r / 4] >> (r % 4 * 8) & 0xff)) zero_columns<T, kN>(table + (v + r) * a.g.table_stride + c, left);
+                if (left > 0 && v + r < a.g.n_classes && !(word[r / 4] >> (r % 4 * 8) & 0xff)) zero_columns<T, kN>(a.g, table + (v + r) * a.g.table_stride + c, left);
         }
         return;
     }
@@ -628,7 +630,8 @@ int nuts_lookup(const nuts_lookup_desc* d, const void* table, const void* ids, v
     if (!table || !ids || !rows) return api_fail(NUTS_E_INVALID_ARG, "nuts_lookup: null pointer");
     if (int rc = api_have_device()) return rc;
     LookupArgs a{table, ids, rows, 0, (long)d->n_ids, (long)d->n_classes, (long)d->dim, (long)d->table_stride, (long)d->row_stride,
-                 (float)d->scale, d->id_type, lane_bits_of(d->dim, d->dtype, 0)};
+                 (float)d->scale, d->id_type, lane_bits_of(d->dim, d->dtype, 0),
+                 d->n_ids * d->dim * (int64_t)cat_size(d->dtype) >= kStreamed};
     const int groups = kThreads >> a.lane_bits;
     by_dtype(d->dtype, [&](auto t) {
         using T = decltype(t);
@@ -663,7 +666,7 @@ int nuts_lookup_grad(const nuts_lookup_desc* d, const void* grad_rows, const voi
     hipStream_t stream = api_stream();
     SumArgs a{};
     a.g = GradArgs{grad_rows, ids, grad_table, (long)d->n_ids, (long)d->n_classes, (long)d->dim, (long)d->table_stride, (long)d->row_stride,
-                   (float)d->scale, d->id_type, d->accumulate, 0};
+                   (float)d->scale, d->id_type, d->accumulate, 0, d->n_classes * d->dim * (int64_t)cat_size(d->dtype) >= kStreamed};
     if (p.few) {
         a.g.lane_bits = std::min(6, lane_bits_of(d->dim, d->dtype, 0));
         by_dtype(d->dtype, [&](auto t) {
