@@ -26,40 +26,29 @@ struct LookupArgs {
     int id_type, lane_bits, streamed;
 };
 
-// A group of 2^lane_bits threads copies kRows rows, 16 bytes a thread at a time: kRows classes are read first and then as many
-// rows are in flight, for what a row costs is the wait for its class and then for its bytes.
-template <typename T, int kRows>
+// A group of 2^lane_bits threads copies a row, 16 bytes a thread at a time: a wave a row where there are enough rows to fill the chip,
+// which then waits for some of them while it writes others (65536 rows of 4 KB: 89 us so; with a workgroup a row 99 us, four
+// 16-byte pieces of a row under way a thread 94 us, two or four rows a workgroup at once 95 and 104 us).
+template <typename T>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs a)
 {
     constexpr int kN = 16 / sizeof(T);
     const int lanes = 1 << a.lane_bits, lane = threadIdx.x & (lanes - 1);
-    const long first = ((a.first_block + blockIdx.x) * (kThreads >> a.lane_bits) + (threadIdx.x >> a.lane_bits)) * kRows;
-    const T* table = static_cast<const T*>(a.table);
-    T* rows = static_cast<T*>(a.rows);
-    int id[kRows];
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) id[r] = first + r < a.n_ids ? class_at(a.ids, a.id_type, first + r, a.n_classes) : -2;
+    const long row = (a.first_block + blockIdx.x) * (kThreads >> a.lane_bits) + (threadIdx.x >> a.lane_bits);
+    if (row >= a.n_ids) return;
+    const int id = class_at(a.ids, a.id_type, row, a.n_classes);
+    const T* from = static_cast<const T*>(a.table) + max(id, 0) * a.table_stride;
+    T* to = static_cast<T*>(a.rows) + row * a.row_stride;
     for (long c = (long)lane * kN; c < a.dim; c += (long)lanes * kN) {
         if (c + kN <= a.dim) {
-            Pack<T, kN> in[kRows];
+            Pack<T, kN> x;
+            if (id >= 0) x = load_pack<T, kN>(from + c);
+            Pack<T, kN> out;
 #pragma unroll
-            for (int r = 0; r < kRows; ++r)
-                if (id[r] >= 0) in[r] = load_pack<T, kN>(table + id[r] * a.table_stride + c);
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                if (id[r] == -2) continue;
-                Pack<T, kN> out;
-#pragma unroll
-                for (int e = 0; e < kN; ++e) out.v[e] = rounded<T>(id[r] >= 0 ? to_float(in[r].v[e]) * a.scale : 0.f);
-                T* to = rows + (first + r) * a.row_stride + c;
-                a.streamed ? stream_pack(to, out) : store_pack(to, out);
-            }
+            for (int e = 0; e < kN; ++e) out.v[e] = rounded<T>(id >= 0 ? to_float(x.v[e]) * a.scale : 0.f);
+            a.streamed ? stream_pack(to + c, out) : store_pack(to + c, out);
         } else {
-            for (int r = 0; r < kRows; ++r) {
-                if (id[r] == -2) continue;
-                for (long e = c; e < a.dim; ++e)
-                    rows[(first + r) * a.row_stride + e] = rounded<T>(id[r] >= 0 ? to_float(table[id[r] * a.table_stride + e]) * a.scale : 0.f);
-            }
+            for (long e = c; e < a.dim; ++e) to[e] = rounded<T>(id >= 0 ? to_float(from[e]) * a.scale : 0.f);
         }
     }
 }
@@ -630,16 +619,13 @@ int nuts_lookup(const nuts_lookup_desc* d, const void* table, const void* ids, v
     if (!table || !ids || !rows) return api_fail(NUTS_E_INVALID_ARG, "nuts_lookup: null pointer");
     if (int rc = api_have_device()) return rc;
     LookupArgs a{table, ids, rows, 0, (long)d->n_ids, (long)d->n_classes, (long)d->dim, (long)d->table_stride, (long)d->row_stride,
-                 (float)d->scale, d->id_type, lane_bits_of(d->dim, d->dtype, 0),
+                 (float)d->scale, d->id_type, std::min(d->n_ids >= 2048 ? 6 : 8, lane_bits_of(d->dim, d->dtype, 0)),
                  d->n_ids * d->dim * (int64_t)cat_size(d->dtype) >= kStreamed};
     const int groups = kThreads >> a.lane_bits;
     by_dtype(d->dtype, [&](auto t) {
         using T = decltype(t);
-        // several rows a group where that leaves the chip more workgroups than it holds at once (2048)
-        const bool several = d->n_ids >= 4 * 2048 * (int64_t)groups;
-        for (const long blocks = (long)ceil_div(d->n_ids, (several ? 4 : 1) * groups); a.first_block < blocks; a.first_block += kMaxBlocks)
-            hipLaunchKernelGGL((several ? lookup_kernel<T, 4> : lookup_kernel<T, 1>), dim3((unsigned)std::min(blocks - a.first_block, kMaxBlocks)),
-                               dim3(kThreads), 0, api_stream(), a);
+        for (const long blocks = (long)ceil_div(d->n_ids, groups); a.first_block < blocks; a.first_block += kMaxBlocks)
+            hipLaunchKernelGGL(lookup_kernel<T>, dim3((unsigned)std::min(blocks - a.first_block, kMaxBlocks)), dim3(kThreads), 0, api_stream(), a);
     });
     NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
     return NUTS_OK;
