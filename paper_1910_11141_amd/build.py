@@ -25,9 +25,10 @@ FLAGS = [
 # addresses out of it (the compiler's habit) fills the register file and spills the state itself (chip kernel: 400 bytes a
 # lane; the others: nuts_gauss.hip).
 NO_LICM = ["-mllvm", "-disable-machine-licm", "-mllvm", "-sink-insts-to-avoid-spills=1"]
-# (pcvm.hip asks for the register limit of eight waves, not for eight waves, and names M0 among the registers that its assembly changes,
-# which the compiler keeps for itself: it says so of every place)
-EXTRA_FLAGS = {"nuts_chip.hip": NO_LICM, "nuts_gauss.hip": NO_LICM, "pcvm.hip": ["-Wno-pass-failed", "-Wno-inline-asm"]}
+# (pcvm.hip asks for the register limit of eight waves, not for eight waves; it and nuts_score.hip name M0 among the registers that their
+# assembly changes, which the compiler keeps for itself: it says so of every place)
+EXTRA_FLAGS = {"nuts_chip.hip": NO_LICM, "nuts_gauss.hip": NO_LICM, "pcvm.hip": ["-Wno-pass-failed", "-Wno-inline-asm"],
+               "nuts_score.hip": ["-Wno-inline-asm"]}
 
 
 def flags_of(source):

@@ -1,16 +1,26 @@
-// C = A B' on the matrix instructions: rows of A and rows of B lie along the contraction, binary32 or bfloat16, sums binary32.
+// C = A B' on the matrix instructions: binary32 or bfloat16, sums binary32.  A is m x k, B is n x k.
 //
-// A workgroup makes a tile of kM x kN; its waves divide it.  Per step the workgroup takes 128 bytes of each of its rows of A
-// and B from memory straight into LDS (no registers in between), kStages - 1 steps ahead.  A row's eight 16-byte pieces lie
-// in LDS in the order piece ^ (row % 8), so that the 16 rows that a matrix instruction reads at one place of the
-// contraction are in different banks.  What lies outside the matrices is read as zero by the bounds of the buffer
-// descriptors: rows behind the last by their offset, and pieces behind the contraction's end by an offset that no
-// buffer has.  (Rows have to begin at multiples of 16 bytes and to consist of whole pieces: others are copied first.)
+// A workgroup makes a tile of kM x kN; its waves divide it.  Per step along the contraction the workgroup takes 128 bytes for each row
+// of its tile of A and of B from memory straight into LDS (no registers in between), kStages - 1 steps ahead.  Either
+// matrix may lie in memory along its rows ("along": a row's elements, which are the contraction's, are neighbours) or across them
+// (its transpose lies along: the elements that belong to one place of the contraction are neighbours); the tile in LDS lies as
+// the memory does.
+//
+// Along: a row's eight 16-byte pieces lie in LDS in the order piece ^ (row % 8), so that the 16 rows that a matrix
+// instruction reads at one place of the contraction are in different banks.  Across: a place's 16-byte pieces are exchanged
+// likewise, 32 bytes (16 bfloat16 rows) at a time by bits 0, 1 and 3 of the place, or 64 bytes (16 binary32 rows) by bits 2 and 3;
+// binary32 rows are read element by element, bfloat16 by the loads that transpose 4 x 16 elements.
+//
+// What lies outside the matrices is read as zero by the bounds of the buffer descriptors: rows behind the last by their
+// offset, and pieces behind the contraction's end by an offset that no buffer has.  (Rows have to begin at multiples of 16
+// bytes; a row that lies along has to consist of whole pieces.  Others are copied first.)
 //
 // The first operand of an instruction is B: a lane then holds four neighbouring columns of one row of C, which are stored
 // together, and most of a reduction along a row of C stays within lanes.
 #pragma once
 #include "nuts_softmax.h"
+
+#include <type_traits>
 
 namespace nuts {
 
@@ -26,8 +36,8 @@ enum ProductKind { kScores, kSums, kOutput };
 struct ProductArgs {
     const char* a;
     const char* b;
-    long a_stride, b_stride;  // bytes
-    int m, n, k_bytes;
+    long a_stride, b_stride;  // bytes from row to row (across: from place to place of the contraction)
+    int m, n, k;              // (along: zeros behind k up to a whole piece)
     int tiles_m, tiles_n;
     int splits, split_steps;  // the contraction is divided: steps of a division
     // kSums: binary32 [split][m][n], added to what is there if `add`
@@ -36,6 +46,7 @@ struct ProductArgs {
     // kOutput, and kScores' logits (or NULL)
     void* c;
     long c_stride;  // elements
+    int streamed;   // what is stored goes past the caches
     // kScores
     float scale;
     const void* targets;
@@ -68,6 +79,105 @@ struct Piece<bf16> {
     __device__ __forceinline__ static f32x4 multiply_add(const Piece& b, const Piece& a, f32x4 c) { return multiply(b.v, a.v, c); }
 };
 
+#ifdef __HIP_DEVICE_COMPILE__  // (the host's pass knows neither buffer descriptors nor loads to LDS)
+
+// One operand's tile of kRows rows: its way from memory to LDS, and from there to the matrix instructions.
+template <typename T, int kRows, bool kAcross, int kWaves>
+struct Operand {
+    static constexpr int kSize = sizeof(T), kPlaces = kStepBytes / kSize, kBytes = kRows * kStepBytes;
+    static constexpr int kLoads = kBytes / 1024 / kWaves;                        // of a wave, 1024 bytes each
+    static constexpr int kPieces = kAcross ? kRows * kSize / 16 : kStepBytes / 16;  // of a line in LDS
+    static_assert(kLoads * 1024 * kWaves == kBytes, "");
+    typedef __attribute__((ext_vector_type(4))) unsigned Descriptor;
+    const char* from;
+    long stride;
+    int rows, k;       // of this tile; the contraction's length
+    int piece;         // along: this lane's in each of its loads
+    unsigned at[kLoads];
+
+    __device__ __forceinline__ static int exchange(int place)
+    {
+        return (kSize == 4 ? (place >> 2 & 3) << 2 : ((place & 3) | (place >> 3 & 1) << 2) << 1) & (kPieces - 1);
+    }
+
+    __device__ __forceinline__ void begin(const char* matrix, long matrix_stride, int first_row, int all_rows, int all_k, int wave, int lane)
+    {
+        stride = matrix_stride;
+        rows = min(kRows, all_rows - first_row);
+        k = all_k;
+        from = matrix + (kAcross ? (long)first_row * kSize : (long)first_row * stride);
+        piece = (lane % 8) ^ (lane / 8);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int unit = (j * kWaves + wave) * 64 + lane, line = unit / kPieces;
+            if (kAcross) at[j] = (unsigned)(line * stride + ((unit % kPieces) ^ exchange(line)) * 16);
+            else at[j] = line < rows ? (unsigned)(line * stride + piece * 16) : kNowhere;
+        }
+    }
+
+    // What a step's loads have in common.  Every step has the same number of them, also those behind the last (`none`), which read
+    // nothing: waits count loads.
+    struct Step {
+        Descriptor buffer;
+        unsigned skip, place, to;
+    };
+    __device__ __forceinline__ Step at_step(const char* to, int step, bool none, int wave) const
+    {
+        const int left = k - step * kPlaces;
+        // (the last line up to a whole piece: a buffer reads no part of a word)
+        const int line = ((kAcross ? rows : k) * kSize + 15) / 16 * 16;
+        const int bytes = (int)((kAcross ? min(left, kPlaces) - 1 : rows - 1) * stride) + line;
+        const unsigned long long base = (unsigned long long)(from + (kAcross && !none ? (long)step * kPlaces * stride : 0));
+        return Step{Descriptor{(unsigned)base, (unsigned)(base >> 32), none ? 0u : (unsigned)bytes, 0x00027000u},
+                    none || (!kAcross && piece * (16 / kSize) >= left) ? kNowhere : 0u, kAcross || none ? 0u : (unsigned)(step * kStepBytes),
+                    (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)to + wave * 1024u};
+    }
+    // Load j of a step.  (In assembly: of its own loads to LDS the compiler knows that they write there, and has some reads of other
+    // places of LDS wait for them.  It has no result; who needs what it writes waits for it in wait_and_meet.)
+    __device__ __forceinline__ void fetch(const Step& s, int j) const
+    {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(s.to + j * (kWaves * 1024u)), "v"(at[j] | s.skip), "s"(s.buffer),
+                     "s"(s.place)
+                     : "m0");
+    }
+
+    // Where a lane reads: its place in a tile, and what its row is exchanged by.
+    struct Reader {
+        unsigned at, swap;
+    };
+    __device__ __forceinline__ static Reader reader(int lane)
+    {
+        if constexpr (!kAcross) return Reader{(unsigned)(lane % 16 * kStepBytes), (unsigned)(lane % 8 * 16)};
+        const int place = kSize == 4 ? lane / 16 * 4 : lane / 16 * 8 + lane % 16 / 4;
+        return Reader{(unsigned)(place * kPieces * 16 + (kSize == 4 ? lane % 16 * 4 : lane % 4 * 8)), (unsigned)(exchange(place) * 16)};
+    }
+    // 16 rows from `row` on, half a step: lane l has row l % 16 and the places of its quarter l / 16.
+    __device__ __forceinline__ static Piece<T> read(const char* tile, int row, int half, int lane, const Reader& r)
+    {
+        Piece<T> p;
+        if constexpr (!kAcross) {
+            p = *reinterpret_cast<const Piece<T>*>(tile + r.at + row * kStepBytes + ((half * 64 + lane / 16 * 16) ^ r.swap));
+        } else if constexpr (kSize == 4) {
+            const char* line = tile + r.at + half * 16 * kPieces * 16 + ((row * 4) ^ r.swap);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p.v[e] = *reinterpret_cast<const float*>(line + e * kPieces * 16);
+        } else {
+            typedef __attribute__((ext_vector_type(4))) short Four;
+            const char* line = tile + r.at + half * 32 * kPieces * 16 + ((row * 2) ^ r.swap);
+            struct {
+                Four four[2];
+            } both;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                both.four[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) Four*)(line + t * 4 * kPieces * 16));
+            p.v = __builtin_bit_cast(bf16x8, both);
+        }
+        return p;
+    }
+};
+
+#endif
+
 // The tile of a workgroup: workgroups go to the eight dies in turn, each die gets neighbouring tiles (its own cache keeps
 // what they share), four rows of tiles at a time.
 __device__ __forceinline__ void tile_of(unsigned id, int tiles_m, int tiles_n, int& tm, int& tn)
@@ -87,127 +197,139 @@ __device__ __forceinline__ void wait_and_meet()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kOutstanding) : "memory");
 }
 
-template <typename T, int kM, int kN, int kWavesM, int kWavesN, int kStages, ProductKind kKind>
+// kAhead steps are under way to LDS while one is multiplied; B has a buffer more than A, so that its loads are spread over the
+// first half of a step and those of A over the second, behind the barrier at which all are done with the step before.
+template <typename T, int kM, int kN, int kWavesM, int kWavesN, int kAhead, bool kAcrossA, bool kAcrossB, ProductKind kKind>
 __global__ __launch_bounds__(64 * kWavesM * kWavesN) void product_kernel(ProductArgs p)
 {
-#ifdef __HIP_DEVICE_COMPILE__  // (the host's pass knows neither buffer descriptors nor loads to LDS)
+#ifdef __HIP_DEVICE_COMPILE__
     constexpr int kWaves = kWavesM * kWavesN;
     constexpr int kFM = kM / kWavesM / 16, kFN = kN / kWavesN / 16;
-    constexpr int kLoadsA = kM / 8 / kWaves, kLoadsB = kN / 8 / kWaves;  // of a wave: 8 rows each
-    constexpr int kStageBytes = (kM + kN) * kStepBytes;
-    static_assert(kLoadsA * 8 * kWaves == kM && kLoadsB * 8 * kWaves == kN, "");
-    __shared__ __attribute__((aligned(1024))) char stage[kStages][kStageBytes];
+    using A = Operand<T, kM, kAcrossA, kWaves>;
+    using B = Operand<T, kN, kAcrossB, kWaves>;
+    constexpr int kColumns = kFN * 16, kOutSize = kKind == kOutput ? sizeof(T) : 4, kPitch = kColumns * kOutSize + 16;
+    constexpr int kStages = kAhead * A::kBytes + (kAhead + 1) * B::kBytes, kStores = 16 * kPitch * kWaves;
+    __shared__ __attribute__((aligned(1024))) char lds[kStages > kStores ? kStages : kStores];
+    auto tile_a = [&](int s) { return lds + (s % kAhead) * A::kBytes; };
+    auto tile_b = [&](int s) { return lds + kAhead * A::kBytes + (s % (kAhead + 1)) * B::kBytes; };
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const int wave_m = wave / kWavesN, wave_n = wave % kWavesN;
     int tm, tn;
     tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
     const int m0 = tm * kM, n0 = tn * kN;
-    const int rows_a = min(kM, p.m - m0), rows_b = min(kN, p.n - n0);
-    const int all_steps = (p.k_bytes + kStepBytes - 1) / kStepBytes;
+    const int all_steps = (p.k + A::kPlaces - 1) / A::kPlaces;
     const int first = blockIdx.y * p.split_steps, steps = min(p.split_steps, all_steps - first);
-    const __amdgpu_buffer_rsrc_t from_a = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p.a + (long)m0 * p.a_stride), 0, (int)((rows_a - 1) * p.a_stride + p.k_bytes), 0x00027000);
-    const __amdgpu_buffer_rsrc_t from_b = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p.b + (long)n0 * p.b_stride), 0, (int)((rows_b - 1) * p.b_stride + p.k_bytes), 0x00027000);
-    // this lane's piece of a step, and its place in each of the wave's loads
-    const int piece = (lane % 8) ^ (lane / 8);
-    unsigned at_a[kLoadsA], at_b[kLoadsB];
+    A from_a;
+    B from_b;
+    from_a.begin(p.a, p.a_stride, m0, p.m, p.k, wave, lane);
+    from_b.begin(p.b, p.b_stride, n0, p.n, p.k, wave, lane);
 #pragma unroll
-    for (int j = 0; j < kLoadsA; ++j) {
-        const int row = (j * kWaves + wave) * 8 + lane / 8;
-        at_a[j] = row < rows_a ? (unsigned)(row * p.a_stride + piece * 16) : kNowhere;
+    for (int s = 0; s < kAhead; ++s) {
+        const typename B::Step step_b = from_b.at_step(tile_b(s), first + s, s >= steps, wave);
+#pragma unroll
+        for (int l = 0; l < B::kLoads; ++l) from_b.fetch(step_b, l);
+        const typename A::Step step_a = from_a.at_step(tile_a(s), first + s, s >= steps, wave);
+#pragma unroll
+        for (int l = 0; l < A::kLoads; ++l) from_a.fetch(step_a, l);
     }
-#pragma unroll
-    for (int j = 0; j < kLoadsB; ++j) {
-        const int row = (j * kWaves + wave) * 8 + lane / 8;
-        at_b[j] = row < rows_b ? (unsigned)(row * p.b_stride + piece * 16) : kNowhere;
-    }
-    // every step has the same number of loads, also those behind the last, which read nothing: waits count loads
-    auto fetch = [&](int s) {
-        char* to = stage[s % kStages];
-        const int step = first + s;
-        const unsigned skip = s >= steps || step * kStepBytes + piece * 16 >= p.k_bytes ? kNowhere : 0u;
-        const int k = s < steps ? step * kStepBytes : 0;
-#pragma unroll
-        for (int j = 0; j < kLoadsA; ++j)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from_a, (__attribute__((address_space(3))) void*)(to + (j * kWaves + wave) * 1024), 16, at_a[j] | skip, k, 0, 0);
-#pragma unroll
-        for (int j = 0; j < kLoadsB; ++j)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from_b, (__attribute__((address_space(3))) void*)(to + kM * kStepBytes + (j * kWaves + wave) * 1024), 16, at_b[j] | skip, k, 0, 0);
-    };
-    const int wave_m = wave / kWavesN, wave_n = wave % kWavesN;
     f32x4 c[kFM][kFN];
 #pragma unroll
     for (int i = 0; i < kFM; ++i)
 #pragma unroll
         for (int j = 0; j < kFN; ++j) c[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    wait_and_meet<(kAhead - 1) * (A::kLoads + B::kLoads)>();
+    // A half step in kFN turns: a column of the products of this half, behind which the column's piece of the next half takes
+    // the place of this one's, and with each a part of the rows' pieces of the next half and of the loads.
+    typename A::Reader read_a = A::reader(lane);
+    typename B::Reader read_b = B::reader(lane);
+    Piece<T> a[2][kFM], b[kFN];
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) fetch(s);
-    for (int s = 0; s < steps; ++s) {
-        wait_and_meet<(kStages - 2) * (kLoadsA + kLoadsB)>();
-        fetch(s + kStages - 1);
-        const char* a_rows = stage[s % kStages] + (wave_m * kFM * 16 + lane % 16) * kStepBytes;
-        const char* b_rows = stage[s % kStages] + (kM + wave_n * kFN * 16 + lane % 16) * kStepBytes;
+    for (int i = 0; i < kFM; ++i) a[0][i] = A::read(tile_a(0), (wave_m * kFM + i) * 16, 0, lane, read_a);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int at = ((half * 4 + lane / 16) ^ (lane % 8)) * 16;
-            Piece<T> a[kFM], b[kFN];
+    for (int j = 0; j < kFN; ++j) b[j] = B::read(tile_b(0), (wave_n * kFN + j) * 16, 0, lane, read_b);
+    auto half_step = [&](int half, int next, auto load, int loads) {
+        const char* next_a = tile_a(next);
+        const char* next_b = tile_b(next);
+        // (across, addresses are made from these here, each where it is used: kept for all pieces they would take the registers of the sums)
+        if constexpr (kAcrossA) asm volatile("" : "+v"(read_a.at), "+v"(read_a.swap));
+        if constexpr (kAcrossB) asm volatile("" : "+v"(read_b.at), "+v"(read_b.swap));
 #pragma unroll
-            for (int i = 0; i < kFM; ++i) a[i] = *reinterpret_cast<const Piece<T>*>(a_rows + i * 16 * kStepBytes + at);
+        for (int j = 0; j < kFN; ++j) {
 #pragma unroll
-            for (int j = 0; j < kFN; ++j) b[j] = *reinterpret_cast<const Piece<T>*>(b_rows + j * 16 * kStepBytes + at);
+            for (int i = j * kFM / kFN; i < (j + 1) * kFM / kFN; ++i) a[1 - half][i] = A::read(next_a, (wave_m * kFM + i) * 16, 1 - half, lane, read_a);
 #pragma unroll
-            for (int i = 0; i < kFM; ++i)
+            for (int l = j * loads / kFN; l < (j + 1) * loads / kFN; ++l) load(l);
 #pragma unroll
-                for (int j = 0; j < kFN; ++j) c[i][j] = Piece<T>::multiply_add(b[j], a[i], c[i][j]);
+            for (int i = 0; i < kFM; ++i) c[i][j] = Piece<T>::multiply_add(b[j], a[half][i], c[i][j]);
+            b[j] = B::read(next_b, (wave_n * kFN + j) * 16, 1 - half, lane, read_b);
+            __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    for (int s = 0; s < steps; ++s) {
+        const typename B::Step step_b = from_b.at_step(tile_b(s + kAhead), first + s + kAhead, s + kAhead >= steps, wave);
+        half_step(0, s, [&](int l) { from_b.fetch(step_b, l); }, B::kLoads);
+        wait_and_meet<(kAhead - 1) * B::kLoads + (kAhead - 2) * A::kLoads>();
+        const typename A::Step step_a = from_a.at_step(tile_a(s + kAhead), first + s + kAhead, s + kAhead >= steps, wave);
+        half_step(1, s + 1, [&](int l) { from_a.fetch(step_a, l); }, A::kLoads);
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (loads of nothing may still be under way to LDS)
+    wait_and_meet<0>();  // (loads of nothing may still be under way to LDS, and other waves may still read there)
 
-    const int row0 = m0 + wave_m * kFM * 16 + lane % 16, col0 = n0 + wave_n * kFN * 16 + lane / 16 * 4;
-    const bool whole = n0 + kN <= p.n;
-    if (kKind == kSums) {
-        float* sums = p.sums + (long)blockIdx.y * p.m * p.n;
+    // A wave stores 16 rows of its part of the tile at a time.  A lane has four neighbouring columns of one of them, which would
+    // make stores of 32 or 64 bytes a row: the rows go through LDS and are stored whole.
+    const int row0 = m0 + wave_m * kFM * 16, col0 = n0 + wave_n * kColumns;
+    const int own_row = lane % 16, own_col = lane / 16 * 4;
+    auto store_rows = [&](auto* to, long stride, int rows, const f32x4 (&values)[kFN], bool add) {
+        using Out = std::remove_pointer_t<decltype(to)>;
+        constexpr int kPack = 16 / sizeof(Out), kLanes = kColumns / kPack;  // kLanes: of a row
+        static_assert(sizeof(Out) == kOutSize && kLanes >= 4 && kLanes <= 64, "");
+        char* own = lds + wave * (16 * kPitch);
 #pragma unroll
-        for (int i = 0; i < kFM; ++i)
+        for (int j = 0; j < kFN; ++j) {
+            Pack<Out, 4> four;
 #pragma unroll
-            for (int j = 0; j < kFN; ++j) {
-                const int row = row0 + i * 16, col = col0 + j * 16;
-                if (row >= p.m) continue;
-                float* to = sums + (long)row * p.n + col;
+            for (int e = 0; e < 4; ++e) four.v[e] = rounded<Out>(values[j][e]);
+            *reinterpret_cast<Pack<Out, 4>*>(__builtin_assume_aligned(own + own_row * kPitch + (j * 16 + own_col) * sizeof(Out), 4 * sizeof(Out))) = four;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int col = lane % kLanes * kPack, left = p.n - col0 - col;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (col + e < p.n) to[e] = p.add ? to[e] + c[i][j][e] : c[i][j][e];
-            }
-    }
-    if (kKind == kOutput) {
-        T* out = static_cast<T*>(p.c);
+        for (int r = lane / kLanes; r < 16; r += 64 / kLanes) {
+            if (r >= rows || left <= 0) continue;
+            Pack<Out, kPack> pack = *reinterpret_cast<const Pack<Out, kPack>*>(__builtin_assume_aligned(own + r * kPitch + col * sizeof(Out), 16));
+            Out* at = to + r * stride + col;
+            if (left >= kPack) {
+                if (add) {
+                    const Pack<Out, kPack> old = load_pack<Out, kPack>(at);
 #pragma unroll
-        for (int i = 0; i < kFM; ++i)
-#pragma unroll
-            for (int j = 0; j < kFN; ++j) {
-                const int row = row0 + i * 16, col = col0 + j * 16;
-                if (row >= p.m) continue;
-                Pack<T, 4> values;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) values.v[e] = rounded<T>(c[i][j][e]);
-                if (whole) {
-                    store_pack(out + row * p.c_stride + col, values);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (col + e < p.n) out[row * p.c_stride + col + e] = values.v[e];
+                    for (int e = 0; e < kPack; ++e) pack.v[e] = rounded<Out>(to_float(pack.v[e]) + to_float(old.v[e]));
                 }
-            }
-    }
-    if (kKind == kScores) {
-        const int parts = p.tiles_n * kWavesN;
+                p.streamed ? stream_pack(at, pack) : store_pack(at, pack);
+            } else {
 #pragma unroll
-        for (int i = 0; i < kFM; ++i) {
-            const int row = row0 + i * 16;
-            float z[kFN * 4];
+                for (int e = 0; e < kPack; ++e)
+                    if (e < left) at[e] = add ? rounded<Out>(to_float(pack.v[e]) + to_float(at[e])) : pack.v[e];
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+#pragma unroll
+    for (int i = 0; i < kFM; ++i) {
+        const int row = row0 + i * 16, rows = p.m - row;
+        if constexpr (kKind == kSums) store_rows(p.sums + ((long)blockIdx.y * p.m + row) * p.n + col0, p.n, rows, c[i], p.add != 0);
+        if constexpr (kKind == kOutput) store_rows(static_cast<T*>(p.c) + row * p.c_stride + col0, p.c_stride, rows, c[i], false);
+        if constexpr (kKind == kScores) {
+            const int own = row + own_row, col = col0 + own_col;
+            const bool whole = n0 + kN <= p.n;
 #pragma unroll
             for (int j = 0; j < kFN; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) z[j * 4 + e] = whole || col0 + j * 16 + e < p.n ? c[i][j][e] * p.scale : -INFINITY;
+                for (int e = 0; e < 4; ++e) c[i][j][e] = whole || col + j * 16 + e < p.n ? c[i][j][e] * p.scale : -INFINITY;
             if (p.stats) {
+                float z[kFN * 4];
+#pragma unroll
+                for (int j = 0; j < kFN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[j * 4 + e] = c[i][j][e];
                 Stats v{-INFINITY, 0.f, 0.f};
                 float m = z[0];
 #pragma unroll
@@ -219,33 +341,17 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void product_kernel(Product
                 v.s += __shfl_xor(v.s, 32);
                 v.t += __shfl_xor(v.t, 16);
                 v.t += __shfl_xor(v.t, 32);
-                if (lane < 16 && row < p.m) p.stats[(long)row * parts + tn * kWavesN + wave_n] = float4{v.m, v.s, v.t, 0.f};
-                const int target = p.targets && row < p.m ? class_at(p.targets, p.id_type, row, p.n) : -1;
-                const int away = target - col0;
-                const bool here = target >= 0 && away >= 0 && away < kFN * 16 && away % 16 < 4;
+                if (lane < 16 && own < p.m) p.stats[(long)own * (p.tiles_n * kWavesN) + tn * kWavesN + wave_n] = float4{v.m, v.s, v.t, 0.f};
+                const int target = p.targets && own < p.m ? class_at(p.targets, p.id_type, own, p.n) : -1;
+                const int away = target - col;
+                const bool here = target >= 0 && away >= 0 && away < kColumns && away % 16 < 4;
                 if (__ballot(here)) {
 #pragma unroll
-                    for (int j = 0; j < kFN; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (here && away == j * 16 + e) p.target_logit[row] = z[j * 4 + e];
+                    for (int e = 0; e < kFN * 4; ++e)
+                        if (here && away == e / 4 * 16 + e % 4) p.target_logit[own] = z[e];
                 }
             }
-            if (p.c && row < p.m) {
-                float* out = static_cast<float*>(p.c) + row * p.c_stride;
-#pragma unroll
-                for (int j = 0; j < kFN; ++j) {
-                    const int col = col0 + j * 16;
-                    if (whole) {
-                        Pack<float, 4> values{{z[j * 4], z[j * 4 + 1], z[j * 4 + 2], z[j * 4 + 3]}};
-                        store_pack(out + col, values);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (col + e < p.n) out[col + e] = z[j * 4 + e];
-                    }
-                }
-            }
+            if (p.c) store_rows(static_cast<float*>(p.c) + row * p.c_stride + col0, p.c_stride, rows, c[i], false);
         }
     }
 #endif

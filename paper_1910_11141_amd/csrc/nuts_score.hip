@@ -4,9 +4,9 @@
 //
 // The work is matrix products (2 n V D operations forward, 4 n V D backward), which run on the matrix instructions
 // (nuts_product.h).  Forward, a workgroup reduces its tile of z to each row's maximum, sum and weighted sum in
-// registers and only those are stored; backward, dZ is made from binary32 z (kept, or computed again) and stored along both of its
-// axes, so that all three products have their contraction along rows.  A large batch goes in pieces that bound
-// the workspace: of rows forward, of classes backward.
+// registers and only those are stored; backward, dZ is made from binary32 z (kept, or computed again) and stored once, and the two
+// products read it and the other operands along or across as they lie.  A large batch goes in pieces that bound the
+// workspace: of rows forward, of classes backward.
 #include "nuts_product.h"
 
 #include <algorithm>
@@ -26,24 +26,6 @@ __global__ __launch_bounds__(kThreads) void pack_rows_kernel(const T* from, long
         for (int i = threadIdx.x; i < to_stride; i += kThreads) to[row * to_stride + i] = i < columns ? from[row * stride + i] : static_cast<T>(0.f);
 }
 
-constexpr int kSquare = 64;
-
-// to[column][row] = from[row][column]: squares through LDS, zeros for rows behind the last up to to_stride.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void transpose_kernel(const T* from, long stride, int rows, int columns, T* to, long to_stride)
-{
-    __shared__ T square[kSquare][kSquare + 4 / sizeof(T)];  // (a word more: columns are in different banks)
-    const int row0 = blockIdx.x * kSquare, column0 = blockIdx.y * kSquare;
-    const int x = threadIdx.x % 64, y = threadIdx.x / 64;
-    for (int i = y; i < kSquare; i += kThreads / 64) {
-        const int row = row0 + i, column = column0 + x;
-        square[i][x] = row < rows && column < columns ? from[(long)row * stride + column] : static_cast<T>(0.f);
-    }
-    __syncthreads();
-    for (int i = y; i < kSquare; i += kThreads / 64)
-        if (column0 + i < columns && row0 + x < to_stride) to[(long)(column0 + i) * to_stride + row0 + x] = square[x][i];
-}
-
 struct GradArgs {
     const float* z;  // of the classes [first, first + classes)
     const void* targets;
@@ -52,43 +34,60 @@ struct GradArgs {
     const float* grad_logprob;
     const float* grad_lse;
     const float* grad_entropy;
-    void* dz;    // [rows][dz_stride] or NULL
-    void* dz_t;  // [classes][dz_t_stride] or NULL
-    long z_stride, dz_stride, dz_t_stride;
-    int n_rows, first, classes, n_classes, id_type;
+    void* dz;        // [rows][dz_stride], zeros behind the last class
+    long z_stride;
+    int dz_stride, parts, first, classes, n_classes, id_type, streamed;
     float scale;
 };
 
-// dZ and its transpose, a square at a time; zeros beyond the matrix up to the strides.
+constexpr int kGradPacks = 4;  // of a thread
+
+// dZ, rounded to the features' type: a workgroup a part of a row.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dz_kernel(GradArgs a)
 {
-    __shared__ T square[kSquare][kSquare + 4 / sizeof(T)];
-    const int row0 = blockIdx.x * kSquare, column0 = blockIdx.y * kSquare;
-    const int x = threadIdx.x % 64, y = threadIdx.x / 64;
-    T* dz = static_cast<T*>(a.dz);
-    T* dz_t = static_cast<T*>(a.dz_t);
-    for (int i = y; i < kSquare; i += kThreads / 64) {
-        const int row = row0 + i, column = column0 + x;
-        float g = 0.f;
-        if (row < a.n_rows && column < a.classes) {
-            const int target = a.targets ? class_at(a.targets, a.id_type, row, a.n_classes) : -1;
-            const float lse = a.lse[row], g_lp = a.grad_logprob && target >= 0 ? a.grad_logprob[row] : 0.f;
-            const float log_p = a.z[(long)row * a.z_stride + column] - lse, p = __builtin_amdgcn_exp2f(log_p * kLog2e);
-            g = (a.grad_lse ? a.grad_lse[row] : 0.f) - g_lp;
-            if (a.grad_entropy) g = __builtin_fmaf(-a.grad_entropy[row], fmaxf(log_p, kNothing) + a.entropy[row], g);
-            g *= p;
-            if (a.first + column == target) g += g_lp;
-            g = lse == -INFINITY ? 0.f : g * a.scale;
+    constexpr int kN = 16 / sizeof(T);
+    const long row = blockIdx.x / (unsigned)a.parts;
+    const int begin = (int)(blockIdx.x % (unsigned)a.parts) * (kGradPacks * kThreads * kN) + (int)threadIdx.x * kN;
+    const float* z = a.z + row * a.z_stride;
+    T* to = static_cast<T*>(a.dz) + row * a.dz_stride;
+    float x[kGradPacks][kN];
+#pragma unroll
+    for (int u = 0; u < kGradPacks; ++u) {
+        const int v = begin + u * kThreads * kN;
+#pragma unroll
+        for (int e = 0; e < kN; e += 4) {
+            if (v + e + 4 <= a.classes) {
+                const Pack<float, 4> four = load_pack<float, 4>(z + v + e);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[u][e + i] = four.v[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[u][e + i] = v + e + i < a.classes ? z[v + e + i] : -INFINITY;
+            }
         }
-        const T value = rounded<T>(g);
-        if (dz && row < a.n_rows && column < a.dz_stride) dz[(long)row * a.dz_stride + column] = value;
-        square[i][x] = value;
     }
-    if (!dz_t) return;
-    __syncthreads();
-    for (int i = y; i < kSquare; i += kThreads / 64)
-        if (column0 + i < a.classes && row0 + x < a.dz_t_stride) dz_t[(long)(column0 + i) * a.dz_t_stride + row0 + x] = square[x][i];
+    const int target = a.targets ? class_at(a.targets, a.id_type, row, a.n_classes) : -1;
+    const int y = target >= a.first && target < a.first + a.classes ? target - a.first : -1;
+    const float lse = a.lse[row];
+    const bool empty = lse == -INFINITY;
+    const float g_lp = a.grad_logprob && target >= 0 && !empty ? a.grad_logprob[row] * a.scale : 0.f;
+    const float g_p = (a.grad_lse ? a.grad_lse[row] * a.scale : 0.f) - g_lp, g_h = a.grad_entropy ? -a.grad_entropy[row] * a.scale : 0.f;
+    const float h = a.grad_entropy ? a.entropy[row] : 0.f, ln_s = empty ? INFINITY : lse;
+#pragma unroll
+    for (int u = 0; u < kGradPacks; ++u) {
+        const int v = begin + u * kThreads * kN;
+        if (v >= a.dz_stride) break;
+        Pack<T, kN> out;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            const float log_p = x[u][e] - ln_s, p = __builtin_amdgcn_exp2f(log_p * kLog2e);
+            float g = p * __builtin_fmaf(g_h, fmaxf(log_p, kNothing) + h, g_p);
+            if (v + e == y) g += g_lp;
+            out.v[e] = rounded<T>(g);
+        }
+        a.streamed ? stream_pack(to + v, out) : store_pack(to + v, out);
+    }
 }
 
 // out[row][column] = scale * sum over the divisions of a contraction, in order.
@@ -139,13 +138,14 @@ __global__ __launch_bounds__(kThreads) void join_scores_kernel(JoinArgs a)
 
 enum Tiles { kLarge, kMiddle, kSmall };
 struct TileShape {
-    int m, n, parts_n;     // parts_n: waves along the columns
-    int per_cu;            // workgroups that a compute unit holds
-    float step;            // time of a step when so many run, relative to the others'
+    int m, n, parts_n;  // parts_n: waves along the columns
+    int per_cu;         // workgroups that a compute unit holds
+    float step[2];      // us for a step when so many run: bfloat16, binary32
 };
-constexpr TileShape kShapes[] = {{256, 256, 2, 1, 2.1f}, {128, 128, 2, 2, 1.7f}, {32, 64, 2, 3, 0.5f}};
+constexpr TileShape kShapes[] = {{256, 256, 2, 1, {2.1f, 7.5f}}, {128, 128, 2, 2, {1.5f, 3.8f}}, {32, 64, 2, 5, {0.75f, 1.3f}}};
+constexpr float kTileCost = 8.f;   // us for what a tile takes besides its steps
 constexpr int kUnits = 256;        // compute units
-constexpr int kLeastSteps = 8;     // of a division of a contraction
+constexpr int kLeastSteps = 4;     // of a division of a contraction
 
 struct Choice {
     Tiles tiles;
@@ -153,15 +153,15 @@ struct Choice {
     int64_t groups() const { return (int64_t)tiles_m * tiles_n * splits; }
 };
 
-int steps_of(int64_t k_bytes) { return (int)ceil_div(k_bytes, kStepBytes); }
+int steps_of(int64_t k, int dtype) { return (int)ceil_div(k * cat_size(dtype), kStepBytes); }
 
 // The tiles, and the divisions of the contraction (1, unless it may be divided), that take least time by rounds of
 // workgroups over the chip.
-Choice choose(int64_t m, int64_t n, int64_t k_bytes, bool may_split)
+Choice choose(int64_t m, int64_t n, int64_t k, int dtype, bool may_split)
 {
     Choice best{};
     float least = INFINITY;
-    const int steps = std::max(1, steps_of(k_bytes));
+    const int steps = std::max(1, steps_of(k, dtype));
     for (int t = kLarge; t <= kSmall; ++t) {
         const TileShape& s = kShapes[t];
         Choice c{(Tiles)t, (int)ceil_div(m, s.m), (int)ceil_div(n, s.n), 1, steps};
@@ -171,7 +171,7 @@ Choice choose(int64_t m, int64_t n, int64_t k_bytes, bool may_split)
             c.split_steps = (int)ceil_div(steps, c.splits);
             c.splits = (int)ceil_div(steps, c.split_steps);
         }
-        const float time = (float)ceil_div(c.groups(), slots) * s.step * (c.split_steps + 8);
+        const float time = (float)ceil_div(c.groups(), slots) * (s.step[dtype == NUTS_F32] * c.split_steps + kTileCost) + (c.splits > 1 ? 3.f : 0.f);
         if (time < least) {
             least = time;
             best = c;
@@ -180,18 +180,19 @@ Choice choose(int64_t m, int64_t n, int64_t k_bytes, bool may_split)
     return best;
 }
 
-template <ProductKind kKind, typename T>
+template <ProductKind kKind, bool kAcrossA, bool kAcrossB, typename T>
 void launch_product(const Choice& c, ProductArgs p, hipStream_t stream)
 {
     p.tiles_m = c.tiles_m;
     p.tiles_n = c.tiles_n;
     p.splits = c.splits;
     p.split_steps = c.split_steps;
+    p.streamed = (int64_t)p.m * p.n * (kKind == kOutput ? sizeof(T) : sizeof(float) * c.splits) >= kStreamed;
     const dim3 grid((unsigned)c.tiles_m * c.tiles_n, c.splits);
     switch (c.tiles) {
-    case kLarge: hipLaunchKernelGGL((product_kernel<T, 256, 256, 4, 2, 2, kKind>), grid, dim3(512), 0, stream, p); break;
-    case kMiddle: hipLaunchKernelGGL((product_kernel<T, 128, 128, 2, 2, 2, kKind>), grid, dim3(256), 0, stream, p); break;
-    case kSmall: hipLaunchKernelGGL((product_kernel<T, 32, 64, 2, 2, 4, kKind>), grid, dim3(256), 0, stream, p); break;
+    case kLarge: hipLaunchKernelGGL((product_kernel<T, 256, 256, 4, 2, 2, kAcrossA, kAcrossB, kKind>), grid, dim3(512), 0, stream, p); break;
+    case kMiddle: hipLaunchKernelGGL((product_kernel<T, 128, 128, 2, 2, 2, kAcrossA, kAcrossB, kKind>), grid, dim3(256), 0, stream, p); break;
+    case kSmall: hipLaunchKernelGGL((product_kernel<T, 32, 64, 2, 2, 2, kAcrossA, kAcrossB, kKind>), grid, dim3(256), 0, stream, p); break;
     }
 }
 
@@ -257,13 +258,12 @@ ScorePlan plan_score(const nuts_score_desc* d)
     ScorePlan p{};
     const size_t size = cat_size(d->dtype);
     p.dim_pad = round_up(d->dim, 64);
-    const int64_t k_bytes = d->dim * size;
-    p.choice = choose(d->n_rows, d->n_classes, k_bytes, false);
-    p.separate = p.choice.groups() < kSeparateGroups && steps_of(k_bytes) >= 2 * kLeastSteps;
+    p.choice = choose(d->n_rows, d->n_classes, d->dim, d->dtype, false);
+    p.separate = p.choice.groups() < kSeparateGroups && steps_of(d->dim, d->dtype) >= 4 * kLeastSteps;
     p.x = p.space.take(rows_fit(d->x_stride, d->dim, size) ? 0 : (size_t)d->n_rows * p.dim_pad * size);
     p.weight = p.space.take(rows_fit(d->weight_stride, d->dim, size) ? 0 : (size_t)d->n_classes * p.dim_pad * size);
     if (p.separate) {
-        p.choice = choose(d->n_rows, d->n_classes, k_bytes, true);
+        p.choice = choose(d->n_rows, d->n_classes, d->dim, d->dtype, true);
         p.piece = d->n_rows;
         p.logits = nuts_logits_desc{NUTS_F32, d->id_type, d->n_rows, d->n_classes, round_up(d->n_classes, 4), 0, 1.0, 0, 0};
         p.sums = p.space.take((size_t)p.choice.splits * d->n_rows * d->n_classes * sizeof(float));
@@ -286,13 +286,6 @@ void pack(const void* from, int64_t stride, int64_t rows, int64_t dim, void* to,
 {
     hipLaunchKernelGGL(pack_rows_kernel<T>, dim3((unsigned)std::min<int64_t>(rows, 65536)), dim3(kThreads), 0, stream, static_cast<const T*>(from),
                        (long)stride, (long)rows, (int)dim, static_cast<T*>(to), (long)to_stride);
-}
-
-template <typename T>
-void transpose(const void* from, int64_t stride, int64_t rows, int64_t columns, void* to, int64_t to_stride, hipStream_t stream)
-{
-    hipLaunchKernelGGL(transpose_kernel<T>, dim3((unsigned)ceil_div(to_stride, kSquare), (unsigned)ceil_div(columns, kSquare)), dim3(kThreads), 0, stream,
-                       static_cast<const T*>(from), (long)stride, (int)rows, (int)columns, static_cast<T*>(to), (long)to_stride);
 }
 
 template <typename T>
@@ -319,19 +312,17 @@ int score(const nuts_score_desc* d, const ScorePlan& p, const void* x, const voi
         weight = w + p.weight;
         weight_stride = p.dim_pad;
     }
-    // (packed rows are zero from dim to dim_pad: both then are, or both end where a piece does)
-    const int64_t k_bytes = round_up(dim * size, 16);
     ProductArgs a{};
     a.a = static_cast<const char*>(x);
     a.b = static_cast<const char*>(weight);
     a.a_stride = (long)(x_stride * size);
     a.b_stride = (long)(weight_stride * size);
     a.n = (int)d->n_classes;
-    a.k_bytes = (int)k_bytes;
+    a.k = (int)dim;
     if (p.separate) {
         a.m = (int)d->n_rows;
         a.sums = reinterpret_cast<float*>(w + p.sums);
-        launch_product<kSums, T>(p.choice, a, stream);
+        launch_product<kSums, false, false, T>(p.choice, a, stream);
         float* z = logits ? logits : reinterpret_cast<float*>(w + p.z);
         nuts_logits_desc l = p.logits;
         if (logits) l.row_stride = d->logits_stride;
@@ -353,7 +344,7 @@ int score(const nuts_score_desc* d, const ScorePlan& p, const void* x, const voi
         a.target_logit = reinterpret_cast<float*>(w + p.target_logit);
         Choice c = p.choice;
         c.tiles_m = (int)ceil_div(rows, kShapes[c.tiles].m);
-        launch_product<kScores, T>(c, a, stream);
+        launch_product<kScores, false, false, T>(c, a, stream);
         if (wanted) {
             const JoinArgs j{a.stats, a.target_logit, targets, logprob, lse, entropy, (long)row, (long)rows, p.parts, (int)d->n_classes, d->id_type};
             hipLaunchKernelGGL(join_scores_kernel, dim3((unsigned)ceil_div(rows, kThreads / 64)), dim3(kThreads), 0, stream, j);
@@ -363,11 +354,11 @@ int score(const nuts_score_desc* d, const ScorePlan& p, const void* x, const voi
     return NUTS_OK;
 }
 
-// Backward: pieces of the classes.
+// Backward: pieces of the classes.  dX reads the class weights across (classes are the contraction), dW both dZ and the features.
 struct ScoreGradPlan {
-    int64_t dim_pad, rows_pad, piece, piece_pad, pieces;
+    int64_t dim_pad, piece, piece_pad, pieces;
     Choice scores, grad_x, grad_weight;
-    size_t x, weight, x_t, weight_t, z, dz, dz_t, sums_x, sums_weight;
+    size_t x, weight, z, dz, sums_x, sums_weight;
     Space space;
 };
 
@@ -375,24 +366,20 @@ ScoreGradPlan plan_score_grad(const nuts_score_desc* d)
 {
     ScoreGradPlan p{};
     const size_t size = cat_size(d->dtype);
+    const int64_t n = std::max<int64_t>(d->n_rows, 1);
     p.dim_pad = round_up(d->dim, 64);
-    p.rows_pad = round_up(std::max<int64_t>(d->n_rows, 1), 64);
-    p.piece = std::clamp<int64_t>(kMostPiece / p.rows_pad / 256 * 256, 256, 1 << 20);
+    p.piece = std::clamp<int64_t>(kMostPiece / n / 256 * 256, 256, 1 << 20);
     p.piece = std::min(p.piece, d->n_classes);
     p.pieces = ceil_div(d->n_classes, p.piece);
     p.piece_pad = round_up(p.piece, 64);
-    const int64_t some_rows = std::max<int64_t>(d->n_rows, 1);
-    p.scores = choose(some_rows, p.piece, d->dim * size, false);
-    p.grad_x = choose(some_rows, d->dim, p.piece_pad * size, true);
-    p.grad_weight = choose(p.piece, d->dim, p.rows_pad * size, true);
+    p.scores = choose(n, p.piece, d->dim, d->dtype, false);
+    p.grad_x = choose(n, d->dim, p.piece, d->dtype, true);
+    p.grad_weight = choose(p.piece, d->dim, n, d->dtype, true);
     // (whether z is computed again is the call's)
     p.x = p.space.take(rows_fit(d->x_stride, d->dim, size) ? 0 : (size_t)d->n_rows * p.dim_pad * size);
-    p.weight = p.space.take(rows_fit(d->weight_stride, d->dim, size) ? 0 : (size_t)p.piece * p.dim_pad * size);
+    p.weight = p.space.take(rows_fit(d->weight_stride, d->dim, size) ? 0 : (size_t)d->n_classes * p.dim_pad * size);
     p.z = p.space.take((size_t)d->n_rows * p.piece_pad * sizeof(float));
-    p.x_t = p.space.take((size_t)d->dim * p.rows_pad * size);
-    p.weight_t = p.space.take((size_t)d->dim * p.piece_pad * size);
     p.dz = p.space.take((size_t)d->n_rows * p.piece_pad * size);
-    p.dz_t = p.space.take((size_t)p.piece * p.rows_pad * size);
     p.sums_x = p.space.take(p.grad_x.splits > 1 || p.pieces > 1 ? (size_t)p.grad_x.splits * d->n_rows * d->dim * sizeof(float) : 0);
     p.sums_weight = p.space.take(p.grad_weight.splits > 1 ? (size_t)p.grad_weight.splits * p.piece * d->dim * sizeof(float) : 0);
     return p;
@@ -405,84 +392,81 @@ int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, 
 {
     hipStream_t stream = api_stream();
     const int64_t size = sizeof(T), n = d->n_rows, dim = d->dim;
-    const void* own_x = x;
-    int64_t x_stride = d->x_stride;
-    if (!logits && !rows_fit(x_stride, dim, size) && n > 0) {
+    int64_t x_stride = d->x_stride, weight_stride = d->weight_stride;
+    if (!rows_fit(x_stride, dim, size) && n > 0 && (grad_weight || !logits)) {
         pack<T>(x, x_stride, n, dim, w + p.x, p.dim_pad, stream);
-        own_x = w + p.x;
+        x = w + p.x;
         x_stride = p.dim_pad;
     }
-    if (grad_weight && n > 0) transpose<T>(x, d->x_stride, n, dim, w + p.x_t, p.rows_pad, stream);
+    if (!rows_fit(weight_stride, dim, size) && n > 0 && (grad_x || !logits)) {
+        pack<T>(weight, weight_stride, d->n_classes, dim, w + p.weight, p.dim_pad, stream);
+        weight = w + p.weight;
+        weight_stride = p.dim_pad;
+    }
     for (int64_t first = 0; first < d->n_classes; first += p.piece) {
         const int64_t classes = std::min(p.piece, d->n_classes - first);
-        const char* own_weight = static_cast<const char*>(weight) + first * d->weight_stride * size;
+        const char* own_weight = static_cast<const char*>(weight) + first * weight_stride * size;
         const float* z = logits ? logits + first : nullptr;
         int64_t z_stride = d->logits_stride;
         if (!logits && n > 0) {
-            const char* rows = own_weight;
-            int64_t weight_stride = d->weight_stride;
-            if (!rows_fit(weight_stride, dim, size)) {
-                pack<T>(own_weight, weight_stride, classes, dim, w + p.weight, p.dim_pad, stream);
-                rows = w + p.weight;
-                weight_stride = p.dim_pad;
-            }
             ProductArgs a{};
-            a.a = static_cast<const char*>(own_x);
-            a.b = rows;
+            a.a = static_cast<const char*>(x);
+            a.b = own_weight;
             a.a_stride = (long)(x_stride * size);
             a.b_stride = (long)(weight_stride * size);
             a.m = (int)n;
             a.n = (int)classes;
-            a.k_bytes = (int)round_up(dim * size, 16);
+            a.k = (int)dim;
             a.c = w + p.z;
             a.c_stride = (long)p.piece_pad;
             a.scale = (float)d->scale;
             Choice c = p.scores;
             c.tiles_n = (int)ceil_div(classes, kShapes[c.tiles].n);
-            launch_product<kScores, T>(c, a, stream);
+            launch_product<kScores, false, false, T>(c, a, stream);
             z = reinterpret_cast<const float*>(w + p.z);
             z_stride = p.piece_pad;
         }
         if (n > 0) {
-            const GradArgs g{z, targets, lse, entropy, grad_logprob, grad_lse, grad_entropy, grad_x ? w + p.dz : nullptr, grad_weight ? w + p.dz_t : nullptr,
-                             (long)z_stride, (long)p.piece_pad, (long)p.rows_pad, (int)n, (int)first, (int)classes, (int)d->n_classes, d->id_type,
-                             (float)d->scale};
-            hipLaunchKernelGGL(dz_kernel<T>, dim3((unsigned)ceil_div(p.rows_pad, kSquare), (unsigned)ceil_div(p.piece_pad, kSquare)), dim3(kThreads), 0, stream, g);
+            const int parts = (int)ceil_div(p.piece_pad, kGradPacks * kThreads * (16 / size));
+            const GradArgs g{z, targets, lse, entropy, grad_logprob, grad_lse, grad_entropy, w + p.dz, (long)z_stride, (int)p.piece_pad, parts, (int)first,
+                             (int)classes, (int)d->n_classes, d->id_type, n * p.piece_pad * size >= kStreamed, (float)d->scale};
+            hipLaunchKernelGGL(dz_kernel<T>, dim3((unsigned)(n * parts)), dim3(kThreads), 0, stream, g);
         }
         if (grad_x && n > 0) {
-            transpose<T>(own_weight, d->weight_stride, classes, dim, w + p.weight_t, p.piece_pad, stream);
             ProductArgs a{};
             a.a = w + p.dz;
-            a.b = w + p.weight_t;
-            a.a_stride = a.b_stride = (long)(p.piece_pad * size);
+            a.b = own_weight;
+            a.a_stride = (long)(p.piece_pad * size);
+            a.b_stride = (long)(weight_stride * size);
             a.m = (int)n;
             a.n = (int)dim;
-            a.k_bytes = (int)(p.piece_pad * size);  // (zeros behind the last class)
+            a.k = (int)classes;
             a.sums = reinterpret_cast<float*>(w + p.sums_x);
             a.add = first > 0;
             a.c = grad_x;
             a.c_stride = (long)d->grad_x_stride;
-            if (p.grad_x.splits > 1 || p.pieces > 1) launch_product<kSums, T>(p.grad_x, a, stream);
-            else launch_product<kOutput, T>(p.grad_x, a, stream);
+            if (p.grad_x.splits > 1 || p.pieces > 1) launch_product<kSums, false, true, T>(p.grad_x, a, stream);
+            else launch_product<kOutput, false, true, T>(p.grad_x, a, stream);
         }
         if (grad_weight) {
             ProductArgs a{};
-            a.a = w + p.dz_t;
-            a.b = w + p.x_t;
-            a.a_stride = a.b_stride = (long)(p.rows_pad * size);
+            a.a = w + p.dz;
+            a.b = static_cast<const char*>(x);
+            a.a_stride = (long)(p.piece_pad * size);
+            a.b_stride = (long)(x_stride * size);
             a.m = (int)classes;
             a.n = (int)dim;
-            a.k_bytes = n > 0 ? (int)(p.rows_pad * size) : 0;  // (zeros behind the last row)
+            a.k = (int)n;
             a.sums = reinterpret_cast<float*>(w + p.sums_weight);
             a.c = static_cast<char*>(grad_weight) + first * d->grad_weight_stride * size;
             a.c_stride = (long)d->grad_weight_stride;
             Choice c = p.grad_weight;
             c.tiles_m = (int)ceil_div(classes, kShapes[c.tiles].m);
             if (c.splits > 1) {
-                launch_product<kSums, T>(c, a, stream);
+                launch_product<kSums, true, true, T>(c, a, stream);
                 add_up<T>(a.sums, c.splits, classes, dim, 1.f, a.c, d->grad_weight_stride, stream);
             } else {
-                launch_product<kOutput, T>(c, a, stream);
+                launch_product<kOutput, true, true, T>(c, a, stream);
             }
         }
     }

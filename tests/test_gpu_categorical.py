@@ -390,7 +390,8 @@ def _score_bounds(x, w, scale):
 
 
 SHAPES = [(1, 1, 1), (3, 5, 25), (2, 7, 8), (1000, 1000, 25), (100, 300, 100), (17, 1001, 72), (33, 4100, 64), (300, 513, 200), (257, 1030, 1000),
-          (1, 5000, 512), (8, 20001, 256), (130, 70, 4096), (520, 600, 130), (1500, 2100, 96)]
+          (1, 5000, 512), (8, 20001, 256), (130, 70, 4096), (520, 600, 130), (1500, 2100, 96),
+          (2000, 8200, 2104), (2050, 3000, 2100)]     # the last two: every product in the largest tiles
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
