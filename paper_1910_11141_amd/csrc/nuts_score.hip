@@ -18,12 +18,34 @@ constexpr int kThreads = 256;
 
 // ---- small kernels --------------------------------------------------------------------------------------------------
 
-// Rows at any place copied to rows of `to_stride` elements, zeros behind their end.
+struct PackArgs {
+    const void* from[2];
+    void* to[2];
+    long stride[2], rows[2];
+    int columns, to_stride;
+};
+
+// Rows at any place copied to rows of `to_stride` elements (whole 16 bytes), zeros behind their end: those of two matrices, one behind the other.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void pack_rows_kernel(const T* from, long stride, long rows, int columns, T* to, long to_stride)
+__global__ __launch_bounds__(kThreads) void pack_rows_kernel(PackArgs a)
 {
-    for (long row = blockIdx.x; row < rows; row += gridDim.x)
-        for (int i = threadIdx.x; i < to_stride; i += kThreads) to[row * to_stride + i] = i < columns ? from[row * stride + i] : static_cast<T>(0.f);
+    constexpr int kN = 16 / sizeof(T);
+    const int packs = a.to_stride / kN;
+    const long first = a.rows[0] * packs, all = first + a.rows[1] * packs;
+    for (long i = (long)blockIdx.x * kThreads + threadIdx.x; i < all; i += (long)gridDim.x * kThreads) {
+        const int which = i >= first;
+        const long at = which ? i - first : i, row = at / packs;
+        const int c = (int)(at % packs) * kN;
+        const T* from = static_cast<const T*>(a.from[which]) + row * a.stride[which] + c;
+        Pack<T, kN> x;
+        if (c + kN <= a.columns) {
+            x = load_pack<T, kN>(from);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) x.v[e] = c + e < a.columns ? from[e] : static_cast<T>(0.f);
+        }
+        store_pack(static_cast<T*>(a.to[which]) + row * a.to_stride + c, x);
+    }
 }
 
 struct GradArgs {
@@ -90,14 +112,21 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(GradArgs a)
     }
 }
 
-// out[row][column] = scale * sum over the divisions of a contraction, in order.
+// out[row][column] = scale * sum over the divisions of a contraction, in order, eight of them under way at a time.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void add_up_kernel(const float* sums, int splits, long rows, int columns, float scale, T* out, long stride)
 {
+    constexpr int kFlight = 8;
     const long all = rows * columns;
     for (long i = (long)blockIdx.x * kThreads + threadIdx.x; i < all; i += (long)gridDim.x * kThreads) {
-        float sum = sums[i];
-        for (int s = 1; s < splits; ++s) sum += sums[s * all + i];
+        float sum = 0.f;
+        for (int s = 0; s < splits; s += kFlight) {
+            float x[kFlight];
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u) x[u] = s + u < splits ? sums[(s + u) * all + i] : 0.f;
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u) sum += x[u];
+        }
         out[i / columns * stride + i % columns] = rounded<T>(sum * scale);
     }
 }
@@ -137,15 +166,17 @@ __global__ __launch_bounds__(kThreads) void join_scores_kernel(JoinArgs a)
 // ---- which tiles ------------------------------------------------------------------------------------------------------
 
 enum Tiles { kLarge, kMiddle, kSmall };
+// What tiles cost, measured on products of whole rounds of workgroups: us for a step and for the rest, when a compute unit holds as
+// many workgroups as it can.  (binary32 runs at the matrix instructions' rate in all of them.)
 struct TileShape {
-    int m, n, parts_n;  // parts_n: waves along the columns
-    int per_cu;         // workgroups that a compute unit holds
-    float step[2];      // us for a step when so many run: bfloat16, binary32
+    int m, n, parts_n;    // parts_n: waves along the columns
+    int per_cu;           // workgroups that a compute unit holds
+    float step[2], rest;  // bfloat16, binary32
 };
-constexpr TileShape kShapes[] = {{256, 256, 2, 1, {2.1f, 7.5f}}, {128, 128, 2, 2, {1.5f, 3.8f}}, {32, 64, 2, 5, {0.75f, 1.3f}}};
-constexpr float kTileCost = 8.f;   // us for what a tile takes besides its steps
-constexpr int kUnits = 256;        // compute units
-constexpr int kLeastSteps = 4;     // of a division of a contraction
+constexpr TileShape kShapes[] = {{256, 256, 2, 1, {1.5f, 7.5f}, 10.f}, {128, 128, 2, 2, {0.87f, 4.05f}, 6.f}, {32, 64, 2, 5, {0.62f, 1.33f}, 3.5f}};
+constexpr float kLeastStep = 0.35f;  // us, however few workgroups a compute unit holds: the wait for memory
+constexpr int kUnits = 256;          // compute units
+constexpr int kLeastSteps = 4;       // of a division of a contraction
 
 struct Choice {
     Tiles tiles;
@@ -155,8 +186,15 @@ struct Choice {
 
 int steps_of(int64_t k, int dtype) { return (int)ceil_div(k * cat_size(dtype), kStepBytes); }
 
-// The tiles, and the divisions of the contraction (1, unless it may be divided), that take least time by rounds of
-// workgroups over the chip.
+// us for so many workgroups of so many steps: whole rounds of them over the chip, and a last one that may leave room.
+float time_of(const TileShape& s, int dtype, int64_t groups, int steps)
+{
+    const float step = s.step[dtype == NUTS_F32];
+    const int64_t rounds = groups / (kUnits * s.per_cu), more = ceil_div(groups % (kUnits * s.per_cu), kUnits);
+    return rounds * (step * steps + s.rest) + (more ? std::max(step * more / s.per_cu, kLeastStep) * steps + s.rest : 0.f);
+}
+
+// The tiles, and the divisions of the contraction (1, unless it may be divided), that take least time.
 Choice choose(int64_t m, int64_t n, int64_t k, int dtype, bool may_split)
 {
     Choice best{};
@@ -164,17 +202,18 @@ Choice choose(int64_t m, int64_t n, int64_t k, int dtype, bool may_split)
     const int steps = std::max(1, steps_of(k, dtype));
     for (int t = kLarge; t <= kSmall; ++t) {
         const TileShape& s = kShapes[t];
-        Choice c{(Tiles)t, (int)ceil_div(m, s.m), (int)ceil_div(n, s.n), 1, steps};
-        const int64_t tiles = (int64_t)c.tiles_m * c.tiles_n, slots = (int64_t)kUnits * s.per_cu;
-        if (may_split && tiles < slots) {
-            c.splits = (int)std::max<int64_t>(1, std::min<int64_t>(slots / tiles, steps / kLeastSteps));
-            c.split_steps = (int)ceil_div(steps, c.splits);
+        const int64_t tiles = ceil_div(m, s.m) * ceil_div(n, s.n), slots = (int64_t)kUnits * s.per_cu;
+        const int most = may_split && tiles < slots ? (int)std::max<int64_t>(1, std::min<int64_t>(slots / tiles, steps / kLeastSteps)) : 1;
+        for (int splits = 1; splits <= most; ++splits) {
+            Choice c{(Tiles)t, (int)ceil_div(m, s.m), (int)ceil_div(n, s.n), 1, (int)ceil_div(steps, splits)};
             c.splits = (int)ceil_div(steps, c.split_steps);
-        }
-        const float time = (float)ceil_div(c.groups(), slots) * (s.step[dtype == NUTS_F32] * c.split_steps + kTileCost) + (c.splits > 1 ? 3.f : 0.f);
-        if (time < least) {
-            least = time;
-            best = c;
+            // the divisions' sums are stored, read and added up at 4 TB/s or so, in a launch of its own
+            const float join = c.splits > 1 ? 4.f + 8e-6f * (float)(m * n) * c.splits / 4.f : 0.f;
+            const float time = time_of(s, dtype, c.groups(), c.split_steps) + join;
+            if (time < least) {
+                least = time;
+                best = c;
+            }
         }
     }
     return best;
@@ -281,11 +320,30 @@ ScorePlan plan_score(const nuts_score_desc* d)
     return p;
 }
 
+// x and weight as the products read them: as they lie, or (`room`) copied to rows that begin at multiples of 16 bytes.
+struct Matrices {
+    const void *x, *weight;
+    int64_t x_stride, weight_stride;
+};
 template <typename T>
-void pack(const void* from, int64_t stride, int64_t rows, int64_t dim, void* to, int64_t to_stride, hipStream_t stream)
+Matrices pack(const nuts_score_desc* d, const void* x, const void* weight, bool want_x, bool want_weight, char* x_room, char* weight_room, int64_t dim_pad,
+              hipStream_t stream)
 {
-    hipLaunchKernelGGL(pack_rows_kernel<T>, dim3((unsigned)std::min<int64_t>(rows, 65536)), dim3(kThreads), 0, stream, static_cast<const T*>(from),
-                       (long)stride, (long)rows, (int)dim, static_cast<T*>(to), (long)to_stride);
+    Matrices m{x, weight, d->x_stride, d->weight_stride};
+    PackArgs a{{x, weight}, {x_room, weight_room}, {(long)d->x_stride, (long)d->weight_stride}, {0, 0}, (int)d->dim, (int)dim_pad};
+    if (want_x && !rows_fit(d->x_stride, d->dim, sizeof(T))) {
+        a.rows[0] = (long)d->n_rows;
+        m.x = x_room;
+        m.x_stride = dim_pad;
+    }
+    if (want_weight && !rows_fit(d->weight_stride, d->dim, sizeof(T))) {
+        a.rows[1] = (long)d->n_classes;
+        m.weight = weight_room;
+        m.weight_stride = dim_pad;
+    }
+    const int64_t packs = (a.rows[0] + a.rows[1]) * (dim_pad * (int64_t)sizeof(T) / 16);
+    if (packs > 0) hipLaunchKernelGGL(pack_rows_kernel<T>, dim3((unsigned)std::min<int64_t>(ceil_div(packs, kThreads), 1 << 16)), dim3(kThreads), 0, stream, a);
+    return m;
 }
 
 template <typename T>
@@ -301,22 +359,13 @@ int score(const nuts_score_desc* d, const ScorePlan& p, const void* x, const voi
 {
     hipStream_t stream = api_stream();
     const size_t size = sizeof(T);
-    int64_t x_stride = d->x_stride, weight_stride = d->weight_stride, dim = d->dim;
-    if (!rows_fit(x_stride, dim, size)) {
-        pack<T>(x, x_stride, d->n_rows, dim, w + p.x, p.dim_pad, stream);
-        x = w + p.x;
-        x_stride = p.dim_pad;
-    }
-    if (!rows_fit(weight_stride, dim, size)) {
-        pack<T>(weight, weight_stride, d->n_classes, dim, w + p.weight, p.dim_pad, stream);
-        weight = w + p.weight;
-        weight_stride = p.dim_pad;
-    }
+    const int64_t dim = d->dim;
+    const Matrices m = pack<T>(d, x, weight, true, true, w + p.x, w + p.weight, p.dim_pad, stream);
     ProductArgs a{};
-    a.a = static_cast<const char*>(x);
-    a.b = static_cast<const char*>(weight);
-    a.a_stride = (long)(x_stride * size);
-    a.b_stride = (long)(weight_stride * size);
+    a.a = static_cast<const char*>(m.x);
+    a.b = static_cast<const char*>(m.weight);
+    a.a_stride = (long)(m.x_stride * size);
+    a.b_stride = (long)(m.weight_stride * size);
     a.n = (int)d->n_classes;
     a.k = (int)dim;
     if (p.separate) {
@@ -333,7 +382,7 @@ int score(const nuts_score_desc* d, const ScorePlan& p, const void* x, const voi
     const bool wanted = logprob || lse || entropy;
     for (int64_t row = 0; row < d->n_rows; row += p.piece) {
         const int64_t rows = std::min(p.piece, d->n_rows - row);
-        a.a = static_cast<const char*>(x) + row * a.a_stride;
+        a.a = static_cast<const char*>(m.x) + row * a.a_stride;
         a.m = (int)rows;
         a.c = logits ? logits + row * d->logits_stride : nullptr;
         a.c_stride = (long)d->logits_stride;
@@ -392,28 +441,18 @@ int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, 
 {
     hipStream_t stream = api_stream();
     const int64_t size = sizeof(T), n = d->n_rows, dim = d->dim;
-    int64_t x_stride = d->x_stride, weight_stride = d->weight_stride;
-    if (!rows_fit(x_stride, dim, size) && n > 0 && (grad_weight || !logits)) {
-        pack<T>(x, x_stride, n, dim, w + p.x, p.dim_pad, stream);
-        x = w + p.x;
-        x_stride = p.dim_pad;
-    }
-    if (!rows_fit(weight_stride, dim, size) && n > 0 && (grad_x || !logits)) {
-        pack<T>(weight, weight_stride, d->n_classes, dim, w + p.weight, p.dim_pad, stream);
-        weight = w + p.weight;
-        weight_stride = p.dim_pad;
-    }
+    const Matrices m = pack<T>(d, x, weight, n > 0 && (grad_weight || !logits), n > 0 && (grad_x || !logits), w + p.x, w + p.weight, p.dim_pad, stream);
     for (int64_t first = 0; first < d->n_classes; first += p.piece) {
         const int64_t classes = std::min(p.piece, d->n_classes - first);
-        const char* own_weight = static_cast<const char*>(weight) + first * weight_stride * size;
+        const char* own_weight = static_cast<const char*>(m.weight) + first * m.weight_stride * size;
         const float* z = logits ? logits + first : nullptr;
         int64_t z_stride = d->logits_stride;
         if (!logits && n > 0) {
             ProductArgs a{};
-            a.a = static_cast<const char*>(x);
+            a.a = static_cast<const char*>(m.x);
             a.b = own_weight;
-            a.a_stride = (long)(x_stride * size);
-            a.b_stride = (long)(weight_stride * size);
+            a.a_stride = (long)(m.x_stride * size);
+            a.b_stride = (long)(m.weight_stride * size);
             a.m = (int)n;
             a.n = (int)classes;
             a.k = (int)dim;
@@ -437,7 +476,7 @@ int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, 
             a.a = w + p.dz;
             a.b = own_weight;
             a.a_stride = (long)(p.piece_pad * size);
-            a.b_stride = (long)(weight_stride * size);
+            a.b_stride = (long)(m.weight_stride * size);
             a.m = (int)n;
             a.n = (int)dim;
             a.k = (int)classes;
@@ -451,9 +490,9 @@ int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, 
         if (grad_weight) {
             ProductArgs a{};
             a.a = w + p.dz;
-            a.b = static_cast<const char*>(x);
+            a.b = static_cast<const char*>(m.x);
             a.a_stride = (long)(p.piece_pad * size);
-            a.b_stride = (long)(x_stride * size);
+            a.b_stride = (long)(m.x_stride * size);
             a.m = (int)classes;
             a.n = (int)dim;
             a.k = (int)n;
