@@ -349,8 +349,9 @@ int nuts_score(const nuts_score_desc* desc, const void* x, const void* weight, c
 /* Gradients of sum_rows grad_logprob * logprob + grad_lse * lse + grad_entropy * entropy:
  *   grad_x = dz weight, grad_weight = dz' x, dz as in nuts_logprobs_grad.
  * `logits`: what nuts_score stored, or NULL, when z is computed again.  Either gradient may be NULL.  With bfloat16 features dz is
- * rounded to bfloat16, for the matrix instructions multiply nothing wider; the products' sums are binary32.  The
- * workspace's size is that for the larger of both ways. */
+ * rounded to bfloat16, for the matrix instructions multiply nothing wider; the products' sums are binary32, and what the
+ * entries of the targets lose in that rounding, which is most of it, is added to them.  The workspace's size is that
+ * for the larger of both ways. */
 int nuts_score_grad_workspace(const nuts_score_desc* desc, int64_t* bytes);
 int nuts_score_grad(const nuts_score_desc* desc, const void* x, const void* weight, const void* targets,
                     const float* logits, const float* lse, const float* entropy, const float* grad_logprob,

@@ -49,8 +49,11 @@ struct ProductArgs {
     int streamed;   // what is stored goes past the caches
     // kScores
     float scale;
-    const void* targets;
+    const void* targets;  // (and with `residual`)
     int id_type;
+    // Of bfloat16 products with dZ, what its targets' entries lost when they were rounded, or NULL; of classes from `first_class` on
+    const float* residual;  // [row]
+    int first_class, n_classes;
     float4* stats;        // [row][tiles_n x waves along n]: m, S, T of z = scale C
     float* target_logit;  // [row]
 };
@@ -274,10 +277,95 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void product_kernel(Product
     }
     wait_and_meet<0>();  // (loads of nothing may still be under way to LDS, and other waves may still read there)
 
+    const int own_row = lane % 16, own_col = lane / 16 * 4;
+    // The entry of a row's target is most of dZ, and its rounding to 8 bits would be most of the error: what it lost is made up for.
+    if constexpr (sizeof(T) == 2 && kAcrossB && !kAcrossA) {
+        // dX: the lost part times the target's weights, in binary32
+        if (p.residual && blockIdx.y == 0) {
+#pragma unroll
+            for (int i = 0; i < kFM; ++i) {
+                const int row = m0 + (wave_m * kFM + i) * 16 + own_row;
+                const int target = row < p.m ? class_at(p.targets, p.id_type, row, p.n_classes) - p.first_class : -1;
+                if (target < 0 || target >= p.k) continue;
+                const float lost = p.residual[row];
+                const T* weights = reinterpret_cast<const T*>(p.b + (long)target * p.b_stride);
+#pragma unroll
+                for (int j = 0; j < kFN; ++j) {
+                    const int col = n0 + (wave_n * kFN + j) * 16 + own_col;
+                    if (col >= p.n) continue;  // (rows are padded to whole pieces)
+                    const Pack<T, 4> w = load_pack<T, 4>(weights + col);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) c[i][j][e] = __builtin_fmaf(lost, to_float(w.v[e]), c[i][j][e]);
+                }
+            }
+        }
+    }
+    if constexpr (sizeof(T) == 2 && kAcrossB && kAcrossA) {
+        // dW: the places of this contraction whose targets are rows of this tile, as further steps: 64 of them at a time, A with the lost
+        // parts in their targets' rows and nothing else, B with the places' features.
+        if (p.residual) {
+            constexpr int kThreads = 64 * kWaves, kEach = 8;
+            int* list = reinterpret_cast<int*>(tile_b(1));             // place in the chunk << 8 | row
+            int(*found)[kWaves] = reinterpret_cast<int(*)[kWaves]>(tile_b(2));
+            static_assert(kThreads * kEach * 4 <= B::kBytes && kM <= 256 && kAhead == 2, "");
+            const int last = min(p.k, (first + steps) * A::kPlaces);
+            for (int chunk = first * A::kPlaces; chunk < last; chunk += kThreads * kEach) {
+                int row[kEach];
+                unsigned long long hits[kEach];
+#pragma unroll
+                for (int u = 0; u < kEach; ++u) {
+                    const int place = chunk + u * kThreads + (int)threadIdx.x;
+                    row[u] = place < last ? class_at(p.targets, p.id_type, place, p.n_classes) - p.first_class - m0 : -1;
+                }
+#pragma unroll
+                for (int u = 0; u < kEach; ++u) {
+                    hits[u] = __ballot(row[u] >= 0 && row[u] < from_a.rows);
+                    if (lane == 0) found[u][wave] = __popcll(hits[u]);
+                }
+                __syncthreads();
+                int count = 0;
+                for (int u = 0; u < kEach; ++u)
+                    for (int w = 0; w < kWaves; ++w) {
+                        if (w == wave && (hits[u] >> lane & 1)) list[count + __popcll(hits[u] & ((1ull << lane) - 1))] = (u * kThreads + (int)threadIdx.x) << 8 | row[u];
+                        count += found[u][w];
+                    }
+                __syncthreads();
+                for (int g = 0; g < count; g += A::kPlaces) {
+                    for (int at = threadIdx.x * 16; at < A::kBytes; at += kThreads * 16) *reinterpret_cast<uint4*>(tile_a(0) + at) = uint4{0, 0, 0, 0};
+#pragma unroll
+                    for (int j = 0; j < B::kLoads; ++j) {
+                        const int unit = (j * kWaves + wave) * 64 + lane, line = unit / B::kPieces, piece = unit % B::kPieces ^ B::exchange(line);
+                        uint4 x{0, 0, 0, 0};
+                        if (g + line < count && piece * 8 < from_b.rows)
+                            x = *reinterpret_cast<const uint4*>(from_b.from + (long)(chunk + (list[g + line] >> 8)) * p.b_stride + piece * 16);
+                        *reinterpret_cast<uint4*>(tile_b(0) + unit * 16) = x;
+                    }
+                    __syncthreads();
+                    if ((int)threadIdx.x < A::kPlaces && g + (int)threadIdx.x < count) {
+                        const int line = threadIdx.x, entry = list[g + line], r = entry & 255;
+                        *reinterpret_cast<T*>(tile_a(0) + line * A::kPieces * 16 + ((r / 8) ^ A::exchange(line)) * 16 + r % 8 * 2) = rounded<T>(p.residual[chunk + (entry >> 8)]);
+                    }
+                    __syncthreads();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                        for (int i = 0; i < kFM; ++i) a[0][i] = A::read(tile_a(0), (wave_m * kFM + i) * 16, half, lane, read_a);
+#pragma unroll
+                        for (int j = 0; j < kFN; ++j) {
+                            const Piece<T> x = B::read(tile_b(0), (wave_n * kFN + j) * 16, half, lane, read_b);
+#pragma unroll
+                            for (int i = 0; i < kFM; ++i) c[i][j] = Piece<T>::multiply_add(x, a[0][i], c[i][j]);
+                        }
+                    }
+                    __syncthreads();
+                }
+            }
+        }
+    }
+
     // A wave stores 16 rows of its part of the tile at a time.  A lane has four neighbouring columns of one of them, which would
     // make stores of 32 or 64 bytes a row: the rows go through LDS and are stored whole.
     const int row0 = m0 + wave_m * kFM * 16, col0 = n0 + wave_n * kColumns;
-    const int own_row = lane % 16, own_col = lane / 16 * 4;
     auto store_rows = [&](auto* to, long stride, int rows, const f32x4 (&values)[kFN], bool add) {
         using Out = std::remove_pointer_t<decltype(to)>;
         constexpr int kPack = 16 / sizeof(Out), kLanes = kColumns / kPack;  // kLanes: of a row

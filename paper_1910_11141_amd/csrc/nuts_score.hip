@@ -56,7 +56,8 @@ struct GradArgs {
     const float* grad_logprob;
     const float* grad_lse;
     const float* grad_entropy;
-    void* dz;        // [rows][dz_stride], zeros behind the last class
+    void* dz;         // [rows][dz_stride], zeros behind the last class
+    float* residual;  // [rows]: what the target's entry lost in its rounding, 0 where the piece has no target; or NULL
     long z_stride;
     int dz_stride, parts, first, classes, n_classes, id_type, streamed;
     float scale;
@@ -96,18 +97,31 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(GradArgs a)
     const float g_lp = a.grad_logprob && target >= 0 && !empty ? a.grad_logprob[row] * a.scale : 0.f;
     const float g_p = (a.grad_lse ? a.grad_lse[row] * a.scale : 0.f) - g_lp, g_h = a.grad_entropy ? -a.grad_entropy[row] * a.scale : 0.f;
     const float h = a.grad_entropy ? a.entropy[row] : 0.f, ln_s = empty ? INFINITY : lse;
+    if (a.residual && y < 0 && begin == 0) a.residual[row] = 0.f;
 #pragma unroll
     for (int u = 0; u < kGradPacks; ++u) {
         const int v = begin + u * kThreads * kN;
         if (v >= a.dz_stride) break;
-        Pack<T, kN> out;
+        float g[kN];
 #pragma unroll
         for (int e = 0; e < kN; ++e) {
             const float log_p = x[u][e] - ln_s, p = __builtin_amdgcn_exp2f(log_p * kLog2e);
-            float g = p * __builtin_fmaf(g_h, fmaxf(log_p, kNothing) + h, g_p);
-            if (v + e == y) g += g_lp;
-            out.v[e] = rounded<T>(g);
+            g[e] = p * __builtin_fmaf(g_h, fmaxf(log_p, kNothing) + h, g_p);
         }
+        if (y >= v && y < v + kN) {
+#pragma unroll
+            for (int e = 0; e < kN; ++e)
+                if (v + e == y) {
+                    g[e] += g_lp;
+                    if (a.residual) {
+                        const float lost = g[e] - to_float(rounded<T>(g[e]));
+                        a.residual[row] = __builtin_fabsf(lost) < INFINITY ? lost : 0.f;
+                    }
+                }
+        }
+        Pack<T, kN> out;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) out.v[e] = rounded<T>(g[e]);
         a.streamed ? stream_pack(to + v, out) : store_pack(to + v, out);
     }
 }
@@ -407,7 +421,7 @@ int score(const nuts_score_desc* d, const ScorePlan& p, const void* x, const voi
 struct ScoreGradPlan {
     int64_t dim_pad, piece, piece_pad, pieces;
     Choice scores, grad_x, grad_weight;
-    size_t x, weight, z, dz, sums_x, sums_weight;
+    size_t x, weight, z, dz, residual, sums_x, sums_weight;
     Space space;
 };
 
@@ -429,6 +443,7 @@ ScoreGradPlan plan_score_grad(const nuts_score_desc* d)
     p.weight = p.space.take(rows_fit(d->weight_stride, d->dim, size) ? 0 : (size_t)d->n_classes * p.dim_pad * size);
     p.z = p.space.take((size_t)d->n_rows * p.piece_pad * sizeof(float));
     p.dz = p.space.take((size_t)d->n_rows * p.piece_pad * size);
+    p.residual = p.space.take((size_t)d->n_rows * sizeof(float));
     p.sums_x = p.space.take(p.grad_x.splits > 1 || p.pieces > 1 ? (size_t)p.grad_x.splits * d->n_rows * d->dim * sizeof(float) : 0);
     p.sums_weight = p.space.take(p.grad_weight.splits > 1 ? (size_t)p.grad_weight.splits * p.piece * d->dim * sizeof(float) : 0);
     return p;
@@ -442,6 +457,7 @@ int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, 
     hipStream_t stream = api_stream();
     const int64_t size = sizeof(T), n = d->n_rows, dim = d->dim;
     const Matrices m = pack<T>(d, x, weight, n > 0 && (grad_weight || !logits), n > 0 && (grad_x || !logits), w + p.x, w + p.weight, p.dim_pad, stream);
+    float* residual = targets && grad_logprob && size == 2 ? reinterpret_cast<float*>(w + p.residual) : nullptr;
     for (int64_t first = 0; first < d->n_classes; first += p.piece) {
         const int64_t classes = std::min(p.piece, d->n_classes - first);
         const char* own_weight = static_cast<const char*>(m.weight) + first * m.weight_stride * size;
@@ -467,7 +483,7 @@ int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, 
         }
         if (n > 0) {
             const int parts = (int)ceil_div(p.piece_pad, kGradPacks * kThreads * (16 / size));
-            const GradArgs g{z, targets, lse, entropy, grad_logprob, grad_lse, grad_entropy, w + p.dz, (long)z_stride, (int)p.piece_pad, parts, (int)first,
+            const GradArgs g{z, targets, lse, entropy, grad_logprob, grad_lse, grad_entropy, w + p.dz, residual, (long)z_stride, (int)p.piece_pad, parts, (int)first,
                              (int)classes, (int)d->n_classes, d->id_type, n * p.piece_pad * size >= kStreamed, (float)d->scale};
             hipLaunchKernelGGL(dz_kernel<T>, dim3((unsigned)(n * parts)), dim3(kThreads), 0, stream, g);
         }
@@ -484,6 +500,11 @@ int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, 
             a.add = first > 0;
             a.c = grad_x;
             a.c_stride = (long)d->grad_x_stride;
+            a.targets = targets;
+            a.id_type = d->id_type;
+            a.residual = residual;
+            a.first_class = (int)first;
+            a.n_classes = (int)d->n_classes;
             if (p.grad_x.splits > 1 || p.pieces > 1) launch_product<kSums, false, true, T>(p.grad_x, a, stream);
             else launch_product<kOutput, false, true, T>(p.grad_x, a, stream);
         }
@@ -499,6 +520,11 @@ int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, 
             a.sums = reinterpret_cast<float*>(w + p.sums_weight);
             a.c = static_cast<char*>(grad_weight) + first * d->grad_weight_stride * size;
             a.c_stride = (long)d->grad_weight_stride;
+            a.targets = targets;
+            a.id_type = d->id_type;
+            a.residual = n > 0 ? residual : nullptr;
+            a.first_class = (int)first;
+            a.n_classes = (int)d->n_classes;
             Choice c = p.grad_weight;
             c.tiles_m = (int)ceil_div(classes, kShapes[c.tiles].m);
             if (c.splits > 1) {

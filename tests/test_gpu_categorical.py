@@ -452,6 +452,25 @@ def test_score_grad(dtype, n, classes, dim, kept):
     assert none is None and torch.equal(only_w, grad_w)
 
 
+@pytest.mark.parametrize("n,classes,dim", [(3, 5000, 128), (700, 9000, 72), (3000, 3000, 520), (2000, 8200, 2104)])
+@pytest.mark.parametrize("kept", [True, False])
+def test_score_grad_loses_nothing_to_dz_of_8_bits(n, classes, dim, kept):
+    """Where probabilities are spread, nearly all of dZ are its targets' entries, and what these lose in their rounding is made up
+    for: the gradients are then as far off as rounding the exact ones alone makes them (the rest of dZ, of some per cent
+    in the 2-norm, adds as much of the same to it: 1.1 allows half of that again)."""
+    nuts, g = ops(), gen(n + dim)
+    x = torch.randn(n, dim, generator=g, device="cuda").bfloat16()
+    w = (torch.randn(classes, dim, generator=g, device="cuda") / math.sqrt(dim)).bfloat16()
+    targets = (torch.rand(n, generator=g, device="cuda") ** 3 * classes).long()
+    weight = torch.randn(n, generator=g, device="cuda")
+    fwd = nuts.nuts_score(x, w, targets, keep_logits=kept)
+    got = nuts.nuts_score_grad(x, w, targets, fwd.lse, grad_logprob=weight, logits=fwd.logits)
+    dz = R.grad_logits(x.double() @ w.double().t(), targets, None, 1.0, weight)
+    for a, want in zip(got, (dz @ w.double(), dz.t() @ x.double())):
+        least = float((want.bfloat16().double() - want).norm())
+        assert float((a.double() - want).norm()) <= 1.1 * least
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_score_strides_and_addresses(dtype):
     nuts, g = ops(), gen(21)
