@@ -53,34 +53,43 @@ __device__ __forceinline__ f16 rounded<f16>(float v)
     return static_cast<f16>(v);
 }
 
-// kN elements that lie next to each other at any address that suits one element.  (Loads and stores of up to 16 bytes need
-// no more than the element's alignment here: rows of an odd number of 16-bit values are read as wide as all others.)
+// kN elements that lie next to each other, 4, 8 or 16 bytes, at any address that suits one element.  (Loads and stores need no more
+// than the element's alignment here: rows of an odd number of 16-bit values are read as wide as all others.  They
+// are written as those of words: as those of a structure of elements the compiler takes many apart again.)
 template <typename T, int kN>
 struct Pack {
     T v[kN];
+    typedef __attribute__((ext_vector_type(sizeof(T) * kN / 4))) unsigned Value;
+    typedef __attribute__((ext_vector_type(sizeof(T) * kN / 4), aligned(sizeof(T)))) unsigned Words;
 };
 template <typename T, int kN>
 __device__ __forceinline__ Pack<T, kN> load_pack(const T* p)
 {
+    const typename Pack<T, kN>::Value words = *reinterpret_cast<const typename Pack<T, kN>::Words*>(p);
     Pack<T, kN> r;
-    __builtin_memcpy(&r, p, sizeof(r));
+    __builtin_memcpy(&r, &words, sizeof(r));
     return r;
 }
 template <typename T, int kN>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T, kN>& r)
 {
-    __builtin_memcpy(p, &r, sizeof(r));
+    typename Pack<T, kN>::Value words;
+    __builtin_memcpy(&words, &r, sizeof(r));
+    *reinterpret_cast<typename Pack<T, kN>::Words*>(p) = words;
 }
-
 // The same past the caches, for outputs that would push out of them what is still to be read (kStreamed).
 template <typename T, int kN>
 __device__ __forceinline__ void stream_pack(T* p, const Pack<T, kN>& r)
 {
-    static_assert(sizeof(r) == 16, "");
-    typedef __attribute__((ext_vector_type(4), aligned(2))) unsigned Words;
-    Words w;
-    __builtin_memcpy(&w, &r, sizeof(r));
-    __builtin_nontemporal_store(w, reinterpret_cast<Words*>(p));
+    typename Pack<T, kN>::Value words;
+    __builtin_memcpy(&words, &r, sizeof(r));
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("");  // (where a plain store stands beside this one the compiler would make them one: a plain one)
+#endif
+    __builtin_nontemporal_store(words, reinterpret_cast<typename Pack<T, kN>::Words*>(p));
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("");
+#endif
 }
 
 // Outputs of this many bytes and more go past the caches: half the last-level cache (256 MB).

@@ -226,10 +226,12 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogitsArgs a)
     Target target;
     if (kWhole) ask_target(a, row, target);
     Stats v{-INFINITY, 0.f, 0.f};
-    // Four packs of a thread at a time, the next four under way while these are added up; the maximum is settled once for all of them.
-    constexpr int kFlight = 4, kStep = kFlight * kThreads * kN;
+    // Two packs of a thread at a time, the next two under way while these are added up; the maximum is settled once for all of them.
+    // (Four took registers that further rows of a compute unit could use while this one names its alternatives: 4096 rows of 32001
+    // with five 75 us, with two packs 67 us; workgroups of 128 or 512 threads 68 and 88 us.)
+    constexpr int kFlight = 2, kStep = kFlight * kThreads * kN;
     int at = begin + (int)threadIdx.x * kN;
-    const int last = end - (kFlight - 1) * kThreads * kN - kN;  // where four whole packs still fit
+    const int last = end - (kFlight - 1) * kThreads * kN - kN;  // where two whole packs still fit
     if (at <= last) {
         Pack<T, kN> next[kFlight];
         unsigned may[kFlight];
@@ -373,8 +375,8 @@ struct GradArgs {
 constexpr int kGradPacks = 4;  // of a thread
 
 // A workgroup a part of a row.  Bound by its reads and writes: one exponential an element.  A large gradient is written past the
-// caches, which then keep the logits that the forward pass left there (4096 x 50001 bfloat16: 220 us with plain stores,
-// 141 us so).
+// caches, which then keep the logits that the forward pass left there (both passes on 4096 x 50001 bfloat16: 252 us with plain
+// stores, 231 us so).
 template <typename T, bool kMask, bool kEntropy>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
 {

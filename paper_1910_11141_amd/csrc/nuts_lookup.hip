@@ -9,6 +9,7 @@
 #include "nuts_cat.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace nuts {
 namespace {
@@ -64,15 +65,22 @@ struct GradArgs {
     int id_type, accumulate, lane_bits, streamed;
 };
 
-// kN columns of a row, zeros where only `left` are left.
-template <typename T, int kN>
+// kN columns of a row; fewer, and zeros behind them, for the threads at a row's ragged end (kWhole = false).  Which of both a
+// thread does is settled outside of its loops: loads on two ways that meet would be waited for one by one.
+template <typename T, int kN, bool kWhole>
 __device__ __forceinline__ Pack<T, kN> load_part(const T* p, int left)
 {
-    if (left >= kN) return load_pack<T, kN>(p);
+    if (kWhole) return load_pack<T, kN>(p);
     Pack<T, kN> x;
 #pragma unroll
     for (int e = 0; e < kN; ++e) x.v[e] = e < left ? p[e] : static_cast<T>(0.f);
     return x;
+}
+template <typename F>
+__device__ __forceinline__ void by_width(bool whole, F f)
+{
+    if (whole) f(std::true_type{});
+    else f(std::false_type{});
 }
 
 // A class's finished sum to its row of the table's gradient.
@@ -189,18 +197,20 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int clas
                 if (hit) mine[wave][__popcll(all & ((1ull << lane) - 1))] = position[m + lane];
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 const int n = left > 0 ? __popcll(all) : 0;
-                for (int q = worker; q < n; q += workers * kFlight) {
-                    Pack<T, kN> x[kFlight];
+                by_width(left >= kN, [&](auto whole) {
+                    for (int q = worker; q < n; q += workers * kFlight) {
+                        Pack<T, kN> x[kFlight];
 #pragma unroll
-                    for (int u = 0; u < kFlight; ++u)
-                        if (q + u * workers < n) x[u] = load_part<T, kN>(rows + (long)mine[wave][q + u * workers] * a.row_stride + c, left);
+                        for (int u = 0; u < kFlight; ++u)  // (one row again where there are no more)
+                            x[u] = load_part<T, kN, decltype(whole)::value>(rows + (long)mine[wave][q + u * workers < n ? q + u * workers : q] * a.row_stride + c, left);
 #pragma unroll
-                    for (int u = 0; u < kFlight; ++u)
-                        if (q + u * workers < n) {
+                        for (int u = 0; u < kFlight; ++u)
+                            if (q + u * workers < n) {
 #pragma unroll
-                            for (int e = 0; e < kN; ++e) sum[e] += to_float(x[u].v[e]);
-                        }
-                }
+                                for (int e = 0; e < kN; ++e) sum[e] += to_float(x[u].v[e]);
+                            }
+                    }
+                });
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
             for (int step = lanes; step < 64; step *= 2)
@@ -215,6 +225,40 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int clas
                 finish_columns<T, kN>(a, table + r * a.table_stride + c, left, sum);
             }
             __syncthreads();
+        }
+    }
+}
+
+// ---- gradient: clearing the rows of classes that do not come -------------------------------------------------------------
+
+constexpr int kClear = 16;  // neighbouring classes that a wave looks at to clear them
+
+struct ClearArgs {
+    const unsigned char* present;  // NULL: nothing to clear
+    char* table;
+    long stride, bytes;            // of a row
+    long from, to;                 // classes; from: a multiple of kClear
+    int first_block, streamed;
+};
+
+// Workgroups of a kernel from first_block on: a wave looks at 16 classes at once and writes the rows of those that are not present.
+__device__ void clear_rows(const ClearArgs& a)
+{
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, waves = blockDim.x / 64;
+    const long step = (long)(gridDim.x - a.first_block) * waves * kClear;
+    for (long v = a.from + ((long)(blockIdx.x - a.first_block) * waves + wave) * kClear; v < a.to; v += step) {
+        const uint4 flags = *reinterpret_cast<const uint4*>(a.present + v);  // (padded to whole words)
+        const unsigned word[4] = {flags.x, flags.y, flags.z, flags.w};
+        for (int r = 0; r < kClear; ++r) {
+            if (v + r >= a.to || (word[r / 4] >> (r % 4 * 8) & 0xff)) continue;
+            char* row = a.table + (v + r) * a.stride;
+            long b = lane * 16l;
+            const Pack<f16, 8> zeros{};
+            for (; b + 16 <= a.bytes; b += 64 * 16) {
+                f16* to = reinterpret_cast<f16*>(row + b);
+                a.streamed ? stream_pack(to, zeros) : store_pack(to, zeros);
+            }
+            for (; b < a.bytes; b += 2) *reinterpret_cast<f16*>(row + b) = static_cast<f16>(0.f);
         }
     }
 }
@@ -242,6 +286,7 @@ struct SortArgs {
     unsigned char* present;   // [n_classes]: 1 where a class comes
     long n_ids, n_classes;
     int id_type, shift, digit_bits, tile, tiles;
+    ClearArgs clear;          // what the workgroups behind those of the tiles do: small kernels leave the chip to that
 };
 
 template <bool kFirst>
@@ -255,6 +300,7 @@ __device__ __forceinline__ unsigned key_at(const SortArgs& a, long i)
 template <bool kFirst>
 __global__ __launch_bounds__(kThreads) void count_kernel(SortArgs a)
 {
+    if (!kFirst && (int)blockIdx.x >= a.tiles) return clear_rows(a.clear);
     __shared__ unsigned count[1 << kMaxDigitBits];
     const int digits = 1 << a.digit_bits;
     for (int d = threadIdx.x; d < digits; d += kThreads) count[d] = 0;
@@ -274,12 +320,13 @@ __global__ __launch_bounds__(kThreads) void count_kernel(SortArgs a)
     if (kFirst && a.present) {  // nothing is present yet
         const long words = (a.n_classes + 15) / 16;
         uint4* p = reinterpret_cast<uint4*>(a.present);
-        for (long w = (long)blockIdx.x * kThreads + threadIdx.x; w < words; w += (long)gridDim.x * kThreads) p[w] = uint4{0, 0, 0, 0};
+        for (long w = (long)blockIdx.x * kThreads + threadIdx.x; w < words; w += (long)a.tiles * kThreads) p[w] = uint4{0, 0, 0, 0};
     }
 }
 
 __global__ __launch_bounds__(1024) void places_kernel(SortArgs a)
 {
+    if (blockIdx.x >= 1) return clear_rows(a.clear);
     __shared__ unsigned total[1 << kMaxDigitBits];
     const int digits = 1 << a.digit_bits;
     for (int d = threadIdx.x; d < digits; d += 1024) {
@@ -322,6 +369,7 @@ __global__ __launch_bounds__(1024) void places_kernel(SortArgs a)
 template <bool kFirst, int kRounds>
 __global__ __launch_bounds__(kThreads) void place_kernel(SortArgs a)
 {
+    if (!kFirst && (int)blockIdx.x >= a.tiles) return clear_rows(a.clear);
     extern __shared__ unsigned next[];  // [wave][digit]
     const int digits = 1 << a.digit_bits, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
     const long begin = (long)blockIdx.x * a.tile + wave * kRounds * 64 + lane;
@@ -377,19 +425,18 @@ struct SumArgs {
     GradArgs g;
     const unsigned* keys;
     const unsigned* pos;
-    const unsigned char* present;  // NULL: no rows to clear
+    ClearArgs clear;               // of the workgroups behind sum_blocks
     float* part;                   // [chunk][2][part_stride]
     long chunks, sum_blocks, part_stride;
     int chunk;                     // positions in a chunk
 };
 
 constexpr int kBatch = 32;         // positions whose keys are read at once; a chunk is a multiple
-constexpr int kClear = 16;         // neighbouring classes that a group looks at to clear them
 constexpr int kLeastLanes = 3;     // groups of 8 threads and more: at most 32 in a workgroup
 
 // A group of 2^lane_bits threads adds the rows of one chunk of the sorted positions, a thread 16 bytes of columns.  A class that
 // lies wholly in the chunk is finished; what belongs to one that began before goes to the chunk's part 0, to one that begins
-// here and goes on to part 1.  The workgroups behind the last chunk's clear the rows of classes that do not come.
+// here and goes on to part 1.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a)
 {
@@ -402,14 +449,7 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a)
     const long c = ((long)blockIdx.y * lanes + lane) * kN;
     const int left = (int)max(0l, min((long)kN, a.g.dim - c));
     if ((long)blockIdx.x >= a.sum_blocks) {
-        const long step = ((long)gridDim.x - a.sum_blocks) * groups * kClear;
-        for (long v = (((long)blockIdx.x - a.sum_blocks) * groups + group) * kClear; v < a.g.n_classes; v += step) {
-            const uint4 flags = *reinterpret_cast<const uint4*>(a.present + v);  // (padded to whole words)
-            const unsigned word[4] = {flags.x, flags.y, flags.z, flags.w};
-#pragma unroll
-            for (int r = 0; r < kClear; ++r)
-                if (left > 0 && v + r < a.g.n_classes && !(word[r / 4] >> (r % 4 * 8) & 0xff)) zero_columns<T, kN>(a.g, table + (v + r) * a.g.table_stride + c, left);
-        }
+        if (blockIdx.y == 0) clear_rows(a.clear);
         return;
     }
     const long q = (long)blockIdx.x * groups + group;
@@ -443,28 +483,29 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a)
             current = keys[group][0];
             entered = current == before;
         }
-        for (int i = 0; i < kBatch && keys[group][i] != none; i += kFlight) {  // (no class: such keys are the last)
-            Pack<T, kN> x[kFlight];
+        if (left > 0)
+            by_width(left >= kN, [&](auto whole) {
+                for (int i = 0; i < kBatch && keys[group][i] != none; i += kFlight) {  // (no class: such keys are the last)
+                    Pack<T, kN> x[kFlight];
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u)
-                if (keys[group][i + u] != none && left > 0) x[u] = load_part<T, kN>(rows + (long)positions[group][i + u] * a.g.row_stride, left);
+                    for (int u = 0; u < kFlight; ++u)  // (a row of no class is read and not used)
+                        x[u] = load_part<T, kN, decltype(whole)::value>(rows + (long)positions[group][i + u] * a.g.row_stride, left);
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u) {
-                const unsigned key = keys[group][i + u];
-                if (key == none) break;
-                if (key != current) {
-                    flush(false);
-                    current = key;
-                    entered = false;
+                    for (int u = 0; u < kFlight; ++u) {
+                        const unsigned key = keys[group][i + u];
+                        if (key == none) break;
+                        if (key != current) {
+                            flush(false);
+                            current = key;
+                            entered = false;
 #pragma unroll
-                    for (int e = 0; e < kN; ++e) sum[e] = 0.f;
+                            for (int e = 0; e < kN; ++e) sum[e] = 0.f;
+                        }
+#pragma unroll
+                        for (int e = 0; e < kN; ++e) sum[e] += to_float(x[u].v[e]);
+                    }
                 }
-                if (left > 0) {
-#pragma unroll
-                    for (int e = 0; e < kN; ++e) sum[e] += to_float(x[u].v[e]);
-                }
-            }
-        }
+            });
         __syncthreads();
     }
     flush(current == after);
@@ -499,19 +540,18 @@ __global__ __launch_bounds__(kThreads) void join_kernel(SumArgs a)
     }
     const long parts = more + 2;  // this chunk's, those of the chunks that it goes on beyond, that of the one where it ends
     const long c = ((long)blockIdx.y * 64 + lane) * 4;
-    const bool inside = c < a.part_stride;
-    const float* part = a.part + q * 2 * a.part_stride + c;
+    const float* part = a.part + q * 2 * a.part_stride + min(c, a.part_stride - 4);
     float4 sum{0.f, 0.f, 0.f, 0.f};
     for (long r = wave; r < parts; r += kThreads / 64 * kFlight) {
         float4 x[kFlight];
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
-            const long at = r + u * (kThreads / 64);
-            if (at < parts && inside) x[u] = *reinterpret_cast<const float4*>(part + (at * 2 + (at == 0 ? 1 : 0)) * a.part_stride);
+            const long at = min(r + u * (kThreads / 64), parts - 1);  // (one part again where there are no more)
+            x[u] = *reinterpret_cast<const float4*>(part + (at * 2 + (at == 0 ? 1 : 0)) * a.part_stride);
         }
 #pragma unroll
         for (int u = 0; u < kFlight; ++u)
-            if (r + u * (kThreads / 64) < parts && inside) {
+            if (r + u * (kThreads / 64) < parts) {
                 sum.x += x[u].x;
                 sum.y += x[u].y;
                 sum.z += x[u].z;
@@ -665,21 +705,37 @@ int nuts_lookup_grad(const nuts_lookup_desc* d, const void* grad_rows, const voi
     }
     char* w = static_cast<char*>(workspace);
     unsigned char* present = d->accumulate ? nullptr : reinterpret_cast<unsigned char*>(w + p.present);
+    // The rows to clear are known when the first digit has been placed: what is left of the sort, three small kernels a digit, clears
+    // them in equal shares beside it (with one digit the kernel of the sums does).
+    const int64_t size = (int64_t)cat_size(d->dtype);
+    const int shares = std::max(1, 3 * (p.passes - 1));
+    const int64_t share = ceil_div(ceil_div(d->n_classes, shares), kClear) * kClear;
+    int shared_out = 0;
+    auto next_share = [&](int first_block, int waves, unsigned* more) {
+        ClearArgs c{present, static_cast<char*>(grad_table), (long)(d->table_stride * size), (long)(d->dim * size),
+                    (long)std::min(d->n_classes, share * shared_out), (long)std::min(d->n_classes, share * (shared_out + 1)), first_block, a.g.streamed};
+        ++shared_out;
+        *more = present ? (unsigned)std::min<int64_t>(ceil_div(c.to - c.from, waves * kClear), 1 << 16) : 0u;
+        return c;
+    };
+    unsigned more = 0;
     for (int k = 0; k < p.passes; ++k) {
         SortArgs s{ids, reinterpret_cast<unsigned*>(w + p.keys[(k + 1) & 1]), reinterpret_cast<unsigned*>(w + p.pos[(k + 1) & 1]),
                    reinterpret_cast<unsigned*>(w + p.keys[k & 1]), reinterpret_cast<unsigned*>(w + p.pos[k & 1]),
                    reinterpret_cast<unsigned*>(w + p.counts), reinterpret_cast<unsigned*>(w + p.starts), present,
-                   (long)d->n_ids, (long)d->n_classes, d->id_type, k * p.digit_bits, p.digit_bits, p.tile, p.tiles};
+                   (long)d->n_ids, (long)d->n_classes, d->id_type, k * p.digit_bits, p.digit_bits, p.tile, p.tiles, ClearArgs{}};
         const size_t lds = (size_t)kWaves * sizeof(unsigned) << p.digit_bits;
-        hipLaunchKernelGGL(k == 0 ? count_kernel<true> : count_kernel<false>, dim3(p.tiles), dim3(kThreads), 0, stream, s);
-        hipLaunchKernelGGL(places_kernel, dim3(1), dim3(1024), 0, stream, s);
+        if (k > 0) s.clear = next_share(p.tiles, kWaves, &more);
+        hipLaunchKernelGGL(k == 0 ? count_kernel<true> : count_kernel<false>, dim3(p.tiles + more), dim3(kThreads), 0, stream, s);
+        if (k > 0) s.clear = next_share(1, 1024 / 64, &more);
+        hipLaunchKernelGGL(places_kernel, dim3(1 + more), dim3(1024), 0, stream, s);
         void (*place)(SortArgs) = d->n_ids <= kManyIds ? (k == 0 ? place_kernel<true, kFewRounds> : place_kernel<false, kFewRounds>)
                                                        : (k == 0 ? place_kernel<true, kManyRounds> : place_kernel<false, kManyRounds>);
-        hipLaunchKernelGGL(place, dim3(p.tiles), dim3(kThreads), lds, stream, s);
+        if (k > 0) s.clear = next_share(p.tiles, kWaves, &more);
+        hipLaunchKernelGGL(place, dim3(p.tiles + more), dim3(kThreads), lds, stream, s);
     }
     a.keys = reinterpret_cast<unsigned*>(w + p.keys[(p.passes - 1) & 1]);
     a.pos = reinterpret_cast<unsigned*>(w + p.pos[(p.passes - 1) & 1]);
-    a.present = present;
     a.part = reinterpret_cast<float*>(w + p.part);
     a.chunks = p.chunks;
     a.chunk = p.chunk;
@@ -688,11 +744,12 @@ int nuts_lookup_grad(const nuts_lookup_desc* d, const void* grad_rows, const voi
     const int groups = kThreads >> a.g.lane_bits;
     const int64_t columns = (int64_t)(16 / cat_size(d->dtype)) << a.g.lane_bits;
     a.sum_blocks = (long)ceil_div(p.chunks, groups);
-    const unsigned clear = present ? (unsigned)std::min<int64_t>(ceil_div(d->n_classes, groups * kClear), 1 << 16) : 0u;
     const unsigned slices = (unsigned)ceil_div(d->dim, columns);
+    more = 0;
+    if (p.passes == 1) a.clear = next_share((int)a.sum_blocks, kWaves, &more);
     by_dtype(d->dtype, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)a.sum_blocks + clear, slices), dim3(kThreads), 0, stream, a);
+        hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)a.sum_blocks + more, slices), dim3(kThreads), 0, stream, a);
         if (p.chunks > 1)
             hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)(p.chunks - 1), (unsigned)ceil_div(d->dim, 256)), dim3(kThreads), 0, stream, a);
     });
