@@ -40,7 +40,8 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs a)
     const int id = class_at(a.ids, a.id_type, row, a.n_classes);
     const T* from = static_cast<const T*>(a.table) + max(id, 0) * a.table_stride;
     T* to = static_cast<T*>(a.rows) + row * a.row_stride;
-    for (long c = (long)lane * kN; c < a.dim; c += (long)lanes * kN) {
+    for (long first = (long)lane * kN; first < a.dim; first += (long)lanes * kN) {
+        const long c = max(0l, min(first, a.dim - kN));  // (a ragged row's last columns: 16 bytes that end with the row)
         if (c + kN <= a.dim) {
             Pack<T, kN> x;
             if (id >= 0) x = load_pack<T, kN>(from + c);
@@ -63,6 +64,19 @@ struct GradArgs {
     long n_ids, n_classes, dim, table_stride, row_stride;
     float scale;
     int id_type, accumulate, lane_bits, streamed;
+};
+
+// The columns of the pack that begins at column `first`: where nothing is accumulated, the last pack of a ragged row ends with the
+// row and shares columns with the one before, which has the same sums.
+template <typename T, int kN>
+struct Columns {
+    long c;
+    int left;  // columns from c on, at most kN; 0 behind the row
+    __device__ Columns(const GradArgs& a, long first)
+    {
+        c = a.accumulate || a.dim < kN ? first : min(first, a.dim - kN);
+        left = first < a.dim ? (int)min((long)kN, a.dim - c) : 0;
+    }
 };
 
 // kN columns of a row; fewer, and zeros behind them, for the threads at a row's ragged end (kWhole = false).  Which of both a
@@ -119,17 +133,39 @@ __device__ __forceinline__ void zero_columns(const GradArgs& a, T* p, int left)
     }
 }
 
+// Threads that go together over the pieces of neighbouring rows: piece `first` of all rows' and every step-th behind it, without a
+// division at each.
+struct Steps {
+    long row;
+    int piece;
+    const int pieces, piece_step;
+    const long row_step;
+    __device__ Steps(long first, long step, int n) : row(first / n), piece((int)(first % n)), pieces(n), piece_step((int)(step % n)), row_step(step / n) {}
+    __device__ void next()
+    {
+        row += row_step;
+        piece += piece_step;
+        if (piece >= pieces) {
+            piece -= pieces;
+            ++row;
+        }
+    }
+};
+
 // ---- gradient of few rows: one launch --------------------------------------------------------------------------------
 
 constexpr int kFewEach = 4;                    // positions of a thread
 constexpr int kFew = kFewEach * kThreads;      // positions that a workgroup looks through by itself
 constexpr int kFewRows = 64;                   // at most so many classes a workgroup (an occupancy mask is one word)
 
-// A workgroup owns `classes` neighbouring rows of the table: it finds the positions of theirs among all n (few, from
-// cache) and adds them up.  What bounds it is the wait for memory, twice at least, and again for every 32 rows or so of
-// the class that comes most often.
+// A workgroup owns `classes` neighbouring rows of the table, or a slice of their columns: it finds the positions of theirs among all
+// n (few, from cache) and adds them up.  What bounds it is the wait for memory, twice at least, and again for every 32 rows or so of
+// the class that comes most often (1000 positions, 1000 classes of 100 in binary32: 8 us; without the slices, 1000 classes of 2048 in
+// binary32 took 76 us, now 16).  Sorting them first, as for more positions, takes three launches: 15 us for 1100 positions where
+// this takes 11 for 1000.  Only a table that has to be cleared and is too large for the caches is cleared faster beside a sort
+// (100003 classes of 2048 in bfloat16, 1000 positions: 77 us so, 92 by this kernel).
 template <typename T>
-__global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int classes, long first_block)
+__global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int classes, long slice_packs, long first_block)
 {
     constexpr int kN = 16 / sizeof(T);
     constexpr int kFlight = 8;
@@ -171,14 +207,13 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int clas
         }
     __syncthreads();
     const unsigned long long occupied = occupied_half[0] | (unsigned long long)occupied_half[1] << 32;
-    const int packs = (int)((a.dim + kN - 1) / kN);
+    const int first = (int)(blockIdx.y * slice_packs), packs = (int)min(slice_packs, (a.dim + kN - 1) / kN - first);
     T* table = static_cast<T*>(a.table) + v0 * a.table_stride;
     const T* rows = static_cast<const T*>(a.rows);
     if (!a.accumulate)
-        for (long i = threadIdx.x; i < (long)own * packs; i += kThreads) {
-            const int r = (int)(i / packs);
-            const long c = i % packs * kN;
-            if (!(occupied >> r & 1)) zero_columns<T, kN>(a, table + r * a.table_stride + c, (int)min((long)kN, a.dim - c));
+        for (Steps at(threadIdx.x, kThreads, packs); at.row < own; at.next()) {
+            const Columns<T, kN> at_row(a, (long)(first + at.piece) * kN);
+            if (!(occupied >> at.row & 1)) zero_columns<T, kN>(a, table + at.row * a.table_stride + at_row.c, at_row.left);
         }
     // Each class is added up by the whole workgroup: a row is read by 2^lane_bits lanes of a wave (or by a wave in several
     // turns), and every wave has a list of the class's positions for itself, of which its groups of lanes take turns.
@@ -186,8 +221,9 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int clas
     for (unsigned long long rest = occupied; rest; rest &= rest - 1) {
         const int r = __builtin_ctzll(rest);
         for (int p = lane & (lanes - 1); p < ((packs + lanes - 1) & -lanes); p += lanes) {
-            const long c = (long)p * kN;
-            const int left = (int)max(0l, min((long)kN, a.dim - c));
+            const Columns<T, kN> columns(a, (long)(first + p) * kN);
+            const long c = columns.c;
+            const int left = p < packs ? columns.left : 0;
             float sum[kN];
 #pragma unroll
             for (int e = 0; e < kN; ++e) sum[e] = 0.f;
@@ -234,32 +270,47 @@ __global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int clas
 constexpr int kClear = 16;  // neighbouring classes that a wave looks at to clear them
 
 struct ClearArgs {
-    const unsigned char* present;  // NULL: nothing to clear
+    const unsigned char* present;  // NULL: every row is cleared
     char* table;
     long stride, bytes;            // of a row
     long from, to;                 // classes; from: a multiple of kClear
     int first_block, streamed;
 };
 
-// Workgroups of a kernel from first_block on: a wave looks at 16 classes at once and writes the rows of those that are not present.
+// 16 bytes of a row of zeros, the last of them up to its end; shorter rows element by element.
+__device__ __forceinline__ void clear_piece(const ClearArgs& a, long row, int piece)
+{
+    char* to = a.table + row * a.stride;
+    const Pack<f16, 8> zeros{};
+    if (a.bytes >= 16) {
+        f16* p = reinterpret_cast<f16*>(to + min(piece * 16l, a.bytes - 16));
+        a.streamed ? stream_pack(p, zeros) : store_pack(p, zeros);
+    } else {
+        for (int b = 0; b < a.bytes; b += 2) *reinterpret_cast<f16*>(to + b) = static_cast<f16>(0.f);
+    }
+}
+
+// Workgroups of a kernel from first_block on.  Where not all rows are cleared, a wave looks at 16 classes at once.
 __device__ void clear_rows(const ClearArgs& a)
 {
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, waves = blockDim.x / 64;
-    const long step = (long)(gridDim.x - a.first_block) * waves * kClear;
-    for (long v = a.from + ((long)(blockIdx.x - a.first_block) * waves + wave) * kClear; v < a.to; v += step) {
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, waves = blockDim.x / 64, pieces = (int)((a.bytes + 15) / 16);
+    const long block = (long)blockIdx.x - a.first_block, blocks = (long)gridDim.x - a.first_block;
+    if (!a.present) {
+        for (Steps at(block * blockDim.x + threadIdx.x, blocks * blockDim.x, pieces); a.from + at.row < a.to; at.next())
+            clear_piece(a, a.from + at.row, at.piece);
+        return;
+    }
+    for (long v = a.from + (block * waves + wave) * kClear; v < a.to; v += blocks * waves * kClear) {
         const uint4 flags = *reinterpret_cast<const uint4*>(a.present + v);  // (padded to whole words)
-        const unsigned word[4] = {flags.x, flags.y, flags.z, flags.w};
+        unsigned absent = 0;
+#pragma unroll
         for (int r = 0; r < kClear; ++r) {
-            if (v + r >= a.to || (word[r / 4] >> (r % 4 * 8) & 0xff)) continue;
-            char* row = a.table + (v + r) * a.stride;
-            long b = lane * 16l;
-            const Pack<f16, 8> zeros{};
-            for (; b + 16 <= a.bytes; b += 64 * 16) {
-                f16* to = reinterpret_cast<f16*>(row + b);
-                a.streamed ? stream_pack(to, zeros) : store_pack(to, zeros);
-            }
-            for (; b < a.bytes; b += 2) *reinterpret_cast<f16*>(row + b) = static_cast<f16>(0.f);
+            const unsigned word = r < 4 ? flags.x : r < 8 ? flags.y : r < 12 ? flags.z : flags.w;
+            absent |= (unsigned)!(word >> r % 4 * 8 & 0xff) << r;
         }
+        const long rows = min((long)kClear, a.to - v);
+        for (Steps at(lane, 64, pieces); at.row < rows; at.next())
+            if (absent >> at.row & 1) clear_piece(a, v + at.row, at.piece);
     }
 }
 
@@ -419,6 +470,75 @@ __global__ __launch_bounds__(kThreads) void place_kernel(SortArgs a)
     }
 }
 
+// Up to 10240 positions are sorted in one launch: a position's place is the number of those of lower classes and of those before it
+// of its own.  A workgroup finds the places of 16 positions, each of its threads counts for all of them among every 256th: n^2 / 64
+// comparisons of a wave, 7 us at 2000 positions, where the launches of the digits' sort take 25 us together.  At 8000 the whole
+// gradient takes 27 us so and 41 by digits (1000 classes of 25, binary32), at 16000 54 and 40.
+constexpr int kRanked = 16;
+constexpr long kRankedIds = 10240;
+
+struct RankArgs {
+    const void* ids;
+    unsigned* keys;
+    unsigned* pos;
+    long n_ids, n_classes;
+    int id_type, blocks;
+    ClearArgs clear;  // of the workgroups behind `blocks`
+};
+
+__global__ __launch_bounds__(kThreads) void rank_kernel(RankArgs a)
+{
+    if ((int)blockIdx.x >= a.blocks) return clear_rows(a.clear);
+    constexpr int kFlight = 8, kLanes = kThreads / kRanked;
+    __shared__ unsigned own_keys[kRanked];
+    __shared__ int counts[kRanked][kThreads + 1];
+    const int n = (int)a.n_ids, first = (int)blockIdx.x * kRanked, last = min(first + kRanked, n);
+    auto key_of = [&](int i) {
+        const int id = class_at(a.ids, a.id_type, i, a.n_classes);
+        return id < 0 ? (unsigned)a.n_classes : (unsigned)id;
+    };
+    if (threadIdx.x < kRanked) own_keys[threadIdx.x] = key_of(min(first + (int)threadIdx.x, n - 1));
+    __syncthreads();
+    unsigned own[kRanked];
+    int count[kRanked];
+#pragma unroll
+    for (int o = 0; o < kRanked; ++o) {
+        own[o] = __builtin_amdgcn_readfirstlane(own_keys[o]);
+        count[o] = 0;
+    }
+    auto count_below = [&](int begin, int end) {  // positions of keys below own[]
+        for (int j = begin + (int)threadIdx.x; j < end; j += kFlight * kThreads) {
+            unsigned key[kFlight];
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u) key[u] = j + u * kThreads < end ? key_of(j + u * kThreads) : ~0u;
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u)
+#pragma unroll
+                for (int o = 0; o < kRanked; ++o) count[o] += key[u] < own[o] ? 1 : 0;
+        }
+    };
+    count_below(first, n);
+#pragma unroll
+    for (int o = 0; o < kRanked; ++o) ++own[o];  // before its own position equal keys count too
+    count_below(0, first);
+    if ((int)threadIdx.x < last - first) {
+        const unsigned key = own_keys[threadIdx.x];
+#pragma unroll
+        for (int o = 0; o < kRanked; ++o) count[o] += (int)threadIdx.x < o && key == own_keys[o] ? 1 : 0;
+    }
+#pragma unroll
+    for (int o = 0; o < kRanked; ++o) counts[o][threadIdx.x] = count[o];
+    __syncthreads();
+    const int o = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    int place = 0;
+    for (int t = lane; t < kThreads; t += kLanes) place += counts[o][t];
+    for (int step = kLanes / 2; step; step /= 2) place += __shfl_xor(place, step);
+    if (lane == 0 && first + o < last) {
+        a.keys[place] = own_keys[o];
+        a.pos[place] = (unsigned)(first + o);
+    }
+}
+
 // ---- gradient: adding up sorted rows ---------------------------------------------------------------------------------
 
 struct SumArgs {
@@ -432,6 +552,10 @@ struct SumArgs {
 };
 
 constexpr int kBatch = 32;         // positions whose keys are read at once; a chunk is a multiple
+// Where the whole call waits for single groups, chunks are shorter (1000 classes of 25, binary32: 1100 positions 20 us with 32 in a
+// chunk, 17 with 16, 15 with 8; of 2048, bfloat16, 4000 positions 22 us with 16, 24 with 8, and 10000 41 and 46).
+constexpr int kFewChunk = 8;
+constexpr long kFewChunkIds = 4096;
 constexpr int kLeastLanes = 3;     // groups of 8 threads and more: at most 32 in a workgroup
 
 // A group of 2^lane_bits threads adds the rows of one chunk of the sorted positions, a thread 16 bytes of columns.  A class that
@@ -446,8 +570,9 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a)
     const int lanes = 1 << a.g.lane_bits, groups = kThreads >> a.g.lane_bits, group = threadIdx.x >> a.g.lane_bits;
     const int lane = threadIdx.x & (lanes - 1);
     T* table = static_cast<T*>(a.g.table);
-    const long c = ((long)blockIdx.y * lanes + lane) * kN;
-    const int left = (int)max(0l, min((long)kN, a.g.dim - c));
+    const Columns<T, kN> columns(a.g, ((long)blockIdx.y * lanes + lane) * kN);
+    const long c = columns.c;
+    const int left = columns.left;
     if ((long)blockIdx.x >= a.sum_blocks) {
         if (blockIdx.y == 0) clear_rows(a.clear);
         return;
@@ -467,7 +592,7 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a)
         if (entered || open) {  // (parts are padded to whole packs)
             float* to = a.part + (q * 2 + (entered ? 0 : 1)) * a.part_stride + c;
 #pragma unroll
-            for (int e = 0; e < kN; e += 4) *reinterpret_cast<float4*>(to + e) = float4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
+            for (int e = 0; e < kN; e += 4) store_pack(to + e, Pack<float, 4>{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]});
         } else {
             finish_columns<T, kN>(a.g, table + current * a.g.table_stride + c, left, sum);
         }
@@ -600,8 +725,9 @@ int lane_bits_of(int64_t dim, int dtype, int least)
 }
 
 struct GradPlan {
-    bool few;
+    bool few, ranked;
     int few_classes;
+    long slice_packs;
     int digit_bits, passes, tile, tiles;
     int chunk;
     long chunks, part_stride;
@@ -612,20 +738,26 @@ struct GradPlan {
 GradPlan plan_grad(const nuts_lookup_desc* d)
 {
     GradPlan p{};
-    p.few = d->n_ids <= kFew;
+    const bool large = !d->accumulate && d->n_classes * d->dim * (int64_t)cat_size(d->dtype) >= kStreamed;
+    p.few = d->n_ids <= kFew && !large;
+    p.ranked = !p.few && d->n_ids <= kRankedIds;
     if (p.few) {
-        // about a thousand workgroups where the table has so many rows: each looks through all positions again
+        // about a thousand workgroups where the table has so many rows: each looks through all positions again; else the columns
+        // are shared out too
         p.few_classes = (int)std::clamp<int64_t>(d->n_classes / 1024, 4, kFewRows);
+        const int64_t packs = ceil_div(d->dim, 16 / (int64_t)cat_size(d->dtype)), lanes = 1 << std::min(6, lane_bits_of(d->dim, d->dtype, 0));
+        const int64_t slices = std::clamp<int64_t>(2048 / ceil_div(d->n_classes, p.few_classes), 1, ceil_div(packs, lanes));
+        p.slice_packs = (long)(ceil_div(ceil_div(packs, lanes), slices) * lanes);
         return p;
     }
     int bits = 1;
     while (d->n_classes >> bits) ++bits;  // n_classes itself is a key
-    p.passes = (bits + kMaxDigitBits - 1) / kMaxDigitBits;
-    p.digit_bits = (bits + p.passes - 1) / p.passes;
+    p.passes = p.ranked ? 0 : (bits + kMaxDigitBits - 1) / kMaxDigitBits;
+    p.digit_bits = p.ranked ? 0 : (bits + p.passes - 1) / p.passes;
     p.tile = (d->n_ids <= kManyIds ? kFewRounds : kManyRounds) * kThreads;
     p.tiles = (int)ceil_div(d->n_ids, p.tile);
     // chunks: short enough that there are a thousand workgroups, long enough that a class over many of them is joined from few parts
-    p.chunk = kBatch;
+    p.chunk = d->n_ids <= kFewChunkIds ? kFewChunk : p.ranked ? 2 * kFewChunk : kBatch;
     while (d->n_ids / (p.chunk * 2) >= 1024 * (int64_t)(kThreads >> lane_bits_of(d->dim, d->dtype, kLeastLanes))) p.chunk *= 2;
     p.chunks = ceil_div(d->n_ids, p.chunk);
     auto take = [&](size_t bytes) {
@@ -633,13 +765,15 @@ GradPlan plan_grad(const nuts_lookup_desc* d)
         p.bytes += (bytes + 255) & ~(size_t)255;
         return at;
     };
-    p.counts = take((size_t)p.tiles * sizeof(unsigned) << p.digit_bits);
-    p.starts = take(sizeof(unsigned) << p.digit_bits);
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < std::min(2, std::max(1, p.passes)); ++s) {
         p.keys[s] = take(sizeof(unsigned) * d->n_ids);
         p.pos[s] = take(sizeof(unsigned) * d->n_ids);
     }
-    p.present = take((size_t)d->n_classes + kClear);
+    if (!p.ranked) {
+        p.counts = take((size_t)p.tiles * sizeof(unsigned) << p.digit_bits);
+        p.starts = take(sizeof(unsigned) << p.digit_bits);
+        p.present = take((size_t)d->n_classes + kClear);
+    }
     p.part_stride = (long)(ceil_div(d->dim, 8) * 8);
     p.part = take((size_t)p.chunks * 2 * p.part_stride * sizeof(float));
     return p;
@@ -696,9 +830,11 @@ int nuts_lookup_grad(const nuts_lookup_desc* d, const void* grad_rows, const voi
     if (p.few) {
         a.g.lane_bits = std::min(6, lane_bits_of(d->dim, d->dtype, 0));
         by_dtype(d->dtype, [&](auto t) {
+            constexpr int64_t kN = 16 / sizeof(decltype(t));
+            const unsigned slices = (unsigned)ceil_div(ceil_div(d->dim, kN), p.slice_packs);
             for (long first = 0, blocks = (long)ceil_div(d->n_classes, p.few_classes); first < blocks; first += kMaxBlocks)
-                hipLaunchKernelGGL(few_rows_kernel<decltype(t)>, dim3((unsigned)std::min(blocks - first, kMaxBlocks)), dim3(kThreads), 0, stream, a.g,
-                                   p.few_classes, first);
+                hipLaunchKernelGGL(few_rows_kernel<decltype(t)>, dim3((unsigned)std::min(blocks - first, kMaxBlocks), slices), dim3(kThreads), 0, stream,
+                                   a.g, p.few_classes, p.slice_packs, first);
         });
         NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
         return NUTS_OK;
@@ -719,6 +855,15 @@ int nuts_lookup_grad(const nuts_lookup_desc* d, const void* grad_rows, const voi
         return c;
     };
     unsigned more = 0;
+    if (p.ranked) {
+        // So few positions' rows cost less to write twice than to find out about beforehand: all are cleared, 8 pieces a thread.
+        RankArgs r{ids, reinterpret_cast<unsigned*>(w + p.keys[0]), reinterpret_cast<unsigned*>(w + p.pos[0]), (long)d->n_ids, (long)d->n_classes,
+                   d->id_type, (int)ceil_div(d->n_ids, kRanked), ClearArgs{}};
+        r.clear = ClearArgs{nullptr, static_cast<char*>(grad_table), (long)(d->table_stride * size), (long)(d->dim * size), 0, (long)d->n_classes,
+                            r.blocks, a.g.streamed};
+        if (!d->accumulate) more = (unsigned)std::min<int64_t>(ceil_div(d->n_classes * ceil_div(d->dim * size, 16), 8 * kThreads), 1 << 16);
+        hipLaunchKernelGGL(rank_kernel, dim3(r.blocks + more), dim3(kThreads), 0, stream, r);
+    }
     for (int k = 0; k < p.passes; ++k) {
         SortArgs s{ids, reinterpret_cast<unsigned*>(w + p.keys[(k + 1) & 1]), reinterpret_cast<unsigned*>(w + p.pos[(k + 1) & 1]),
                    reinterpret_cast<unsigned*>(w + p.keys[k & 1]), reinterpret_cast<unsigned*>(w + p.pos[k & 1]),
@@ -734,8 +879,9 @@ int nuts_lookup_grad(const nuts_lookup_desc* d, const void* grad_rows, const voi
         if (k > 0) s.clear = next_share(p.tiles, kWaves, &more);
         hipLaunchKernelGGL(place, dim3(p.tiles + more), dim3(kThreads), lds, stream, s);
     }
-    a.keys = reinterpret_cast<unsigned*>(w + p.keys[(p.passes - 1) & 1]);
-    a.pos = reinterpret_cast<unsigned*>(w + p.pos[(p.passes - 1) & 1]);
+    const int sorted = p.ranked ? 0 : (p.passes - 1) & 1;
+    a.keys = reinterpret_cast<unsigned*>(w + p.keys[sorted]);
+    a.pos = reinterpret_cast<unsigned*>(w + p.pos[sorted]);
     a.part = reinterpret_cast<float*>(w + p.part);
     a.chunks = p.chunks;
     a.chunk = p.chunk;

@@ -114,6 +114,15 @@ def test_lookup_grad(dtype, kind, n, classes, dim):
     assert torch.equal(into[absent], old[absent])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kind", ["skewed", "one", "outside"])
+@pytest.mark.parametrize("n,classes,dim", [
+    (255, 9, 2100), (256, 1000, 1025), (257, 100, 25), (1000, 20011, 100), (1025, 70001, 3), (2049, 1000, 130), (4097, 9, 515), (8191, 3000, 33),
+    (16384, 5000, 7), (16385, 1500, 34), (16385, 70001, 5), (20001, 2048, 9)])
+def test_lookup_grad_of_many_lengths(dtype, kind, n, classes, dim):
+    test_lookup_grad(dtype, kind, n, classes, dim)
+
+
 @pytest.mark.parametrize("n", [700, 3000])
 def test_lookup_grad_strides_and_infinities(n):
     nuts, g = ops(), gen(n)
