@@ -12,8 +12,10 @@
 // binary32 rows are read element by element, bfloat16 by the loads that transpose 4 x 16 elements.
 //
 // What lies outside the matrices is read as zero by the bounds of the buffer descriptors: rows behind the last by their
-// offset, and pieces behind the contraction's end by an offset that no buffer has.  (Rows have to begin at multiples of 16
-// bytes; a row that lies along has to consist of whole pieces.  Others are copied first.)
+// offset, and pieces behind the contraction's end by an offset that no buffer has.  Rows have to begin at multiples of 4
+// bytes (others are copied first).  A piece at the ragged end of a row holds the beginning of the next one too.  Across, that makes
+// sums that are not stored; along, it is cleared in LDS before it is read (kRagged; or, dZ, it is zero beside lines that are: behind the
+// contraction's end 0 times infinity would count).
 //
 // The first operand of an instruction is B: a lane then holds four neighbouring columns of one row of C, which are stored
 // together, and most of a reduction along a row of C stays within lanes.
@@ -37,7 +39,7 @@ struct ProductArgs {
     const char* a;
     const char* b;
     long a_stride, b_stride;  // bytes from row to row (across: from place to place of the contraction)
-    int m, n, k;              // (along: zeros behind k up to a whole piece)
+    int m, n, k;
     int tiles_m, tiles_n;
     int splits, split_steps;  // the contraction is divided: steps of a division
     // kSums: binary32 [split][m][n], added to what is there if `add`
@@ -127,8 +129,8 @@ struct Operand {
     __device__ __forceinline__ Step at_step(const char* to, int step, bool none, int wave) const
     {
         const int left = k - step * kPlaces;
-        // (the last line up to a whole piece: a buffer reads no part of a word)
-        const int line = ((kAcross ? rows : k) * kSize + 15) / 16 * 16;
+        // (a buffer reads no part of a word)
+        const int line = ((kAcross ? rows : k) * kSize + 3) & ~3;
         const int bytes = (int)((kAcross ? min(left, kPlaces) - 1 : rows - 1) * stride) + line;
         const unsigned long long base = (unsigned long long)(from + (kAcross && !none ? (long)step * kPlaces * stride : 0));
         return Step{Descriptor{(unsigned)base, (unsigned)(base >> 32), none ? 0u : (unsigned)bytes, 0x00027000u},
@@ -142,6 +144,16 @@ struct Operand {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(s.to + j * (kWaves * 1024u)), "v"(at[j] | s.skip), "s"(s.buffer),
                      "s"(s.place)
                      : "m0");
+    }
+
+    // Along, a tile of the step in which the contraction ends inside a piece: the rest of that piece.
+    __device__ __forceinline__ void clear_tail(char* tile, int step) const
+    {
+        static_assert(!kAcross, "");
+        constexpr int kPer = 16 / kSize;
+        const int left = k - step * kPlaces;
+        for (int row = threadIdx.x; row < kRows; row += 64 * kWaves)
+            for (int e = left % kPer; e < kPer; ++e) reinterpret_cast<T*>(tile + row * kStepBytes + (left / kPer ^ row % 8) * 16)[e] = static_cast<T>(0.f);
     }
 
     // Where a lane reads: its place in a tile, and what its row is exchanged by.
@@ -202,7 +214,7 @@ __device__ __forceinline__ void wait_and_meet()
 
 // kAhead steps are under way to LDS while one is multiplied; B has a buffer more than A, so that its loads are spread over the
 // first half of a step and those of A over the second, behind the barrier at which all are done with the step before.
-template <typename T, int kM, int kN, int kWavesM, int kWavesN, int kAhead, bool kAcrossA, bool kAcrossB, ProductKind kKind>
+template <typename T, int kM, int kN, int kWavesM, int kWavesN, int kAhead, bool kAcrossA, bool kAcrossB, bool kRagged, ProductKind kKind>
 __global__ __launch_bounds__(64 * kWavesM * kWavesN) void product_kernel(ProductArgs p)
 {
 #ifdef __HIP_DEVICE_COMPILE__
@@ -241,6 +253,16 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void product_kernel(Product
 #pragma unroll
         for (int j = 0; j < kFN; ++j) c[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     wait_and_meet<(kAhead - 1) * (A::kLoads + B::kLoads)>();
+    const int ragged = first + steps == all_steps ? steps - 1 : -1;  // the step in which the contraction ends
+    auto clear_tails = [&](int s) {
+        if constexpr (kRagged) {
+            if (s != ragged) return;
+            from_a.clear_tail(tile_a(s), first + s);
+            from_b.clear_tail(tile_b(s), first + s);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        }
+    };
+    clear_tails(0);
     // A half step in kFN turns: a column of the products of this half, behind which the column's piece of the next half takes
     // the place of this one's, and with each a part of the rows' pieces of the next half and of the loads.
     typename A::Reader read_a = A::reader(lane);
@@ -272,6 +294,7 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void product_kernel(Product
         const typename B::Step step_b = from_b.at_step(tile_b(s + kAhead), first + s + kAhead, s + kAhead >= steps, wave);
         half_step(0, s, [&](int l) { from_b.fetch(step_b, l); }, B::kLoads);
         wait_and_meet<(kAhead - 1) * B::kLoads + (kAhead - 2) * A::kLoads>();
+        clear_tails(s + 1);
         const typename A::Step step_a = from_a.at_step(tile_a(s + kAhead), first + s + kAhead, s + kAhead >= steps, wave);
         half_step(1, s + 1, [&](int l) { from_a.fetch(step_a, l); }, A::kLoads);
     }
@@ -292,10 +315,15 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void product_kernel(Product
 #pragma unroll
                 for (int j = 0; j < kFN; ++j) {
                     const int col = n0 + (wave_n * kFN + j) * 16 + own_col;
-                    if (col >= p.n) continue;  // (rows are padded to whole pieces)
-                    const Pack<T, 4> w = load_pack<T, 4>(weights + col);
+                    if (col + 4 <= p.n) {
+                        const Pack<T, 4> w = load_pack<T, 4>(weights + col);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) c[i][j][e] = __builtin_fmaf(lost, to_float(w.v[e]), c[i][j][e]);
+                        for (int e = 0; e < 4; ++e) c[i][j][e] = __builtin_fmaf(lost, to_float(w.v[e]), c[i][j][e]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 3; ++e)
+                            if (col + e < p.n) c[i][j][e] = __builtin_fmaf(lost, to_float(weights[col + e]), c[i][j][e]);
+                    }
                 }
             }
         }
@@ -335,10 +363,18 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void product_kernel(Product
 #pragma unroll
                     for (int j = 0; j < B::kLoads; ++j) {
                         const int unit = (j * kWaves + wave) * 64 + lane, line = unit / B::kPieces, piece = unit % B::kPieces ^ B::exchange(line);
-                        uint4 x{0, 0, 0, 0};
-                        if (g + line < count && piece * 8 < from_b.rows)
-                            x = *reinterpret_cast<const uint4*>(from_b.from + (long)(chunk + (list[g + line] >> 8)) * p.b_stride + piece * 16);
-                        *reinterpret_cast<uint4*>(tile_b(0) + unit * 16) = x;
+                        Pack<T, 8> x{};
+                        if (g + line < count) {
+                            const T* features = reinterpret_cast<const T*>(from_b.from + (long)(chunk + (list[g + line] >> 8)) * p.b_stride) + piece * 8;
+                            if (piece * 8 + 8 <= from_b.rows) {
+                                x = load_pack<T, 8>(features);
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 7; ++e)
+                                    if (piece * 8 + e < from_b.rows) x.v[e] = features[e];
+                            }
+                        }
+                        *reinterpret_cast<Pack<T, 8>*>(__builtin_assume_aligned(tile_b(0) + unit * 16, 16)) = x;
                     }
                     __syncthreads();
                     if ((int)threadIdx.x < A::kPlaces && g + (int)threadIdx.x < count) {

@@ -242,11 +242,18 @@ void launch_product(const Choice& c, ProductArgs p, hipStream_t stream)
     p.split_steps = c.split_steps;
     p.streamed = (int64_t)p.m * p.n * (kKind == kOutput ? sizeof(T) : sizeof(float) * c.splits) >= kStreamed;
     const dim3 grid((unsigned)c.tiles_m * c.tiles_n, c.splits);
-    switch (c.tiles) {
-    case kLarge: hipLaunchKernelGGL((product_kernel<T, 256, 256, 4, 2, 2, kAcrossA, kAcrossB, kKind>), grid, dim3(512), 0, stream, p); break;
-    case kMiddle: hipLaunchKernelGGL((product_kernel<T, 128, 128, 2, 2, 2, kAcrossA, kAcrossB, kKind>), grid, dim3(256), 0, stream, p); break;
-    case kSmall: hipLaunchKernelGGL((product_kernel<T, 32, 64, 2, 2, 2, kAcrossA, kAcrossB, kKind>), grid, dim3(256), 0, stream, p); break;
+    auto launch = [&](auto ragged) {  // (a kernel of its own: what it does beside the steps would cost the others 3 %)
+        constexpr bool kRagged = decltype(ragged)::value;
+        switch (c.tiles) {
+        case kLarge: hipLaunchKernelGGL((product_kernel<T, 256, 256, 4, 2, 2, kAcrossA, kAcrossB, kRagged, kKind>), grid, dim3(512), 0, stream, p); break;
+        case kMiddle: hipLaunchKernelGGL((product_kernel<T, 128, 128, 2, 2, 2, kAcrossA, kAcrossB, kRagged, kKind>), grid, dim3(256), 0, stream, p); break;
+        case kSmall: hipLaunchKernelGGL((product_kernel<T, 32, 64, 2, 2, 2, kAcrossA, kAcrossB, kRagged, kKind>), grid, dim3(256), 0, stream, p); break;
+        }
+    };
+    if constexpr (!kAcrossA && !kAcrossB) {
+        if (p.k % (int)(16 / sizeof(T)) != 0) return launch(std::true_type{});
     }
+    launch(std::false_type{});
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------------
@@ -281,10 +288,14 @@ struct Space {
 
 int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 
-// Whether rows can be read as they lie.
-bool rows_fit(int64_t stride, int64_t dim, size_t size)
+// Whether rows are read as they lie.  Rows that begin between 16 bytes touch a line of memory more each step, which costs less than
+// to copy them, up to several thousand rows of x: with 2046 or 4094 bfloat16 features, 1000 rows' gradients of 32001 classes 530 us
+// and 597 with copies, 4096 rows' 1593 and 1610, but 8192 rows' scores of 32000 classes 1785 and 1675.
+constexpr int64_t kCopiedRows = 6144;
+bool rows_fit(const nuts_score_desc* d, int64_t stride)
 {
-    return stride * size % 16 == 0 && dim * size % 16 == 0 && stride * size <= (size_t)kMostBufferBytes / 256;
+    const int64_t bytes = stride * (int64_t)cat_size(d->dtype);
+    return bytes <= kMostBufferBytes / 256 && (bytes % 16 == 0 || (bytes % 4 == 0 && d->n_rows < kCopiedRows));
 }
 bool aligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -313,8 +324,8 @@ ScorePlan plan_score(const nuts_score_desc* d)
     p.dim_pad = round_up(d->dim, 64);
     p.choice = choose(d->n_rows, d->n_classes, d->dim, d->dtype, false);
     p.separate = p.choice.groups() < kSeparateGroups && steps_of(d->dim, d->dtype) >= 4 * kLeastSteps;
-    p.x = p.space.take(rows_fit(d->x_stride, d->dim, size) ? 0 : (size_t)d->n_rows * p.dim_pad * size);
-    p.weight = p.space.take(rows_fit(d->weight_stride, d->dim, size) ? 0 : (size_t)d->n_classes * p.dim_pad * size);
+    p.x = p.space.take(rows_fit(d, d->x_stride) ? 0 : (size_t)d->n_rows * p.dim_pad * size);
+    p.weight = p.space.take(rows_fit(d, d->weight_stride) ? 0 : (size_t)d->n_classes * p.dim_pad * size);
     if (p.separate) {
         p.choice = choose(d->n_rows, d->n_classes, d->dim, d->dtype, true);
         p.piece = d->n_rows;
@@ -338,23 +349,25 @@ ScorePlan plan_score(const nuts_score_desc* d)
 struct Matrices {
     const void *x, *weight;
     int64_t x_stride, weight_stride;
+    int64_t dim;  // with the zeros behind rows of whole pieces
 };
 template <typename T>
 Matrices pack(const nuts_score_desc* d, const void* x, const void* weight, bool want_x, bool want_weight, char* x_room, char* weight_room, int64_t dim_pad,
               hipStream_t stream)
 {
-    Matrices m{x, weight, d->x_stride, d->weight_stride};
+    Matrices m{x, weight, d->x_stride, d->weight_stride, d->dim};
     PackArgs a{{x, weight}, {x_room, weight_room}, {(long)d->x_stride, (long)d->weight_stride}, {0, 0}, (int)d->dim, (int)dim_pad};
-    if (want_x && !rows_fit(d->x_stride, d->dim, sizeof(T))) {
+    if (want_x && !rows_fit(d, d->x_stride)) {
         a.rows[0] = (long)d->n_rows;
         m.x = x_room;
         m.x_stride = dim_pad;
     }
-    if (want_weight && !rows_fit(d->weight_stride, d->dim, sizeof(T))) {
+    if (want_weight && !rows_fit(d, d->weight_stride)) {
         a.rows[1] = (long)d->n_classes;
         m.weight = weight_room;
         m.weight_stride = dim_pad;
     }
+    if (a.rows[0] && a.rows[1]) m.dim = round_up(d->dim, 16 / sizeof(T));
     const int64_t packs = (a.rows[0] + a.rows[1]) * (dim_pad * (int64_t)sizeof(T) / 16);
     if (packs > 0) hipLaunchKernelGGL(pack_rows_kernel<T>, dim3((unsigned)std::min<int64_t>(ceil_div(packs, kThreads), 1 << 16)), dim3(kThreads), 0, stream, a);
     return m;
@@ -373,7 +386,6 @@ int score(const nuts_score_desc* d, const ScorePlan& p, const void* x, const voi
 {
     hipStream_t stream = api_stream();
     const size_t size = sizeof(T);
-    const int64_t dim = d->dim;
     const Matrices m = pack<T>(d, x, weight, true, true, w + p.x, w + p.weight, p.dim_pad, stream);
     ProductArgs a{};
     a.a = static_cast<const char*>(m.x);
@@ -381,7 +393,7 @@ int score(const nuts_score_desc* d, const ScorePlan& p, const void* x, const voi
     a.a_stride = (long)(m.x_stride * size);
     a.b_stride = (long)(m.weight_stride * size);
     a.n = (int)d->n_classes;
-    a.k = (int)dim;
+    a.k = (int)m.dim;
     if (p.separate) {
         a.m = (int)d->n_rows;
         a.sums = reinterpret_cast<float*>(w + p.sums);
@@ -439,8 +451,8 @@ ScoreGradPlan plan_score_grad(const nuts_score_desc* d)
     p.grad_x = choose(n, d->dim, p.piece, d->dtype, true);
     p.grad_weight = choose(p.piece, d->dim, n, d->dtype, true);
     // (whether z is computed again is the call's)
-    p.x = p.space.take(rows_fit(d->x_stride, d->dim, size) ? 0 : (size_t)d->n_rows * p.dim_pad * size);
-    p.weight = p.space.take(rows_fit(d->weight_stride, d->dim, size) ? 0 : (size_t)d->n_classes * p.dim_pad * size);
+    p.x = p.space.take(rows_fit(d, d->x_stride) ? 0 : (size_t)d->n_rows * p.dim_pad * size);
+    p.weight = p.space.take(rows_fit(d, d->weight_stride) ? 0 : (size_t)d->n_classes * p.dim_pad * size);
     p.z = p.space.take((size_t)d->n_rows * p.piece_pad * sizeof(float));
     p.dz = p.space.take((size_t)d->n_rows * p.piece_pad * size);
     p.residual = p.space.take((size_t)d->n_rows * sizeof(float));
@@ -471,7 +483,7 @@ int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, 
             a.b_stride = (long)(m.weight_stride * size);
             a.m = (int)n;
             a.n = (int)classes;
-            a.k = (int)dim;
+            a.k = (int)m.dim;
             a.c = w + p.z;
             a.c_stride = (long)p.piece_pad;
             a.scale = (float)d->scale;

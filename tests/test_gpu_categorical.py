@@ -497,6 +497,33 @@ def test_score_strides_and_addresses(dtype):
             assert all(torch.equal(p, q) for p, q in zip(u, v))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,classes,dim,stride", [(5, 70, 1, 1), (5, 70, 3, 4), (40, 500, 25, 26), (3, 9000, 301, 302), (300, 600, 97, 100), (64, 6000, 1030, 1030),
+                                                  (520, 2300, 513, 514), (600, 2100, 2101, 2101), (6200, 300, 37, 38)])
+def test_score_reads_nothing_but_its_rows(dtype, n, classes, dim, stride):
+    """What lies between the rows and behind the last is not finite."""
+    nuts, g = ops(), gen(n + dim)
+    x, w = (torch.randn(rows, dim, generator=g, device="cuda").to(dtype) for rows in (n, classes))
+    targets = torch.randint(-1, classes, (n,), generator=g, device="cuda")
+    ones = torch.ones(n, device="cuda")
+    views = []
+    for a in (x, w):
+        room = torch.full((a.shape[0] * stride + 64,), math.nan, dtype=dtype, device="cuda")
+        room[1::2] = math.inf
+        view = room[:a.shape[0] * stride].view(-1, stride)[:, :dim]
+        view.copy_(a)
+        views.append(view)
+    got, want = nuts.nuts_score(*views, targets, keep_logits=True), nuts.nuts_score(x, w, targets, keep_logits=True)
+    z, off = _score_bounds(x, w, 1.0)
+    assert bool(((got.logits.double() - z).abs() <= off).all())
+    assert all(torch.allclose(p, q, rtol=1e-4, atol=1e-3) for p, q in zip(got, want))
+    for kept in (got.logits, None):
+        u = nuts.nuts_score_grad(*views, targets, want.lse, grad_logprob=ones, logits=kept)
+        v = nuts.nuts_score_grad(x, w, targets, want.lse, grad_logprob=ones, logits=want.logits if kept is not None else None)
+        for p, q in zip(u, v):
+            assert bool(torch.isfinite(p).all()) and float((p.double() - q.double()).norm()) <= 0.01 * float(q.double().norm()) + 1e-6
+
+
 def test_score_grad_over_several_pieces():
     """More logits than one piece of the classes holds: what is summed over pieces is the same gradient."""
     nuts, g = ops(), gen(22)
