@@ -161,7 +161,7 @@ constexpr int kFewRows = 64;                   // at most so many classes a work
 // A workgroup owns `classes` neighbouring rows of the table, or a slice of their columns: it finds the positions of theirs among all
 // n (few, from cache) and adds them up.  What bounds it is the wait for memory, twice at least, and again for every 32 rows or so of
 // the class that comes most often (1000 positions, 1000 classes of 100 in binary32: 8 us; without the slices, 1000 classes of 2048 in
-// binary32 took 76 us, now 16).  Sorting them first, as for more positions, takes three launches: 15 us for 1100 positions where
+// binary32 took 76 us, now 16; up to 4096 workgroups: 100 positions, 4168 classes of 1842, binary32 14 us, 23 with 2048 and 19 with 16384).  Sorting them first, as for more positions, takes three launches: 15 us for 1100 positions where
 // this takes 11 for 1000.  Only a table that has to be cleared and is too large for the caches is cleared faster beside a sort
 // (100003 classes of 2048 in bfloat16, 1000 positions: 77 us so, 92 by this kernel).
 template <typename T>
@@ -470,12 +470,13 @@ __global__ __launch_bounds__(kThreads) void place_kernel(SortArgs a)
     }
 }
 
-// Up to 10240 positions are sorted in one launch: a position's place is the number of those of lower classes and of those before it
+// Not too many positions are sorted in one launch: a position's place is the number of those of lower classes and of those before it
 // of its own.  A workgroup finds the places of 16 positions, each of its threads counts for all of them among every 256th: n^2 / 64
-// comparisons of a wave, 7 us at 2000 positions, where the launches of the digits' sort take 25 us together.  At 8000 the whole
-// gradient takes 27 us so and 41 by digits (1000 classes of 25, binary32), at 16000 54 and 40.
+// comparisons of a wave, 7 us at 2000 positions, where the launches of the digits' sort take 25 us together.  The whole gradient of 1000
+// classes of 25 (one digit), binary32: 8000 positions 26 us so and 41 by digits, 16000 54 and 40; of 160000 classes of 800 (two
+// digits), bfloat16: 16000 positions 70 and 83.
 constexpr int kRanked = 16;
-constexpr long kRankedIds = 10240;
+constexpr long kRankedIds = 10240, kRankedIdsOfMany = 16384;  // one digit; more
 
 struct RankArgs {
     const void* ids;
@@ -740,18 +741,18 @@ GradPlan plan_grad(const nuts_lookup_desc* d)
     GradPlan p{};
     const bool large = !d->accumulate && d->n_classes * d->dim * (int64_t)cat_size(d->dtype) >= kStreamed;
     p.few = d->n_ids <= kFew && !large;
-    p.ranked = !p.few && d->n_ids <= kRankedIds;
     if (p.few) {
         // about a thousand workgroups where the table has so many rows: each looks through all positions again; else the columns
         // are shared out too
         p.few_classes = (int)std::clamp<int64_t>(d->n_classes / 1024, 4, kFewRows);
         const int64_t packs = ceil_div(d->dim, 16 / (int64_t)cat_size(d->dtype)), lanes = 1 << std::min(6, lane_bits_of(d->dim, d->dtype, 0));
-        const int64_t slices = std::clamp<int64_t>(2048 / ceil_div(d->n_classes, p.few_classes), 1, ceil_div(packs, lanes));
+        const int64_t slices = std::clamp<int64_t>(4096 / ceil_div(d->n_classes, p.few_classes), 1, ceil_div(packs, lanes));
         p.slice_packs = (long)(ceil_div(ceil_div(packs, lanes), slices) * lanes);
         return p;
     }
     int bits = 1;
     while (d->n_classes >> bits) ++bits;  // n_classes itself is a key
+    p.ranked = d->n_ids <= (bits <= kMaxDigitBits ? kRankedIds : kRankedIdsOfMany);
     p.passes = p.ranked ? 0 : (bits + kMaxDigitBits - 1) / kMaxDigitBits;
     p.digit_bits = p.ranked ? 0 : (bits + p.passes - 1) / p.passes;
     p.tile = (d->n_ids <= kManyIds ? kFewRounds : kManyRounds) * kThreads;
