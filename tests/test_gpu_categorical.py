@@ -118,9 +118,20 @@ def test_lookup_grad(dtype, kind, n, classes, dim):
 @pytest.mark.parametrize("kind", ["skewed", "one", "outside"])
 @pytest.mark.parametrize("n,classes,dim", [
     (255, 9, 2100), (256, 1000, 1025), (257, 100, 25), (1000, 20011, 100), (1025, 70001, 3), (2049, 1000, 130), (4097, 9, 515), (8191, 3000, 33),
-    (16384, 5000, 7), (16385, 1500, 34), (16385, 70001, 5), (20001, 2048, 9)])
+    (16384, 5000, 7), (16385, 1500, 34), (16385, 70001, 5), (20001, 2048, 9),
+    (70000, 2000, 5), (70000, 1000003, 3), (140000, 20000, 4)])
 def test_lookup_grad_of_many_lengths(dtype, kind, n, classes, dim):
-    test_lookup_grad(dtype, kind, n, classes, dim)
+    nuts, g = ops(), gen(n + classes + dim)
+    grad = torch.randn(n, dim, generator=g, device="cuda").to(dtype)
+    ids = _ids(kind, n, classes, g).to(torch.int32 if dim % 2 else torch.int64)
+    old = torch.randn(classes, dim, generator=g, device="cuda").to(dtype)
+    for start in (None, old):
+        into = torch.full_like(old, 7.0) if start is None else old.clone()
+        got = nuts.nuts_lookup_grad(grad, ids, classes, scale=0.75, out=into, accumulate=start is not None)
+        # (added up on the CPU: many additions of 64 bits to one place take seconds on the GPU)
+        want, bound = R.lookup_grad(grad.cpu(), ids.cpu(), classes, 0.75, None if start is None else start.cpu())
+        assert bool(((got.cpu().double() - want).abs() <= bound).all())
+    assert torch.equal(nuts.nuts_lookup_grad(grad, ids, classes, scale=0.75), nuts.nuts_lookup_grad(grad, ids, classes, scale=0.75))
 
 
 @pytest.mark.parametrize("n", [700, 3000])
