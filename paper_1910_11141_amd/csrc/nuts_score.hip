@@ -65,7 +65,8 @@ struct GradArgs {
 
 constexpr int kGradPacks = 4;  // of a thread
 
-// dZ, rounded to the features' type: a workgroup a part of a row.
+// dZ, rounded to the features' type: a workgroup a part of a row.  Bound by its reads and writes: 4096 x 32001, to bfloat16, 142 us, 787
+// MB at 5.5 TB/s.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dz_kernel(GradArgs a)
 {
@@ -126,22 +127,38 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(GradArgs a)
     }
 }
 
-// out[row][column] = scale * sum over the divisions of a contraction, in order, eight of them under way at a time.
-template <typename T>
+// out[row][column] = scale * sum over the divisions of a contraction, in order, eight of them under way at a time, kN columns a thread.
+// Bound by its reads and writes (2 divisions of 4096 x 2048, to bfloat16: 17 us, 84 MB at 5 TB/s; a column a thread 23 us).
+template <typename T, int kN>
 __global__ __launch_bounds__(kThreads) void add_up_kernel(const float* sums, int splits, long rows, int columns, float scale, T* out, long stride)
 {
     constexpr int kFlight = 8;
     const long all = rows * columns;
-    for (long i = (long)blockIdx.x * kThreads + threadIdx.x; i < all; i += (long)gridDim.x * kThreads) {
-        float sum = 0.f;
+    for (long i = ((long)blockIdx.x * kThreads + threadIdx.x) * kN; i < all; i += (long)gridDim.x * kThreads * kN) {
+        float sum[kN];
+#pragma unroll
+        for (int e = 0; e < kN; ++e) sum[e] = 0.f;
         for (int s = 0; s < splits; s += kFlight) {
-            float x[kFlight];
+            Pack<float, kN> x[kFlight];
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u) x[u] = s + u < splits ? sums[(s + u) * all + i] : 0.f;
+            for (int u = 0; u < kFlight; ++u)
+                if (s + u < splits) x[u] = load_pack<float, kN>(sums + (s + u) * all + i);
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u) sum += x[u];
+            for (int u = 0; u < kFlight; ++u)
+                if (s + u < splits) {
+#pragma unroll
+                    for (int e = 0; e < kN; ++e) sum[e] += x[u].v[e];
+                }
         }
-        out[i / columns * stride + i % columns] = rounded<T>(sum * scale);
+        T* to = out + i / columns * stride + i % columns;
+        if constexpr (kN == 1) {
+            *to = rounded<T>(sum[0] * scale);
+        } else {
+            Pack<T, kN> pack;
+#pragma unroll
+            for (int e = 0; e < kN; ++e) pack.v[e] = rounded<T>(sum[e] * scale);
+            store_pack(to, pack);
+        }
     }
 }
 
@@ -156,7 +173,7 @@ struct JoinArgs {
     int parts, n_classes, id_type;
 };
 
-// A wave a row: the statistics of its tiles joined.
+// A wave a row: the statistics of its tiles joined (8192 rows of 250 parts: 10 us, 34 MB).
 __global__ __launch_bounds__(kThreads) void join_scores_kernel(JoinArgs a)
 {
     const long row = (long)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
@@ -376,8 +393,9 @@ Matrices pack(const nuts_score_desc* d, const void* x, const void* weight, bool 
 template <typename T>
 void add_up(const float* sums, int splits, int64_t rows, int64_t columns, float scale, void* out, int64_t stride, hipStream_t stream)
 {
-    hipLaunchKernelGGL(add_up_kernel<T>, dim3((unsigned)std::min<int64_t>(ceil_div(rows * columns, kThreads), 16384)), dim3(kThreads), 0, stream, sums,
-                       splits, (long)rows, (int)columns, scale, static_cast<T*>(out), (long)stride);
+    const int each = columns % 4 == 0 ? 4 : 1;
+    hipLaunchKernelGGL((each == 4 ? add_up_kernel<T, 4> : add_up_kernel<T, 1>), dim3((unsigned)std::min<int64_t>(ceil_div(rows * columns, kThreads * each), 16384)),
+                       dim3(kThreads), 0, stream, sums, splits, (long)rows, (int)columns, scale, static_cast<T*>(out), (long)stride);
 }
 
 template <typename T>
