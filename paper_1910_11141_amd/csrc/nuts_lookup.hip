@@ -963,7 +963,7 @@ int nuts_lookup_grad(const nuts_lookup_desc* d, const void* grad_rows, const voi
     if (p.passes == 1) a.clear = next_share((int)a.sum_blocks, kWaves, &more);
     by_dtype(d->dtype, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)a.sum_blocks + more, slices), dim3(kThreads), 0, stream, a);
+        if (p.chunks > 0) hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)a.sum_blocks + more, slices), dim3(kThreads), 0, stream, a);
         if (p.chunks > 1)
             hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)(p.chunks - 1), (unsigned)ceil_div(d->dim, 256)), dim3(kThreads), 0, stream, a);
     });

@@ -134,6 +134,22 @@ def test_lookup_grad_of_many_lengths(dtype, kind, n, classes, dim):
     assert torch.equal(nuts.nuts_lookup_grad(grad, ids, classes, scale=0.75), nuts.nuts_lookup_grad(grad, ids, classes, scale=0.75))
 
 
+@pytest.mark.parametrize("n", [0, 1, 40, 1025])
+def test_lookup_grad_of_a_table_past_the_caches(n):
+    nuts, g = ops(), gen(n)
+    classes, dim = 70001, 1027
+    grad = torch.randn(n, dim, generator=g, device="cuda").bfloat16()
+    ids = torch.randint(0, classes, (n,), generator=g, device="cuda")
+    ids[n // 2:] = 70000
+    out = torch.full((classes, dim), 3.0, dtype=torch.bfloat16, device="cuda")
+    nuts.nuts_lookup_grad(grad, ids, classes, out=out)
+    there, back = ids.unique(return_inverse=True)
+    want, bound = R.lookup_grad(grad.cpu(), back.cpu(), max(1, len(there)), 1.0)
+    assert bool(((out[there].cpu().double() - want[:len(there)]).abs() <= bound[:len(there)]).all())
+    out[there] = 0
+    assert not bool(out.any())
+
+
 @pytest.mark.parametrize("n", [700, 3000])
 def test_lookup_grad_strides_and_infinities(n):
     nuts, g = ops(), gen(n)
@@ -510,7 +526,7 @@ def test_score_strides_and_addresses(dtype):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("n,classes,dim,stride", [(5, 70, 1, 1), (5, 70, 3, 4), (40, 500, 25, 26), (3, 9000, 301, 302), (300, 600, 97, 100), (64, 6000, 1030, 1030),
-                                                  (520, 2300, 513, 514), (600, 2100, 2101, 2101), (6200, 300, 37, 38)])
+                                                  (520, 2300, 513, 514), (600, 2100, 2101, 2101), (6200, 300, 37, 38), (3, 900, 1031, 1032), (40, 300, 2051, 2054)])
 def test_score_reads_nothing_but_its_rows(dtype, n, classes, dim, stride):
     """What lies between the rows and behind the last is not finite."""
     nuts, g = ops(), gen(n + dim)
