@@ -533,11 +533,12 @@ __global__ __launch_bounds__(kThreads) void place_kernel(SortArgs a)
 }
 
 // Not too many positions are sorted in one launch: a position's place is the number of those of lower classes and of those before it
-// of its own.  A workgroup finds the places of 16 positions, each of its threads counts for all of them among every 256th: n^2 / 64
-// comparisons of a wave, 7 us at 2000 positions, where the launches of the digits' sort take 25 us together.  The whole gradient of 1000
-// classes of 25 (one digit), binary32: 8000 positions 26 us so and 41 by digits, 16000 54 and 40; of 160000 classes of 800 (two
-// digits), bfloat16: 16000 positions 70 and 83.
-constexpr int kRanked = 16;
+// of its own.  A workgroup finds the places of 16 positions, each of its 512 threads counts for all of them among every 512th: n^2 / 64
+// comparisons of a wave, 6 us at 2000 positions, where the launches of the digits' sort take 25 us together.  The whole gradient of 1000
+// classes of 25 (one digit), binary32: 8000 positions 25 us so and 41 by digits, 16000 54 and 28; of 160000 classes of 800 (two
+// digits), bfloat16: 16000 positions 70 and 79.  4000 positions, 50000 classes of 512, bfloat16: 21 us with 512 threads, 24 with 256 or
+// 1024, 25 with 1024 and 32 positions.
+constexpr int kRanked = 16, kRankThreads = 512;
 constexpr long kRankedIds = 10240, kRankedIdsOfMany = 16384;  // one digit; more
 
 struct RankArgs {
@@ -549,12 +550,12 @@ struct RankArgs {
     ClearArgs clear;  // of the workgroups behind `blocks`
 };
 
-__global__ __launch_bounds__(kThreads) void rank_kernel(RankArgs a)
+__global__ __launch_bounds__(kRankThreads) void rank_kernel(RankArgs a)
 {
     if ((int)blockIdx.x >= a.blocks) return clear_rows(a.clear);
-    constexpr int kFlight = 8, kLanes = kThreads / kRanked;
+    constexpr int kFlight = 8, kLanes = kRankThreads / kRanked;
     __shared__ unsigned own_keys[kRanked];
-    __shared__ int counts[kRanked][kThreads + 1];
+    __shared__ int counts[kRanked][kRankThreads + 1];
     const int n = (int)a.n_ids, first = (int)blockIdx.x * kRanked, last = min(first + kRanked, n);
     auto key_of = [&](int i) {
         const int id = class_at(a.ids, a.id_type, i, a.n_classes);
@@ -570,10 +571,10 @@ __global__ __launch_bounds__(kThreads) void rank_kernel(RankArgs a)
         count[o] = 0;
     }
     auto count_below = [&](int begin, int end) {  // positions of keys below own[]
-        for (int j = begin + (int)threadIdx.x; j < end; j += kFlight * kThreads) {
+        for (int j = begin + (int)threadIdx.x; j < end; j += kFlight * kRankThreads) {
             unsigned key[kFlight];
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u) key[u] = j + u * kThreads < end ? key_of(j + u * kThreads) : ~0u;
+            for (int u = 0; u < kFlight; ++u) key[u] = j + u * kRankThreads < end ? key_of(j + u * kRankThreads) : ~0u;
 #pragma unroll
             for (int u = 0; u < kFlight; ++u)
 #pragma unroll
@@ -594,7 +595,7 @@ __global__ __launch_bounds__(kThreads) void rank_kernel(RankArgs a)
     __syncthreads();
     const int o = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
     int place = 0;
-    for (int t = lane; t < kThreads; t += kLanes) place += counts[o][t];
+    for (int t = lane; t < kRankThreads; t += kLanes) place += counts[o][t];
     for (int step = kLanes / 2; step; step /= 2) place += __shfl_xor(place, step);
     if (lane == 0 && first + o < last) {
         a.keys[place] = own_keys[o];
@@ -927,8 +928,8 @@ int nuts_lookup_grad(const nuts_lookup_desc* d, const void* grad_rows, const voi
                    d->id_type, (int)ceil_div(d->n_ids, kRanked), ClearArgs{}};
         r.clear = ClearArgs{nullptr, static_cast<char*>(grad_table), (long)(d->table_stride * size), (long)(d->dim * size), 0, (long)d->n_classes,
                             r.blocks, 0, a.g.streamed};
-        if (!d->accumulate) more = (unsigned)std::min<int64_t>(ceil_div(d->n_classes * ceil_div(d->dim * size, 16), 8 * kThreads), 1 << 16);
-        hipLaunchKernelGGL(rank_kernel, dim3(r.blocks + more), dim3(kThreads), 0, stream, r);
+        if (!d->accumulate) more = (unsigned)std::min<int64_t>(ceil_div(d->n_classes * ceil_div(d->dim * size, 16), 8 * kRankThreads), 1 << 16);
+        hipLaunchKernelGGL(rank_kernel, dim3(r.blocks + more), dim3(kRankThreads), 0, stream, r);
     }
     for (int k = 0; k < p.passes; ++k) {
         SortArgs s{ids, reinterpret_cast<unsigned*>(w + p.keys[(k + 1) & 1]), reinterpret_cast<unsigned*>(w + p.pos[(k + 1) & 1]),
