@@ -162,6 +162,94 @@ __global__ __launch_bounds__(kThreads) void add_up_kernel(const float* sums, int
     }
 }
 
+struct FewArgs {
+    const void* dz;         // [rows][dz_stride], rows padded with zeros to whole packs of kFewClasses
+    const void* x;
+    const void* targets;
+    const float* residual;  // as in ProductArgs
+    void* out;
+    long x_stride, stride;
+    int rows, dz_stride, dim, first, classes, n_classes, id_type, lane_bits, streamed;
+};
+
+template <typename T>
+constexpr int kFewRows = 2 * sizeof(T);  // of x, which a thread's registers hold
+constexpr int kFewClasses = 8;  // at a time
+constexpr int64_t kFewGroups = 512;  // workgroups (62565 classes of 2262, bfloat16: 76 us, with 1024 90)
+
+// dW of few rows: sums of so few products that it is all writing.  A thread has 16 bytes of columns of the rows of x in its registers and
+// goes through the classes, eight at a time; workgroups are few, so that x is read for many classes.  dz and dW of 4 rows, bfloat16,
+// 128000 classes of 4096: 205 us, 5.1 TB/s (341 by the product kernel, whose tiles begin and end for one step), 32000 of 1024 21 and 31;
+// 8 rows, binary32, 50000 classes of 512: 24 and 39.  With 8 rows in bfloat16, which take twice the registers and additions, it is no faster than
+// the product kernel.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void few_rows_weights_kernel(FewArgs a)
+{
+    constexpr int kN = 16 / sizeof(T), kRows = kFewRows<T>;
+    const int lanes = 1 << a.lane_bits, lane = threadIdx.x & (lanes - 1);
+    const int begin = (int)(blockIdx.y * lanes + lane) * kN;
+    if (begin >= a.dim) return;
+    const int c = max(0, min(begin, a.dim - kN));  // (a ragged row's last columns: 16 bytes that end with the row)
+    float x[kRows][kN], lost[kRows];
+    int target[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const T* from = static_cast<const T*>(a.x) + i * a.x_stride + c;
+        Pack<T, kN> pack{};
+        if (i < a.rows) {
+            if (a.dim >= kN) {
+                pack = load_pack<T, kN>(from);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kN - 1; ++e)
+                    if (e < a.dim) pack.v[e] = from[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < kN; ++e) x[i][e] = to_float(pack.v[e]);
+        target[i] = a.residual && i < a.rows ? class_at(a.targets, a.id_type, i, a.n_classes) - a.first : -1;
+        lost[i] = a.residual && i < a.rows ? a.residual[i] : 0.f;
+    }
+    const long step = (long)gridDim.x * (kThreads >> a.lane_bits) * kFewClasses;
+    for (long v = ((long)blockIdx.x * (kThreads >> a.lane_bits) + (threadIdx.x >> a.lane_bits)) * kFewClasses; v < a.classes; v += step) {
+        float dz[kRows][kFewClasses];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            Pack<T, kFewClasses> pack{};
+            if (i < a.rows) pack = load_pack<T, kFewClasses>(static_cast<const T*>(a.dz) + (long)i * a.dz_stride + v);
+#pragma unroll
+            for (int r = 0; r < kFewClasses; ++r) dz[i][r] = to_float(pack.v[r]);
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+            if (target[i] >= v && target[i] < v + kFewClasses) {
+#pragma unroll
+                for (int r = 0; r < kFewClasses; ++r)
+                    if (target[i] == v + r) dz[i][r] += lost[i];
+            }
+        T* to = static_cast<T*>(a.out) + v * a.stride + c;
+#pragma unroll
+        for (int r = 0; r < kFewClasses; ++r) {
+            if (v + r >= a.classes) break;
+            Pack<T, kN> out;
+#pragma unroll
+            for (int e = 0; e < kN; ++e) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) sum = __builtin_fmaf(dz[i][r], x[i][e], sum);
+                out.v[e] = rounded<T>(sum);
+            }
+            if (a.dim >= kN) {
+                a.streamed ? stream_pack(to + r * a.stride, out) : store_pack(to + r * a.stride, out);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kN - 1; ++e)
+                    if (e < a.dim) to[r * a.stride + e] = out.v[e];
+            }
+        }
+    }
+}
+
 struct JoinArgs {
     const float4* stats;
     const float* target_logit;
@@ -555,7 +643,17 @@ int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, 
             if (p.grad_x.splits > 1 || p.pieces > 1) launch_product<kSums, false, true, T>(p.grad_x, a, stream);
             else launch_product<kOutput, false, true, T>(p.grad_x, a, stream);
         }
-        if (grad_weight) {
+        if (grad_weight && n > 0 && n <= kFewRows<T>) {
+            int lane_bits = 0;
+            while (lane_bits < 8 && (1 << lane_bits) * (16 / size) < dim) ++lane_bits;
+            const FewArgs a{w + p.dz, m.x, targets, residual, static_cast<char*>(grad_weight) + first * d->grad_weight_stride * size, (long)m.x_stride,
+                            (long)d->grad_weight_stride, (int)n, (int)p.piece_pad, (int)dim, (int)first, (int)classes, (int)d->n_classes, d->id_type,
+                            lane_bits, classes * dim * size >= kStreamed};
+            const int64_t groups = ceil_div(ceil_div(classes, kFewClasses), kThreads >> lane_bits);
+            const int64_t slices = ceil_div(dim, (int64_t)(16 / size) << lane_bits);
+            const dim3 grid((unsigned)std::min<int64_t>(groups, ceil_div(kFewGroups, slices)), (unsigned)slices);
+            hipLaunchKernelGGL(few_rows_weights_kernel<T>, grid, dim3(kThreads), 0, stream, a);
+        } else if (grad_weight) {
             ProductArgs a{};
             a.a = w + p.dz;
             a.b = static_cast<const char*>(m.x);

@@ -488,6 +488,13 @@ def test_score_grad(dtype, n, classes, dim, kept):
     assert none is None and torch.equal(only_w, grad_w)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,classes,dim", [(1, 9, 3), (2, 130, 9), (4, 20000, 33), (7, 4100, 2100), (8, 1000, 4100), (8, 70001, 130), (9, 1000, 130)])
+@pytest.mark.parametrize("kept", [True, False])
+def test_score_grad_of_few_rows(dtype, n, classes, dim, kept):
+    test_score_grad(dtype, n, classes, dim, kept)
+
+
 @pytest.mark.parametrize("n,classes,dim", [(3, 5000, 128), (700, 9000, 72), (3000, 3000, 520), (2000, 8200, 2104)])
 @pytest.mark.parametrize("kept", [True, False])
 def test_score_grad_loses_nothing_to_dz_of_8_bits(n, classes, dim, kept):
