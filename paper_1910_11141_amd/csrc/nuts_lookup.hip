@@ -161,10 +161,11 @@ constexpr int kFewRows = 64;                   // at most so many classes a work
 
 // A workgroup owns `classes` neighbouring rows of the table, or a slice of their columns: it finds the positions of theirs among all
 // n (few, from cache) and adds them up.  What bounds it is the wait for memory, twice at least, and again for every 32 rows or so of
-// the class that comes most often (1000 positions, 1000 classes of 100 in binary32: 8 us; without the slices, 1000 classes of 2048 in
-// binary32 took 76 us, now 16; up to 4096 workgroups: 100 positions, 4168 classes of 1842, binary32 14 us, 23 with 2048 and 19 with 16384).  Sorting them first, as for more positions, takes three launches: 15 us for 1100 positions where
-// this takes 11 for 1000.  Only a table that has to be cleared and is too large for the caches is cleared faster beside a sort
-// (100003 classes of 2048 in bfloat16, 1000 positions: 77 us so, 92 by this kernel).
+// the class that comes most often: 1000 positions, 5000 classes of 100 in binary32 9 us.  Slices: 1000 positions, 1000 classes of 2048 in
+// binary32 16 us, 76 without; up to 4096 workgroups: 100 positions, 4168 classes of 1842, binary32 14 us, 23 with 2048 and 19 with
+// 16384.  Sorting the positions first, as is done with more of them, takes three launches: 15 us for 1100 positions where this takes 11
+// for 1000.  Only a table that has to be cleared and is too large for the caches is cleared faster beside a sort (100003 classes of
+// 2048 in bfloat16, 1000 positions: 77 us so, 92 by this kernel).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int classes, long slice_packs, long first_block)
 {
@@ -534,12 +535,12 @@ __global__ __launch_bounds__(kThreads) void place_kernel(SortArgs a)
 
 // Not too many positions are sorted in one launch: a position's place is the number of those of lower classes and of those before it
 // of its own.  A workgroup finds the places of 16 positions, each of its 512 threads counts for all of them among every 512th: n^2 / 64
-// comparisons of a wave, 6 us at 2000 positions, where the launches of the digits' sort take 25 us together.  The whole gradient of 1000
-// classes of 25 (one digit), binary32: 8000 positions 25 us so and 41 by digits, 16000 54 and 28; of 160000 classes of 800 (two
-// digits), bfloat16: 16000 positions 70 and 79.  4000 positions, 50000 classes of 512, bfloat16: 21 us with 512 threads, 24 with 256 or
-// 1024, 25 with 1024 and 32 positions.
+// comparisons of a wave, which bound it.  2000 positions take 6 us, where the launches of the digits' sort take 25 us together.  The whole
+// gradient of 1000 classes of 25 (one digit), binary32: 10000 positions 28 us so, as long as 16000 by digits; of 50000 classes of 512 (two
+// digits) 10000 positions 37 us and 16384 54, 16385 by digits 46; of 100003 classes of 2048, bfloat16, cleared beside the sort, 102
+// and 119.  1000 classes of 25, 10000 positions with 256 threads 30 us, with 1024 33.
 constexpr int kRanked = 16, kRankThreads = 512;
-constexpr long kRankedIds = 10240, kRankedIdsOfMany = 16384;  // one digit; more
+constexpr long kRankedIds = 10240, kRankedIdsOfMany = 12288, kRankedIdsBesideClearing = 16384;  // one digit; more; a table past the caches
 
 struct RankArgs {
     const void* ids;
@@ -554,51 +555,57 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(RankArgs a)
 {
     if ((int)blockIdx.x >= a.blocks) return clear_rows(a.clear);
     constexpr int kFlight = 8, kLanes = kRankThreads / kRanked;
-    __shared__ unsigned own_keys[kRanked];
+    __shared__ int own_keys[kRanked];
     __shared__ int counts[kRanked][kRankThreads + 1];
     const int n = (int)a.n_ids, first = (int)blockIdx.x * kRanked, last = min(first + kRanked, n);
     auto key_of = [&](int i) {
         const int id = class_at(a.ids, a.id_type, i, a.n_classes);
-        return id < 0 ? (unsigned)a.n_classes : (unsigned)id;
+        return id < 0 ? (int)a.n_classes : id;
     };
+    // Before its own position equal keys count too: those keys are taken one less.
+    int key[kFlight];
+    auto load = [&](int at) {
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) {
+            const int j = at + u * kRankThreads;
+            key[u] = j < n ? key_of(j) - (j < first) : INT32_MAX;
+        }
+    };
+    int at = threadIdx.x;
+    load(at);
     if (threadIdx.x < kRanked) own_keys[threadIdx.x] = key_of(min(first + (int)threadIdx.x, n - 1));
     __syncthreads();
-    unsigned own[kRanked];
-    int count[kRanked];
+    int own[kRanked], count[kRanked];
 #pragma unroll
     for (int o = 0; o < kRanked; ++o) {
         own[o] = __builtin_amdgcn_readfirstlane(own_keys[o]);
         count[o] = 0;
     }
-    auto count_below = [&](int begin, int end) {  // positions of keys below own[]
-        for (int j = begin + (int)threadIdx.x; j < end; j += kFlight * kRankThreads) {
-            unsigned key[kFlight];
+    for (;;) {
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u) key[u] = j + u * kRankThreads < end ? key_of(j + u * kRankThreads) : ~0u;
+        for (int u = 0; u < kFlight; ++u) {
+            if (__builtin_amdgcn_readfirstlane(at) + u * kRankThreads >= n) break;  // (for the whole wave)
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u)
-#pragma unroll
-                for (int o = 0; o < kRanked; ++o) count[o] += key[u] < own[o] ? 1 : 0;
+            for (int o = 0; o < kRanked; ++o) count[o] += key[u] < own[o] ? 1 : 0;
         }
-    };
-    count_below(first, n);
-#pragma unroll
-    for (int o = 0; o < kRanked; ++o) ++own[o];  // before its own position equal keys count too
-    count_below(0, first);
+        at += kFlight * kRankThreads;
+        if (at >= n) break;
+        load(at);
+    }
     if ((int)threadIdx.x < last - first) {
-        const unsigned key = own_keys[threadIdx.x];
+        const int mine = own_keys[threadIdx.x];
 #pragma unroll
-        for (int o = 0; o < kRanked; ++o) count[o] += (int)threadIdx.x < o && key == own_keys[o] ? 1 : 0;
+        for (int o = 0; o < kRanked; ++o) count[o] += (int)threadIdx.x < o && mine == own[o] ? 1 : 0;
     }
 #pragma unroll
     for (int o = 0; o < kRanked; ++o) counts[o][threadIdx.x] = count[o];
     __syncthreads();
-    const int o = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    const int o = threadIdx.x / kLanes, member = threadIdx.x % kLanes;
     int place = 0;
-    for (int t = lane; t < kRankThreads; t += kLanes) place += counts[o][t];
+    for (int t = member; t < kRankThreads; t += kLanes) place += counts[o][t];
     for (int step = kLanes / 2; step; step /= 2) place += __shfl_xor(place, step);
-    if (lane == 0 && first + o < last) {
-        a.keys[place] = own_keys[o];
+    if (member == 0 && first + o < last) {
+        a.keys[place] = (unsigned)own_keys[o];
         a.pos[place] = (unsigned)(first + o);
     }
 }
@@ -816,7 +823,7 @@ GradPlan plan_grad(const nuts_lookup_desc* d)
     }
     int bits = 1;
     while (d->n_classes >> bits) ++bits;  // n_classes itself is a key
-    p.ranked = d->n_ids <= (bits <= kMaxDigitBits ? kRankedIds : kRankedIdsOfMany);
+    p.ranked = d->n_ids <= (large ? kRankedIdsBesideClearing : bits > kMaxDigitBits ? kRankedIdsOfMany : kRankedIds);
     p.passes = p.ranked ? 0 : (bits + kMaxDigitBits - 1) / kMaxDigitBits;
     p.digit_bits = p.ranked ? 0 : (bits + p.passes - 1) / p.passes;
     p.tile = (d->n_ids <= kManyIds ? kFewRounds : kManyRounds) * kThreads;
