@@ -489,7 +489,7 @@ def test_score_grad(dtype, n, classes, dim, kept):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("n,classes,dim", [(1, 9, 3), (2, 130, 9), (4, 20000, 33), (7, 4100, 2100), (8, 1000, 4100), (8, 70001, 130), (9, 1000, 130)])
+@pytest.mark.parametrize("n,classes,dim", [(1, 9, 3), (2, 130, 9), (4, 20000, 33), (7, 4100, 2100), (8, 1000, 4100), (8, 70001, 130), (9, 1000, 130), (3, 1100001, 5)])
 @pytest.mark.parametrize("kept", [True, False])
 def test_score_grad_of_few_rows(dtype, n, classes, dim, kept):
     test_score_grad(dtype, n, classes, dim, kept)
