@@ -211,7 +211,7 @@ struct Packs {
 };
 
 // One workgroup a row, or a part of one where there are few rows (kWhole = false: join_rows_kernel ends them).  One pass, bound by its
-// reads where there are many rows: 4096 x 32001 bfloat16 with 5 alternatives 61 us, 4.3 TB/s; of few rows by the wait for one
+// reads where there are many rows: 4096 x 32001 bfloat16 with 5 alternatives 61 us, 4.3 TB/s of them; of few rows by the wait for one
 // read of memory and the alternatives' exchange through LDS: 8 x 128000, masked, with 20 alternatives 9 us and 7 for join_rows_kernel.
 template <typename T, bool kMask, bool kTop, bool kWhole>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogitsArgs a)
