@@ -14,7 +14,10 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kCandidates = 1024;  // alternatives that are put in order at once
 constexpr int kJoinKeys = 4096;    // alternatives of a row's parts that are joined: no more than 16 a thread
-constexpr float kFar = 1e30f;      // beyond this lse has no digits left for what it is the sum of
+// Half a unit in the last place of lse is an error of p, relative to it: up to here 2^-19, or 2^-15 where p is rounded to 16 bits.  Of
+// rows farther from 0 the gradient finds maximum and sum itself.
+template <typename T>
+constexpr float kFar = sizeof(T) == 4 ? 64.f : 1024.f;
 
 struct LogitsArgs {
     const void* logits;
@@ -380,6 +383,10 @@ constexpr int kGradPacks = 4;  // of a thread
 // 140 us, 819 MB at 5.9 TB/s.  A large gradient is written past the
 // caches, which then keep the logits that the forward pass left there (both passes on 4096 x 50001 bfloat16: 252 us with plain
 // stores, 231 us so).
+//
+// p = e^(z - lse) takes half a unit in the last place of lse as an error.  Far from 0 (kFar) each of the row's workgroups goes through all of it
+// for its maximum and sum, from the caches (4096 x 50001 bfloat16 490 us where lse is enough for 140; to leave such rows to one workgroup
+// each takes 250, and registers that cost all others 3 %).
 template <typename T, bool kMask, bool kEntropy>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
 {
@@ -399,21 +406,24 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
     }
     const int y = a.targets ? class_at(a.targets, a.id_type, row, a.n_classes) : -1;
     const float lse = a.lse[row];
-    const bool empty = lse == -INFINITY;
+    const bool empty = lse == -INFINITY, far = __builtin_fabsf(lse) > kFar<T> && !empty;
     const float g_lp = a.grad_logprob && y >= 0 && !empty ? a.grad_logprob[row] * a.scale : 0.f;
     const float g_p = (a.grad_lse ? a.grad_lse[row] * a.scale : 0.f) - g_lp;
     const float g_h = kEntropy ? -a.grad_entropy[row] * a.scale : 0.f, entropy = kEntropy ? a.entropy[row] : 0.f;
-    float base = 0.f, ln_s = empty ? INFINITY : lse;  // log p = s (x - base) - ln_s
-    if (__builtin_fabsf(lse) > kFar && !empty) {
+    // p = e^(s (x - base) - shift) / sum
+    float base = 0.f, shift = empty ? INFINITY : lse, one_by_sum = 1.f, ln_sum = 0.f;
+    if (far) {
         Stats v{-INFINITY, 0.f, 0.f};
-        for (int i = threadIdx.x * kN; i < a.n_classes; i += kThreads * kN) {
-            float far[kN];
-            load_logits<T, kN, kMask>(x_row, allowed, i, a.n_classes, far);
-            add_logits<kN>(v, far, a.scale * kLog2e);
+        for (int i = threadIdx.x * kN; i < a.n_classes; i += kThreads * kN) {  // (a pack at a time: x is in registers, too)
+            float some[kN];
+            load_logits<T, kN, kMask>(x_row, allowed, i, a.n_classes, some);
+            add_logits<kN>(v, some, a.scale * kLog2e);
         }
         v = join_block(v, a.scale * kLog2e, shared);
         base = v.m;
-        ln_s = logf(v.s);
+        shift = 0.f;
+        one_by_sum = 1.f / v.s;
+        ln_sum = logf(v.s);
     }
 #pragma unroll
     for (int u = 0; u < kGradPacks; ++u) {
@@ -422,9 +432,9 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
         float g[kN];
 #pragma unroll
         for (int e = 0; e < kN; ++e) {
-            const float log_p = __builtin_fmaf(x[u][e] - base, a.scale, -ln_s), p = __builtin_amdgcn_exp2f(log_p * kLog2e);
+            const float w = __builtin_fmaf(x[u][e] - base, a.scale, -shift), p = __builtin_amdgcn_exp2f(w * kLog2e) * one_by_sum;
             // (where p is 0 there is no gradient, however far below log p is)
-            g[e] = p * (kEntropy ? __builtin_fmaf(g_h, fmaxf(log_p, kNothing) + entropy, g_p) : g_p);
+            g[e] = p * (kEntropy ? __builtin_fmaf(g_h, fmaxf(w - ln_sum, kNothing) + entropy, g_p) : g_p);
         }
         if (y >= v && y < v + kN) {
 #pragma unroll

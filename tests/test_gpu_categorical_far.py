@@ -1,0 +1,83 @@
+"""Gradients of rows whose logits lie far from 0, where the logarithm of their sum has few digits left for the sum itself.
+
+The logits of these tests are exact, so bounds do not grow with them: log p = s (x - m) - ln S has the roundings of the
+difference, of its product and of the sum (5 u |log p| with that by log2 e), ln S the error TOL of tests/test_gpu_categorical.py, and
+lse, where it is used in place of both, half a unit in its last place (2^-19 up to 64 for binary32, 2^-15 up to 1024 for 16 bits): in
+all less than 2 TOL + 6 u |log p|, relative to p.  The entropy is off by 30 TOL."""
+import math
+
+import pytest
+import torch
+
+import categorical_ref as R
+
+pytestmark = pytest.mark.gpu
+
+TOL = 4e-5
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def ops():
+    import paper_1910_11141_amd as nuts
+    return nuts
+
+
+def _bound(want, z, targets, scale, parts, dtype):
+    """What the gradient `want` with respect to exact logits may be off by, rounded to `dtype`."""
+    _, _, entropy, p = R.logprobs(z, targets)
+    log_p = torch.where(p == 0, torch.zeros_like(p), torch.log(p.clamp(min=1e-300))).abs()
+    rel = 2 * TOL + 6 * R.U * log_p
+    total = (parts[0].double().abs() + parts[1].double().abs())[:, None]
+    h = parts[2].double().abs()[:, None] * (log_p + entropy[:, None] + 60)
+    bound = (p * (total + h) * rel + R.U * 4 * total * (p > 0)) * scale + want.abs() * 4 * R.U
+    return bound + (want.abs() + bound) * R.EPS[dtype] * 1.01 + R.TINY[dtype] + 2.0 ** -126
+
+
+FAR = [0.0, 40.0, 100.0, -300.0, 1e3, 6e4, -6e4, 1e6, 1e8, -1e9, 2.0 ** 27, 3e30, -3e38]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,classes", [(3, 4), (2, 1000), (5, 5000), (3, 20011), (300, 700)])
+@pytest.mark.parametrize("masked", [False, True])
+def test_logprobs_grad_of_rows_far_from_0(dtype, n, classes, masked):
+    nuts, g = ops(), gen(n + classes)
+    for shift in FAR:
+        if dtype == torch.float16 and abs(shift) > 6e4:
+            continue
+        for scale in (1.0, 0.8):
+            logits = (torch.randn(n, classes, generator=g, device="cuda", dtype=torch.float64) * 3 + shift).to(dtype)
+            targets = torch.randint(-1, classes, (n,), generator=g, device="cuda")
+            allowed = None
+            if masked:
+                allowed = torch.rand(n, classes, generator=g, device="cuda") < 0.6
+                allowed[:, 0] = True
+            packed = None if allowed is None else R.pack_bits(allowed)
+            parts = [torch.randn(n, generator=g, device="cuda") for _ in range(3)]
+            fwd = nuts.nuts_logprobs(logits, targets, scale=scale, allowed=packed)
+            got = nuts.nuts_logprobs_grad(logits, targets, fwd.lse, fwd.entropy, grad_logprob=parts[0], grad_lse=parts[1],
+                                          grad_entropy=parts[2], scale=scale, allowed=packed)
+            s = torch.tensor(scale, dtype=torch.float32).double().item()
+            z = logits.double() * s
+            if allowed is not None:
+                z = torch.where(allowed, z, torch.full_like(z, -math.inf))
+            want = R.grad_logits(z, targets, allowed, s, *parts)
+            off = (got.double() - want).abs() - _bound(want, z, targets, s, parts, dtype)
+            assert float(off.max()) <= 0, (shift, scale, float(off.max()))
+
+
+@pytest.mark.parametrize("classes", [4, 1000, 30000])
+@pytest.mark.parametrize("far", [1e5, -1e6, 1e7, 2.0 ** 27, -1e9])
+def test_probabilities_of_far_rows_add_up_to_1(classes, far):
+    nuts = ops()
+    logits = torch.full((2, classes), far, device="cuda")
+    logits[1] += torch.randn(classes, generator=gen(1), device="cuda") * 3
+    targets = torch.tensor([0, classes - 1], device="cuda")
+    fwd = nuts.nuts_logprobs(logits, targets)
+    grad = nuts.nuts_logprobs_grad(logits, targets, fwd.lse, grad_logprob=torch.ones(2, device="cuda")).double()
+    assert float((grad[0, 1:] * classes + 1).abs().max()) <= 2 * TOL
+    # p's sum is 1 but for the same relative error of each, and each entry's rounding (the target's: of numbers up to 1)
+    assert float(grad.sum(1).abs().max()) <= 2 * TOL + 4 * R.U
