@@ -384,9 +384,11 @@ constexpr int kGradPacks = 4;  // of a thread
 // caches, which then keep the logits that the forward pass left there (both passes on 4096 x 50001 bfloat16: 252 us with plain
 // stores, 231 us so).
 //
-// p = e^(z - lse) takes half a unit in the last place of lse as an error.  Far from 0 (kFar) each of the row's workgroups goes through all of it
-// for its maximum and sum, from the caches (4096 x 50001 bfloat16 490 us where lse is enough for 140; to leave such rows to one workgroup
-// each takes 250, and registers that cost all others 3 %).
+// p = e^(z - lse) takes half a unit in the last place of lse as an error.  In binary32 that is more than all else is off by, and a row
+// that a workgroup holds in its registers is divided by the sum of its p, which without that error is 1 (8000 x 4000: 41 us, 39
+// without).  Far from 0 (kFar) each of the row's workgroups goes through all of it for its maximum and sum, from the caches (4096 x 50001
+// bfloat16 490 us where lse is enough for 140; to leave such rows to one workgroup each takes 250, and registers that cost all
+// others 3 %).
 template <typename T, bool kMask, bool kEntropy>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
 {
@@ -424,6 +426,21 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
         shift = 0.f;
         one_by_sum = 1.f / v.s;
         ln_sum = logf(v.s);
+    } else if (sizeof(T) == 4 && a.parts == 1 && !empty) {
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < kGradPacks; ++u)
+            if (begin + u * kThreads * kN < a.n_classes) {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][e], a.scale, -lse) * kLog2e);
+            }
+#pragma unroll
+        for (int step = 32; step >= 1; step /= 2) sum += __shfl_xor(sum, step);
+        if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64].s = sum;
+        __syncthreads();
+        sum = (shared[0].s + shared[1].s) + (shared[2].s + shared[3].s);
+        one_by_sum = 1.f / sum;
+        ln_sum = logf(sum);
     }
 #pragma unroll
     for (int u = 0; u < kGradPacks; ++u) {

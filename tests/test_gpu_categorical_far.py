@@ -81,3 +81,19 @@ def test_probabilities_of_far_rows_add_up_to_1(classes, far):
     assert float((grad[0, 1:] * classes + 1).abs().max()) <= 2 * TOL
     # p's sum is 1 but for the same relative error of each, and each entry's rounding (the target's: of numbers up to 1)
     assert float(grad.sum(1).abs().max()) <= 2 * TOL + 4 * R.U
+
+
+def test_binary32_gradients_of_short_rows_lose_nothing_to_lse():
+    """Rows that a workgroup holds: half a unit in lse's last place, here 32 u, does not reach p = 2^w / S.  The 2-norm is that of the
+    largest p, with |x - m| below 6: two roundings of w (6 u each), 2 u of the exponential and of the quotient, and of S's sum,
+    whose terms' errors of either sign add up to less than one of them, as much as of one term: 8 u where they are as often up as down."""
+    nuts, g = ops(), gen(3)
+    logits = torch.randn(500, 1000, generator=g, device="cuda") * 3 + 40
+    targets = torch.randint(0, 1000, (500,), generator=g, device="cuda")
+    weight = torch.rand(500, generator=g, device="cuda") + 0.5
+    fwd = nuts.nuts_logprobs(logits, targets)
+    assert bool(((fwd.lse > 32) & (fwd.lse < 64)).all())
+    grad = nuts.nuts_logprobs_grad(logits, targets, fwd.lse, grad_logprob=weight)
+    want = R.grad_logits(logits.double(), targets, None, 1.0, weight)
+    others = torch.ones_like(want, dtype=torch.bool).scatter_(1, targets[:, None], False)  # (the target's is g - g p)
+    assert float((grad.double() - want)[others].norm()) <= 8 * R.U * float(want[others].norm())
