@@ -14,10 +14,6 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kCandidates = 1024;  // alternatives that are put in order at once
 constexpr int kJoinKeys = 4096;    // alternatives of a row's parts that are joined: no more than 16 a thread
-// Half a unit in the last place of lse is an error of p, relative to it: up to here 2^-19, or 2^-15 where p is rounded to 16 bits.  Of
-// rows farther from 0 the gradient finds maximum and sum itself.
-template <typename T>
-constexpr float kFar = sizeof(T) == 4 ? 64.f : 1024.f;
 
 struct LogitsArgs {
     const void* logits;
@@ -34,19 +30,6 @@ struct LogitsArgs {
     float scale;
     int n_classes, id_type, n_top, parts, part_len;
 };
-
-// All threads get the workgroup's.
-__device__ __forceinline__ Stats join_block(Stats v, float c, Stats (&shared)[kWaves])
-{
-#pragma unroll
-    for (int step = 32; step >= 1; step /= 2) v = join(v, Stats{__shfl_xor(v.m, step), __shfl_xor(v.s, step), __shfl_xor(v.t, step)}, c);
-    if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = v;
-    __syncthreads();
-    v = shared[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) v = join(v, shared[w], c);
-    return v;
-}
 
 // The order of alternatives as whole numbers: larger logit first, NaN before all, the lower class first of equal ones.  0 is none.
 __device__ __forceinline__ unsigned long long key_of(float x, int v)
@@ -408,7 +391,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
     }
     const int y = a.targets ? class_at(a.targets, a.id_type, row, a.n_classes) : -1;
     const float lse = a.lse[row];
-    const bool empty = lse == -INFINITY, far = __builtin_fabsf(lse) > kFar<T> && !empty;
+    const bool empty = lse == -INFINITY, far = far_from_0<T>(lse);
     const float g_lp = a.grad_logprob && y >= 0 && !empty ? a.grad_logprob[row] * a.scale : 0.f;
     const float g_p = (a.grad_lse ? a.grad_lse[row] * a.scale : 0.f) - g_lp;
     const float g_h = kEntropy ? -a.grad_entropy[row] * a.scale : 0.f, entropy = kEntropy ? a.entropy[row] : 0.f;

@@ -58,6 +58,7 @@ struct ProductArgs {
     int first_class, n_classes;
     float4* stats;        // [row][tiles_n x waves along n]: m, S, T of z = scale C
     float* target_logit;  // [row]
+    const float* lse;     // [row]: tiles without a row far from 0 are left out; or NULL: none is
 };
 
 __device__ __forceinline__ f32x4 multiply(const float (&b)[4], const float (&a)[4], f32x4 c)
@@ -237,6 +238,13 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void product_kernel(Product
     int tm, tn;
     tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
     const int m0 = tm * kM, n0 = tn * kN;
+    if constexpr (kKind == kScores) {
+        if (p.lse) {
+            bool far = false;
+            for (int r = lane; r < kM; r += 64) far |= m0 + r < p.m && far_from_0<T>(p.lse[m0 + r]);
+            if (!__ballot(far)) return;  // (each wave has looked at all rows)
+        }
+    }
     const int all_steps = (p.k + A::kPlaces - 1) / A::kPlaces;
     const int first = blockIdx.y * p.split_steps, steps = min(p.split_steps, all_steps - first);
     A from_a;

@@ -49,7 +49,8 @@ __global__ __launch_bounds__(kThreads) void pack_rows_kernel(PackArgs a)
 }
 
 struct GradArgs {
-    const float* z;  // of the classes [first, first + classes)
+    const float* z;     // of the classes [first, first + classes)
+    const float4* far;  // [row]: statistics of rows far from 0 where z does not lie beside the rest of its row; or NULL
     const void* targets;
     const float* lse;
     const float* entropy;
@@ -66,11 +67,14 @@ struct GradArgs {
 constexpr int kGradPacks = 4;  // of a thread
 
 // dZ, rounded to the features' type: a workgroup a part of a row.  Bound by its reads and writes: 4096 x 32001, to bfloat16, 142 us, 787
-// MB at 5.5 TB/s.
+// MB at 5.5 TB/s.  Of a row far from 0 (kFar) each of its workgroups goes through all of it for its maximum and sum (all rows of 4096 x
+// 32001 far: 470 us).  Where z is made anew piece by piece, the tiles of such rows are multiplied once more before that, for their statistics
+// (9000 x 40000 x 512 bfloat16 in two pieces: 2.07 ms, 2.52 with all rows far; 2.04 without the launches that ask which are).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dz_kernel(GradArgs a)
 {
     constexpr int kN = 16 / sizeof(T);
+    __shared__ Stats shared[kThreads / 64];
     const long row = blockIdx.x / (unsigned)a.parts;
     const int begin = (int)(blockIdx.x % (unsigned)a.parts) * (kGradPacks * kThreads * kN) + (int)threadIdx.x * kN;
     const float* z = a.z + row * a.z_stride;
@@ -97,7 +101,26 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(GradArgs a)
     const bool empty = lse == -INFINITY;
     const float g_lp = a.grad_logprob && target >= 0 && !empty ? a.grad_logprob[row] * a.scale : 0.f;
     const float g_p = (a.grad_lse ? a.grad_lse[row] * a.scale : 0.f) - g_lp, g_h = a.grad_entropy ? -a.grad_entropy[row] * a.scale : 0.f;
-    const float h = a.grad_entropy ? a.entropy[row] : 0.f, ln_s = empty ? INFINITY : lse;
+    const float h = a.grad_entropy ? a.entropy[row] : 0.f;
+    float base = 0.f, ln_s = empty ? INFINITY : lse;  // log p = (z - base) - ln_s
+    if (far_from_0<T>(lse)) {
+        Stats v{-INFINITY, 0.f, 0.f};
+        if (a.far) {
+            const float4 s = a.far[row];
+            v = Stats{s.x, s.y, s.z};
+        } else {
+            const float* all = z - a.first;
+            for (int i = threadIdx.x * 4; i < a.n_classes; i += kThreads * 4) {  // (four at a time: x is in registers, too)
+                float some[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) some[e] = i + e < a.n_classes ? all[i + e] : -INFINITY;
+                add_logits<4>(v, some, kLog2e);
+            }
+            v = join_block(v, kLog2e, shared);
+        }
+        base = v.m;
+        ln_s = logf(v.s);
+    }
     if (a.residual && y < 0 && begin == 0) a.residual[row] = 0.f;
 #pragma unroll
     for (int u = 0; u < kGradPacks; ++u) {
@@ -106,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(GradArgs a)
         float g[kN];
 #pragma unroll
         for (int e = 0; e < kN; ++e) {
-            const float log_p = x[u][e] - ln_s, p = __builtin_amdgcn_exp2f(log_p * kLog2e);
+            const float log_p = (x[u][e] - base) - ln_s, p = __builtin_amdgcn_exp2f(log_p * kLog2e);
             g[e] = p * __builtin_fmaf(g_h, fmaxf(log_p, kNothing) + h, g_p);
         }
         if (y >= v && y < v + kN) {
@@ -294,6 +317,24 @@ __global__ __launch_bounds__(kThreads) void join_scores_kernel(JoinArgs a)
     if (a.lse) a.lse[at] = r.lse;
     if (a.entropy) a.entropy[at] = r.entropy;
     if (a.logprob) a.logprob[at] = a.targets && class_at(a.targets, a.id_type, at, a.n_classes) >= 0 ? logprob_of(r, a.target_logit[row], 1.f) : 0.f;
+}
+
+// The statistics of the rows far from 0, of a piece of the classes joined to those before it: a wave a row.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void join_far_kernel(const float4* stats, const float* lse, float4* far, int rows, int parts, int first)
+{
+    const int row = blockIdx.x * (kThreads / 64) + threadIdx.x / 64, lane = threadIdx.x % 64;
+    if (row >= rows || !far_from_0<T>(lse[row])) return;
+    Stats v{-INFINITY, 0.f, 0.f};
+    for (int p = lane; p < parts; p += 64) {
+        const float4 x = stats[(long)row * parts + p];
+        v = join(v, Stats{x.x, x.y, x.z}, kLog2e);
+    }
+#pragma unroll
+    for (int step = 32; step >= 1; step /= 2) v = join(v, Stats{__shfl_xor(v.m, step), __shfl_xor(v.s, step), __shfl_xor(v.t, step)}, kLog2e);
+    if (lane != 0) return;
+    if (first > 0) v = join(Stats{far[row].x, far[row].y, far[row].z}, v, kLog2e);
+    far[row] = float4{v.m, v.s, v.t, 0.f};
 }
 
 constexpr int64_t kJoinedByOneWave = 1024;  // rows, from which on there are waves enough
@@ -556,7 +597,7 @@ int score(const nuts_score_desc* d, const ScorePlan& p, const void* x, const voi
 struct ScoreGradPlan {
     int64_t dim_pad, piece, piece_pad, pieces;
     Choice scores, grad_x, grad_weight;
-    size_t x, weight, z, dz, residual, sums_x, sums_weight;
+    size_t x, weight, z, dz, residual, far, sums_x, sums_weight;
     Space space;
 };
 
@@ -579,6 +620,7 @@ ScoreGradPlan plan_score_grad(const nuts_score_desc* d)
     p.z = p.space.take((size_t)d->n_rows * p.piece_pad * sizeof(float));
     p.dz = p.space.take((size_t)d->n_rows * p.piece_pad * size);
     p.residual = p.space.take((size_t)d->n_rows * sizeof(float));
+    p.far = p.space.take(p.pieces > 1 ? (size_t)d->n_rows * sizeof(float4) : 0);
     p.sums_x = p.space.take(p.grad_x.splits > 1 || p.pieces > 1 ? (size_t)p.grad_x.splits * d->n_rows * d->dim * sizeof(float) : 0);
     p.sums_weight = p.space.take(p.grad_weight.splits > 1 ? (size_t)p.grad_weight.splits * p.piece * d->dim * sizeof(float) : 0);
     return p;
@@ -593,32 +635,45 @@ int score_grad(const nuts_score_desc* d, const ScoreGradPlan& p, const void* x, 
     const int64_t size = sizeof(T), n = d->n_rows, dim = d->dim;
     const Matrices m = pack<T>(d, x, weight, n > 0 && (grad_weight || !logits), n > 0 && (grad_x || !logits), w + p.x, w + p.weight, p.dim_pad, stream);
     float* residual = targets && grad_logprob && size == 2 ? reinterpret_cast<float*>(w + p.residual) : nullptr;
+    // z of the classes [first, first + classes), or their statistics in the rows far from 0
+    auto scores = [&](int64_t first, int64_t classes, float4* stats) {
+        ProductArgs a{};
+        a.a = static_cast<const char*>(m.x);
+        a.b = static_cast<const char*>(m.weight) + first * m.weight_stride * size;
+        a.a_stride = (long)(m.x_stride * size);
+        a.b_stride = (long)(m.weight_stride * size);
+        a.m = (int)n;
+        a.n = (int)classes;
+        a.k = (int)m.dim;
+        a.c = stats ? nullptr : w + p.z;
+        a.c_stride = (long)p.piece_pad;
+        a.scale = (float)d->scale;
+        a.stats = stats;
+        a.lse = stats ? lse : nullptr;
+        Choice c = p.scores;
+        c.tiles_n = (int)ceil_div(classes, kShapes[c.tiles].n);
+        launch_product<kScores, false, false, T>(c, a, stream);
+        return c.tiles_n * kShapes[c.tiles].parts_n;
+    };
+    float4* far = !logits && p.pieces > 1 ? reinterpret_cast<float4*>(w + p.far) : nullptr;
+    for (int64_t first = 0; far && n > 0 && first < d->n_classes; first += p.piece) {
+        float4* stats = reinterpret_cast<float4*>(w + p.dz);  // (16 bytes for 32 columns and more; dZ comes later)
+        const int parts = scores(first, std::min(p.piece, d->n_classes - first), stats);
+        hipLaunchKernelGGL(join_far_kernel<T>, dim3((unsigned)ceil_div(n, kThreads / 64)), dim3(kThreads), 0, stream, stats, lse, far, (int)n, parts, (int)first);
+    }
     for (int64_t first = 0; first < d->n_classes; first += p.piece) {
         const int64_t classes = std::min(p.piece, d->n_classes - first);
         const char* own_weight = static_cast<const char*>(m.weight) + first * m.weight_stride * size;
         const float* z = logits ? logits + first : nullptr;
         int64_t z_stride = d->logits_stride;
         if (!logits && n > 0) {
-            ProductArgs a{};
-            a.a = static_cast<const char*>(m.x);
-            a.b = own_weight;
-            a.a_stride = (long)(m.x_stride * size);
-            a.b_stride = (long)(m.weight_stride * size);
-            a.m = (int)n;
-            a.n = (int)classes;
-            a.k = (int)m.dim;
-            a.c = w + p.z;
-            a.c_stride = (long)p.piece_pad;
-            a.scale = (float)d->scale;
-            Choice c = p.scores;
-            c.tiles_n = (int)ceil_div(classes, kShapes[c.tiles].n);
-            launch_product<kScores, false, false, T>(c, a, stream);
+            scores(first, classes, nullptr);
             z = reinterpret_cast<const float*>(w + p.z);
             z_stride = p.piece_pad;
         }
         if (n > 0) {
             const int parts = (int)ceil_div(p.piece_pad, kGradPacks * kThreads * (16 / size));
-            const GradArgs g{z, targets, lse, entropy, grad_logprob, grad_lse, grad_entropy, w + p.dz, residual, (long)z_stride, (int)p.piece_pad, parts, (int)first,
+            const GradArgs g{z, far, targets, lse, entropy, grad_logprob, grad_lse, grad_entropy, w + p.dz, residual, (long)z_stride, (int)p.piece_pad, parts, (int)first,
                              (int)classes, (int)d->n_classes, d->id_type, n * p.piece_pad * size >= kStreamed, (float)d->scale};
             hipLaunchKernelGGL(dz_kernel<T>, dim3((unsigned)(n * parts)), dim3(kThreads), 0, stream, g);
         }

@@ -49,6 +49,20 @@ __device__ __forceinline__ void add_logits(Stats& a, const float (&x)[kN], float
     }
 }
 
+// All threads get the workgroup's.
+template <int kWaves>
+__device__ __forceinline__ Stats join_block(Stats v, float c, Stats (&shared)[kWaves])
+{
+#pragma unroll
+    for (int step = 32; step >= 1; step /= 2) v = join(v, Stats{__shfl_xor(v.m, step), __shfl_xor(v.s, step), __shfl_xor(v.t, step)}, c);
+    if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = shared[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v = join(v, shared[w], c);
+    return v;
+}
+
 // A row's results.  ln S and the row's largest logit stand for lse where a difference is wanted.
 struct Row {
     float m, ln_s, lse, entropy;
@@ -70,6 +84,16 @@ __device__ __forceinline__ Row finish(const Stats& v, float scale)
 __device__ __forceinline__ float logprob_of(const Row& r, float x, float scale)
 {
     return r.empty ? -INFINITY : __builtin_fmaf(x - r.m, scale, -r.ln_s);
+}
+
+// Half a unit in the last place of lse is an error of p = e^(z - lse), relative to it: up to here 2^-19, or 2^-15 where gradients are rounded
+// to 16 bits.  For rows farther from 0 they find maximum and sum themselves.
+template <typename T>
+constexpr float kFar = sizeof(T) == 4 ? 64.f : 1024.f;
+template <typename T>
+__device__ __forceinline__ bool far_from_0(float lse)
+{
+    return __builtin_fabsf(lse) > kFar<T> && lse != -INFINITY;  // (-infinity: an empty row)
 }
 
 }  // namespace nuts

@@ -97,3 +97,69 @@ def test_binary32_gradients_of_short_rows_lose_nothing_to_lse():
     want = R.grad_logits(logits.double(), targets, None, 1.0, weight)
     others = torch.ones_like(want, dtype=torch.bool).scatter_(1, targets[:, None], False)  # (the target's is g - g p)
     assert float((grad.double() - want)[others].norm()) <= 8 * R.U * float(want[others].norm())
+
+
+def _far_scores(n, classes, dim, shift, dtype, seed):
+    """Features and weights of small whole numbers, and one that takes all scores `shift` away from 0; every score and every part of its sum
+    is a multiple of four units in its last place, so that binary32 products are exact."""
+    g = gen(seed)
+    unit = max(0.25, 2.0 ** (math.floor(math.log2(abs(shift))) - 23 + 2)) if shift else 0.25
+    x = torch.randint(-2, 3, (n, dim), generator=g, device="cuda").to(dtype)
+    w = torch.randint(-2, 3, (classes, dim), generator=g, device="cuda").to(dtype) * unit
+    x[:, 0], w[:, 0] = 1.0, shift
+    targets = torch.randint(-1, classes, (n,), generator=g, device="cuda")
+    return x, w, targets, [torch.randn(n, generator=g, device="cuda") for _ in range(3)]
+
+
+def _check_far_rows(x, w, targets, parts, rows, grad_x, dtype):
+    """The gradient with respect to some rows of x against 64 bits; returns what they add to the weights' and what that may be off by."""
+    z = x[rows].double() @ w.double().t()
+    own = [p[rows] for p in parts]
+    dz = R.grad_logits(z, targets[rows], None, 1.0, *own)
+    dz_off = _bound(dz, z, targets[rows], 1.0, own, dtype)
+    want_x = dz @ w.double()
+    bound_x = dz_off @ w.double().abs() + (dz.abs() @ w.double().abs()) * (w.shape[0] + 2) * R.U
+    bound_x = bound_x * 1.01 + (want_x.abs() + bound_x) * R.EPS[dtype] * 1.01
+    off = ((grad_x[rows].double() - want_x).abs() - bound_x).amax(0)
+    assert float(off.max()) <= 0, off
+    bound_w = dz_off.t() @ x[rows].double().abs() + (dz.abs().t() @ x[rows].double().abs()) * (x.shape[0] + 2) * R.U
+    return dz.t() @ x[rows].double(), bound_w
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,classes,dim", [(3, 1000, 9), (300, 5000, 40), (2, 20011, 16), (600, 3000, 130)])
+@pytest.mark.parametrize("shift", [0.0, 128.0, -2.0 ** 13, 2.0 ** 20, -2.0 ** 27])
+@pytest.mark.parametrize("kept", [True, False])
+def test_score_grad_of_rows_far_from_0(dtype, n, classes, dim, shift, kept):
+    nuts = ops()
+    x, w, targets, parts = _far_scores(n, classes, dim, shift, dtype, n + dim)
+    fwd = nuts.nuts_score(x, w, targets, keep_logits=True)
+    assert torch.equal(fwd.logits.double(), x.double() @ w.double().t())
+    grad_x, grad_w = nuts.nuts_score_grad(x, w, targets, fwd.lse, fwd.entropy, grad_logprob=parts[0], grad_lse=parts[1], grad_entropy=parts[2],
+                                          logits=fwd.logits if kept else None)
+    want_w, bound_w = _check_far_rows(x, w, targets, parts, slice(0, n), grad_x, dtype)
+    bound_w = bound_w * 1.01 + (want_w.abs() + bound_w) * R.EPS[dtype] * 1.01
+    assert float(((grad_w.double() - want_w).abs() - bound_w).max()) <= 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kept", [True, False])
+def test_score_grad_of_some_far_rows_over_several_pieces(dtype, kept):
+    """More scores than one piece of the classes holds: rows that begin far from 0, and one that does alone among its neighbours."""
+    nuts = ops()
+    n, classes, dim = 65536 + 40, 9000, 32
+    x, w, targets, parts = _far_scores(n, classes, dim, 2.0 ** 20, dtype, 5)
+    far = torch.zeros(n, dtype=torch.bool, device="cuda")
+    far[:700], far[30000], far[n - 1] = True, True, True
+    w[:, 1:] = w[:, 1:].sign() * 0.25
+    x[~far, 0] = 0.0
+    fwd = nuts.nuts_score(x, w, targets, keep_logits=kept)
+    grad_x, grad_w = nuts.nuts_score_grad(x, w, targets, fwd.lse, fwd.entropy, grad_logprob=parts[0], grad_lse=parts[1], grad_entropy=parts[2],
+                                          logits=fwd.logits)
+    want_w, bound_w = 0.0, 0.0
+    for r in range(0, n, 8192):
+        rows = slice(r, min(r + 8192, n))
+        some_w, some_bound = _check_far_rows(x, w, targets, parts, rows, grad_x, dtype)
+        want_w, bound_w = want_w + some_w, bound_w + some_bound
+    bound_w = bound_w * 1.01 + (want_w.abs() + bound_w) * R.EPS[dtype] * 1.01
+    assert float(((grad_w.double() - want_w).abs() - bound_w).max()) <= 0
