@@ -435,6 +435,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
             const float w = __builtin_fmaf(x[u][e] - base, a.scale, -shift), p = __builtin_amdgcn_exp2f(w * kLog2e) * one_by_sum;
             // (where p is 0 there is no gradient, however far below log p is)
             g[e] = p * (kEntropy ? __builtin_fmaf(g_h, fmaxf(w - ln_sum, kNothing) + entropy, g_p) : g_p);
+            if (kMask && !(may[u] >> e & 1)) g[e] = 0.f;  // (also where the row has no lse, or no finite gradient)
         }
         if (y >= v && y < v + kN) {
 #pragma unroll
