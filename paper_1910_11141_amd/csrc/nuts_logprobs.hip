@@ -433,8 +433,8 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
 #pragma unroll
         for (int e = 0; e < kN; ++e) {
             const float w = __builtin_fmaf(x[u][e] - base, a.scale, -shift), p = __builtin_amdgcn_exp2f(w * kLog2e) * one_by_sum;
-            // (where p is 0 there is no gradient, however far below log p is)
-            g[e] = p * (kEntropy ? __builtin_fmaf(g_h, fmaxf(w - ln_sum, kNothing) + entropy, g_p) : g_p);
+            // (where p is 0 there is no gradient, however far below log p is and whatever comes in)
+            g[e] = p == 0.f ? 0.f : p * (kEntropy ? __builtin_fmaf(g_h, fmaxf(w - ln_sum, kNothing) + entropy, g_p) : g_p);
             if (kMask && !(may[u] >> e & 1)) g[e] = 0.f;  // (also where the row has no lse, or no finite gradient)
         }
         if (y >= v && y < v + kN) {

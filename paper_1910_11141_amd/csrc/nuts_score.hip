@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(GradArgs a)
 #pragma unroll
         for (int e = 0; e < kN; ++e) {
             const float log_p = (x[u][e] - base) - ln_s, p = __builtin_amdgcn_exp2f(log_p * kLog2e);
-            g[e] = p * __builtin_fmaf(g_h, fmaxf(log_p, kNothing) + h, g_p);
+            g[e] = p == 0.f ? 0.f : p * __builtin_fmaf(g_h, fmaxf(log_p, kNothing) + h, g_p);  // (0 whatever comes in)
         }
         if (y >= v && y < v + kN) {
 #pragma unroll
