@@ -1,0 +1,25 @@
+"""The categorical operators' Python face: what loading it costs others, what calls are told apart, which shapes fit."""
+import subprocess
+import sys
+
+import pytest
+import torch
+
+import paper_1910_11141_amd as nuts
+from paper_1910_11141_amd import binding as B
+
+
+def test_the_samplers_names_and_modules_need_no_categorical_ones():
+    """Names of the binding and modules of the package are found without PyTorch, which the categorical operators import."""
+    code = ("import sys, paper_1910_11141_amd as n; from paper_1910_11141_amd import build, workloads; n.NUTS_OK, n.Target, n.nuts_sample; "
+            "assert not hasattr(n, 'no_such_name'); assert 'torch' not in sys.modules; "
+            "n.nuts_lookup, n.Scores; assert 'torch' in sys.modules; assert 'nuts_lookup' in vars(n)")
+    subprocess.run([sys.executable, "-c", code], check=True)
+
+
+def test_all_names_of_the_operators_are_the_packages():
+    from paper_1910_11141_amd import categorical
+    for name in categorical.__all__:
+        assert getattr(nuts, name) is getattr(categorical, name)
+    with pytest.raises(AttributeError):
+        nuts.no_such_name
