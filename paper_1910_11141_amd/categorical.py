@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 from collections import namedtuple
 from functools import lru_cache
+from math import copysign
 
 import torch
 
@@ -28,7 +29,7 @@ _ID_TYPES = {torch.int32: _b.NUTS_I32, torch.int64: _b.NUTS_I64}
 
 # Descriptors (and the workspaces that their calls need) depend on sizes alone.
 @lru_cache(maxsize=512)
-def _lookup_desc(grad, *fields):
+def _lookup_desc(grad, sign, *fields):  # (sign: of the scale, for its zeros are equal)
     desc = _b.nuts_lookup_desc(*fields, 0)
     return C.byref(desc), _bytes(_b.lib().nuts_lookup_grad_workspace, desc) if grad else 0
 
@@ -137,8 +138,9 @@ def nuts_lookup(table, ids, *, scale=1.0, out=None):
     if rows.dtype != table.dtype:
         raise ValueError(f"out must be {table.dtype}")
     _matrix(rows, "out", shape=(n, dim))
-    desc, _ = _lookup_desc(False, _DTYPES[table.dtype], _ID_TYPES[ids.dtype], n, classes, dim, _stride(table), _stride(rows),
-                           float(scale), 0)
+    scale = float(scale)
+    desc, _ = _lookup_desc(False, copysign(1.0, scale), _DTYPES[table.dtype], _ID_TYPES[ids.dtype], n, classes, dim, _stride(table),
+                           _stride(rows), scale, 0)
     _call(_b.lib().nuts_lookup, desc, (table, ids, rows))
     return out
 
@@ -156,8 +158,9 @@ def nuts_lookup_grad(grad, ids, n_classes, *, scale=1.0, out=None, accumulate=Fa
     elif out.dtype != grad.dtype:
         raise ValueError(f"out must be {grad.dtype}")
     _matrix(out, "out", shape=(n_classes, dim))
-    desc, size = _lookup_desc(True, _DTYPES[grad.dtype], _ID_TYPES[ids.dtype], n, n_classes, dim, _stride(out), _stride(rows),
-                              float(scale), int(bool(accumulate)))
+    scale = float(scale)
+    desc, size = _lookup_desc(True, copysign(1.0, scale), _DTYPES[grad.dtype], _ID_TYPES[ids.dtype], n, n_classes, dim, _stride(out),
+                              _stride(rows), scale, int(bool(accumulate)))
     _call(_b.lib().nuts_lookup_grad, desc, (rows, ids, out), size)
     return out
 

@@ -23,3 +23,16 @@ def test_all_names_of_the_operators_are_the_packages():
         assert getattr(nuts, name) is getattr(categorical, name)
     with pytest.raises(AttributeError):
         nuts.no_such_name
+
+
+def test_both_zeros_are_scales_of_their_own(monkeypatch):
+    """0.0 == -0.0, but the rows' signs differ: what a call gives must not be what an earlier one with the other zero asked for."""
+    import math
+    from paper_1910_11141_amd import categorical
+    seen = []
+    monkeypatch.setattr(categorical, "_call", lambda entry, desc, *rest, **kw: seen.append(math.copysign(1.0, desc._obj.scale)))
+    table, ids = torch.ones(7, 11), torch.zeros(3, dtype=torch.int64)
+    for scale in (0.0, -0.0, 0.0):
+        nuts.nuts_lookup(table, ids, scale=scale)
+        nuts.nuts_lookup_grad(table[:3], ids, 7, scale=scale)
+    assert seen == [1.0, 1.0, -1.0, -1.0, 1.0, 1.0]
