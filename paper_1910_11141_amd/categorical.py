@@ -73,6 +73,16 @@ def _ids(t, what, n=None):
     return t if t.is_contiguous() else t.contiguous()
 
 
+def _in_line(t, what, ids, dim, turn=torch.Tensor.view):
+    """`t`, the rows [*ids.shape, dim] of ids (or of as many ids in one line), as a matrix."""
+    if t.dim() == 0 or t.shape[-1] != dim or t.numel() != ids.numel() * dim or (ids.dim() != 1 and t.shape[:-1] != ids.shape):
+        raise ValueError(f"{what} must be {[*ids.shape, dim]}, not {list(t.shape)}")
+    try:
+        return turn(t, (ids.numel(), dim))
+    except RuntimeError:  # (a view of rows that have no one distance from each other)
+        raise ValueError(f"{what} must have its rows at one distance from each other") from None
+
+
 def _per_row(t, what, n):
     if t is None:
         return None
@@ -131,13 +141,12 @@ def nuts_lookup(table, ids, *, scale=1.0, out=None):
     _matrix(table, "table")
     ids = _ids(ids, "ids")
     classes, dim = table.shape
+    n = ids.numel()
     if out is None:
         out = table.new_empty((*ids.shape, dim))
-    n = ids.numel()
-    rows = out.view(n, dim) if out.dim() != 2 else out
-    if rows.dtype != table.dtype:
+    elif out.dtype != table.dtype:
         raise ValueError(f"out must be {table.dtype}")
-    _matrix(rows, "out", shape=(n, dim))
+    rows = _matrix(out if out.dim() == 2 else _in_line(out, "out", ids, dim), "out", shape=(n, dim))
     scale = float(scale)
     desc, _ = _lookup_desc(False, copysign(1.0, scale), _DTYPES[table.dtype], _ID_TYPES[ids.dtype], n, classes, dim, _stride(table),
                            _stride(rows), scale, 0)
@@ -149,8 +158,8 @@ def nuts_lookup_grad(grad, ids, n_classes, *, scale=1.0, out=None, accumulate=Fa
     """Gradient of nuts_lookup with respect to its table [n_classes, dim], from that with respect to its rows, `grad`
     [*ids.shape, dim].  accumulate: it is added to `out`, and rows of classes that do not come are not touched."""
     ids = _ids(ids, "ids")
-    n, dim = ids.numel(), grad.shape[-1]
-    rows = _matrix(grad if grad.dim() == 2 else grad.reshape(n, dim), "grad", shape=(n, dim))
+    n, dim = ids.numel(), grad.shape[-1] if grad.dim() else 0
+    rows = _matrix(grad if grad.dim() == 2 else _in_line(grad, "grad", ids, dim, torch.Tensor.reshape), "grad", shape=(n, dim))
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")

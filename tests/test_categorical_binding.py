@@ -36,3 +36,26 @@ def test_both_zeros_are_scales_of_their_own(monkeypatch):
         nuts.nuts_lookup(table, ids, scale=scale)
         nuts.nuts_lookup_grad(table[:3], ids, 7, scale=scale)
     assert seen == [1.0, 1.0, -1.0, -1.0, 1.0, 1.0]
+
+
+def test_rows_must_lie_as_their_classes_do():
+    """As many rows as classes are not enough: those of [3, 2] classes are not [2, 3] rows."""
+    table, ids = torch.zeros(7, 11), torch.zeros(3, 2, dtype=torch.int64)
+    for call in (lambda: nuts.nuts_lookup(table, ids, out=torch.zeros(2, 3, 11)), lambda: nuts.nuts_lookup(table, ids, out=torch.zeros(3, 22)),
+                 lambda: nuts.nuts_lookup(table, ids, out=torch.zeros(66)), lambda: nuts.nuts_lookup(table, ids, out=torch.zeros(3, 11, 2).transpose(1, 2)),
+                 lambda: nuts.nuts_lookup_grad(torch.zeros(2, 3, 11), ids, 7), lambda: nuts.nuts_lookup_grad(torch.zeros(3, 22), ids, 7),
+                 lambda: nuts.nuts_lookup_grad(torch.zeros(66), ids, 7), lambda: nuts.nuts_lookup_grad(torch.zeros(()), ids, 7)):
+        with pytest.raises(ValueError):
+            call()
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="tensors without a GPU")
+def test_rows_in_one_line_are_rows_too():
+    table, ids = torch.zeros(7, 11), torch.zeros(3, 2, dtype=torch.int64)
+    for call in (lambda: nuts.nuts_lookup(table, ids, out=torch.zeros(3, 2, 11)), lambda: nuts.nuts_lookup(table, ids, out=torch.zeros(6, 11)),
+                 lambda: nuts.nuts_lookup(table, ids[0, 0], out=torch.zeros(11)), lambda: nuts.nuts_lookup_grad(torch.zeros(3, 2, 11), ids, 7),
+                 lambda: nuts.nuts_lookup_grad(torch.zeros(6, 11), ids, 7), lambda: nuts.nuts_lookup_grad(torch.zeros(3, 2, 11), ids.view(-1), 7),
+                 lambda: nuts.nuts_lookup_grad(torch.zeros(11), ids[0, 0], 7)):
+        with pytest.raises(B.NutsError) as e:  # (of the shapes there is nothing to say)
+            call()
+        assert e.value.code == B.NUTS_E_DEVICE
