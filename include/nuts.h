@@ -327,7 +327,7 @@ int nuts_logprobs_grad(const nuts_logits_desc* desc, const void* logits, const v
 typedef struct {
     int32_t dtype;         /* NUTS_F32 or NUTS_BF16: x, weight and their gradients                         */
     int32_t id_type;       /* of the targets                                                               */
-    int64_t n_rows;        /* 0 .. 2^24                                                                    */
+    int64_t n_rows;        /* 0 .. 2^20                                                                    */
     int64_t n_classes;     /* 1 .. 2^24                                                                    */
     int64_t dim;           /* 1 .. 2^20                                                                    */
     int64_t x_stride;      /* from row to row, >= dim; and so on                                           */

@@ -59,3 +59,27 @@ def test_rows_in_one_line_are_rows_too():
         with pytest.raises(B.NutsError) as e:  # (of the shapes there is nothing to say)
             call()
         assert e.value.code == B.NUTS_E_DEVICE
+
+
+def test_sizes_are_the_headers():
+    """Each size that the header gives a range for is taken up to its end, and not beyond."""
+    import ctypes as C
+    import os
+    import re
+    from paper_1910_11141_amd import build
+    with open(os.path.join(os.path.dirname(build.HERE), "include", "nuts.h")) as f:
+        header = f.read()
+    bytes_needed, checked = C.c_int64(), 0
+    for struct, query, strides in ((B.nuts_lookup_desc, B.lib().nuts_lookup_grad_workspace, ("table_stride", "row_stride")),
+                                   (B.nuts_logits_desc, B.lib().nuts_logprobs_workspace, ("row_stride",)),
+                                   (B.nuts_score_desc, B.lib().nuts_score_workspace,
+                                    ("x_stride", "weight_stride", "logits_stride", "grad_x_stride", "grad_weight_stride"))):
+        text = re.search(r"typedef struct \{([^{}]*)\} " + struct.__name__ + ";", header).group(1)
+        for name, low, high in re.findall(r"int\d+_t (\w+);\s*/\*[^*]*?(\d+) \.\. ([-0-9^ ]*[0-9]|NUTS_CAT_MAX_TOP)", text):
+            low, high = int(low), eval(high.replace("^", "**"), {"NUTS_CAT_MAX_TOP": B.NUTS_CAT_MAX_TOP})
+            for value, want in ((low - 1, B.NUTS_E_INVALID_ARG), (low, B.NUTS_OK), (high, B.NUTS_OK), (high + 1, B.NUTS_E_INVALID_ARG)):
+                sizes = {k: 2 for k, t in struct._fields_ if t is C.c_int64 and k not in strides and k != "allowed_stride"}
+                desc = struct(**{**sizes, "scale": 1.0, **{k: 1 << 31 for k in strides}, name: value})
+                assert query(C.byref(desc), C.byref(bytes_needed)) == want, (struct.__name__, name, value)
+            checked += 1
+    assert checked == 3 + 3 + 3
