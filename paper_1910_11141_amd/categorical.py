@@ -4,7 +4,8 @@ Where one of the sampler's targets has two classes, these operators are the part
 class and their gradient, log-probabilities of given classes with entropies and alternatives, from logits or from features and
 weights, and their gradients.  Tensors are on the current device; matrices have unit stride along their rows and any from one to
 the next.  A call is enqueued on the stream of nuts_set_stream, or on PyTorch's current one if that is not set, so that calls
-under torch.cuda.stream() or in a torch.cuda.graph() go where PyTorch's own would.
+under torch.cuda.stream() or in a torch.cuda.graph() go where PyTorch's own would.  Autograd knows none of these calls: results never
+require a gradient, also where an argument does, and gradients are what the *_grad calls are asked for.
 """
 from __future__ import annotations
 

@@ -361,6 +361,7 @@ struct GradArgs {
 };
 
 constexpr int kGradPacks = 4;  // of a thread
+constexpr float kOffOne = 1e-4f;  // more than what lse's rounding and the order of its sum can put the sum of p off 1
 
 // A workgroup a part of a row.  Bound by its reads and writes: one exponential an element; 4096 x 50001 bfloat16 with entropies
 // 140 us, 819 MB at 5.9 TB/s.  A large gradient is written past the
@@ -369,7 +370,7 @@ constexpr int kGradPacks = 4;  // of a thread
 //
 // p = e^(z - lse) takes half a unit in the last place of lse as an error.  In binary32 that is more than all else is off by, and a row
 // that a workgroup holds in its registers is divided by the sum of its p, which without that error is 1 (8000 x 4000: 41 us, 39
-// without).  Far from 0 (kFar) each of the row's workgroups goes through all of it for its maximum and sum, from the caches (4096 x 50001
+// without), unless that is far off: then lse is that of a longer row.  Far from 0 (kFar) each of the row's workgroups goes through all of it for its maximum and sum, from the caches (4096 x 50001
 // bfloat16 490 us where lse is enough for 140; to leave such rows to one workgroup each takes 250, and registers that cost all
 // others 3 %).
 template <typename T, bool kMask, bool kEntropy>
@@ -422,8 +423,10 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
         if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64].s = sum;
         __syncthreads();
         sum = (shared[0].s + shared[1].s) + (shared[2].s + shared[3].s);
-        one_by_sum = 1.f / sum;
-        ln_sum = logf(sum);
+        if (__builtin_fabsf(sum - 1.f) <= kOffOne) {
+            one_by_sum = 1.f / sum;
+            ln_sum = logf(sum);
+        }
     }
 #pragma unroll
     for (int u = 0; u < kGradPacks; ++u) {

@@ -163,3 +163,25 @@ def test_score_grad_of_some_far_rows_over_several_pieces(dtype, kept):
         want_w, bound_w = want_w + some_w, bound_w + some_bound
     bound_w = bound_w * 1.01 + (want_w.abs() + bound_w) * R.EPS[dtype] * 1.01
     assert float(((grad_w.double() - want_w).abs() - bound_w).max()) <= 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("classes", [1000, 4000, 20000])
+def test_logprobs_grad_of_a_part_of_the_classes(dtype, classes):
+    """A row's classes in two parts, each with the whole row's lse and entropy: the parts of its gradient."""
+    nuts, g = ops(), gen(classes)
+    logits = (torch.randn(6, classes, generator=g, device="cuda") * 3).to(dtype)
+    targets = torch.randint(0, classes, (6,), generator=g, device="cuda")
+    parts = [torch.randn(6, generator=g, device="cuda") for _ in range(3)]
+    fwd = nuts.nuts_logprobs(logits, targets)
+    cut = classes * 2 // 5
+    got = [nuts.nuts_logprobs_grad(logits[:, own], targets - own.start, fwd.lse, fwd.entropy, grad_logprob=parts[0], grad_lse=parts[1], grad_entropy=parts[2])
+           for own in (slice(0, cut), slice(cut, classes))]
+    want = R.grad_logits(logits.double(), targets, None, 1.0, *parts)
+    # (a target in the other part: this part's classes lose their share all the same, from grad_lse)
+    known = [(targets >= 0) & (targets < cut), targets >= cut]
+    lost = [torch.where(k, 0.0, parts[0]).double()[:, None] for k in known]
+    p = torch.softmax(logits.double(), 1)
+    want = torch.cat([want[:, :cut] + lost[0] * p[:, :cut], want[:, cut:] + lost[1] * p[:, cut:]], 1)
+    off = (torch.cat(got, 1).double() - want).abs() - _bound(want, logits.double(), targets, 1.0, parts, dtype)
+    assert float(off.max()) <= 0, float(off.max())
