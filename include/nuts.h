@@ -319,8 +319,9 @@ int nuts_logprobs(const nuts_logits_desc* desc, const void* logits, const void* 
  * [n_rows] or NULL), from the forward pass's lse and entropy (entropy only with grad_entropy):
  *   scale * (grad_logprob ([v = target] - p_v) + grad_lse p_v - grad_entropy p_v (log p_v + entropy)),
  * where a row without a target has no grad_logprob; 0 for classes that may not come, and where p_v is 0 but for the target.
- * A row in which every z is -infinity has gradient 0.  Rows of grad_logits are grad_stride apart.  p is e^(z - lse) where
- * that has the digits for it; of rows with |lse| > 64 (16-bit logits: 1024) maximum and sum are found again, and lse is not used. */
+ * A row in which every z is -infinity has gradient 0.  Rows of grad_logits are grad_stride apart.  lse and entropy may be those
+ * of a longer row that this one is a part of.  Where |lse| is above 64 (16-bit logits: 1024), p = e^(z - lse) would be off by lse's rounding:
+ * such rows are read once more for their maximum and sum. */
 int nuts_logprobs_grad(const nuts_logits_desc* desc, const void* logits, const void* targets, const uint32_t* allowed,
                        const float* lse, const float* entropy, const float* grad_logprob, const float* grad_lse,
                        const float* grad_entropy, void* grad_logits, int64_t grad_stride);
@@ -353,7 +354,8 @@ int nuts_score(const nuts_score_desc* desc, const void* x, const void* weight, c
  * rounded to bfloat16, for the matrix instructions multiply nothing wider; the products' sums are binary32, and what the
  * entries of the rows' targets lose in that rounding is added to them.  Where probabilities are spread, that is nearly all that is lost;
  * another class that is nearly certain, and the parts of grad_lse and grad_entropy, keep it (2^-8 of each entry at most).  Features and
- * weights in binary32 have dz in binary32.  The workspace's size is that for the larger of both ways. */
+ * weights in binary32 have dz in binary32.  Rows with |lse| above 64 (bfloat16: 1024) have p from their own maximum and sum, and lse may
+ * not be a longer row's there.  The workspace's size is that for the larger of both ways. */
 int nuts_score_grad_workspace(const nuts_score_desc* desc, int64_t* bytes);
 int nuts_score_grad(const nuts_score_desc* desc, const void* x, const void* weight, const void* targets,
                     const float* logits, const float* lse, const float* entropy, const float* grad_logprob,

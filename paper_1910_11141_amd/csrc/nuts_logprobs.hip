@@ -406,10 +406,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
             add_logits<kN>(v, some, a.scale * kLog2e);
         }
         v = join_block(v, a.scale * kLog2e, shared);
+        // (lse - s m has fewer digits than ln S, and is to be taken where it is another number: lse is that of a longer row)
         base = v.m;
-        shift = 0.f;
-        one_by_sum = 1.f / v.s;
-        ln_sum = logf(v.s);
+        shift = logf(v.s);
+        const float given = __builtin_fmaf(-v.m, a.scale, lse);
+        if (__builtin_fabsf(given - shift) > __builtin_fmaf(__builtin_fabsf(lse), 0x1p-22f, kOffOne)) shift = given;
     } else if (sizeof(T) == 4 && a.parts == 1 && !empty) {
         float sum = 0.f;
 #pragma unroll
