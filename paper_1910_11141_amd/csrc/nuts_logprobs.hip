@@ -197,7 +197,7 @@ struct Packs {
 };
 
 // One workgroup a row, or a part of one where there are few rows (kWhole = false: join_rows_kernel ends them).  One pass, bound by its
-// reads where there are many rows: 4096 x 32001 bfloat16 with 5 alternatives 61 us, 4.3 TB/s of them; of few rows by the wait for one
+// reads where there are many rows: 4096 x 32001 bfloat16 with 5 alternatives 63 us, 4.7 TB/s of them; of few rows by the wait for one
 // read of memory and the alternatives' exchange through LDS: 8 x 128000, masked, with 20 alternatives 9 us and 7 for join_rows_kernel.
 template <typename T, bool kMask, bool kTop, bool kWhole>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogitsArgs a)
@@ -364,7 +364,7 @@ constexpr int kGradPacks = 4;  // of a thread
 constexpr float kOffOne = 1e-4f;  // more than what lse's rounding and the order of its sum can put the sum of p off 1
 
 // A workgroup a part of a row.  Bound by its reads and writes: one exponential an element; 4096 x 50001 bfloat16 with entropies
-// 140 us, 819 MB at 5.9 TB/s.  A large gradient is written past the
+// 139 us one after the other, 144 in turn with the forward pass, 833 MB at 5.8 TB/s; with a mask 155.  A large gradient is written past the
 // caches, which then keep the logits that the forward pass left there (both passes on 4096 x 50001 bfloat16: 252 us with plain
 // stores, 231 us so).
 //

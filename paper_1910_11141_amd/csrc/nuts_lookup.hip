@@ -161,11 +161,11 @@ constexpr int kFewRows = 64;                   // at most so many classes a work
 
 // A workgroup owns `classes` neighbouring rows of the table, or a slice of their columns: it finds the positions of theirs among all
 // n (few, from cache) and adds them up.  What bounds it is the wait for memory, twice at least, and again for every 32 rows or so of
-// the class that comes most often: 1000 positions, 5000 classes of 100 in binary32 9 us.  Slices: 1000 positions, 1000 classes of 2048 in
-// binary32 16 us, 76 without; up to 4096 workgroups: 100 positions, 4168 classes of 1842, binary32 14 us, 23 with 2048 and 19 with
-// 16384.  Sorting the positions first, as is done with more of them, takes three launches: 15 us for 1100 positions where this takes 11
-// for 1000.  Only a table that has to be cleared and is too large for the caches is cleared faster beside a sort (100003 classes of
-// 2048 in bfloat16, 1000 positions: 77 us so, 92 by this kernel).
+// the class that comes most often: 1000 positions, 5000 classes of 100 in binary32 9 us (13 where the frequent classes are neighbours).
+// Slices: 1000 positions, 1000 classes of 2048 in binary32 16 us, 76 without; up to 4096 workgroups: 100 positions, 4168 classes of 1842,
+// binary32 14 us, 23 with 2048 and 19 with 16384.  Sorting the positions first, as is done with more of them, takes three launches: 15 us
+// for 1100 positions where this takes 11 for 1000.  Only a table that has to be cleared and is too large for the caches is cleared
+// faster beside a sort (100003 classes of 2048 in bfloat16, 1000 positions: 77 us so, 92 by this kernel).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void few_rows_kernel(GradArgs a, int classes, long slice_packs, long first_block)
 {

@@ -1,7 +1,7 @@
 // C = A B' on the matrix instructions: binary32 or bfloat16, sums binary32.  A is m x k, B is n x k.
 //
 // A workgroup makes a tile of kM x kN; its waves divide it.  Per step along the contraction the workgroup takes 128 bytes for each row
-// of its tile of A and of B from memory straight into LDS (no registers in between), kStages - 1 steps ahead.  Either
+// of its tile of A and of B from memory straight into LDS (no registers in between), kAhead (two) steps ahead.  Either
 // matrix may lie in memory along its rows ("along": a row's elements, which are the contraction's, are neighbours) or across them
 // (its transpose lies along: the elements that belong to one place of the contraction are neighbours); the tile in LDS lies as
 // the memory does.
@@ -217,9 +217,9 @@ __device__ __forceinline__ void wait_and_meet()
 // first half of a step and those of A over the second, behind the barrier at which all are done with the step before.
 //
 // Bound by the matrix instructions and, between them, by the rate at which the chip lets them run (kept busy with random
-// numbers and nothing else they reach 2.0 PFLOP/s in bfloat16): 8192 x 32000 x 4096 in 1.57 ms with the statistics, 1.37 PFLOP/s, the
-// instructions busy 74 % of the time; 4096 x 32001 x 2048 with z stored 489 us, 1.10 PFLOP/s, dX 426 us, dW 480 us (1.26 and
-// 1.12).  binary32: 2048 x 16384 x 512 in 262 us, 131 TFLOP/s.  One row of x: the reads of the weights, 45 us for 262 MB.
+// numbers and nothing else they reach 2.0 PFLOP/s in bfloat16): 8192 x 32000 x 4096 in 1.56 ms with the statistics, 1.38 PFLOP/s, the
+// instructions busy 75 % of the time; 4096 x 32001 x 2048 with z stored 482 us, 1.12 PFLOP/s, dX 422 us, dW 474 us (1.27 and
+// 1.13).  binary32: 2048 x 16384 x 512 in 262 us, 131 TFLOP/s.  One row of x: the reads of the weights, 41 us for 262 MB.
 template <typename T, int kM, int kN, int kWavesM, int kWavesN, int kAhead, bool kAcrossA, bool kAcrossB, bool kRagged, ProductKind kKind>
 __global__ __launch_bounds__(64 * kWavesM * kWavesN) void product_kernel(ProductArgs p)
 {

@@ -66,7 +66,7 @@ struct GradArgs {
 
 constexpr int kGradPacks = 4;  // of a thread
 
-// dZ, rounded to the features' type: a workgroup a part of a row.  Bound by its reads and writes: 4096 x 32001, to bfloat16, 142 us, 787
+// dZ, rounded to the features' type: a workgroup a part of a row.  Bound by its reads and writes: 4096 x 32001, to bfloat16, 145 us, 789
 // MB at 5.5 TB/s.  Of a row far from 0 (kFar) each of its workgroups goes through all of it for its maximum and sum (all rows of 4096 x
 // 32001 far: 470 us).  Where z is made anew piece by piece, the tiles of such rows are multiplied once more before that, for their statistics
 // (9000 x 40000 x 512 bfloat16 in two pieces: 2.07 ms, 2.52 with all rows far; 2.04 without the launches that ask which are).
