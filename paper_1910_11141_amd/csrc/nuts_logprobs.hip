@@ -370,9 +370,9 @@ constexpr float kOffOne = 1e-4f;  // more than what lse's rounding and the order
 //
 // p = e^(z - lse) takes half a unit in the last place of lse as an error.  In binary32 that is more than all else is off by, and a row
 // that a workgroup holds in its registers is divided by the sum of its p, which without that error is 1 (8000 x 4000: 41 us, 39
-// without), unless that is far off: then lse is that of a longer row.  Far from 0 (kFar) each of the row's workgroups goes through all of it for its maximum and sum, from the caches (4096 x 50001
-// bfloat16 490 us where lse is enough for 140; to leave such rows to one workgroup each takes 250, and registers that cost all
-// others 3 %).
+// without), unless that is far off: then lse is that of a longer row.  Far from 0 (kFar) each of the row's workgroups goes through all
+// of it for its maximum and sum, from the caches (4096 x 50001 bfloat16 490 us where lse is enough for 140; to leave such rows to one
+// workgroup each takes 250, and registers that cost all others 3 %).
 template <typename T, bool kMask, bool kEntropy>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
 {
@@ -407,10 +407,12 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(GradArgs a)
         }
         v = join_block(v, a.scale * kLog2e, shared);
         // (lse - s m has fewer digits than ln S, and is to be taken where it is another number: lse is that of a longer row)
-        base = v.m;
-        shift = logf(v.s);
-        const float given = __builtin_fmaf(-v.m, a.scale, lse);
-        if (__builtin_fabsf(given - shift) > __builtin_fmaf(__builtin_fabsf(lse), 0x1p-22f, kOffOne)) shift = given;
+        if (v.m > -INFINITY) {
+            base = v.m;
+            shift = logf(v.s);
+            const float given = __builtin_fmaf(-v.m, a.scale, lse);
+            if (__builtin_fabsf(given - shift) > __builtin_fmaf(__builtin_fabsf(lse), 0x1p-22f, kOffOne)) shift = given;
+        }
     } else if (sizeof(T) == 4 && a.parts == 1 && !empty) {
         float sum = 0.f;
 #pragma unroll

@@ -118,8 +118,10 @@ __global__ __launch_bounds__(kThreads) void dz_kernel(GradArgs a)
             }
             v = join_block(v, kLog2e, shared);
         }
-        base = v.m;
-        ln_s = logf(v.s);
+        if (v.m > -INFINITY) {
+            base = v.m;
+            ln_s = logf(v.s);
+        }
     }
     if (a.residual && y < 0 && begin == 0) a.residual[row] = 0.f;
 #pragma unroll

@@ -93,3 +93,21 @@ def test_score_grad_of_classes_of_probability_0(dtype, n, classes, dim, value, k
         others = torch.arange(n, device="cuda") != 1
         assert not bool(got_w[never].any()) and not bool(torch.isfinite(got_w[~never]).all())
         assert torch.equal(got_x[others], clean_x[others]) and not bool(torch.isfinite(got_x[1]).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("classes", [5, 1000, 20011])
+@pytest.mark.parametrize("lse", [3.0, -500.0, 5000.0])
+def test_a_part_of_the_classes_of_which_none_may_come_has_no_gradient(dtype, classes, lse):
+    """With the lse of a longer row, which is finite, and near 0 or far from it."""
+    nuts, g = ops(), gen(classes)
+    logits = torch.randn(3, classes, generator=g, device="cuda").to(dtype)
+    logits[1] = -math.inf
+    allowed = torch.ones(3, classes, dtype=torch.bool, device="cuda")
+    allowed[0] = False
+    allowed[2] = False
+    logits[2] = -math.inf
+    ones = torch.ones(3, device="cuda")
+    for mask in (None, R.pack_bits(allowed)):
+        got = nuts.nuts_logprobs_grad(logits, torch.full((3,), -1, device="cuda"), ones * lse, ones * 2.0, grad_lse=ones, grad_entropy=ones, allowed=mask)
+        assert not bool(got[1:].any()) and (mask is None or not bool(got[0].any()))
