@@ -32,7 +32,7 @@ enum { NUTS_OK = 0, NUTS_E_INVALID_ARG = -1, NUTS_E_ALLOC = -2, NUTS_E_DEVICE = 
  * log-weights and U-turn dot products are binary64 in both cases. */
 enum { NUTS_F32 = 0, NUTS_F64 = 1 };
 
-/* The categorical operators (last section) take NUTS_F32 and these two: bfloat16, binary16. */
+/* The categorical operators (last sections) take NUTS_F32 and these two: bfloat16, binary16. */
 enum { NUTS_BF16 = 2, NUTS_F16 = 3 };
 
 /* Type of an array of classes. */
@@ -361,6 +361,112 @@ int nuts_score_grad(const nuts_score_desc* desc, const void* x, const void* weig
                     const float* logits, const float* lse, const float* entropy, const float* grad_logprob,
                     const float* grad_lse, const float* grad_entropy, void* grad_x, void* grad_weight, void* workspace,
                     int64_t workspace_bytes);
+
+/* ---- What a categorical model answers through and learns with ---------------------------------------------------------
+ *
+ * Logits are adjusted before a class is chosen from them (nuts_penalties, and its gradient for models that are trained
+ * through that); all parameters of a model are moved at once along their gradients (nuts_adamw), as far as the gradients' common norm
+ * lets them (nuts_norm).  What is said of the operators above holds here: streams, capture, workspaces, strides, ids that are no class,
+ * sums in a fixed order, sizes of zero.  Tables of tensors are HOST arrays that are read during the call. */
+
+#define NUTS_CAT_MAX_BIAS 1024
+
+typedef struct {
+    int32_t dtype;          /* NUTS_F32, NUTS_BF16 or NUTS_F16: logits, their gradients                    */
+    int32_t id_type;        /* of the history and of bias_ids                                              */
+    int64_t n_rows;         /* 0 .. 2^31 - 2                                                               */
+    int64_t n_classes;      /* 1 .. 2^31 - 2^18 - 1                                                        */
+    int64_t row_stride;     /* of the logits, >= n_classes                                                 */
+    int64_t out_stride;     /* of what is written, >= n_classes                                            */
+    int64_t allowed_stride; /* 32-bit words from one row of `allowed` to the next; 0: one row for all      */
+    int64_t bias_stride;    /* of `bias`, >= n_classes; 0: one row for all                                 */
+    int64_t history_len;    /* 0 .. 2^30 - 1: places in a row of the history                               */
+    int64_t history_stride; /* >= history_len; 0: one row for all                                          */
+    int64_t n_bias;         /* 0 .. 1024: single classes with a bias, in each row                          */
+    double repetition;      /* what all rows have where the array of that name is NULL: finite, > 0        */
+    double frequency, presence; /* finite                                                                  */
+} nuts_penalties_desc;
+
+/* A row's history is the first lengths[row] of its places (all of them where `lengths` is NULL; a length is taken as
+ * the nearest in [0, history_len]), the first prompts[row] of which are not the model's own (NULL: none).  With seen_v = class v comes in it
+ * and count_v = how often it comes behind the prompt, and z = logits_v,
+ *   z = z > 0 ? z / repetition : z * repetition   where seen_v;     z = z - (frequency count_v + presence [count_v > 0]);
+ *   z = z + bias_v, then + the sum of the row's bias_values whose bias_ids are v, in their order;     z = -infinity where v is not allowed,
+ * whatever was there (NaN, too).  The arrays repetition, frequency and presence are [n_rows], bias [n_classes] or rows of it, bias_ids and
+ * bias_values [n_rows][n_bias]; each may be NULL, and `allowed` is that of nuts_logprobs.  All of it is binary32 and rounded once.
+ * `out` may be `logits` itself, with the same stride: then classes that nothing changes are neither read nor written. */
+int nuts_penalties(const nuts_penalties_desc* desc, const void* logits, const void* history, const int32_t* lengths,
+                   const int32_t* prompts, const float* repetition, const float* frequency, const float* presence,
+                   const float* bias, const void* bias_ids, const float* bias_values, const uint32_t* allowed, void* out);
+
+/* From grad_out, the gradient with respect to what nuts_penalties writes (rows grad_stride apart), that with respect to its logits,
+ *   grad_logits_v = grad_out_v * (seen_v ? (logits_v > 0 ? 1 / repetition : repetition) : 1), 0 where v is not allowed,
+ * and that with respect to a bias that all rows share, grad_bias_v = sum over the rows of grad_out_v where v is allowed.  Either may be
+ * NULL.  grad_logits (rows out_stride apart) may be grad_out itself.  logits are those that nuts_penalties was given, and
+ * are read where a class was seen. */
+int nuts_penalties_grad_workspace(const nuts_penalties_desc* desc, int64_t* bytes);
+int nuts_penalties_grad(const nuts_penalties_desc* desc, const void* grad_out, int64_t grad_stride, const void* logits,
+                        const void* history, const int32_t* lengths, const float* repetition, const uint32_t* allowed,
+                        void* grad_logits, float* grad_bias, void* workspace, int64_t workspace_bytes);
+
+typedef struct {
+    const void* data;  /* DEVICE; n numbers without gaps; NULL where n is 0                                */
+    int64_t n;         /* 0 .. 2^40                                                                        */
+    int32_t dtype;     /* NUTS_F32, NUTS_BF16 or NUTS_F16                                                  */
+    int32_t reserved;
+} nuts_tensor;
+
+/* norm = square root of the sum of all squares, summed in binary64; factor = min(1, max_norm / norm), which times all
+ * numbers keeps their norm to max_norm (finite, > 0), and NaN where the norm is not finite.  Either may be NULL; one number each. */
+int nuts_norm_workspace(const nuts_tensor* tensors, int64_t n_tensors, int64_t* bytes);
+int nuts_norm(const nuts_tensor* tensors, int64_t n_tensors, double max_norm, float* norm, float* factor, void* workspace,
+              int64_t workspace_bytes);
+
+typedef struct {
+    void* param;       /* DEVICE pointers, each to n numbers without gaps                                  */
+    const void* grad;  /* NULL: this tensor is left alone                                                  */
+    void* copy;        /* NULL, or: receives the new parameters in copy_dtype                              */
+    void* m;           /* float, or int8_t where state_bits is 8                                           */
+    void* v;           /* float, or uint8_t                                                                */
+    float* m_scale;    /* state_bits 8: one for each NUTS_STATE_BLOCK numbers of the tensor, the last ones together */
+    float* v_scale;
+    int64_t n;         /* 0 .. 2^40                                                                        */
+} nuts_adamw_tensor;
+#define NUTS_STATE_BLOCK 256
+
+typedef struct {
+    int32_t param_dtype;  /* NUTS_F32 or NUTS_BF16                                                         */
+    int32_t grad_dtype;   /* NUTS_F32, NUTS_BF16 or NUTS_F16                                               */
+    int32_t copy_dtype;   /* NUTS_BF16 or NUTS_F16                                                         */
+    int32_t state_bits;   /* 32 or 8                                                                       */
+    double lr;            /* finite                                                                        */
+    double beta1, beta2;  /* [0, 1)                                                                        */
+    double eps;           /* finite, >= 0                                                                  */
+    double weight_decay;  /* finite                                                                        */
+    double scale;         /* of the gradients; finite (-1: uphill)                                         */
+    int64_t step;         /* >= 1: number of this step, the first is 1                                     */
+    uint64_t seed;        /* of what is rounded at random                                                  */
+} nuts_adamw_desc;
+
+/* One step of AdamW (Loshchilov & Hutter, 2019) for every tensor:
+ *   g = scale factor grad;   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2;
+ *   param = param (1 - lr weight_decay) - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps).
+ * `step`, `lr` and `factor` are DEVICE scalars or NULL; the first two take the descriptor's place (a captured step that is replayed needs
+ * them there; a step below 1 counts as 1), and where factor is NaN the call changes nothing.  No two things that are written may overlap.
+ *
+ * Arithmetic is binary32.  Moments of 8 bits stand for powers of their codes, m = sign(c) c^2 m_scale (c = -127 .. 127), v = (c^2 v_scale)^2
+ * (c = 0 .. 254); a block's largest has the last code.  What stands between two codes becomes one of them, at random so that
+ * the mean is kept, but a v above 0 does not become 0.  c = -128 and c = 255 are what is not finite and count as NaN.
+ * Parameters of bfloat16 are rounded at random, too (a step is mostly less than half a unit in their last place, and to the nearest they would stay where they
+ * are); the parameters' copies are rounded to the nearest.  The random bits of the four numbers from 4 q of tensor t on are the four words of
+ * Philox4x32-10 with the key `seed` and the counter (q mod 2^32, 6 + 256 (q / 2^32), step mod 2^32, t): bits 0-9 of a word are m's, 10-19 v's,
+ * 20-31 the parameter's. */
+int nuts_adamw(const nuts_adamw_desc* desc, const nuts_adamw_tensor* tensors, int64_t n_tensors, const int64_t* step,
+               const float* lr, const float* factor);
+
+/* The moments of 8 bits as numbers: `param` receives m and `copy` v, in dtype (NUTS_F32, NUTS_BF16, NUTS_F16); either may
+ * be NULL.  grad is not looked at. */
+int nuts_adamw_values(const nuts_adamw_tensor* tensors, int64_t n_tensors, int32_t dtype);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,8 @@ NUTS_F32, NUTS_F64 = 0, 1
 NUTS_BF16, NUTS_F16 = 2, 3
 NUTS_I32, NUTS_I64 = 0, 1
 NUTS_CAT_MAX_TOP = 64
+NUTS_CAT_MAX_BIAS = 1024
+NUTS_STATE_BLOCK = 256
 NUTS_TARGET_STD_NORMAL, NUTS_TARGET_GAUSS_DENSE_PRECISION, NUTS_TARGET_GAUSS_DIAG, NUTS_TARGET_LOGISTIC_REGRESSION = 0, 1, 2, 3
 NUTS_VARIANT_AUTO, NUTS_VARIANT_WAVE, NUTS_VARIANT_TILE, NUTS_VARIANT_ELEM, NUTS_VARIANT_GRID = 0, 1, 2, 3, 4
 NUTS_VARIANT_DENSE, NUTS_VARIANT_QUAD = 5, 6
@@ -30,6 +32,8 @@ EXPORTS = ("nuts_create_target", "nuts_destroy_target", "nuts_sample", "nuts_sam
            "nuts_sample_static", "nuts_set_stream", "nuts_tile_pack",
            "nuts_lookup", "nuts_lookup_grad", "nuts_lookup_grad_workspace", "nuts_logprobs", "nuts_logprobs_workspace",
            "nuts_logprobs_grad", "nuts_score", "nuts_score_workspace", "nuts_score_grad", "nuts_score_grad_workspace",
+           "nuts_penalties", "nuts_penalties_grad", "nuts_penalties_grad_workspace", "nuts_norm", "nuts_norm_workspace",
+           "nuts_adamw", "nuts_adamw_values",
            "nuts_last_error")
 NUTS_STATIC_SCRATCH_BYTES = 64 << 20
 
@@ -67,6 +71,28 @@ class nuts_score_desc(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("id_type", C.c_int32), ("n_rows", C.c_int64), ("n_classes", C.c_int64), ("dim", C.c_int64),
                 ("x_stride", C.c_int64), ("weight_stride", C.c_int64), ("logits_stride", C.c_int64),
                 ("grad_x_stride", C.c_int64), ("grad_weight_stride", C.c_int64), ("scale", C.c_double)]
+
+
+class nuts_penalties_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("id_type", C.c_int32), ("n_rows", C.c_int64), ("n_classes", C.c_int64), ("row_stride", C.c_int64),
+                ("out_stride", C.c_int64), ("allowed_stride", C.c_int64), ("bias_stride", C.c_int64), ("history_len", C.c_int64),
+                ("history_stride", C.c_int64), ("n_bias", C.c_int64), ("repetition", C.c_double), ("frequency", C.c_double),
+                ("presence", C.c_double)]
+
+
+class nuts_tensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class nuts_adamw_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64)]
+
+
+class nuts_adamw_desc(C.Structure):
+    _fields_ = [("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("copy_dtype", C.c_int32), ("state_bits", C.c_int32),
+                ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("scale", C.c_double), ("step", C.c_int64), ("seed", C.c_uint64)]
 
 
 class NutsError(RuntimeError):
@@ -109,6 +135,14 @@ def lib() -> C.CDLL:
         L.nuts_score_workspace.argtypes = [score, bytes_out]
         L.nuts_score_grad.argtypes = [score] + [ptr] * 12 + [size]
         L.nuts_score_grad_workspace.argtypes = [score, bytes_out]
+        penalties = C.POINTER(nuts_penalties_desc)
+        L.nuts_penalties.argtypes = [penalties] + [ptr] * 12
+        L.nuts_penalties_grad.argtypes = [penalties, ptr, size] + [ptr] * 8 + [size]
+        L.nuts_penalties_grad_workspace.argtypes = [penalties, bytes_out]
+        L.nuts_norm.argtypes = [ptr, size, C.c_double, ptr, ptr, ptr, size]
+        L.nuts_norm_workspace.argtypes = [ptr, size, bytes_out]
+        L.nuts_adamw.argtypes = [C.POINTER(nuts_adamw_desc), ptr, size, ptr, ptr, ptr]
+        L.nuts_adamw_values.argtypes = [ptr, size, C.c_int32]
         L.nuts_last_error.argtypes = []
         L.nuts_last_error.restype = C.c_char_p
         for name in EXPORTS[:-1]:

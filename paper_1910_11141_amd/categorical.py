@@ -1,8 +1,8 @@
-"""ctypes binding of the categorical operators (include/nuts.h, last section): argument marshalling only.
+"""ctypes binding of the categorical operators (include/nuts.h, last sections): argument marshalling only.
 
 Where one of the sampler's targets has two classes, these operators are the parts of models with many: rows of a table by
 class and their gradient, log-probabilities of given classes with entropies and alternatives, from logits or from features and
-weights, and their gradients.  Tensors are on the current device; matrices have unit stride along their rows and any from one to
+weights, and their gradients, and logits adjusted by what was said before.  Tensors are on the current device; matrices have unit stride along their rows and any from one to
 the next.  A call is enqueued on the stream of nuts_set_stream, or on PyTorch's current one if that is not set, so that calls
 under torch.cuda.stream() or in a torch.cuda.graph() go where PyTorch's own would.  Autograd knows none of these calls: results never
 require a gradient, also where an argument does, and gradients are what the *_grad calls are asked for.
@@ -19,7 +19,7 @@ import torch
 from . import binding as _b
 
 __all__ = ("nuts_lookup", "nuts_lookup_grad", "nuts_logprobs", "nuts_logprobs_grad", "nuts_score", "nuts_score_grad",
-           "Logprobs", "Scores")
+           "Logprobs", "Scores", "nuts_penalties", "nuts_penalties_grad")
 
 Logprobs = namedtuple("Logprobs", "logprob lse entropy top_ids top_logprobs")
 Scores = namedtuple("Scores", "logprob lse entropy logits")
@@ -39,6 +39,12 @@ def _lookup_desc(grad, sign, *fields):  # (sign: of the scale, for its zeros are
 def _logits_desc(forward, *fields):
     desc = _b.nuts_logits_desc(*fields, 0)
     return C.byref(desc), _bytes(_b.lib().nuts_logprobs_workspace, desc) if forward else 0
+
+
+@lru_cache(maxsize=512)
+def _penalties_desc(grad, signs, *fields):  # (signs: of frequency and presence, for zeros are equal)
+    desc = _b.nuts_penalties_desc(*fields)
+    return C.byref(desc), _bytes(_b.lib().nuts_penalties_grad_workspace, desc) if grad else 0
 
 
 @lru_cache(maxsize=512)
@@ -93,7 +99,7 @@ def _per_row(t, what, n):
 
 
 def _call(entry, desc, tensors, workspace_bytes=None, last=()):
-    """`entry` on the library's stream; `tensors`: its pointers in order (None: NULL), then the workspace."""
+    """`entry` of a descriptor and `tensors`, its pointers in order (None: NULL), then the workspace."""
     device = tensors[0].device
     args = [desc]
     for t in tensors:
@@ -115,7 +121,11 @@ def _call(entry, desc, tensors, workspace_bytes=None, last=()):
         workspace = torch.empty(workspace_bytes, dtype=torch.uint8, device=device) if workspace_bytes else None
         args += (workspace.data_ptr() if workspace_bytes else None, workspace_bytes)
         tensors = (*tensors, workspace)
-    args += last
+    _enqueue(entry, args + list(last), tensors, device)
+
+
+def _enqueue(entry, args, tensors, device):
+    """`entry` on the library's stream, or PyTorch's current one; `tensors`: all that it uses."""
     current = torch._C._cuda_getCurrentRawStream(device.index)
     own = getattr(_b._thread, "stream", 0)
     if own and own != current:
@@ -276,3 +286,106 @@ def nuts_score_grad(x, weight, targets, lse, entropy=None, *, grad_logprob=None,
           (x, weight, targets, logits, _per_row(lse, "lse", n), _per_row(entropy, "entropy", n), _per_row(grad_logprob, "grad_logprob", n),
            _per_row(grad_lse, "grad_lse", n), _per_row(grad_entropy, "grad_entropy", n), grad_x, grad_weight), size)
     return grad_x, grad_weight
+
+
+def _factor(value, what, n, device):
+    """(number of all rows, tensor of each row's) of a penalty's strength."""
+    if isinstance(value, torch.Tensor) and value.dim() > 0:
+        return 1.0, _per_row(value, what, n)
+    return float(value), None
+
+
+def _places(t, what, n):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) != (n,):
+        raise ValueError(f"{what} must be an int32 vector of {n}")
+    return t if t.is_contiguous() else t.contiguous()
+
+
+def _history(t, n):
+    """(tensor, type, places in a row, from row to row) of the classes said before: [places] for all rows or [n, places]."""
+    if t is None:
+        return None, None, 0, 0
+    if t.dtype not in _ID_TYPES or t.dim() not in (1, 2) or (t.dim() == 2 and t.shape[0] not in (1, n)):
+        raise ValueError(f"history must be int32 or int64 [places] or [{n}, places]")
+    one = t.dim() == 1 or t.shape[0] <= 1
+    if (t.shape[-1] > 1 and t.stride(-1) != 1) or (not one and 0 < t.stride(0) < t.shape[-1]):  # (rows that overlap, too)
+        t = t.contiguous()
+    return t, _ID_TYPES[t.dtype], t.shape[-1], 0 if one else t.stride(0)
+
+
+def nuts_penalties(logits, history=None, *, lengths=None, prompts=None, repetition=1.0, frequency=0.0, presence=0.0, bias=None,
+                   bias_ids=None, bias_values=None, allowed=None, out=None):
+    """Logits of which classes that came in a row's history are penalised, to which biases are added, and in which classes that may not
+    come are -infinity.  history: [places] for all rows or [rows, places], of which the first lengths[row] are there, and the
+    first prompts[row] are not the model's own.  repetition, frequency, presence: numbers, or a float32 vector of each row's.
+    bias: float32 [classes] or [rows, classes]; bias_ids, bias_values: [rows, some], biases of single classes.  allowed: bits, as in
+    nuts_logprobs.  out: where to write, which may be `logits`."""
+    _matrix(logits, "logits")
+    n, classes = logits.shape
+    history, id_type, places, history_stride = _history(history, n)
+    if out is None:
+        out = logits.new_empty((n, classes))
+    elif out.dtype != logits.dtype:
+        raise ValueError(f"out must be {logits.dtype}")
+    _matrix(out, "out", shape=(n, classes))
+    n_bias = 0
+    if (bias_ids is None) != (bias_values is None):
+        raise ValueError("bias_ids and bias_values need each other")
+    if bias_ids is not None:
+        if bias_ids.dtype not in _ID_TYPES or bias_ids.dim() != 2 or bias_ids.shape[0] != n:
+            raise ValueError(f"bias_ids must be int32 or int64 [{n}, some]")
+        if bias_values.dtype != torch.float32 or bias_values.shape != bias_ids.shape:
+            raise ValueError(f"bias_values must be float32 {list(bias_ids.shape)}")
+        if id_type is None:
+            id_type = _ID_TYPES[bias_ids.dtype]
+        elif id_type != _ID_TYPES[bias_ids.dtype]:
+            bias_ids = bias_ids.to(history.dtype)
+        bias_ids, bias_values, n_bias = bias_ids.contiguous(), bias_values.contiguous(), bias_ids.shape[1]
+    bias_stride = 0
+    if bias is not None:
+        if bias.dtype != torch.float32 or tuple(bias.shape) not in ((classes,), (1, classes), (n, classes)) or (classes > 1 and bias.stride(-1) != 1):
+            raise ValueError(f"bias must be float32 [{classes}] or [{n}, {classes}] with unit stride along its rows")
+        if bias.dim() == 2 and bias.shape[0] > 1 and bias.stride(0):
+            bias_stride = bias.stride(0)
+    allowed, allowed_stride = _mask(allowed, n, classes)
+    r, rs = _factor(repetition, "repetition", n, logits.device)
+    f, fs = _factor(frequency, "frequency", n, logits.device)
+    q, qs = _factor(presence, "presence", n, logits.device)
+    desc, _ = _penalties_desc(False, (copysign(1.0, f), copysign(1.0, q)), _DTYPES[logits.dtype], _b.NUTS_I32 if id_type is None else id_type, n, classes,
+                              _stride(logits), _stride(out), allowed_stride, bias_stride, places, history_stride, n_bias, r, f, q)
+    _call(_b.lib().nuts_penalties, desc,
+          (logits, history, _places(lengths, "lengths", n), _places(prompts, "prompts", n), rs, fs, qs, bias, bias_ids, bias_values, allowed, out))
+    return out
+
+
+def nuts_penalties_grad(grad, logits, history=None, *, lengths=None, repetition=1.0, allowed=None, out=None, want_logits=True, want_bias=False):
+    """(gradient with respect to the logits, gradient with respect to a bias [classes] that all rows share), from `grad`, that with
+    respect to what nuts_penalties gave for `logits`; None for one that is not wanted.  out: where to write the first, which may be `grad`.
+    (With respect to a bias of each row it is `grad` where classes are allowed.)"""
+    _matrix(logits, "logits")
+    n, classes = logits.shape
+    if grad.dtype != logits.dtype:
+        raise ValueError(f"grad must be {logits.dtype}")
+    _matrix(grad, "grad", shape=(n, classes))
+    history, id_type, places, history_stride = _history(history, n)
+    if not want_logits:
+        if out is not None:
+            raise ValueError("out is for the gradient with respect to the logits")
+    elif out is None:
+        out = logits.new_empty((n, classes))
+    elif out.dtype != logits.dtype:
+        raise ValueError(f"out must be {logits.dtype}")
+    if out is not None:
+        _matrix(out, "out", shape=(n, classes))
+    grad_bias = torch.empty(classes, dtype=torch.float32, device=logits.device) if want_bias else None
+    allowed, allowed_stride = _mask(allowed, n, classes)
+    r, rs = _factor(repetition, "repetition", n, logits.device)
+    desc, size = _penalties_desc(want_bias, (1.0, 1.0), _DTYPES[logits.dtype], _b.NUTS_I32 if id_type is None else id_type, n, classes, _stride(logits),
+                                 _stride(out) if out is not None else classes, allowed_stride, 0, places, history_stride, 0, r, 0.0, 0.0)
+    lengths = _places(lengths, "lengths", n)
+    L = _b.lib()
+    _call(lambda desc, g, *rest: L.nuts_penalties_grad(desc, g, _stride(grad), *rest), desc,
+          (grad, logits, history, lengths, rs, allowed, out, grad_bias), size)
+    return out, grad_bias

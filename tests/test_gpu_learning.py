@@ -1,0 +1,355 @@
+"""The norm of many tensors and AdamW steps over them, with moments of 32 and of 8 bits, against 64 bits."""
+import math
+
+import pytest
+import torch
+
+import learning_ref as L
+import paper_1910_11141_amd as nuts
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+U = L.U
+
+
+def gen(seed=1):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def tensor(n, dtype, g, std=1.0, offset=0):
+    """1-d, `offset` numbers behind the beginning of an allocation."""
+    return (torch.randn(n + offset, generator=g, device="cuda") * std).to(dtype)[offset:]
+
+
+# ---- norm ---------------------------------------------------------------------------------------------------------------
+
+def check_norm(tensors, max_norm=1.0):
+    want = math.sqrt(sum(float(t.double().square().sum()) for t in tensors))
+    got = nuts.nuts_norm(tensors, max_norm=max_norm)
+    assert got.norm.shape == () and got.norm.dtype == F32 and got.factor.dtype == F32
+    # sums in 64 bits: off by their own rounding to 32 bits, and a little
+    assert abs(float(got.norm) - want) <= 1.001 * U * want
+    factor = min(1.0, max_norm / want) if want > 0 else 1.0
+    assert abs(float(got.factor) - factor) <= 1.001 * U * factor
+    return got
+
+
+@pytest.mark.parametrize("sizes", [[1], [0, 3, 0], [7, 8, 9], [8000, 8000], [8191, 8192, 8193], [100000, 1, 40000], [33] * 119, [5] * 120, [1000] * 121, [17] * 300,
+                                   [3_000_001], [20_000_000, 5]])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_norm(sizes, dtype):
+    g = gen(len(sizes))
+    check_norm([tensor(n, dtype, g, offset=i % 3) for i, n in enumerate(sizes)], max_norm=3.5)
+
+
+def test_norm_of_several_types_shapes_and_orders():
+    g = gen(2)
+    check_norm([tensor(300, F32, g).view(3, 100), tensor(5000, BF16, g).view(50, 100).t(), tensor(77, F16, g), tensor(1, F32, g).view(())], 1e6)
+
+
+def test_norm_of_what_32_bits_could_not_square():
+    for x in (1e30, 1e-30, 3e38, 1e-44):
+        t = torch.full((1000,), x, device="cuda")
+        got = nuts.nuts_norm([t], max_norm=1.0)
+        want = float(t[0].double()) * math.sqrt(1000.0)
+        if want > torch.finfo(F32).max:
+            assert float(got.norm) == math.inf
+        else:
+            assert abs(float(got.norm) - want) <= 1.001 * U * want + 2.0 ** -150
+        assert abs(float(got.factor) - min(1.0, 1.0 / want)) <= 1.001 * U + 2.0 ** -150
+
+
+@pytest.mark.parametrize("x", [math.nan, math.inf, -math.inf])
+def test_norm_of_what_is_not_finite(x):
+    t = tensor(30000, BF16, gen(3))
+    t[20001] = x
+    got = nuts.nuts_norm([tensor(10, F32, gen(4)), t])
+    assert not math.isfinite(float(got.norm)) and math.isnan(float(got.factor))
+
+
+def test_norm_of_nothing():
+    got = nuts.nuts_norm([torch.zeros(0, device="cuda"), torch.zeros(5, device="cuda")])
+    assert float(got.norm) == 0.0 and float(got.factor) == 1.0
+
+
+def test_norm_of_more_numbers_than_32_bits_count():
+    t = torch.zeros((1 << 32) + 5, dtype=BF16, device="cuda")
+    t[-1], t[1 << 31], t[(1 << 32) - 1] = 3.0, 4.0, 12.0
+    assert float(nuts.nuts_norm([t]).norm) == 13.0
+
+
+# ---- AdamW --------------------------------------------------------------------------------------------------------------
+
+class Step:
+    """A model's tensors before a step, and what the step has to make of them."""
+
+    def __init__(self, sizes, params, grads, bits, seed=1, copies=None, offset=0, std=None):
+        g = gen(seed)
+        self.bits = bits
+        self.params = [tensor(n, params, g, 0.05, offset) for n in sizes]
+        self.grads = [tensor(n, grads, g, (std or 1e-3) * 10.0 ** (i % 3), offset) for i, n in enumerate(sizes)]
+        copies = [tensor(n, copies, g) if i % 2 == 0 else None for i, n in enumerate(sizes)] if copies else None
+        if bits == 32:
+            states = [[tensor(n, F32, g, 1e-3, offset) for n in sizes], [tensor(n, F32, g, 2e-3, offset).square_() for n in sizes]]
+        else:
+            codes = lambda n, low, high, kind: torch.randint(low, high, (n + offset,), generator=g, device="cuda").to(kind)[offset:]  # noqa: E731
+            scale = lambda n, size: torch.rand(-(-n // 256), generator=g, device="cuda") * size + size  # noqa: E731
+            states = [[codes(n, -127, 128, torch.int8) for n in sizes], [codes(n, 0, 255, torch.uint8) for n in sizes],
+                      [scale(n, 1e-3 / 127 ** 2) for n in sizes], [scale(n, 2e-3 / 254 ** 2) for n in sizes]]
+        self.moments = nuts.Moments(self.params, bits=bits, copies=copies, states=states)
+
+    def values(self, i):
+        mo = self.moments
+        if self.bits == 32:
+            return mo.m[i].double().view(-1), mo.v[i].double().view(-1)
+        return L.m_values(mo.m[i].view(-1), mo.m_scales[i]), L.v_values(mo.v[i].view(-1), mo.v_scales[i])
+
+    def check(self, seed=0, step=7, lr=1e-3, factor=None, call=None, **kw):
+        mo = self.moments
+        before = [(p.clone().view(-1), *self.values(i)) for i, p in enumerate(self.params)]
+        keywords = dict(step=step, lr=lr, seed=seed, factor=torch.tensor(factor, device="cuda") if factor is not None else None, **kw)
+        (call or nuts.nuts_adamw)(mo, self.grads, **keywords)
+        for i, (p, g) in enumerate(zip(self.params, self.grads)):
+            n = p.numel()
+            if g is None or n == 0:
+                assert torch.equal(p.view(-1), before[i][0])
+                continue
+            # (the kernels have lr as 64 bits or, on the device, 32: within the bounds)
+            old, m, v = before[i]
+            f = float(torch.tensor(factor, dtype=F32)) if factor is not None else 1.0
+            new_p, p_bound, new_m, m_bound, new_v, v_bound = L.adamw(old, g.view(-1), m, v, step=step, lr=lr, factor=f, **kw)
+            w = L.words(n, seed, step, i, "cuda") if self.bits == 8 or p.dtype == BF16 else None
+            got = p.view(-1).double()
+            if p.dtype == F32:
+                assert L.close(got, new_p, p_bound), i
+            else:
+                assert bool(((got >= L.rounded_at_random(new_p - p_bound, w)) & (got <= L.rounded_at_random(new_p + p_bound, w))).all()), i
+            copy = mo.copies[i]
+            if copy is not None:
+                assert torch.equal(copy.view(-1), p.view(-1).float().to(copy.dtype))
+            if self.bits == 32:
+                assert L.close(mo.m[i].view(-1), new_m, m_bound) and L.close(mo.v[i].view(-1), new_v, v_bound), i
+                continue
+            # of each block: its scale; of each number: a code that belongs to what it may have been before
+            u = ((w & 1023) + 0.5) / 1024
+            top, top_bound = L.block_max(new_m), L.block_max(m_bound)
+            assert L.close(mo.m_scales[i], top / 127 ** 2, (top_bound + 3 * U * top) / 127 ** 2 + 2.0 ** -149), i
+            scale = mo.m_scales[i].double().repeat_interleave(256)[:n].clamp(min=1e-300)
+            x, off = new_m.abs() / scale, m_bound / scale
+            off = off + 16 * U * (x + 1)  # the quotient, its root's whole part, the difference from its square, the product with chance
+            code = mo.m[i].view(-1).double()
+            assert bool(((code.abs() >= L.m_codes((x - off).clamp(min=0).sqrt(), u)) & (code.abs() <= L.m_codes((x + off).sqrt(), u))).all()), i
+            assert bool(((code == 0) | (torch.sign(code) == torch.sign(new_m)) | (new_m.abs() <= m_bound)).all()), i
+            u = ((w >> 10 & 1023) + 0.5) / 1024
+            root, root_bound = new_v.sqrt(), torch.where(new_v > 0, v_bound / new_v.clamp(min=1e-300).sqrt(), v_bound.sqrt()) + U * new_v.sqrt()
+            top, top_bound = L.block_max(root), L.block_max(root_bound)
+            assert L.close(mo.v_scales[i], top / 254 ** 2, (top_bound + 3 * U * top) / 254 ** 2 + 2.0 ** -149), i
+            scale = mo.v_scales[i].double().repeat_interleave(256)[:n].clamp(min=1e-300)
+            x, off = root / scale, root_bound / scale
+            off = off + 32 * U * (x + 1)
+            code = mo.v[i].view(-1).double()
+            low, high = (x - off).clamp(min=0), x + off
+            low = torch.where(new_v > 2.0 ** -120, torch.maximum(low, torch.full_like(low, 1e-30)), low)
+            high = torch.where((new_v == 0) & (v_bound <= 2.0 ** -130), 0.0, high)
+            assert bool(((code >= L.v_codes(low.sqrt(), u)) & (code <= L.v_codes(high.sqrt(), u))).all()), i
+
+
+SIZES = [[1], [2, 3], [255, 256, 257], [8191, 8192, 8193, 4], [100003], [31] * 47, [260] * 48, [77] * 49 + [9000], [5, 0, 300, 0]]
+
+
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: f"{len(s)}x{s[0]}")
+@pytest.mark.parametrize("params,grads", [(F32, F32), (F32, BF16), (F32, F16), (BF16, BF16), (BF16, F32), (BF16, F16)])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_step(sizes, params, grads, bits):
+    s = Step(sizes, params, grads, bits, seed=len(sizes), copies=None if params == BF16 else BF16 if grads != F16 else F16, offset=len(sizes) % 4)
+    s.check()
+    s.check(step=8, seed=12345678901234567, factor=0.3, scale=-2.0)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_first_step_and_edges_of_what_is_set(bits):
+    g = gen(5)
+    params = [tensor(n, F32, g).view(-1, 1) for n in (300, 1000)]
+    s = Step([1], F32, F32, bits)
+    s.params, s.grads, s.moments = params, [tensor(n, F32, g).view(-1, 1) for n in (300, 1000)], nuts.Moments(params, bits=bits)
+    assert all(bool((t == 0).all()) for t in (*s.moments.m, *s.moments.v))
+    s.check(step=1)
+    s.check(step=2, betas=(0.0, 0.0), eps=0.1)
+    s.check(step=1_000_000, betas=(0.95, 0.99), eps=1e-3, weight_decay=0.0)
+    s.check(step=3, lr=0.0, weight_decay=1.0)
+    s.check(step=3, lr=-0.1, weight_decay=0.5)
+
+
+@pytest.mark.parametrize("params,bits", [(F32, 32), (F32, 8), (BF16, 32), (BF16, 8)])
+def test_gradients_of_zero(params, bits):
+    """Moments of zero stay zero, and the parameters where they are."""
+    p = tensor(1000, params, gen(6))
+    before = p.clone()
+    mo = nuts.Moments([p], bits=bits)
+    for step in (1, 2):
+        nuts.nuts_adamw(mo, [torch.zeros_like(p)], step=step, lr=0.1, weight_decay=0.0)
+    assert torch.equal(p, before) and bool((mo.m[0] == 0).all()) and bool((mo.v[0] == 0).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_parameters_without_gradients_and_steps_that_do_not_happen(bits):
+    s = Step([500, 300, 8200, 40], F32, BF16, bits, copies=BF16)
+    s.grads[1] = s.grads[3] = None
+    kept = [t.clone() for i in (1, 3) for t in (s.moments.m[i], s.moments.v[i])]
+    s.check()
+    assert all(torch.equal(a, b) for a, b in zip(kept, [t for i in (1, 3) for t in (s.moments.m[i], s.moments.v[i])]))
+    before = [t.clone() for t in s.moments._tensors]
+    nuts.nuts_adamw(s.moments, s.grads, step=9, lr=0.1, factor=torch.tensor(math.nan, device="cuda"))
+    nuts.nuts_adamw(s.moments, [None] * 4, step=9, lr=0.1)
+    assert all(torch.equal(a, b) for a, b in zip(before, s.moments._tensors))
+
+
+@pytest.mark.parametrize("params", [F32, BF16])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gradients_that_are_not_finite_stay_among_themselves(params, bits):
+    s, clean = (Step([700], params, F32, bits) for _ in range(2))
+    for i, x in enumerate((math.nan, math.inf, -math.inf)):
+        s.grads[0][100 * i] = x
+        clean.grads[0][100 * i] = 0.0
+        for each in (s, clean):  # (so that none of these places is its block's largest)
+            each.moments.m[0][100 * i] = 0
+            each.moments.v[0][100 * i] = 0
+    for step in (7, 8):
+        for each in (s, clean):
+            nuts.nuts_adamw(each.moments, each.grads, step=step, lr=1e-3)
+        others = torch.ones(700, dtype=torch.bool, device="cuda")
+        others[:300:100] = False
+        assert bool(s.params[0][others].isfinite().all()) and bool(s.params[0][~others].isnan().all())
+        if bits == 8:
+            assert bool((s.moments.m[0][~others] == -128).all()) and bool((s.moments.v[0][~others] == 255).all())
+            m, v = nuts.nuts_adamw_values(s.moments)
+            assert bool(m[0][~others].isnan().all()) and bool(v[0][~others].isnan().all()) and bool(m[0][others].isfinite().all())
+        assert torch.equal(s.params[0][others], clean.params[0][others])
+
+
+def test_step_and_rate_on_the_device():
+    for params, bits in ((F32, 32), (BF16, 8)):
+        s = Step([900, 17], params, BF16, bits)
+        at, lr = torch.tensor([7], device="cuda"), torch.tensor(1e-3, device="cuda")
+        s.check(call=lambda mo, g, **kw: nuts.nuts_adamw(mo, g, **(kw | {"step": at, "lr": lr})))
+        s.check(call=lambda mo, g, **kw: nuts.nuts_adamw(mo, g, **(kw | {"step": at})))
+        s.check(call=lambda mo, g, **kw: nuts.nuts_adamw(mo, g, **(kw | {"lr": lr})))
+
+
+def test_values():
+    s = Step([700, 1, 256, 8193], F32, F32, 8)
+    for dtype in (F32, BF16, F16):
+        m, v = nuts.nuts_adamw_values(s.moments, dtype=dtype)
+        for i in range(4):
+            want_m, want_v = s.values(i)
+            assert m[i].dtype == dtype and m[i].shape == s.params[i].shape
+            assert L.close(m[i].view(-1), want_m, L.rounded_bound(want_m, U * want_m.abs(), dtype))
+            assert L.close(v[i].view(-1), want_v, L.rounded_bound(want_v, 3.1 * U * want_v.abs(), dtype))
+    out = ([torch.zeros(700, device="cuda"), None, None, None], [None, None, torch.zeros(256, device="cuda"), None])
+    got = nuts.nuts_adamw_values(s.moments, out=out)
+    assert got[0][0] is out[0][0] and torch.equal(out[0][0], nuts.nuts_adamw_values(s.moments)[0][0])
+    assert torch.equal(out[1][2], nuts.nuts_adamw_values(s.moments)[1][2])
+
+
+def test_rounding_at_random_keeps_the_mean():
+    """One step of equal numbers in many places: the mean of what they become is what they are, within six deviations of it.  A value between codes a
+    and b has a variance of (b - a)^2 / 4 at most."""
+    n = 1 << 18
+    grad = torch.full((n,), 0.3, device="cuda")
+    grad[::256] = 1.0   # each block's largest
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[::256] = False
+    k = int(rest.sum())
+    p = torch.full((n,), 1.0 + 2.0 ** -9, dtype=BF16, device="cuda")   # (1: to the nearest)
+    mo = nuts.Moments([p], bits=8)
+    nuts.nuts_adamw(mo, [grad], step=1, lr=1e-3, weight_decay=0.0, seed=99)
+    m, v = nuts.nuts_adamw_values(mo)
+    for got, want, gap in ((m[0], 0.1 * 0.3, 2 * 127 * 0.1 / 127 ** 2), (v[0], 0.001 * 0.09, 4 * 254 ** 3 * 0.001 / 254 ** 4)):
+        # (chance has 1024 steps: the mean may be off by half of one of a gap, too)
+        assert abs(float(got[rest].double().mean()) - want) <= 6 * gap / 2 / math.sqrt(k) + gap / 2048 + 1e-5 * want
+        assert got[rest].unique().numel() == 2
+    assert abs(float(p[rest].double().mean()) - (1.0 - 1e-3)) <= 6 * 2.0 ** -8 / 2 / math.sqrt(k) + 2.0 ** -8 / 8192 + 1e-6
+
+
+def test_moments_of_8_bits_follow_those_of_32():
+    """After 300 steps with random gradients of falling size, v is near what 32 bits give, neither stuck nor running away.  Codes of v from a
+    hundredth of the largest on (c >= 80) are at most d = 4 / c = 5 % apart; rounding each step adds d^2 / 6 to the relative variance, of which 1 / (1 - 0.99^2) = 50 steps
+    last: a deviation of 0.15 each, and of 0.001 of the mean over 60000 numbers.  m: codes at the deviation of what is there (c near 76, the largest of 256
+    is 2.8 deviations) are 2.6 % apart, 0.026 / sqrt(6) a step, of which 1 / (1 - 0.9^2) = 5 last: 0.025."""
+    g = gen(8)
+    p8, p32 = torch.zeros(1 << 16, device="cuda"), torch.zeros(1 << 16, device="cuda")
+    m8, m32 = nuts.Moments([p8], bits=8), nuts.Moments([p32])
+    for step in range(1, 301):
+        grad = torch.randn(1 << 16, generator=g, device="cuda") * (1.0 if step < 100 else 0.1)
+        for mo in (m8, m32):
+            nuts.nuts_adamw(mo, [grad], step=step, lr=1e-4, betas=(0.9, 0.99), weight_decay=0.0, seed=4)
+    m, v = nuts.nuts_adamw_values(m8)
+    big = m32.v[0] > m32.v[0].max() / 100
+    assert int(big.sum()) > 60000
+    ratio = v[0][big].double().mean() / m32.v[0][big].double().mean()
+    assert 0.9 < float(ratio) < 1.1
+    off = (m[0] - m32.m[0]).double().norm() / m32.m[0].double().norm()
+    assert float(off) < 0.1   # (codes of m are at most 2 / c = 13 % apart where m is a fiftieth of the largest)
+
+
+def test_many_numbers():
+    n = (1 << 31) + 1000
+    p = torch.ones(n, dtype=BF16, device="cuda")
+    grad = torch.zeros(n, dtype=BF16, device="cuda")
+    mo = nuts.Moments([p], bits=8)
+    grad[-1] = grad[5] = 1.0
+    nuts.nuts_adamw(mo, [grad], step=1, lr=0.5, weight_decay=0.0)
+    assert float(p[-1]) == float(p[5]) == 0.5 and int(mo.m[0][-1]) == 127 and int(mo.v[0][-1]) == 254
+    assert int((p != 1).sum()) == 2
+
+
+def test_other_streams_graphs_and_parameters_that_move():
+    s = Step([5000, 8193], F32, BF16, 8, copies=BF16)
+    twin = Step([5000, 8193], F32, BF16, 8, copies=BF16)
+    at, lr = torch.tensor([1], device="cuda"), torch.tensor(1e-2, device="cuda")
+
+    def go(each, step, rate):
+        got = nuts.nuts_norm(each.grads, max_norm=0.5)
+        nuts.nuts_adamw(each.moments, each.grads, step=step, lr=rate, factor=got.factor, seed=3)
+
+    go(Step([300], F32, BF16, 8, copies=BF16), at, lr)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        at.add_(1)
+        go(s, at, lr)
+    for k in range(5):
+        for g_, h in zip(s.grads, twin.grads):
+            g_.copy_(tensor(g_.numel(), BF16, gen(k)))
+            h.copy_(g_)
+        go(twin, 2 + k, float(torch.tensor(1e-2)))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(s.params, twin.params):
+            # (the size of a step from lr of 32 bits, made on the device: off by a unit or two in its last place)
+            assert float((a - b).abs().max()) <= 1e-6
+    states = [t.clone() for t in s.moments._tensors]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        nuts.nuts_adamw(s.moments, s.grads, step=9, lr=0.1)
+    torch.cuda.current_stream().wait_stream(side)
+    once = [t.clone() for t in s.moments._tensors]
+    for t, old in zip(s.moments._tensors, states):
+        t.copy_(old)
+    nuts.nuts_set_stream(side)
+    try:
+        nuts.nuts_adamw(s.moments, s.grads, step=9, lr=0.1)
+    finally:
+        nuts.nuts_set_stream(None)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(once, s.moments._tensors))
+    # a parameter in another place
+    old = s.params[0]
+    kept = old.clone()
+    leaf = torch.nn.Parameter(kept.clone())
+    mo = nuts.Moments([leaf])
+    leaf.data = kept.clone()
+    nuts.nuts_adamw(mo, [torch.ones_like(kept)], step=1, lr=0.5, weight_decay=0.0)
+    assert float((leaf.detach() - (kept - 0.5)).abs().max()) <= 1e-6
