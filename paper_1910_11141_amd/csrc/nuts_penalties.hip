@@ -5,12 +5,13 @@
 #include "nuts_cat.h"
 
 #include <algorithm>
+#include <climits>
 
 namespace nuts {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kSlice = 8192;        // classes of a workgroup, with a counter each in LDS
+constexpr int kSlice = 4096;        // classes of a workgroup, with a counter each in LDS
 constexpr int kColumns = 64;        // of a workgroup that joins the biases' gradients
 constexpr int kJoinThreads = 1024;
 constexpr int kGroups = 1024;       // workgroups that the rows are divided between where they are added up
@@ -48,124 +49,302 @@ __device__ __forceinline__ int clamped(const int32_t* lengths, long row, int mos
     return lengths ? min(max(lengths[row], 0), most) : otherwise;
 }
 
-// Counters of the classes begin .. begin + kSlice - 1 from the places from .. to - 1 of a history.
-__device__ __forceinline__ void count_history(const PenaltyArgs& a, long row, int begin, int n, int from, int to, int prompt, unsigned* count)
-{
-    const long at = row * a.history_stride;
-    for (int i = from + (int)threadIdx.x; i < to; i += kThreads) {
-        const long v = id_at(a.history, a.id_type, at + i) - begin;
-        if (v < 0 || v >= n) continue;
-        if (i >= prompt) atomicAdd(&count[v], 1u);
-        else atomicOr(&count[v], kPrompt);
-    }
-}
+// What a workgroup's counters hold: the places 0 .. length - 1 of a row's history, the first `prompt` as prompt.
+struct Counted {
+    int length, prompt;
+};
 
 __device__ __forceinline__ bool may_come(const uint32_t* allowed, int v) { return !allowed || (allowed[v >> 5] >> (v & 31) & 1); }
 
-struct RowFactors {
-    float r, f, q;
-};
-__device__ __forceinline__ float penalised(float x, unsigned count, const RowFactors& p)
+// Calls `see` for the places from .. to - 1 of a history that hold one of the classes begin .. begin + n - 1, thread by thread.
+template <typename Id, typename See>
+__device__ __forceinline__ void look_through(const Id* history, int from, int to, int begin, int n, See see)
 {
-    if (!(count & kSeen)) return x;
-    float z = x > 0.f ? x / p.r : x * p.r;
-    const unsigned said = count & kCount;
-    if (said) z -= p.f * (float)said + p.q;
-    return z;
+    constexpr int kEach = 4, kN = 16 / sizeof(Id);
+    for (int i = from + (int)threadIdx.x * kEach; i < to; i += kThreads * kEach) {
+        Id id[kEach];
+        if (i + kEach <= to) {
+#pragma unroll
+            for (int u = 0; u < kEach; u += kN) {
+                const Pack<Id, kN> in = load_pack<Id, kN>(history + i + u);
+#pragma unroll
+                for (int e = 0; e < kN; ++e) id[u + e] = in.v[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) id[e] = i + e < to ? history[i + e] : (Id)-1;
+        }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const uint64_t v = (uint64_t)(int64_t)id[e] - (uint64_t)begin;
+            if (v < (uint64_t)n && i + e < to) see(i + e, (int)v);
+        }
+    }
+}
+template <typename See>
+__device__ __forceinline__ void look_through(const PenaltyArgs& a, long row, int from, int to, int begin, int n, See see)
+{
+    if (a.id_type == NUTS_I64) look_through(static_cast<const int64_t*>(a.history) + row * a.history_stride, from, to, begin, n, see);
+    else look_through(static_cast<const int32_t*>(a.history) + row * a.history_stride, from, to, begin, n, see);
 }
 
-// A workgroup a slice of a row.  The history's counts are made in LDS, where adding whole numbers in any order gives the same.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void penalties_kernel(PenaltyArgs a)
+// Counters for the next row of a workgroup.  Where all rows have one history and the row has seen no less of it than the one before, they
+// are carried on: 4096 rows of one text of 4096 classes are counted once by each workgroup, not once by each row.  No
+// thread may still be reading them; the caller waits before they are read.
+__device__ __forceinline__ void count_on(const PenaltyArgs& a, long row, int begin, int n, Counted& done, const Counted& now, unsigned* count)
 {
+    if (a.history_stride != 0 || now.length < done.length || now.prompt < done.prompt) {
+        for (int i = (int)threadIdx.x * 4; i < n; i += kThreads * 4) *reinterpret_cast<uint4*>(&count[i]) = uint4{0, 0, 0, 0};  // (kSlice is a multiple of 4)
+        done = Counted{0, 0};
+        __syncthreads();
+    }
+    if (now.prompt > done.prompt && done.prompt < done.length)
+        look_through(a, row, done.prompt, min(now.prompt, done.length), begin, n, [&](int, int v) {
+            atomicSub(&count[v], 1u);
+            atomicOr(&count[v], kPrompt);
+        });
+    look_through(a, row, done.length, now.length, begin, n, [&](int i, int v) {
+        if (i >= now.prompt) atomicAdd(&count[v], 1u);
+        else atomicOr(&count[v], kPrompt);
+    });
+    done = now;
+}
+
+struct RowFactors {
+    float r, by_r, f, q;
+};
+// Without branches: of 64 lanes one has a class that was seen nearly always.  (A product with 1 / r is a unit in the last place off x / r at most,
+// and a quotient ten instructions more.)
+__device__ __forceinline__ float penalised(float x, unsigned count, const RowFactors& p)
+{
+    const float z = x * (count & kSeen ? (x > 0.f ? p.by_r : p.r) : 1.f);
+    const unsigned said = count & kCount;
+    return z - (said ? __builtin_fmaf(p.f, (float)said, p.q) : 0.f);
+}
+
+// The packs of a thread in a slice: pack u begins at class (u kThreads + thread) kN.
+template <typename T>
+constexpr int kPackN = 16 / sizeof(T);
+template <typename T>
+constexpr int kPacks = kSlice / kThreads / kPackN<T>;
+
+template <typename T>
+struct Slice {
+    Pack<T, kPackN<T>> pack[kPacks<T>];
+    // whole packs only: what is behind them is read one by one
+    __device__ __forceinline__ void fetch(const T* row, int n)
+    {
+#pragma unroll
+        for (int u = 0; u < kPacks<T>; ++u) {
+            const int v = (u * kThreads + (int)threadIdx.x) * kPackN<T>;
+            if (v + kPackN<T> <= n) pack[u] = load_pack<T, kPackN<T>>(row + v);
+        }
+    }
+};
+template <typename T>
+__device__ __forceinline__ void unpack(const Pack<T, kPackN<T>>& in, const T* row, int v, int n, float (&x)[kPackN<T>])
+{
+#pragma unroll
+    for (int e = 0; e < kPackN<T>; ++e) x[e] = v + kPackN<T> <= n ? to_float(in.v[e]) : v + e < n ? to_float(row[v + e]) : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void write_pack(T* to, const float (&x)[kPackN<T>], int v, int n, bool streamed)
+{
+    Pack<T, kPackN<T>> out;
+#pragma unroll
+    for (int e = 0; e < kPackN<T>; ++e) out.v[e] = rounded<T>(x[e]);
+    if (v + kPackN<T> <= n) {
+        streamed ? stream_pack(to + v, out) : store_pack(to + v, out);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kPackN<T>; ++e)
+            if (v + e < n) to[v + e] = out.v[e];
+    }
+}
+// The counters of a pack, and all of them together.
+template <int kN>
+__device__ __forceinline__ unsigned read_counts(const unsigned* count, unsigned (&c)[kN])
+{
+    unsigned any = 0;
+#pragma unroll
+    for (int e = 0; e < kN; e += 4) {
+        const uint4 in = *reinterpret_cast<const uint4*>(&count[e]);
+        c[e] = in.x, c[e + 1] = in.y, c[e + 2] = in.z, c[e + 3] = in.w;
+        any |= in.x | in.y | in.z | in.w;
+    }
+    return any;
+}
+// A bit for each class of a pack that may come.
+template <int kN>
+__device__ __forceinline__ unsigned allowed_of(const uint32_t* allowed, int v, int n)
+{
+    constexpr unsigned kAll = (1u << kN) - 1;
+    return allowed && v < n ? reinterpret_cast<const unsigned char*>(allowed)[v >> 3] >> (v & 7) & kAll : kAll;
+}
+
+// A workgroup a slice of `rows_each` rows.  The history's counts are made in LDS, where adding whole numbers in any order gives the same.
+template <typename T>
+__global__ __launch_bounds__(kThreads, 8) void penalties_kernel(PenaltyArgs a)
+{
+    constexpr int kN = kPackN<T>;
     __shared__ __attribute__((aligned(16))) unsigned count[kSlice];
     __shared__ int biased[NUTS_CAT_MAX_BIAS];
-    const long block = a.first_block + blockIdx.x, row = block / a.slices;
+    const long block = a.first_block + blockIdx.x, group = block / a.slices;
     const int begin = (int)(block % a.slices) * kSlice, n = min(kSlice, a.n_classes - begin);
-    const T* x_row = static_cast<const T*>(a.logits) + row * a.row_stride + begin;
-    T* to = static_cast<T*>(a.out) + row * a.out_stride + begin;
-    const float* bias = a.bias ? a.bias + row * a.bias_stride + begin : nullptr;
-    const uint32_t* allowed = a.allowed ? a.allowed + row * a.allowed_stride + begin / 32 : nullptr;
-    const bool in_place = a.logits == a.out;
-    const RowFactors p{a.repetition ? a.repetition[row] : a.r, a.frequency ? a.frequency[row] : a.f, a.presence ? a.presence[row] : a.q};
-    for (int i = threadIdx.x; i < kSlice; i += kThreads) count[i] = 0;
-    for (int i = threadIdx.x; i < a.n_bias; i += kThreads) {
-        const long v = id_at(a.bias_ids, a.id_type, row * a.n_bias + i) - begin;
-        biased[i] = v >= 0 && v < n ? (int)v : -1;
-    }
-    __syncthreads();
-    const int length = clamped(a.lengths, row, a.history_len, a.history_len), prompt = clamped(a.prompts, row, a.history_len, 0);
-    count_history(a, row, begin, n, 0, length, prompt, count);
-    for (int i = threadIdx.x; i < a.n_bias; i += kThreads)
-        if (biased[i] >= 0) atomicOr(&count[biased[i]], kBiased);
-    __syncthreads();
-    // classes with biases of their own: by the thread that has the first of them
-    for (int i = threadIdx.x; i < a.n_bias; i += kThreads) {
-        const int v = biased[i];
-        if (v < 0) continue;
-        bool first = true;
-        for (int k = 0; k < i; ++k) first &= biased[k] != v;
-        if (!first) continue;
-        float sum = a.bias_values[row * a.n_bias + i];
-        for (int k = i + 1; k < a.n_bias; ++k)
-            if (biased[k] == v) sum += a.bias_values[row * a.n_bias + k];
-        float z = penalised(to_float(x_row[v]), count[v], p);
-        if (bias) z += bias[v];
-        z += sum;
-        to[v] = rounded<T>(may_come(allowed, v) ? z : -INFINITY);
-    }
-    for (int v = threadIdx.x; v < n; v += kThreads) {
-        const unsigned c = count[v];
-        if (c & kBiased) continue;
-        const bool may = may_come(allowed, v);
-        if (in_place && may && !c && !bias) continue;
-        float z = -INFINITY;
-        if (may) {
-            z = penalised(to_float(x_row[v]), c, p);
-            if (bias) z += bias[v];
+    const bool sparse = a.logits == a.out && !a.bias;  // what nothing changes is left alone
+    const bool counting = a.history_len > 0 || a.n_bias > 0;
+    Counted done{INT_MAX, INT_MAX};  // (nothing yet: the first row begins anew)
+    const long end = min((group + 1) * a.rows_each, a.n_rows);
+    const T* x_row = static_cast<const T*>(a.logits) + group * a.rows_each * a.row_stride + begin;
+    for (long row = group * a.rows_each; row < end; ++row, x_row += a.row_stride) {
+        T* to = static_cast<T*>(a.out) + row * a.out_stride + begin;
+        const float* bias = a.bias ? a.bias + row * a.bias_stride + begin : nullptr;
+        const uint32_t* allowed = a.allowed ? a.allowed + row * a.allowed_stride + begin / 32 : nullptr;
+        const float r = a.repetition ? a.repetition[row] : a.r;
+        const RowFactors p{r, 1.f / r, a.frequency ? a.frequency[row] : a.f, a.presence ? a.presence[row] : a.q};
+        Slice<T> own;  // on its way while the history is counted
+        if (!sparse) own.fetch(x_row, n);
+        if (counting) {
+            for (int i = threadIdx.x; i < a.n_bias; i += kThreads) {
+                const long v = id_at(a.bias_ids, a.id_type, row * a.n_bias + i) - begin;
+                biased[i] = v >= 0 && v < n ? (int)v : -1;
+            }
+            count_on(a, row, begin, n, done, Counted{clamped(a.lengths, row, a.history_len, a.history_len), clamped(a.prompts, row, a.history_len, 0)}, count);
+            for (int i = threadIdx.x; i < a.n_bias; i += kThreads)
+                if (biased[i] >= 0) atomicOr(&count[biased[i]], kBiased);
+            __syncthreads();
         }
-        to[v] = rounded<T>(z);
+        // classes with biases of their own: by the thread that has the first of them
+        for (int i = threadIdx.x; i < a.n_bias; i += kThreads) {
+            const int v = biased[i];
+            if (v < 0) continue;
+            bool first = true;
+            for (int k = 0; k < i; ++k) first &= biased[k] != v;
+            if (!first) continue;
+            float sum = a.bias_values[row * a.n_bias + i];
+            for (int k = i + 1; k < a.n_bias; ++k)
+                if (biased[k] == v) sum += a.bias_values[row * a.n_bias + k];
+            float z = penalised(to_float(x_row[v]), count[v], p);
+            if (bias) z += bias[v];
+            z += sum;
+            to[v] = rounded<T>(may_come(allowed, v) ? z : -INFINITY);
+        }
+#pragma unroll
+        for (int u = 0; u < kPacks<T>; ++u) {
+            const int v = (u * kThreads + (int)threadIdx.x) * kN;
+            if (v >= n) break;
+            unsigned c[kN] = {};
+            const unsigned any = counting ? read_counts<kN>(&count[v], c) : 0;
+            const unsigned may = allowed_of<kN>(allowed, v, n);
+            if (sparse) {
+                if (!any && may == (1u << kN) - 1) continue;
+                if (v + kN <= n) own.pack[u] = load_pack<T, kN>(x_row + v);
+            }
+            float x[kN];
+            unpack(own.pack[u], x_row, v, n, x);
+            if (any) {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) x[e] = penalised(x[e], c[e], p);
+            }
+            if (bias) {
+#pragma unroll
+                for (int e = 0; e < kN; e += 4) {
+                    if (v + kN <= n) {
+                        const Pack<float, 4> b = load_pack<float, 4>(bias + v + e);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[e + k] += b.v[k];
+                    } else {
+#pragma unroll
+                        for (int k = e; k < e + 4; ++k)
+                            if (v + k < n) x[k] += bias[v + k];
+                    }
+                }
+            }
+            if (allowed) {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) x[e] = may >> e & 1 ? x[e] : -INFINITY;
+            }
+            if (any & kBiased) {
+#pragma unroll
+                for (int e = 0; e < kN; ++e)
+                    if (v + e < n && !(c[e] & kBiased)) to[v + e] = rounded<T>(x[e]);
+            } else {
+                write_pack(to, x, v, n, a.streamed);
+            }
+        }
+        if (counting && row + 1 < end) {
+            __syncthreads();
+            if (a.n_bias > 0) {  // the next row's biases are others
+                for (int i = threadIdx.x; i < a.n_bias; i += kThreads)
+                    if (biased[i] >= 0) atomicAnd(&count[biased[i]], ~kBiased);
+                __syncthreads();
+            }
+        }
     }
 }
 
 // A workgroup a slice of `rows_each` rows, whose gradients it adds up.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void penalties_grad_kernel(PenaltyArgs a)
+__global__ __launch_bounds__(kThreads, 8) void penalties_grad_kernel(PenaltyArgs a)
 {
-    constexpr int kEach = kSlice / kThreads;
+    constexpr int kN = kPackN<T>;
     __shared__ __attribute__((aligned(16))) unsigned count[kSlice];
     const long block = a.first_block + blockIdx.x, group = block / a.slices;
     const int begin = (int)(block % a.slices) * kSlice, n = min(kSlice, a.n_classes - begin);
-    float sum[kEach] = {};
-    for (long row = group * a.rows_each; row < min((group + 1) * a.rows_each, a.n_rows); ++row) {
+    const bool sparse = a.grad_out == a.out && !a.grad_bias, counting = a.out && a.history_len > 0;
+    Counted done{INT_MAX, INT_MAX};
+    const long end = min((group + 1) * a.rows_each, a.n_rows);
+    const T* g_row = static_cast<const T*>(a.grad_out) + group * a.rows_each * a.grad_stride + begin;
+    float sum[kPacks<T>][kN] = {};
+    for (long row = group * a.rows_each; row < end; ++row, g_row += a.grad_stride) {
         const T* x_row = static_cast<const T*>(a.logits) + row * a.row_stride + begin;
-        const T* g_row = static_cast<const T*>(a.grad_out) + row * a.grad_stride + begin;
         T* to = a.out ? static_cast<T*>(a.out) + row * a.out_stride + begin : nullptr;
         const uint32_t* allowed = a.allowed ? a.allowed + row * a.allowed_stride + begin / 32 : nullptr;
-        const float r = a.repetition ? a.repetition[row] : a.r;
-        if (to) {
-            for (int i = threadIdx.x; i < kSlice; i += kThreads) count[i] = 0;
-            __syncthreads();
-            count_history(a, row, begin, n, 0, clamped(a.lengths, row, a.history_len, a.history_len), 0, count);
+        const float r = a.repetition ? a.repetition[row] : a.r, by_r = 1.f / r;
+        Slice<T> own;
+        if (!sparse) own.fetch(g_row, n);
+        if (counting) {
+            count_on(a, row, begin, n, done, Counted{clamped(a.lengths, row, a.history_len, a.history_len), 0}, count);
             __syncthreads();
         }
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int v = (int)threadIdx.x + e * kThreads;
+        for (int u = 0; u < kPacks<T>; ++u) {
+            const int v = (u * kThreads + (int)threadIdx.x) * kN;
             if (v >= n) break;
-            float g = may_come(allowed, v) ? to_float(g_row[v]) : 0.f;
-            sum[e] += g;
+            unsigned c[kN] = {};
+            const unsigned any = counting ? read_counts<kN>(&count[v], c) : 0;
+            const unsigned may = allowed_of<kN>(allowed, v, n);
+            if (sparse) {
+                if (!any && may == (1u << kN) - 1) continue;
+                if (v + kN <= n) own.pack[u] = load_pack<T, kN>(g_row + v);
+            }
+            float g[kN];
+            unpack(own.pack[u], g_row, v, n, g);
+#pragma unroll
+            for (int e = 0; e < kN; ++e) {
+                if (!(may >> e & 1)) g[e] = 0.f;
+                sum[u][e] += g[e];
+            }
             if (!to) continue;
-            if (count[v]) g = to_float(x_row[v]) > 0.f ? g / r : g * r;
-            to[v] = rounded<T>(may_come(allowed, v) ? g : 0.f);
+            if (any) {
+                Pack<T, kN> logits{};
+                if (v + kN <= n) logits = load_pack<T, kN>(x_row + v);
+                float x[kN];
+                unpack(logits, x_row, v, n, x);
+#pragma unroll
+                for (int e = 0; e < kN; ++e) g[e] *= c[e] && (may >> e & 1) ? (x[e] > 0.f ? by_r : r) : 1.f;
+            }
+            write_pack(to, g, v, n, a.streamed);
         }
-        __syncthreads();
+        if (counting && row + 1 < end) __syncthreads();
     }
     if (!a.grad_bias) return;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        const int v = (int)threadIdx.x + e * kThreads;
-        if (v < n) a.grad_bias[group * a.n_classes + begin + v] = sum[e];
+    for (int u = 0; u < kPacks<T>; ++u) {
+        const int v = (u * kThreads + (int)threadIdx.x) * kN;
+#pragma unroll
+        for (int e = 0; e < kN; ++e)
+            if (v + e < n) a.grad_bias[group * a.n_classes + begin + v + e] = sum[u][e];
     }
 }
 
@@ -235,11 +414,14 @@ PenaltyArgs args_of(const nuts_penalties_desc* d)
     return a;
 }
 
-// Rows that a workgroup adds up, for a launch of about kGroups.
-int64_t rows_of_group(const nuts_penalties_desc* d)
+// Rows of a workgroup: for a launch of about kGroups, which is what the chip has at a time, but at least `least`.
+int64_t rows_of_group(const nuts_penalties_desc* d, int64_t least)
 {
-    return std::max<int64_t>(1, std::min(ceil_div(d->n_rows * ceil_div(d->n_classes, kSlice), kGroups), d->n_rows));
+    return std::max<int64_t>(1, std::min(std::max(ceil_div(d->n_rows * ceil_div(d->n_classes, kSlice), kGroups), least), d->n_rows));
 }
+// Rows go together where they have one history, whose counts are carried on.
+int64_t rows_of_group_sharing(const nuts_penalties_desc* d) { return d->history_len > 0 && d->history_stride == 0 ? rows_of_group(d, 1) : 1; }
+constexpr int64_t kBiasRows = 4;  // that are added up: their sums are stored
 
 void launch(void (*kernel)(PenaltyArgs), PenaltyArgs a)
 {
@@ -279,6 +461,7 @@ int nuts_penalties(const nuts_penalties_desc* d, const void* logits, const void*
     a.bias_values = bias_values;
     a.allowed = allowed;
     a.out = out;
+    a.rows_each = (int)rows_of_group_sharing(d);
     by_dtype(d->dtype, [&](auto t) { launch(penalties_kernel<decltype(t)>, a); });
     NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
     return NUTS_OK;
@@ -288,7 +471,7 @@ int nuts_penalties_grad_workspace(const nuts_penalties_desc* d, int64_t* bytes)
 {
     if (int rc = check_penalties(d, "nuts_penalties_grad_workspace")) return rc;
     if (!bytes) return api_fail(NUTS_E_INVALID_ARG, "nuts_penalties_grad_workspace: bytes must not be NULL");
-    *bytes = ceil_div(d->n_rows, rows_of_group(d)) * d->n_classes * (int64_t)sizeof(float);
+    *bytes = ceil_div(d->n_rows, rows_of_group(d, kBiasRows)) * d->n_classes * (int64_t)sizeof(float);
     return NUTS_OK;
 }
 
@@ -307,7 +490,7 @@ int nuts_penalties_grad(const nuts_penalties_desc* d, const void* grad_out, int6
         if (grad_logits == grad_out && grad_stride != d->out_stride && d->n_rows > 1)
             return api_fail(NUTS_E_INVALID_ARG, "nuts_penalties_grad: in place grad_stride and out_stride must be the same");
     }
-    const int64_t rows_each = rows_of_group(d), groups = ceil_div(d->n_rows, rows_each);
+    const int64_t rows_each = rows_of_group(d, kBiasRows), groups = ceil_div(d->n_rows, rows_each);
     if (grad_bias && groups > 0) {
         const int64_t bytes = groups * d->n_classes * (int64_t)sizeof(float);
         if (!workspace || workspace_bytes < bytes) return api_fail(NUTS_E_INVALID_ARG, "nuts_penalties_grad: needs a workspace of %lld bytes", (long long)bytes);
@@ -325,7 +508,7 @@ int nuts_penalties_grad(const nuts_penalties_desc* d, const void* grad_out, int6
     a.grad_stride = (long)grad_stride;
     a.out = grad_logits;
     a.grad_bias = grad_bias ? static_cast<float*>(workspace) : nullptr;
-    a.rows_each = grad_bias ? (int)rows_each : 1;
+    a.rows_each = grad_bias ? (int)rows_each : (int)rows_of_group_sharing(d);
     by_dtype(d->dtype, [&](auto t) { launch(penalties_grad_kernel<decltype(t)>, a); });
     if (grad_bias) {
         constexpr long kMost = kMaxBlocks / (kJoinThreads / kThreads);

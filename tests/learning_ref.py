@@ -45,7 +45,7 @@ def penalties(logits, history, lengths=None, prompts=None, repetition=1.0, frequ
     seen, said = counts(history, lengths, prompts, n, classes)
     r, f, q = (_column(v, n, device) for v in (repetition, frequency, presence))
     z = torch.where(seen > 0, torch.where(x > 0, x / r, x * r), x)
-    bound = torch.where(seen > 0, z.abs() * U, 0.0)
+    bound = torch.where(seen > 0, 2.01 * z.abs() * U, 0.0)  # (a product with 1 / r, which is rounded, too)
     less = f * said + q
     bound = bound + torch.where(said > 0, U * ((f * said).abs() + 2 * less.abs()), 0.0)  # (product, sum, and the sum's own error)
     z = torch.where(said > 0, z - less, z)

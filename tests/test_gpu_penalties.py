@@ -113,6 +113,18 @@ def test_one_text_of_which_each_row_has_seen_the_beginning(dtype):
         lengths = order.to("cuda").int()
         for prompts in (None, lengths // 3, (n - lengths) // 2, torch.full_like(lengths, 50)):
             check(logits, text, lengths=lengths, prompts=prompts, repetition=rows(n, 1.0, 2.0, g), frequency=rows(n, 0.0, 1.0, g), presence=0.5)
+        # biases of single classes, each row's its own, among classes that were said and others
+        ids = history_of(n, 11, classes, g, torch.int32)
+        check(logits, text, lengths=lengths, repetition=1.5, bias_ids=ids, bias_values=torch.randn(n, 11, generator=g, device="cuda"))
+
+
+def test_more_rows_of_one_text_than_workgroups_at_a_time():
+    n, classes, g = 2500, 300, gen(21)
+    text = history_of(1, 700, classes, g)
+    lengths = (torch.arange(n, device="cuda") * 700 // n).int()
+    ids = history_of(n, 3, classes, g)
+    check(matrix(n, classes, BF16, g), text, lengths=lengths, prompts=lengths // 2, repetition=1.25, frequency=0.125,
+          bias_ids=ids, bias_values=torch.randn(n, 3, generator=g, device="cuda"), allowed=masks(n, classes, g))
 
 
 def test_a_class_said_very_often():
