@@ -27,9 +27,12 @@ __device__ __forceinline__ int tensor_of(const int (&first)[kTensors], int block
 
 // ---- norm -----------------------------------------------------------------------------------------------------------
 
-constexpr int kNormTensors = 120;
+constexpr int kNormTensors = 190;
 constexpr int kNormBlocks = 2048;   // about so many workgroups in all
 constexpr int kNormLeast = 8192;    // numbers of a workgroup, at least
+constexpr int kNormThreads = 1024;  // of the workgroup that joins theirs
+constexpr int kNormSmall = 32768;   // numbers that it does alone, of kNormFew tensors at most, which it takes one after the other
+constexpr int kNormFew = 4;
 
 struct NormArgs {
     const void* data[kNormTensors];
@@ -52,15 +55,56 @@ __device__ __forceinline__ double block_sum(double v, double* shared, int n_wave
     return v;
 }
 
-template <typename T>
+// The squares of n numbers that lie next to each other, by kCount threads.
+template <typename T, int kCount>
 __device__ __forceinline__ double squares(const T* x, long n)
 {
-    double sum = 0;
-    for (long i = threadIdx.x; i < n; i += kThreads) {
-        const double v = (double)to_float(x[i]);
-        sum = fma(v, v, sum);
+    constexpr int kN = 16 / sizeof(T), kFlight = 4;
+    double sum[kFlight] = {};
+    long i = (long)threadIdx.x * kN;
+    for (; i + (kFlight - 1) * kCount * kN + kN <= n; i += kFlight * kCount * kN) {
+        Pack<T, kN> in[kFlight];
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) in[u] = load_pack<T, kN>(x + i + u * kCount * kN);
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u)
+#pragma unroll
+            for (int e = 0; e < kN; ++e) {
+                const double v = (double)to_float(in[u].v[e]);
+                sum[u] = fma(v, v, sum[u]);
+            }
     }
-    return sum;
+    for (; i < n; i += kCount * kN) {
+        Pack<T, kN> in{};
+        if (i + kN <= n) {
+            in = load_pack<T, kN>(x + i);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kN; ++e)
+                if (i + e < n) in.v[e] = x[i + e];
+        }
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            const double v = (double)to_float(in.v[e]);
+            sum[e % kFlight] = fma(v, v, sum[e % kFlight]);
+        }
+    }
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+template <int kCount>
+__device__ __forceinline__ double squares(const void* data, int dtype, long begin, long n)
+{
+    if (dtype == NUTS_F32) return squares<float, kCount>(static_cast<const float*>(data) + begin, n);
+    if (dtype == NUTS_BF16) return squares<bf16, kCount>(static_cast<const bf16*>(data) + begin, n);
+    return squares<f16, kCount>(static_cast<const f16*>(data) + begin, n);
+}
+
+__device__ __forceinline__ void write_norm(double sum, double max_norm, float* norm, float* factor)
+{
+    if (threadIdx.x != 0) return;
+    const double root = sqrt(sum);
+    if (norm) *norm = (float)root;
+    if (factor) *factor = !(root < INFINITY) ? NAN : root > max_norm ? (float)(max_norm / root) : 1.f;
 }
 
 __global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a)
@@ -68,24 +112,26 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a)
     __shared__ double shared[kThreads / 64];
     const int t = tensor_of(a.first, (int)blockIdx.x);
     const long begin = (long)((int)blockIdx.x - a.first[t]) * a.each, n = min(a.each, a.n[t] - begin);
-    double sum;
-    if (a.dtype[t] == NUTS_F32) sum = squares(static_cast<const float*>(a.data[t]) + begin, n);
-    else if (a.dtype[t] == NUTS_BF16) sum = squares(static_cast<const bf16*>(a.data[t]) + begin, n);
-    else sum = squares(static_cast<const f16*>(a.data[t]) + begin, n);
-    sum = block_sum(sum, shared, kThreads / 64);
+    const double sum = block_sum(squares<kThreads>(a.data[t], a.dtype[t], begin, n), shared, kThreads / 64);
     if (threadIdx.x == 0) a.part[blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(kThreads) void join_norm_kernel(const double* part, long n, double max_norm, float* norm, float* factor)
+__global__ __launch_bounds__(kNormThreads) void join_norm_kernel(const double* part, long n, double max_norm, float* norm, float* factor)
 {
-    __shared__ double shared[kThreads / 64];
+    __shared__ double shared[kNormThreads / 64];
     double sum = 0;
-    for (long i = threadIdx.x; i < n; i += kThreads) sum += part[i];
-    sum = block_sum(sum, shared, kThreads / 64);
-    if (threadIdx.x != 0) return;
-    const double root = sqrt(sum);
-    if (norm) *norm = (float)root;
-    if (factor) *factor = !(root < INFINITY) ? NAN : root > max_norm ? (float)(max_norm / root) : 1.f;
+#pragma unroll 4
+    for (long i = threadIdx.x; i < n; i += kNormThreads) sum += part[i];
+    write_norm(block_sum(sum, shared, kNormThreads / 64), max_norm, norm, factor);
+}
+
+// All of it by one workgroup, where there is little: one launch in place of two.
+__global__ __launch_bounds__(kNormThreads) void small_norm_kernel(NormArgs a, int n_tensors, double max_norm, float* norm, float* factor)
+{
+    __shared__ double shared[kNormThreads / 64];
+    double sum = 0;
+    for (int t = 0; t < n_tensors; ++t) sum += squares<kNormThreads>(a.data[t], a.dtype[t], 0, a.n[t]);
+    write_norm(block_sum(sum, shared, kNormThreads / 64), max_norm, norm, factor);
 }
 
 // Numbers of a workgroup: a multiple of 2048, so that kNormBlocks or so (and one for each tensor) do.
@@ -111,8 +157,16 @@ int check_norm(const nuts_tensor* tensors, int64_t n, const char* who)
     return NUTS_OK;
 }
 
+bool norm_is_small(const nuts_tensor* tensors, int64_t n)
+{
+    int64_t total = 0;
+    for (int64_t i = 0; i < n && n <= kNormFew; ++i) total += tensors[i].n;
+    return n <= kNormFew && total <= kNormSmall;
+}
+
 int64_t norm_blocks(const nuts_tensor* tensors, int64_t n)
 {
+    if (norm_is_small(tensors, n)) return 0;
     const int64_t each = norm_each(tensors, n);
     int64_t blocks = 0;
     for (int64_t i = 0; i < n; ++i) blocks += ceil_div(tensors[i].n, each);
@@ -195,37 +249,154 @@ __device__ __forceinline__ float rounded_at_random(float x, unsigned word)
     return __uint_as_float((bits + (word >> 20 << 4 | 8u)) & 0xffff0000u);
 }
 
-__device__ __forceinline__ float chance(unsigned bits) { return ((float)(bits & 1023u) + 0.5f) * (1.f / 1024.f); }
-
-// Codes of 8 bits.  x is in units of the scale: 127^2 or 254^2 at a block's largest.
-__device__ __forceinline__ float m_value(int code, float scale) { return code == -128 ? NAN : (float)(code * abs(code)) * scale; }
-__device__ __forceinline__ float root_value(unsigned code, float scale) { return code == 255 ? NAN : (float)(code * code) * scale; }
-__device__ __forceinline__ int m_code(float m, float scale, unsigned word)
-{
-    if (!(__builtin_fabsf(m) < INFINITY)) return -128;
-    const float x = scale > 0.f ? __builtin_fabsf(m) / scale : 0.f;
-    float c = fminf(floorf(sqrtf(x)), 126.f);
-    if (x - c * c > (2.f * c + 1.f) * chance(word)) c += 1.f;
-    return m < 0.f ? -(int)c : (int)c;
-}
-__device__ __forceinline__ unsigned v_code(float root, float scale, unsigned word)
-{
-    if (!(root < INFINITY)) return 255;
-    const float x = scale > 0.f ? root / scale : 0.f;
-    float c = fminf(floorf(sqrtf(x)), 253.f);
-    const float below = c * c, above = (c + 1.f) * (c + 1.f);
-    if (x * x - below * below > (above - below) * (above + below) * chance(word >> 10)) c += 1.f;
-    if (root > 0.f) c = fmaxf(c, 1.f);
-    return (unsigned)c;
-}
-
-__device__ __forceinline__ float wave_max(float v)
+// philox4x32_10 of nuts_rng.h with the halves of a product from one instruction and exclusive ors of three from another.
+__device__ __forceinline__ void random_words(unsigned c0, unsigned c1, unsigned c2, unsigned c3, unsigned k0, unsigned k1, unsigned (&words)[4])
 {
 #pragma unroll
-    for (int step = 32; step >= 1; step /= 2) v = fmaxf(v, __shfl_xor(v, step));
-    return v;
+    for (int round = 0; round < 10; ++round) {
+        const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
+#ifdef __HIP_DEVICE_COMPILE__
+        c0 = __builtin_amdgcn_bitop3_b32((unsigned)(p1 >> 32), c1, k0, 0x96);
+        c2 = __builtin_amdgcn_bitop3_b32((unsigned)(p0 >> 32), c3, k1, 0x96);
+#endif
+        c1 = (unsigned)p1;
+        c3 = (unsigned)p0;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    words[0] = c0, words[1] = c1, words[2] = c2, words[3] = c3;
 }
-__device__ __forceinline__ float if_finite(float v) { return __builtin_fabsf(v) < INFINITY ? __builtin_fabsf(v) : 0.f; }
+
+__device__ __forceinline__ float chance(unsigned bits) { return __builtin_fmaf((float)(bits & 1023u), 1.f / 1024.f, 0.5f / 1024.f); }
+
+// Codes of 8 bits.  x is what they stand for in units of the scale: 127^2, or 254^2, at a block's largest.  The code below x is the whole part of
+// its root, and where that comes out one too high or too low for a last place the comparison makes up for it: the
+// square roots need not be exact.
+__device__ __forceinline__ float m_value(float code, float scale) { return code * __builtin_fabsf(code) * scale; }
+__device__ __forceinline__ float root_value(float code, float scale) { return code * code * scale; }
+__device__ __forceinline__ float m_code(float m, float by_scale, unsigned word)
+{
+    const float x = __builtin_fabsf(m) * by_scale, c = fminf(floorf(__builtin_amdgcn_sqrtf(x)), 126.f);
+    const bool up = __builtin_fmaf(-c, c, x) > __builtin_fmaf(2.f, c, 1.f) * chance(word);
+    return __builtin_copysignf(up ? c + 1.f : c, m);
+}
+__device__ __forceinline__ float v_code(float root, float by_scale, unsigned word)
+{
+    const float x = root * by_scale, c = fminf(floorf(__builtin_amdgcn_sqrtf(x)), 253.f);
+    const float below = c * c, gap = __builtin_fmaf(2.f, c, 1.f);  // (c + 1)^2 - c^2
+    // x^2 - c^4 > ((c + 1)^4 - c^4) chance
+    const bool up = (x - below) * (x + below) > gap * __builtin_fmaf(2.f, below, gap) * chance(word >> 10);
+    return up || (c == 0.f && root > 0.f) ? c + 1.f : c;
+}
+
+constexpr unsigned kInfinite = 0x7f800000u;
+__device__ __forceinline__ unsigned size_of(float x) { return __float_as_uint(x) & 0x7fffffffu; }  // rises with |x|; NaN is above infinity
+
+// The largest of a wave's, in all of its lanes.
+__device__ __forceinline__ unsigned wave_max(unsigned v)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+#define NUTS_MAX_STEP(control, rows) v = max(v, (unsigned)__builtin_amdgcn_update_dpp((int)v, (int)v, control, rows, 0xf, false))
+    NUTS_MAX_STEP(0xb1, 0xf);   // quads: neighbours, then pairs
+    NUTS_MAX_STEP(0x4e, 0xf);
+    NUTS_MAX_STEP(0x141, 0xf);  // rows of 16: mirrored halves, then mirrored
+    NUTS_MAX_STEP(0x140, 0xf);
+    NUTS_MAX_STEP(0x142, 0xa);  // rows 1 and 3: the last lane of the row before
+    NUTS_MAX_STEP(0x143, 0xc);  // the upper half: lane 31
+#undef NUTS_MAX_STEP
+    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+#else
+    return v;
+#endif
+}
+
+// The codes of four numbers in a word, as many of them as there are.
+__device__ __forceinline__ unsigned load_codes(const void* codes, long i, int n)
+{
+    const uint8_t* at = static_cast<const uint8_t*>(codes) + i;
+    if (n >= 4) {
+        const Pack<uint8_t, 4> in = load_pack<uint8_t, 4>(at);
+        unsigned word;
+        __builtin_memcpy(&word, &in, 4);
+        return word;
+    }
+    unsigned word = 0;
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (e < n) word |= (unsigned)at[e] << 8 * e;
+    return word;
+}
+__device__ __forceinline__ void store_codes(void* codes, long i, int n, unsigned word)
+{
+    uint8_t* at = static_cast<uint8_t*>(codes) + i;
+    if (n >= 4) {
+        Pack<uint8_t, 4> out;
+        __builtin_memcpy(&out, &word, 4);
+        store_pack(at, out);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (e < n) at[e] = (uint8_t)(word >> 8 * e);
+}
+__device__ __forceinline__ bool has_zero_byte(unsigned word) { return (word - 0x01010101u) & ~word & 0x80808080u; }
+
+// What four codes stand for: m, and the root of v.
+__device__ __forceinline__ void decode(unsigned m_word, unsigned v_word, float m_scale, float v_scale, float (&m)[4], float (&root)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        m[e] = m_value((float)(int8_t)(m_word >> 8 * e), m_scale);
+        root[e] = root_value((float)(uint8_t)(v_word >> 8 * e), v_scale);
+    }
+    if (has_zero_byte(m_word ^ 0x80808080u) || has_zero_byte(~v_word)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if ((m_word >> 8 * e & 255u) == 128u) m[e] = NAN;
+            if ((v_word >> 8 * e & 255u) == 255u) root[e] = NAN;
+        }
+    }
+}
+
+// A block's moments, four in each lane, as codes and scales.  A scale with fewer than 24 places is taken as 0.
+__device__ __forceinline__ void encode(const nuts_adamw_tensor& t, long block, long i, int n, float (&m)[4], float (&root)[4], const unsigned (&words)[4])
+{
+    unsigned m_top = wave_max(max(max(size_of(m[0]), size_of(m[1])), max(size_of(m[2]), size_of(m[3]))));
+    unsigned v_top = wave_max(max(max(size_of(root[0]), size_of(root[1])), max(size_of(root[2]), size_of(root[3]))));
+    unsigned m_lost = 0, v_lost = 0;  // codes that are not finite
+    if (m_top >= kInfinite || v_top >= kInfinite) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (size_of(m[e]) >= kInfinite) {
+                m[e] = 0.f;
+                m_lost |= 255u << 8 * e;
+            }
+            if (size_of(root[e]) >= kInfinite) {
+                root[e] = 0.f;
+                v_lost |= 255u << 8 * e;
+            }
+        }
+        m_top = wave_max(max(max(size_of(m[0]), size_of(m[1])), max(size_of(m[2]), size_of(m[3]))));
+        v_top = wave_max(max(max(size_of(root[0]), size_of(root[1])), max(size_of(root[2]), size_of(root[3]))));
+    }
+    constexpr float kLeast = 0x1p-126f;
+    float m_scale = __uint_as_float(m_top) * (1.f / (127.f * 127.f)), v_scale = __uint_as_float(v_top) * (1.f / (254.f * 254.f));
+    if (m_scale < kLeast) m_scale = 0.f;
+    if (v_scale < kLeast) v_scale = 0.f;
+    const float by_m = m_scale > 0.f ? 1.f / m_scale : 0.f, by_v = v_scale > 0.f ? 1.f / v_scale : 0.f;
+    unsigned m_word = 0, v_word = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        m_word |= ((unsigned)(int)m_code(m[e], by_m, words[e]) & 255u) << 8 * e;
+        v_word |= (unsigned)v_code(root[e], by_v, words[e]) << 8 * e;
+    }
+    store_codes(t.m, i, n, (m_word & ~m_lost) | (m_lost & 0x80808080u));
+    store_codes(t.v, i, n, v_word | v_lost);
+    if (threadIdx.x % 64 == 0) {
+        t.m_scale[block] = m_scale;
+        t.v_scale[block] = v_scale;
+    }
+}
 
 // A workgroup kChunk numbers of a tensor, a wave 256 of them at a time: a block of the moments of 8 bits.
 template <typename P, typename G, bool kEight>
@@ -238,61 +409,35 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a)
     const nuts_adamw_tensor& t = a.tensor[k];
     const long begin = (a.first_block + (long)((int)blockIdx.x - a.first[k])) * kChunk, end = min(begin + kChunk, (long)t.n);
     const int lane = threadIdx.x % 64;
-    for (long block = begin + threadIdx.x / 64 * 256; block < end; block += kThreads * 4) {
-        const long i = block + lane * 4;
+    for (long at = begin + threadIdx.x / 64 * 256; at < end; at += kThreads * 4) {
+        const long i = at + lane * 4, block = at / 256;
         const int n = (int)max(min(end - i, 4l), 0l);
         float p[4], g[4], m[4], v[4], root[4];
         load4(static_cast<const P*>(t.param) + i, n, p);
         load4(static_cast<const G*>(t.grad) + i, n, g);
         if (kEight) {
-            const float m_scale = t.m_scale[block / 256], v_scale = t.v_scale[block / 256];
-            const int8_t* m_at = static_cast<const int8_t*>(t.m) + i;
-            const uint8_t* v_at = static_cast<const uint8_t*>(t.v) + i;
+            decode(load_codes(t.m, i, n), load_codes(t.v, i, n), t.m_scale[block], t.v_scale[block], m, root);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                m[e] = e < n ? m_value(m_at[e], m_scale) : 0.f;
-                root[e] = e < n ? root_value(v_at[e], v_scale) : 0.f;
-                v[e] = root[e] * root[e];
-            }
+            for (int e = 0; e < 4; ++e) v[e] = root[e] * root[e];
         } else {
             load4(static_cast<const float*>(t.m) + i, n, m);
             load4(static_cast<const float*>(t.v) + i, n, v);
         }
-        Words4 w{0, 0, 0, 0};
-        if (kEight || sizeof(P) == 2) w = philox4x32_10((unsigned)(i / 4), 6u | (unsigned)(i / 4 >> 32) << 8, f.t, a.first_tensor + k, a.k0, a.k1);
-        const unsigned words[4] = {w.w0, w.w1, w.w2, w.w3};
+        unsigned words[4] = {};
+        if (kEight || sizeof(P) == 2) random_words((unsigned)(i / 4), 6u | (unsigned)(i / 4 >> 32) << 8, f.t, a.first_tensor + k, a.k0, a.k1, words);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float x = g[e] * f.scale;
             m[e] = m[e] * a.beta1 + x * a.rest1;
             v[e] = v[e] * a.beta2 + x * x * a.rest2;
-            root[e] = sqrtf(v[e]);
-            p[e] = p[e] * f.keep - f.size * m[e] / (root[e] * f.root_scale + a.eps);
+            root[e] = __builtin_amdgcn_sqrtf(v[e]);  // (a unit in the last place off at most, as the reciprocal)
+            p[e] = p[e] * f.keep - f.size * m[e] * __builtin_amdgcn_rcpf(root[e] * f.root_scale + a.eps);
             if (sizeof(P) == 2) p[e] = rounded_at_random(p[e], words[e]);
         }
         store4(static_cast<P*>(t.param) + i, n, p);
         if (t.copy) a.copy_dtype == NUTS_BF16 ? store4(static_cast<bf16*>(t.copy) + i, n, p) : store4(static_cast<f16*>(t.copy) + i, n, p);
         if (kEight) {
-            float m_top = 0.f, v_top = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n) {
-                    m_top = fmaxf(m_top, if_finite(m[e]));
-                    v_top = fmaxf(v_top, if_finite(root[e]));
-                }
-            const float m_scale = wave_max(m_top) * (1.f / (127.f * 127.f)), v_scale = wave_max(v_top) * (1.f / (254.f * 254.f));
-            int8_t* m_at = static_cast<int8_t*>(t.m) + i;
-            uint8_t* v_at = static_cast<uint8_t*>(t.v) + i;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n) {
-                    m_at[e] = (int8_t)m_code(m[e], m_scale, words[e]);
-                    v_at[e] = (uint8_t)v_code(root[e], v_scale, words[e]);
-                }
-            if (lane == 0) {
-                t.m_scale[block / 256] = m_scale;
-                t.v_scale[block / 256] = v_scale;
-            }
+            encode(t, block, i, n, m, root, words);
         } else {
             store4(static_cast<float*>(t.m) + i, n, m);
             store4(static_cast<float*>(t.v) + i, n, v);
@@ -309,14 +454,9 @@ __global__ __launch_bounds__(kThreads) void values_kernel(StepArgs a)
     for (long i = begin + (long)threadIdx.x * 4; i < end; i += kThreads * 4) {
         const int n = (int)min(end - i, 4l);
         float m[4], v[4];
-        const int8_t* m_at = static_cast<const int8_t*>(t.m) + i;
-        const uint8_t* v_at = static_cast<const uint8_t*>(t.v) + i;
+        decode(load_codes(t.m, i, n), load_codes(t.v, i, n), t.m_scale[i / 256], t.v_scale[i / 256], m, v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            m[e] = e < n ? m_value(m_at[e], t.m_scale[i / 256]) : 0.f;
-            const float root = e < n ? root_value(v_at[e], t.v_scale[i / 256]) : 0.f;
-            v[e] = root * root;
-        }
+        for (int e = 0; e < 4; ++e) v[e] *= v[e];
         if (t.param) store4(static_cast<T*>(t.param) + i, n, m);
         if (t.copy) store4(static_cast<T*>(t.copy) + i, n, v);
     }
@@ -399,6 +539,16 @@ int nuts_norm(const nuts_tensor* tensors, int64_t n_tensors, double max_norm, fl
     if (bytes > 0 && reinterpret_cast<uintptr_t>(workspace) % 256) return api_fail(NUTS_E_INVALID_ARG, "nuts_norm: workspace must be aligned to 256 bytes");
     if (int rc = api_have_device()) return rc;
     NormArgs a{};
+    if (norm_is_small(tensors, n_tensors)) {
+        for (int i = 0; i < (int)n_tensors; ++i) {
+            a.data[i] = tensors[i].data;
+            a.n[i] = (long)tensors[i].n;
+            a.dtype[i] = (unsigned char)tensors[i].dtype;
+        }
+        hipLaunchKernelGGL(small_norm_kernel, dim3(1), dim3(kNormThreads), 0, api_stream(), a, (int)n_tensors, max_norm, norm, factor);
+        NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
+        return NUTS_OK;
+    }
     a.each = (long)norm_each(tensors, n_tensors);
     double* part = static_cast<double*>(workspace);
     for (int64_t at = 0; at < n_tensors;) {
@@ -416,7 +566,7 @@ int nuts_norm(const nuts_tensor* tensors, int64_t n_tensors, double max_norm, fl
         if (own > 0) hipLaunchKernelGGL(norm_kernel, dim3((unsigned)own), dim3(kThreads), 0, api_stream(), a);
         part += own;
     }
-    hipLaunchKernelGGL(join_norm_kernel, dim3(1), dim3(kThreads), 0, api_stream(), static_cast<const double*>(workspace), (long)blocks, max_norm, norm, factor);
+    hipLaunchKernelGGL(join_norm_kernel, dim3(1), dim3(kNormThreads), 0, api_stream(), static_cast<const double*>(workspace), (long)blocks, max_norm, norm, factor);
     NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
     return NUTS_OK;
 }

@@ -125,7 +125,7 @@ def test_tables_of_tensors():
         refused(lib.nuts_adamw(adamw(state_bits=8), table(B.nuts_adamw_tensor, tensor(**bad)), 1, None, None, None), "tensor 0")
         refused(lib.nuts_adamw_values(table(B.nuts_adamw_tensor, tensor(**bad)), 1, 0), "tensor 0")
     refused(lib.nuts_adamw_values(one, 1, 1), "dtype")
-    some = lambda **kw: table(B.nuts_tensor, B.nuts_tensor(**{**dict(data=4096, n=5, dtype=0, reserved=0), **kw}))  # noqa: E731
+    some = lambda **kw: table(B.nuts_tensor, B.nuts_tensor(**{**dict(data=4096, n=100000, dtype=0, reserved=0), **kw}))  # noqa: E731
     norm = lambda t, k=1, most=1.0, ws=P, size=1 << 30: lib.nuts_norm(t, k, most, P, P, ws, size)  # noqa: E731
     for bad, word in ((dict(data=None), "data"), (dict(n=-1), "n of"), (dict(n=2 ** 40 + 1), "n of"), (dict(dtype=1), "dtype")):
         refused(norm(some(**bad)), word)
