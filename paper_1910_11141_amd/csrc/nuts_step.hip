@@ -16,12 +16,16 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int64_t kLongest = (int64_t)1 << 40;
 
-// The tensor that a workgroup belongs to: the last whose first workgroup is no later.
+// The tensor that a workgroup belongs to: the last whose first workgroup is no later.  A lane looks at every 64th.
 template <int kTensors>
 __device__ __forceinline__ int tensor_of(const int (&first)[kTensors], int block)
 {
-    int t = 0;
-    for (int k = 1; k < kTensors; ++k) t += first[k] <= block;
+    int t = -1;
+#ifdef __HIP_DEVICE_COMPILE__
+    const int lane = threadIdx.x % 64;
+#pragma unroll
+    for (int k = 0; k < kTensors; k += 64) t += __popcll(__builtin_amdgcn_ballot_w64(k + lane < kTensors && first[min(k + lane, kTensors - 1)] <= block));
+#endif
     return t;
 }
 
@@ -176,7 +180,9 @@ int64_t norm_blocks(const nuts_tensor* tensors, int64_t n)
 // ---- AdamW ----------------------------------------------------------------------------------------------------------
 
 constexpr int kStepTensors = 48;
-constexpr int kChunk = 8192;  // numbers of a workgroup
+// Numbers of a workgroup: 256 a wave at a time, eight times in large calls; in small ones as few times as kStepBlocks workgroups allow (16000
+// numbers: the kernel takes 8.4 us with eight times, 5.3 with one).
+constexpr int64_t kChunkLeast = 1024, kChunkMost = 8192, kStepBlocks = 1024;
 
 struct StepArgs {
     nuts_adamw_tensor tensor[kStepTensors];
@@ -188,6 +194,7 @@ struct StepArgs {
     float beta1, rest1, beta2, rest2, eps, scale;
     float keep, size, root_scale;  // 1 - lr d, lr / (1 - b1^t), 1 / sqrt(1 - b2^t), where neither t nor lr is on the device
     unsigned t, k0, k1, first_tensor;
+    int chunk;
     long first_block;
     int64_t host_step;
     int copy_dtype;
@@ -286,7 +293,7 @@ __device__ __forceinline__ float v_code(float root, float by_scale, unsigned wor
     const float below = c * c, gap = __builtin_fmaf(2.f, c, 1.f);  // (c + 1)^2 - c^2
     // x^2 - c^4 > ((c + 1)^4 - c^4) chance
     const bool up = (x - below) * (x + below) > gap * __builtin_fmaf(2.f, below, gap) * chance(word >> 10);
-    return up || (c == 0.f && root > 0.f) ? c + 1.f : c;
+    return (int)up | ((int)(c == 0.f) & (int)(root > 0.f)) ? c + 1.f : c;
 }
 
 constexpr unsigned kInfinite = 0x7f800000u;
@@ -296,7 +303,7 @@ __device__ __forceinline__ unsigned size_of(float x) { return __float_as_uint(x)
 __device__ __forceinline__ unsigned wave_max(unsigned v)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-#define NUTS_MAX_STEP(control, rows) v = max(v, (unsigned)__builtin_amdgcn_update_dpp((int)v, (int)v, control, rows, 0xf, false))
+#define NUTS_MAX_STEP(control, rows) v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, control, rows, 0xf, rows == 0xf))
     NUTS_MAX_STEP(0xb1, 0xf);   // quads: neighbours, then pairs
     NUTS_MAX_STEP(0x4e, 0xf);
     NUTS_MAX_STEP(0x141, 0xf);  // rows of 16: mirrored halves, then mirrored
@@ -339,7 +346,7 @@ __device__ __forceinline__ void store_codes(void* codes, long i, int n, unsigned
     for (int e = 0; e < 3; ++e)
         if (e < n) at[e] = (uint8_t)(word >> 8 * e);
 }
-__device__ __forceinline__ bool has_zero_byte(unsigned word) { return (word - 0x01010101u) & ~word & 0x80808080u; }
+__device__ __forceinline__ unsigned zero_bytes(unsigned word) { return (word - 0x01010101u) & ~word & 0x80808080u; }  // 0: there is none
 
 // What four codes stand for: m, and the root of v.
 __device__ __forceinline__ void decode(unsigned m_word, unsigned v_word, float m_scale, float v_scale, float (&m)[4], float (&root)[4])
@@ -349,7 +356,7 @@ __device__ __forceinline__ void decode(unsigned m_word, unsigned v_word, float m
         m[e] = m_value((float)(int8_t)(m_word >> 8 * e), m_scale);
         root[e] = root_value((float)(uint8_t)(v_word >> 8 * e), v_scale);
     }
-    if (has_zero_byte(m_word ^ 0x80808080u) || has_zero_byte(~v_word)) {
+    if (__builtin_amdgcn_ballot_w64((zero_bytes(m_word ^ 0x80808080u) | zero_bytes(~v_word)) != 0)) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if ((m_word >> 8 * e & 255u) == 128u) m[e] = NAN;
@@ -383,7 +390,7 @@ __device__ __forceinline__ void encode(const nuts_adamw_tensor& t, long block, l
     float m_scale = __uint_as_float(m_top) * (1.f / (127.f * 127.f)), v_scale = __uint_as_float(v_top) * (1.f / (254.f * 254.f));
     if (m_scale < kLeast) m_scale = 0.f;
     if (v_scale < kLeast) v_scale = 0.f;
-    const float by_m = m_scale > 0.f ? 1.f / m_scale : 0.f, by_v = v_scale > 0.f ? 1.f / v_scale : 0.f;
+    const float by_m = m_scale > 0.f ? __builtin_amdgcn_rcpf(m_scale) : 0.f, by_v = v_scale > 0.f ? __builtin_amdgcn_rcpf(v_scale) : 0.f;
     unsigned m_word = 0, v_word = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -398,7 +405,45 @@ __device__ __forceinline__ void encode(const nuts_adamw_tensor& t, long block, l
     }
 }
 
-// A workgroup kChunk numbers of a tensor, a wave 256 of them at a time: a block of the moments of 8 bits.
+// Four numbers of each lane, from i on; kWhole: every lane has four.
+template <typename P, typename G, bool kEight, bool kWhole>
+__device__ __forceinline__ void step_block(const StepArgs& a, const Factors& f, const nuts_adamw_tensor& t, unsigned tensor, long at, long end)
+{
+    const long i = at + threadIdx.x % 64 * 4, block = at / 256;
+    const int n = kWhole ? 4 : (int)max(min(end - i, 4l), 0l);
+    float p[4], g[4], m[4], v[4], root[4];
+    load4(static_cast<const P*>(t.param) + i, n, p);
+    load4(static_cast<const G*>(t.grad) + i, n, g);
+    if (kEight) {
+        decode(load_codes(t.m, i, n), load_codes(t.v, i, n), t.m_scale[block], t.v_scale[block], m, root);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = root[e] * root[e];
+    } else {
+        load4(static_cast<const float*>(t.m) + i, n, m);
+        load4(static_cast<const float*>(t.v) + i, n, v);
+    }
+    unsigned words[4] = {};
+    if (kEight || sizeof(P) == 2) random_words((unsigned)(i / 4), 6u | (unsigned)(at / 4 >> 32) << 8, f.t, tensor, a.k0, a.k1, words);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float x = g[e] * f.scale;
+        m[e] = m[e] * a.beta1 + x * a.rest1;
+        v[e] = v[e] * a.beta2 + x * x * a.rest2;
+        root[e] = __builtin_amdgcn_sqrtf(v[e]);  // (a unit in the last place off at most, as the reciprocal)
+        p[e] = p[e] * f.keep - f.size * m[e] * __builtin_amdgcn_rcpf(root[e] * f.root_scale + a.eps);
+        if (sizeof(P) == 2) p[e] = rounded_at_random(p[e], words[e]);
+    }
+    store4(static_cast<P*>(t.param) + i, n, p);
+    if (t.copy) a.copy_dtype == NUTS_BF16 ? store4(static_cast<bf16*>(t.copy) + i, n, p) : store4(static_cast<f16*>(t.copy) + i, n, p);
+    if (kEight) {
+        encode(t, block, i, n, m, root, words);
+    } else {
+        store4(static_cast<float*>(t.m) + i, n, m);
+        store4(static_cast<float*>(t.v) + i, n, v);
+    }
+}
+
+// A workgroup `chunk` numbers of a tensor, a wave 256 of them at a time: a block of the moments of 8 bits.
 template <typename P, typename G, bool kEight>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a)
 {
@@ -407,42 +452,11 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a)
     const Factors f = factors_of(a, factor);
     const int k = tensor_of(a.first, (int)blockIdx.x);
     const nuts_adamw_tensor& t = a.tensor[k];
-    const long begin = (a.first_block + (long)((int)blockIdx.x - a.first[k])) * kChunk, end = min(begin + kChunk, (long)t.n);
-    const int lane = threadIdx.x % 64;
-    for (long at = begin + threadIdx.x / 64 * 256; at < end; at += kThreads * 4) {
-        const long i = at + lane * 4, block = at / 256;
-        const int n = (int)max(min(end - i, 4l), 0l);
-        float p[4], g[4], m[4], v[4], root[4];
-        load4(static_cast<const P*>(t.param) + i, n, p);
-        load4(static_cast<const G*>(t.grad) + i, n, g);
-        if (kEight) {
-            decode(load_codes(t.m, i, n), load_codes(t.v, i, n), t.m_scale[block], t.v_scale[block], m, root);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = root[e] * root[e];
-        } else {
-            load4(static_cast<const float*>(t.m) + i, n, m);
-            load4(static_cast<const float*>(t.v) + i, n, v);
-        }
-        unsigned words[4] = {};
-        if (kEight || sizeof(P) == 2) random_words((unsigned)(i / 4), 6u | (unsigned)(i / 4 >> 32) << 8, f.t, a.first_tensor + k, a.k0, a.k1, words);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float x = g[e] * f.scale;
-            m[e] = m[e] * a.beta1 + x * a.rest1;
-            v[e] = v[e] * a.beta2 + x * x * a.rest2;
-            root[e] = __builtin_amdgcn_sqrtf(v[e]);  // (a unit in the last place off at most, as the reciprocal)
-            p[e] = p[e] * f.keep - f.size * m[e] * __builtin_amdgcn_rcpf(root[e] * f.root_scale + a.eps);
-            if (sizeof(P) == 2) p[e] = rounded_at_random(p[e], words[e]);
-        }
-        store4(static_cast<P*>(t.param) + i, n, p);
-        if (t.copy) a.copy_dtype == NUTS_BF16 ? store4(static_cast<bf16*>(t.copy) + i, n, p) : store4(static_cast<f16*>(t.copy) + i, n, p);
-        if (kEight) {
-            encode(t, block, i, n, m, root, words);
-        } else {
-            store4(static_cast<float*>(t.m) + i, n, m);
-            store4(static_cast<float*>(t.v) + i, n, v);
-        }
-    }
+    const long begin = (a.first_block + (long)((int)blockIdx.x - a.first[k])) * a.chunk, end = min(begin + a.chunk, (long)t.n);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    long at = begin + wave * 256;
+    for (; at + 256 <= end; at += kThreads * 4) step_block<P, G, kEight, true>(a, f, t, a.first_tensor + k, at, end);
+    if (at < end) step_block<P, G, kEight, false>(a, f, t, a.first_tensor + k, at, end);
 }
 
 template <typename T>
@@ -450,7 +464,7 @@ __global__ __launch_bounds__(kThreads) void values_kernel(StepArgs a)
 {
     const int k = tensor_of(a.first, (int)blockIdx.x);
     const nuts_adamw_tensor& t = a.tensor[k];
-    const long begin = (a.first_block + (long)((int)blockIdx.x - a.first[k])) * kChunk, end = min(begin + kChunk, (long)t.n);
+    const long begin = (a.first_block + (long)((int)blockIdx.x - a.first[k])) * a.chunk, end = min(begin + a.chunk, (long)t.n);
     for (long i = begin + (long)threadIdx.x * 4; i < end; i += kThreads * 4) {
         const int n = (int)min(end - i, 4l);
         float m[4], v[4];
@@ -466,14 +480,16 @@ __global__ __launch_bounds__(kThreads) void values_kernel(StepArgs a)
 template <typename Wanted, typename Go>
 void by_tables(StepArgs& a, const nuts_adamw_tensor* tensors, int64_t n, Wanted wanted, Go go)
 {
-    int64_t at = 0;
+    int64_t at = 0, total = 0;
+    for (int64_t i = 0; i < n; ++i) total += wanted(tensors[i]) ? tensors[i].n : 0;
+    a.chunk = (int)std::clamp(ceil_div(ceil_div(total, kStepBlocks), kChunkLeast) * kChunkLeast, kChunkLeast, kChunkMost);
     while (at < n) {
         int64_t blocks = 0;
         int used = 0;
         a.first_tensor = (unsigned)at;
         a.first_block = 0;
         for (; used < kStepTensors && at < n; ++used, ++at) {
-            const int64_t own = wanted(tensors[at]) ? ceil_div(tensors[at].n, kChunk) : 0;
+            const int64_t own = wanted(tensors[at]) ? ceil_div(tensors[at].n, a.chunk) : 0;
             if (blocks + own > kMaxBlocks) {
                 if (used > 0) break;
                 // a tensor of more workgroups than a launch has: alone, in several

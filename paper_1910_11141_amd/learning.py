@@ -7,9 +7,9 @@ those of categorical.py go to, and autograd knows none of them, either: paramete
 from __future__ import annotations
 
 import ctypes as C
+from array import array
 from collections import namedtuple
 
-import numpy as np
 import torch
 
 from . import binding as _b
@@ -22,23 +22,24 @@ Norm = namedtuple("Norm", "norm factor")
 _PARAM_DTYPES = {torch.float32: _b.NUTS_F32, torch.bfloat16: _b.NUTS_BF16}
 _COPY_DTYPES = {torch.bfloat16: _b.NUTS_BF16, torch.float16: _b.NUTS_F16}
 _PARAM, _GRAD, _COPY, _M, _V, _M_SCALE, _V_SCALE, _N = range(8)  # columns of a table of nuts_adamw_tensor
-assert C.sizeof(_b.nuts_adamw_tensor) == 64
+assert C.sizeof(_b.nuts_adamw_tensor) == 64 and C.sizeof(_b.nuts_tensor) == 24
 
 
 def _of_one_device(tensors):
     """The device of `tensors` (None where there are none), which must be the current one."""
-    device = None
-    for t in tensors:
-        if device is None:
-            device = t.device
-        elif t.device != device:
-            raise ValueError(f"tensors are on {device} and {t.device}")
+    device = tensors[0].device if tensors else None
+    if device is not None and any([t.get_device() != device.index for t in tensors] if device.type == "cuda" else [t.device != device for t in tensors]):
+        raise ValueError(f"tensors are on {' and '.join(sorted({str(t.device) for t in tensors}))}")
     if device is not None and torch.cuda.is_available():
         if device.type != "cuda":
             raise ValueError(f"tensors must be on the GPU, not on {device}")
         if device.index != torch.cuda.current_device():
             raise ValueError(f"tensors are on {device}, the current device is {torch.cuda.current_device()}")
     return device
+
+
+def _places(tensors):
+    return array("q", [t.data_ptr() if t is not None else 0 for t in tensors])
 
 
 def _run(entry, args, tensors, device):
@@ -64,17 +65,15 @@ def nuts_norm(tensors, *, max_norm=1.0):
     device = _of_one_device(tensors)
     if device is None:
         raise ValueError("nuts_norm needs a tensor")
-    table = np.zeros((len(tensors), 3), dtype=np.int64)
-    assert C.sizeof(_b.nuts_tensor) == 24
     try:
-        table[:] = [(t.data_ptr(), t.numel(), _DTYPES[t.dtype]) for t in tensors]  # (what is reserved behind the type stays 0)
+        table = array("q", [x for t in tensors for x in (t.data_ptr(), t.numel(), _DTYPES[t.dtype])])  # (0 behind the type)
     except KeyError as e:
         raise ValueError(f"tensors must be {' or '.join(str(d) for d in _DTYPES)}, not {e.args[0]}") from None
-    L, size = _b.lib(), C.c_int64()
-    _b._check(L.nuts_norm_workspace(table.ctypes.data, len(tensors), C.byref(size)))
+    L, size, at = _b.lib(), C.c_int64(), table.buffer_info()[0]
+    _b._check(L.nuts_norm_workspace(at, len(tensors), C.byref(size)))
     norm, factor = torch.empty(2, dtype=torch.float32, device=device).unbind(0)
-    workspace = torch.empty(size.value, dtype=torch.uint8, device=device) if device.type == "cuda" else None
-    _run(L.nuts_norm, [table.ctypes.data, len(tensors), float(max_norm), norm.data_ptr(), factor.data_ptr(),
+    workspace = torch.empty(size.value, dtype=torch.uint8, device=device) if size.value and device.type == "cuda" else None
+    _run(L.nuts_norm, [at, len(tensors), float(max_norm), norm.data_ptr(), factor.data_ptr(),
                        workspace.data_ptr() if workspace is not None else 256, size.value], [*tensors, norm, workspace], device)
     return Norm(norm, factor)
 
@@ -118,7 +117,6 @@ class Moments:
                                          (self.copies[i], "a copy", self.copy_dtype, p.numel())):
                 if t is not None and (t.dtype != dtype or t.numel() != size or not t.is_contiguous()):
                     raise ValueError(f"{what} of parameter {i} must be {size} {dtype} without gaps")
-        self._table = np.zeros((n, 8), dtype=np.int64)
         self._tensors = [t for each in zip(self.params, self.copies, *states) for t in each if t is not None]
         self.device = _of_one_device(self._tensors)
         self._describe()
@@ -128,14 +126,16 @@ class Moments:
             raise ValueError("parameters, moments and copies must not overlap")
 
     def _describe(self):
-        self._sizes = [p.numel() for p in self.params]
+        self._sizes, self._shapes = [p.numel() for p in self.params], [p.shape for p in self.params]
+        self._table = array("q", bytes(64 * len(self.params)))
         for column, tensors in ((_PARAM, self.params), (_COPY, self.copies), (_M, self.m), (_V, self.v), (_M_SCALE, self.m_scales), (_V_SCALE, self.v_scales)):
-            self._table[:, column] = [t.data_ptr() if t is not None else 0 for t in tensors]
-        self._table[:, _N] = self._sizes
+            self._table[column::8] = _places(tensors)
+        self._table[_N::8] = array("q", self._sizes)
+        self._at = self._table[_PARAM::8].tolist()
 
     def _check_places(self):
         """A parameter may have been given another place (`.data`) since: then it must still be of its kind."""
-        if [p.data_ptr() for p in self.params] != self._table[:, _PARAM].tolist():
+        if [p.data_ptr() for p in self.params] != self._at:
             if any(p.numel() != n or p.dtype != self.dtype or p.device != self.device or not p.is_contiguous() for p, n in zip(self.params, self._sizes)):
                 raise ValueError("a parameter has changed its size, type or device")
             self.__init__(self.params, bits=self.bits, copies=None if all(c is None for c in self.copies) else self.copies,
@@ -152,23 +152,19 @@ def nuts_adamw(moments, grads, *, step, lr, betas=(0.9, 0.999), eps=1e-8, weight
     if len(grads) != len(moments.params):
         raise ValueError(f"there are {len(moments.params)} parameters and {len(grads)} gradients")
     moments._check_places()
-    device, sizes, dtype, places, used = moments.device, moments._sizes, None, [], []
-    for g, n, p in zip(grads, sizes, moments.params):
-        if g is None:
-            places.append(0)
-            continue
-        if dtype is None:
-            dtype = g.dtype
-            if dtype not in _DTYPES:
-                raise ValueError(f"gradients must be {' or '.join(str(d) for d in _DTYPES)}")
-        if g.dtype != dtype or g.shape != p.shape or g.device != device:
-            raise ValueError(f"gradients must be {dtype} on {device}, each as its parameter")
-        if not g.is_contiguous():
-            g = g.contiguous()
-        places.append(g.data_ptr())
-        used.append(g)
-    if dtype is None:
+    device, used = moments.device, [g for g in grads if g is not None]
+    if not used:
         return
+    dtype = used[0].dtype
+    if dtype not in _DTYPES:
+        raise ValueError(f"gradients must be {' or '.join(str(d) for d in _DTYPES)}")
+    at = used[0].get_device()
+    if used[0].device != device or any([g is not None and (g.shape != shape or g.dtype is not dtype or g.get_device() != at) for g, shape in zip(grads, moments._shapes)]):
+        raise ValueError(f"gradients must be {dtype} on {device}, each as its parameter")
+    if not all([g.is_contiguous() for g in used]):
+        grads = [g.contiguous() if g is not None else None for g in grads]
+        used = [g for g in grads if g is not None]
+    places = _places(grads)
     if device.type == "cuda" and device.index != torch.cuda.current_device():
         raise ValueError(f"tensors are on {device}, the current device is {torch.cuda.current_device()}")
     step_at = lr_at = factor_at = None
@@ -179,11 +175,11 @@ def nuts_adamw(moments, grads, *, step, lr, betas=(0.9, 0.999), eps=1e-8, weight
     if factor is not None:
         factor_at = _scalar(factor, "factor", torch.float32, device)
         used.append(factor)
-    table = moments._table.copy()  # (calls on two threads have gradients of their own)
-    table[:, _GRAD] = places
+    table = moments._table[:]  # (calls on two threads have gradients of their own)
+    table[_GRAD::8] = places
     desc = _b.nuts_adamw_desc(_PARAM_DTYPES[moments.dtype], _DTYPES[dtype], _COPY_DTYPES[moments.copy_dtype], moments.bits, float(lr), float(betas[0]),
                               float(betas[1]), float(eps), float(weight_decay), float(scale), int(step), int(seed) & 0xFFFFFFFFFFFFFFFF)
-    _run(_b.lib().nuts_adamw, [C.byref(desc), table.ctypes.data, len(grads), step_at, lr_at, factor_at], _Both(moments._tensors, used), device)
+    _run(_b.lib().nuts_adamw, [C.byref(desc), table.buffer_info()[0], len(grads), step_at, lr_at, factor_at], _Both(moments._tensors, used), device)
 
 
 class _Both:
@@ -209,15 +205,13 @@ def nuts_adamw_values(moments, *, dtype=torch.float32, out=None):
     used = [t for t in (*m, *v) if t is not None]
     if not used:
         return m, v
-    dtype = used[0].dtype
-    for some in (m, v):
-        for t, n in zip(some, moments._sizes):
-            if t is not None and (t.dtype != dtype or dtype not in _DTYPES or t.numel() != n or not t.is_contiguous() or t.device != moments.device):
-                raise ValueError(f"out must be {' or '.join(str(d) for d in _DTYPES)} without gaps on {moments.device}, each as its parameter")
+    dtype, at = used[0].dtype, used[0].get_device()
+    if dtype not in _DTYPES or used[0].device != moments.device or any(
+            [t is not None and (t.numel() != n or t.dtype is not dtype or t.get_device() != at or not t.is_contiguous()) for some in (m, v) for t, n in zip(some, moments._sizes)]):
+        raise ValueError(f"out must be {' or '.join(str(d) for d in _DTYPES)} without gaps on {moments.device}, each as its parameter")
     if moments.device.type == "cuda" and moments.device.index != torch.cuda.current_device():
         raise ValueError(f"tensors are on {moments.device}, the current device is {torch.cuda.current_device()}")
-    table = moments._table.copy()
-    table[:, _PARAM] = [t.data_ptr() if t is not None else 0 for t in m]
-    table[:, _COPY] = [t.data_ptr() if t is not None else 0 for t in v]
-    _run(_b.lib().nuts_adamw_values, [table.ctypes.data, len(m), _DTYPES[dtype]], _Both(moments._tensors, used), moments.device)
+    table = moments._table[:]
+    table[_PARAM::8], table[_COPY::8] = _places(m), _places(v)
+    _run(_b.lib().nuts_adamw_values, [table.buffer_info()[0], len(m), _DTYPES[dtype]], _Both(moments._tensors, used), moments.device)
     return m, v
