@@ -5,7 +5,7 @@
 #include "nuts_cat.h"
 
 #include <algorithm>
-#include <climits>
+#include <type_traits>
 
 namespace nuts {
 namespace {
@@ -14,7 +14,8 @@ constexpr int kThreads = 512;
 constexpr int kSlice = 4096;        // classes of a workgroup, with a counter each in LDS
 constexpr int kColumns = 64;        // of a workgroup that joins the biases' gradients
 constexpr int kJoinThreads = 1024;
-constexpr int kGroups = 1024;       // workgroups that the rows are divided between where they are added up
+constexpr int64_t kBiasRows = 4;    // that are added up, at least: their sums are stored
+constexpr int kGroups = 1024, kGradGroups = 768;  // workgroups that the chip has at a time
 
 // A class's counter: how often it was said behind the prompt; whether it has a bias of its own; whether it was in the prompt.
 constexpr unsigned kPrompt = 1u << 31, kBiased = 1u << 30, kCount = kBiased - 1, kSeen = kPrompt | kCount;
@@ -39,6 +40,17 @@ struct PenaltyArgs {
     int n_classes, id_type, history_len, n_bias, slices, rows_each, streamed;
 };
 
+// What all threads read at a place that no thread of the launch writes: by way of the scalar cache, whose loads nobody waits for who waits for a row.
+template <typename V>
+__device__ __forceinline__ V uniform(const V* p)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    return *(const __attribute__((address_space(4))) V*)p;
+#else
+    return *p;
+#endif
+}
+
 __device__ __forceinline__ long id_at(const void* ids, int id_type, long i)
 {
     return id_type == NUTS_I64 ? static_cast<const int64_t*>(ids)[i] : (long)static_cast<const int32_t*>(ids)[i];
@@ -46,30 +58,20 @@ __device__ __forceinline__ long id_at(const void* ids, int id_type, long i)
 
 __device__ __forceinline__ int clamped(const int32_t* lengths, long row, int most, int otherwise)
 {
-    return lengths ? min(max(lengths[row], 0), most) : otherwise;
+    return lengths ? min(max(uniform(lengths + row), 0), most) : otherwise;
 }
-
-// What a workgroup's counters hold: the places 0 .. length - 1 of a row's history, the first `prompt` as prompt.
-struct Counted {
-    int length, prompt;
-};
-
-__device__ __forceinline__ bool may_come(const uint32_t* allowed, int v) { return !allowed || (allowed[v >> 5] >> (v & 31) & 1); }
 
 // Calls `see` for the places from .. to - 1 of a history that hold one of the classes begin .. begin + n - 1, thread by thread.
 template <typename Id, typename See>
 __device__ __forceinline__ void look_through(const Id* history, int from, int to, int begin, int n, See see)
 {
-    constexpr int kEach = 4, kN = 16 / sizeof(Id);
+    constexpr int kEach = 16 / sizeof(Id);
     for (int i = from + (int)threadIdx.x * kEach; i < to; i += kThreads * kEach) {
         Id id[kEach];
         if (i + kEach <= to) {
+            const Pack<Id, kEach> in = load_pack<Id, kEach>(history + i);
 #pragma unroll
-            for (int u = 0; u < kEach; u += kN) {
-                const Pack<Id, kN> in = load_pack<Id, kN>(history + i + u);
-#pragma unroll
-                for (int e = 0; e < kN; ++e) id[u + e] = in.v[e];
-            }
+            for (int e = 0; e < kEach; ++e) id[e] = in.v[e];
         } else {
 #pragma unroll
             for (int e = 0; e < kEach; ++e) id[e] = i + e < to ? history[i + e] : (Id)-1;
@@ -88,26 +90,163 @@ __device__ __forceinline__ void look_through(const PenaltyArgs& a, long row, int
     else look_through(static_cast<const int32_t*>(a.history) + row * a.history_stride, from, to, begin, n, see);
 }
 
-// Counters for the next row of a workgroup.  Where all rows have one history and the row has seen no less of it than the one before, they
-// are carried on: 4096 rows of one text of 4096 classes are counted once by each workgroup, not once by each row.  No
-// thread may still be reading them; the caller waits before they are read.
-__device__ __forceinline__ void count_on(const PenaltyArgs& a, long row, int begin, int n, Counted& done, const Counted& now, unsigned* count)
+// The class at a place of a row's history, as one of the slice, or -1: the same for all threads.
+__device__ __forceinline__ int class_in(const PenaltyArgs& a, long row, int i, int begin, int n)
 {
-    if (a.history_stride != 0 || now.length < done.length || now.prompt < done.prompt) {
-        for (int i = (int)threadIdx.x * 4; i < n; i += kThreads * 4) *reinterpret_cast<uint4*>(&count[i]) = uint4{0, 0, 0, 0};  // (kSlice is a multiple of 4)
-        done = Counted{0, 0};
+    const long at = row * a.history_stride + i;
+    const long id = a.id_type == NUTS_I64 ? (long)uniform(static_cast<const int64_t*>(a.history) + at) : (long)uniform(static_cast<const int32_t*>(a.history) + at);
+    const uint64_t v = (uint64_t)id - (uint64_t)begin;
+    return v < (uint64_t)n ? (int)v : -1;
+}
+
+// A row's history: how long it is, and how much of it is prompt.
+struct Seen {
+    int length, prompt;
+};
+__device__ __forceinline__ Seen seen_of(const PenaltyArgs& a, long row)
+{
+    return Seen{clamped(a.lengths, row, a.history_len, a.history_len), clamped(a.prompts, row, a.history_len, 0)};
+}
+
+// The counters of a thread's classes: those of its packs, of which pack u begins at class (u kThreads + thread) kN of the slice.
+template <typename T>
+constexpr int kPackN = 16 / sizeof(T);
+template <typename T>
+constexpr int kPacks = kSlice / kThreads / kPackN<T>;
+template <typename T>
+__device__ __forceinline__ int class_of_pack(int u)
+{
+    return (u * kThreads + (int)threadIdx.x) * kPackN<T>;
+}
+template <typename T>
+struct Counters {
+    unsigned c[kPacks<T>][kPackN<T>];
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int u = 0; u < kPacks<T>; ++u)
+#pragma unroll
+            for (int e = 0; e < kPackN<T>; ++e) c[u][e] = 0;
+    }
+    __device__ __forceinline__ unsigned any(int u) const
+    {
+        unsigned all = 0;
+#pragma unroll
+        for (int e = 0; e < kPackN<T>; ++e) all |= c[u][e];
+        return all;
+    }
+    // Counts from `shared`, which the workgroup makes of the places from .. to - 1, added to what is here.
+    __device__ __forceinline__ void add(const unsigned* shared)
+    {
+#pragma unroll
+        for (int u = 0; u < kPacks<T>; ++u)
+#pragma unroll
+            for (int e = 0; e < kPackN<T>; e += 4) {
+                const uint4 in = *reinterpret_cast<const uint4*>(&shared[class_of_pack<T>(u) + e]);
+                const unsigned more[4] = {in.x, in.y, in.z, in.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) c[u][e + k] = ((c[u][e + k] & ~kPrompt) + (more[k] & ~kPrompt)) | ((c[u][e + k] | more[k]) & kPrompt);
+            }
+    }
+    // One class of the slice (or none) was said, or what was counted as said is prompt.  (A wave whose it is not goes on at once; the one whose it is has no
+    // branches, which the compiler would make an index into memory.)
+    __device__ __forceinline__ void said(int v, bool prompt, bool again)
+    {
+#ifdef __HIP_DEVICE_COMPILE__
+#pragma unroll
+        for (int u = 0; u < kPacks<T>; ++u) {
+            const unsigned off = (unsigned)(v - class_of_pack<T>(u));
+            if (!__builtin_amdgcn_ballot_w64(off < (unsigned)kPackN<T>)) continue;
+#pragma unroll
+            for (int e = 0; e < kPackN<T>; ++e) {
+                const unsigned hit = off == (unsigned)e;
+                c[u][e] = prompt ? (c[u][e] - (hit & (unsigned)again)) | hit << 31 : c[u][e] + hit;
+            }
+        }
+#endif
+    }
+};
+
+// What single classes of a slice have as biases of their own.
+struct Biases {
+    float of[kSlice];
+    uint16_t v[NUTS_CAT_MAX_BIAS];  // (kSlice is less than 2^16)
+    float value[NUTS_CAT_MAX_BIAS];
+    int n;
+};
+// The row's biases of this slice, in their order: by one wave.
+__device__ __forceinline__ void list_biases(const PenaltyArgs& a, long row, int begin, int n, Biases& b)
+{
+    if (threadIdx.x >= 64) return;
+    int listed = 0;
+    for (int i = 0; i < a.n_bias; i += 64) {
+#ifdef __HIP_DEVICE_COMPILE__
+        const int k = i + (int)threadIdx.x;
+        const uint64_t v = k < a.n_bias ? (uint64_t)id_at(a.bias_ids, a.id_type, row * a.n_bias + k) - (uint64_t)begin : ~(uint64_t)0;
+        const unsigned long long mine = __builtin_amdgcn_ballot_w64(v < (uint64_t)n);
+        if (v < (uint64_t)n) {
+            const int at = listed + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mine >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mine, 0u));
+            b.v[at] = (uint16_t)v;
+            b.value[at] = a.bias_values[row * a.n_bias + k];
+        }
+        listed += __popcll(mine);
+#endif
+    }
+    if (threadIdx.x == 0) b.n = listed;
+}
+// The sums of each class's, in its counter's bit and in b.of: by the thread that has the first of them.
+__device__ __forceinline__ void add_biases(Biases& b, unsigned* shared)
+{
+    for (int i = threadIdx.x; i < b.n; i += kThreads) {
+        const int v = b.v[i];
+        bool first = true;
+        for (int k = 0; k < i; ++k) first &= b.v[k] != v;
+        if (!first) continue;
+        float sum = b.value[i];
+        for (int k = i + 1; k < b.n; ++k)
+            if (b.v[k] == v) sum += b.value[k];
+        b.of[v] = sum;
+        shared[v] |= kBiased;
+    }
+}
+
+// The counters of a slice from the places of a row's history, in LDS, where adding whole numbers in any order gives the same; `done`: how much of it they
+// have, if not nothing.
+template <typename T, typename B>
+__device__ __forceinline__ void count(const PenaltyArgs& a, long row, int begin, int n, const Seen& done, const Seen& now, unsigned* shared, B&& biases,
+                                      Counters<T>& counters)
+{
+    __syncthreads();
+    for (int i = (int)threadIdx.x * 4; i < kSlice; i += kThreads * 4) *reinterpret_cast<uint4*>(&shared[i]) = uint4{0, 0, 0, 0};
+    __syncthreads();
+    look_through(a, row, done.length, now.length, begin, n, [&](int i, int v) {
+        if (i >= now.prompt) atomicAdd(&shared[v], 1u);
+        else atomicOr(&shared[v], kPrompt);
+    });
+    __syncthreads();
+    if constexpr (std::is_same_v<B, Biases&>) {
+        add_biases(biases, shared);
         __syncthreads();
     }
-    if (now.prompt > done.prompt && done.prompt < done.length)
-        look_through(a, row, done.prompt, min(now.prompt, done.length), begin, n, [&](int, int v) {
-            atomicSub(&count[v], 1u);
-            atomicOr(&count[v], kPrompt);
-        });
-    look_through(a, row, done.length, now.length, begin, n, [&](int i, int v) {
-        if (i >= now.prompt) atomicAdd(&count[v], 1u);
-        else atomicOr(&count[v], kPrompt);
-    });
-    done = now;
+    if (done.length == 0) counters.clear();
+    counters.add(shared);
+}
+
+// Places of a history that a row has more than the one before and that each thread looks at by itself.
+constexpr int kFew = 16;
+
+// Where all rows have one history and a row has seen a little more of it than the one before, the counters stay in registers and what is new is added
+// to them: rows of one text wait for no one then.  False: it is not so.  (4096 rows of 50001 with their gradients: 362 us with
+// counters in LDS and barriers before and behind each row, MEASURED so.)
+template <typename T>
+__device__ __forceinline__ bool count_on(const PenaltyArgs& a, long row, int begin, int n, const Seen& done, const Seen& now, Counters<T>& counters)
+{
+    const int more = now.length - done.length, less = now.prompt - done.prompt;
+    if (more < 0 || less < 0 || more > kFew || less > kFew) return false;
+    for (int i = done.prompt; i < min(now.prompt, done.length); ++i) counters.said(class_in(a, row, i, begin, n), true, true);
+    for (int i = done.length; i < now.length; ++i) counters.said(class_in(a, row, i, begin, n), i < now.prompt, false);
+    return true;
 }
 
 struct RowFactors {
@@ -122,30 +261,31 @@ __device__ __forceinline__ float penalised(float x, unsigned count, const RowFac
     return z - (said ? __builtin_fmaf(p.f, (float)said, p.q) : 0.f);
 }
 
-// The packs of a thread in a slice: pack u begins at class (u kThreads + thread) kN.
+// A pack of a row, as many of its numbers as there are.
 template <typename T>
-constexpr int kPackN = 16 / sizeof(T);
-template <typename T>
-constexpr int kPacks = kSlice / kThreads / kPackN<T>;
-
+__device__ __forceinline__ Pack<T, kPackN<T>> load_some(const T* row, int v, int n)
+{
+    if (v + kPackN<T> <= n) return load_pack<T, kPackN<T>>(row + v);
+    Pack<T, kPackN<T>> in{};
+#pragma unroll
+    for (int e = 0; e < kPackN<T>; ++e)
+        if (v + e < n) in.v[e] = row[v + e];
+    return in;
+}
 template <typename T>
 struct Slice {
     Pack<T, kPackN<T>> pack[kPacks<T>];
-    // whole packs only: what is behind them is read one by one
     __device__ __forceinline__ void fetch(const T* row, int n)
     {
 #pragma unroll
-        for (int u = 0; u < kPacks<T>; ++u) {
-            const int v = (u * kThreads + (int)threadIdx.x) * kPackN<T>;
-            if (v + kPackN<T> <= n) pack[u] = load_pack<T, kPackN<T>>(row + v);
-        }
+        for (int u = 0; u < kPacks<T>; ++u) pack[u] = load_some(row, class_of_pack<T>(u), n);
     }
 };
 template <typename T>
-__device__ __forceinline__ void unpack(const Pack<T, kPackN<T>>& in, const T* row, int v, int n, float (&x)[kPackN<T>])
+__device__ __forceinline__ void unpack(const Pack<T, kPackN<T>>& in, float (&x)[kPackN<T>])
 {
 #pragma unroll
-    for (int e = 0; e < kPackN<T>; ++e) x[e] = v + kPackN<T> <= n ? to_float(in.v[e]) : v + e < n ? to_float(row[v + e]) : 0.f;
+    for (int e = 0; e < kPackN<T>; ++e) x[e] = to_float(in.v[e]);
 }
 template <typename T>
 __device__ __forceinline__ void write_pack(T* to, const float (&x)[kPackN<T>], int v, int n, bool streamed)
@@ -161,18 +301,20 @@ __device__ __forceinline__ void write_pack(T* to, const float (&x)[kPackN<T>], i
             if (v + e < n) to[v + e] = out.v[e];
     }
 }
-// The counters of a pack, and all of them together.
 template <int kN>
-__device__ __forceinline__ unsigned read_counts(const unsigned* count, unsigned (&c)[kN])
+__device__ __forceinline__ void read_bias(const float* bias, int v, int n, float (&b)[kN])
 {
-    unsigned any = 0;
+    if (v + kN <= n) {
 #pragma unroll
-    for (int e = 0; e < kN; e += 4) {
-        const uint4 in = *reinterpret_cast<const uint4*>(&count[e]);
-        c[e] = in.x, c[e + 1] = in.y, c[e + 2] = in.z, c[e + 3] = in.w;
-        any |= in.x | in.y | in.z | in.w;
+        for (int e = 0; e < kN; e += 4) {
+            const Pack<float, 4> in = load_pack<float, 4>(bias + v + e);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) b[e + k] = in.v[k];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) b[e] = v + e < n ? bias[v + e] : 0.f;
     }
-    return any;
 }
 // A bit for each class of a pack that may come.
 template <int kN>
@@ -182,166 +324,181 @@ __device__ __forceinline__ unsigned allowed_of(const uint32_t* allowed, int v, i
     return allowed && v < n ? reinterpret_cast<const unsigned char*>(allowed)[v >> 3] >> (v & 7) & kAll : kAll;
 }
 
-// A workgroup a slice of `rows_each` rows.  The history's counts are made in LDS, where adding whole numbers in any order gives the same.
-template <typename T>
+// A workgroup a slice of one row, or (kShared) of `rows_each` rows that have one history.
+template <typename T, bool kShared, bool kBiases>
 __global__ __launch_bounds__(kThreads, 8) void penalties_kernel(PenaltyArgs a)
 {
     constexpr int kN = kPackN<T>;
-    __shared__ __attribute__((aligned(16))) unsigned count[kSlice];
-    __shared__ int biased[NUTS_CAT_MAX_BIAS];
+    __shared__ __attribute__((aligned(16))) unsigned shared[kSlice];
+    __shared__ std::conditional_t<kBiases, Biases, int> biases;
     const long block = a.first_block + blockIdx.x, group = block / a.slices;
     const int begin = (int)(block % a.slices) * kSlice, n = min(kSlice, a.n_classes - begin);
     const bool sparse = a.logits == a.out && !a.bias;  // what nothing changes is left alone
-    const bool counting = a.history_len > 0 || a.n_bias > 0;
-    Counted done{INT_MAX, INT_MAX};  // (nothing yet: the first row begins anew)
-    const long end = min((group + 1) * a.rows_each, a.n_rows);
-    const T* x_row = static_cast<const T*>(a.logits) + group * a.rows_each * a.row_stride + begin;
-    for (long row = group * a.rows_each; row < end; ++row, x_row += a.row_stride) {
-        T* to = static_cast<T*>(a.out) + row * a.out_stride + begin;
-        const float* bias = a.bias ? a.bias + row * a.bias_stride + begin : nullptr;
-        const uint32_t* allowed = a.allowed ? a.allowed + row * a.allowed_stride + begin / 32 : nullptr;
-        const float r = a.repetition ? a.repetition[row] : a.r;
-        const RowFactors p{r, 1.f / r, a.frequency ? a.frequency[row] : a.f, a.presence ? a.presence[row] : a.q};
-        Slice<T> own;  // on its way while the history is counted
-        if (!sparse) own.fetch(x_row, n);
-        if (counting) {
-            for (int i = threadIdx.x; i < a.n_bias; i += kThreads) {
-                const long v = id_at(a.bias_ids, a.id_type, row * a.n_bias + i) - begin;
-                biased[i] = v >= 0 && v < n ? (int)v : -1;
-            }
-            count_on(a, row, begin, n, done, Counted{clamped(a.lengths, row, a.history_len, a.history_len), clamped(a.prompts, row, a.history_len, 0)}, count);
-            for (int i = threadIdx.x; i < a.n_bias; i += kThreads)
-                if (biased[i] >= 0) atomicOr(&count[biased[i]], kBiased);
-            __syncthreads();
-        }
-        // classes with biases of their own: by the thread that has the first of them
-        for (int i = threadIdx.x; i < a.n_bias; i += kThreads) {
-            const int v = biased[i];
-            if (v < 0) continue;
-            bool first = true;
-            for (int k = 0; k < i; ++k) first &= biased[k] != v;
-            if (!first) continue;
-            float sum = a.bias_values[row * a.n_bias + i];
-            for (int k = i + 1; k < a.n_bias; ++k)
-                if (biased[k] == v) sum += a.bias_values[row * a.n_bias + k];
-            float z = penalised(to_float(x_row[v]), count[v], p);
-            if (bias) z += bias[v];
-            z += sum;
-            to[v] = rounded<T>(may_come(allowed, v) ? z : -INFINITY);
-        }
+    long row = group * a.rows_each;
+    const long end = min(row + a.rows_each, a.n_rows);
+    const T* x_row = static_cast<const T*>(a.logits) + row * a.row_stride + begin;
+    Slice<T> next;
+    if (!sparse) next.fetch(x_row, n);
+    Counters<T> counters;
+    counters.clear();
+    float bias[kPacks<T>][kN];
+    unsigned may[kPacks<T>];
+    auto prepare = [&]() {  // what may be the same for all rows
 #pragma unroll
         for (int u = 0; u < kPacks<T>; ++u) {
-            const int v = (u * kThreads + (int)threadIdx.x) * kN;
+            if (a.bias) read_bias<kN>(a.bias + row * a.bias_stride + begin, class_of_pack<T>(u), n, bias[u]);
+            may[u] = allowed_of<kN>(a.allowed ? a.allowed + row * a.allowed_stride + begin / 32 : nullptr, class_of_pack<T>(u), n);
+        }
+    };
+    prepare();
+    auto finish_row = [&](const Slice<T>& own) {
+        const float r = a.repetition ? uniform(a.repetition + row) : a.r;
+        const RowFactors p{r, 1.f / r, a.frequency ? uniform(a.frequency + row) : a.f, a.presence ? uniform(a.presence + row) : a.q};
+        T* to = static_cast<T*>(a.out) + row * a.out_stride + begin;
+#pragma unroll
+        for (int u = 0; u < kPacks<T>; ++u) {
+            const int v = class_of_pack<T>(u);
             if (v >= n) break;
-            unsigned c[kN] = {};
-            const unsigned any = counting ? read_counts<kN>(&count[v], c) : 0;
-            const unsigned may = allowed_of<kN>(allowed, v, n);
+            const unsigned any = counters.any(u);
+            Pack<T, kN> in = own.pack[u];
             if (sparse) {
-                if (!any && may == (1u << kN) - 1) continue;
-                if (v + kN <= n) own.pack[u] = load_pack<T, kN>(x_row + v);
+                if (!any && may[u] == (1u << kN) - 1) continue;
+                in = load_some(x_row, v, n);
             }
             float x[kN];
-            unpack(own.pack[u], x_row, v, n, x);
+            unpack(in, x);
             if (any) {
 #pragma unroll
-                for (int e = 0; e < kN; ++e) x[e] = penalised(x[e], c[e], p);
+                for (int e = 0; e < kN; ++e) x[e] = penalised(x[e], counters.c[u][e], p);
             }
-            if (bias) {
+            if (a.bias) {
 #pragma unroll
-                for (int e = 0; e < kN; e += 4) {
-                    if (v + kN <= n) {
-                        const Pack<float, 4> b = load_pack<float, 4>(bias + v + e);
+                for (int e = 0; e < kN; ++e) x[e] += bias[u][e];
+            }
+            if constexpr (kBiases) {
+                if (any & kBiased) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) x[e + k] += b.v[k];
-                    } else {
-#pragma unroll
-                        for (int k = e; k < e + 4; ++k)
-                            if (v + k < n) x[k] += bias[v + k];
-                    }
+                    for (int e = 0; e < kN; ++e)
+                        if (counters.c[u][e] & kBiased) x[e] += biases.of[v + e];
                 }
             }
-            if (allowed) {
+            if (a.allowed) {
 #pragma unroll
-                for (int e = 0; e < kN; ++e) x[e] = may >> e & 1 ? x[e] : -INFINITY;
+                for (int e = 0; e < kN; ++e) x[e] = may[u] >> e & 1 ? x[e] : -INFINITY;
             }
-            if (any & kBiased) {
-#pragma unroll
-                for (int e = 0; e < kN; ++e)
-                    if (v + e < n && !(c[e] & kBiased)) to[v + e] = rounded<T>(x[e]);
-            } else {
-                write_pack(to, x, v, n, a.streamed);
-            }
+            write_pack(to, x, v, n, a.streamed);
         }
-        if (counting && row + 1 < end) {
-            __syncthreads();
-            if (a.n_bias > 0) {  // the next row's biases are others
-                for (int i = threadIdx.x; i < a.n_bias; i += kThreads)
-                    if (biased[i] >= 0) atomicAnd(&count[biased[i]], ~kBiased);
-                __syncthreads();
+    };
+    if constexpr (!kShared) {
+        if constexpr (kBiases) list_biases(a, row, begin, n, biases);
+        count(a, row, begin, n, Seen{0, 0}, seen_of(a, row), shared, biases, counters);
+        finish_row(next);
+    } else {
+        while (row < end) {
+            Seen done = seen_of(a, row);
+            if (a.history_len > 0) count(a, row, begin, n, Seen{0, 0}, done, shared, 0, counters);
+            while (true) {
+                const Slice<T> own = next;
+                if (!sparse && row + 1 < end) next.fetch(x_row + a.row_stride, n);
+                finish_row(own);
+                ++row;
+                x_row += a.row_stride;
+                if (row >= end) break;
+                if (a.bias_stride || a.allowed_stride) prepare();
+                const Seen now = seen_of(a, row);
+                if (!count_on(a, row, begin, n, done, now, counters)) break;
+                done = now;
             }
         }
     }
 }
 
-// A workgroup a slice of `rows_each` rows, whose gradients it adds up.
-template <typename T>
-__global__ __launch_bounds__(kThreads, 8) void penalties_grad_kernel(PenaltyArgs a)
+// A workgroup a slice of `rows_each` rows, whose gradients it adds up.  kShared: they have one history.
+template <typename T, bool kShared>
+__global__ __launch_bounds__(kThreads, 6) void penalties_grad_kernel(PenaltyArgs a)
 {
     constexpr int kN = kPackN<T>;
-    __shared__ __attribute__((aligned(16))) unsigned count[kSlice];
+    __shared__ __attribute__((aligned(16))) unsigned shared[kSlice];
     const long block = a.first_block + blockIdx.x, group = block / a.slices;
     const int begin = (int)(block % a.slices) * kSlice, n = min(kSlice, a.n_classes - begin);
     const bool sparse = a.grad_out == a.out && !a.grad_bias, counting = a.out && a.history_len > 0;
-    Counted done{INT_MAX, INT_MAX};
-    const long end = min((group + 1) * a.rows_each, a.n_rows);
-    const T* g_row = static_cast<const T*>(a.grad_out) + group * a.rows_each * a.grad_stride + begin;
+    long row = group * a.rows_each;
+    const long end = min(row + a.rows_each, a.n_rows);
+    const T* g_row = static_cast<const T*>(a.grad_out) + row * a.grad_stride + begin;
     float sum[kPacks<T>][kN] = {};
-    for (long row = group * a.rows_each; row < end; ++row, g_row += a.grad_stride) {
+    Slice<T> next;
+    if (!sparse) next.fetch(g_row, n);
+    Counters<T> counters;
+    counters.clear();
+    unsigned may[kPacks<T>];
+    auto prepare = [&]() {
+#pragma unroll
+        for (int u = 0; u < kPacks<T>; ++u) may[u] = allowed_of<kN>(a.allowed ? a.allowed + row * a.allowed_stride + begin / 32 : nullptr, class_of_pack<T>(u), n);
+    };
+    prepare();
+    auto finish_row = [&]() {
+        const Slice<T> own = next;
+        const float r = a.repetition ? uniform(a.repetition + row) : a.r, by_r = 1.f / r;
         const T* x_row = static_cast<const T*>(a.logits) + row * a.row_stride + begin;
         T* to = a.out ? static_cast<T*>(a.out) + row * a.out_stride + begin : nullptr;
-        const uint32_t* allowed = a.allowed ? a.allowed + row * a.allowed_stride + begin / 32 : nullptr;
-        const float r = a.repetition ? a.repetition[row] : a.r, by_r = 1.f / r;
-        Slice<T> own;
-        if (!sparse) own.fetch(g_row, n);
-        if (counting) {
-            count_on(a, row, begin, n, done, Counted{clamped(a.lengths, row, a.history_len, a.history_len), 0}, count);
-            __syncthreads();
-        }
+        // (loads come back in their order: what this row waits for goes before what the next one does)
+        Slice<T> logits{};
 #pragma unroll
         for (int u = 0; u < kPacks<T>; ++u) {
-            const int v = (u * kThreads + (int)threadIdx.x) * kN;
+            const int v = class_of_pack<T>(u);
+            if (counters.any(u)) logits.pack[u] = load_some(x_row, v, n);
+        }
+        if (!sparse && row + 1 < end) next.fetch(g_row + a.grad_stride, n);
+#pragma unroll
+        for (int u = 0; u < kPacks<T>; ++u) {
+            const int v = class_of_pack<T>(u);
             if (v >= n) break;
-            unsigned c[kN] = {};
-            const unsigned any = counting ? read_counts<kN>(&count[v], c) : 0;
-            const unsigned may = allowed_of<kN>(allowed, v, n);
+            const unsigned any = counters.any(u);
+            Pack<T, kN> in = own.pack[u];
             if (sparse) {
-                if (!any && may == (1u << kN) - 1) continue;
-                if (v + kN <= n) own.pack[u] = load_pack<T, kN>(g_row + v);
+                if (!any && may[u] == (1u << kN) - 1) continue;
+                in = load_some(g_row, v, n);
             }
             float g[kN];
-            unpack(own.pack[u], g_row, v, n, g);
+            unpack(in, g);
 #pragma unroll
             for (int e = 0; e < kN; ++e) {
-                if (!(may >> e & 1)) g[e] = 0.f;
+                if (a.allowed) g[e] = may[u] >> e & 1 ? g[e] : 0.f;
                 sum[u][e] += g[e];
             }
             if (!to) continue;
             if (any) {
-                Pack<T, kN> logits{};
-                if (v + kN <= n) logits = load_pack<T, kN>(x_row + v);
                 float x[kN];
-                unpack(logits, x_row, v, n, x);
+                unpack(logits.pack[u], x);
 #pragma unroll
-                for (int e = 0; e < kN; ++e) g[e] *= c[e] && (may >> e & 1) ? (x[e] > 0.f ? by_r : r) : 1.f;
+                for (int e = 0; e < kN; ++e) g[e] *= counters.c[u][e] && (may[u] >> e & 1) ? (x[e] > 0.f ? by_r : r) : 1.f;
             }
             write_pack(to, g, v, n, a.streamed);
         }
-        if (counting && row + 1 < end) __syncthreads();
+    };
+    auto seen = [&]() { return Seen{clamped(a.lengths, row, a.history_len, a.history_len), 0}; };
+    while (row < end) {
+        Seen done = seen();
+        if (counting) count(a, row, begin, n, Seen{0, 0}, done, shared, 0, counters);
+        while (true) {
+            finish_row();
+            ++row;
+            g_row += a.grad_stride;
+            if (row >= end) break;
+            if (a.allowed_stride) prepare();
+            if constexpr (!kShared) {
+                if (counting) break;
+            } else {
+                const Seen now = seen();
+                if (counting && !count_on(a, row, begin, n, done, now, counters)) break;
+                done = now;
+            }
+        }
     }
     if (!a.grad_bias) return;
 #pragma unroll
     for (int u = 0; u < kPacks<T>; ++u) {
-        const int v = (u * kThreads + (int)threadIdx.x) * kN;
+        const int v = class_of_pack<T>(u);
 #pragma unroll
         for (int e = 0; e < kN; ++e)
             if (v + e < n) a.grad_bias[group * a.n_classes + begin + v + e] = sum[u][e];
@@ -414,14 +571,18 @@ PenaltyArgs args_of(const nuts_penalties_desc* d)
     return a;
 }
 
-// Rows of a workgroup: for a launch of about kGroups, which is what the chip has at a time, but at least `least`.
-int64_t rows_of_group(const nuts_penalties_desc* d, int64_t least)
+// Rows of a workgroup, for a launch of `groups` workgroups, but at least `least`.
+int64_t rows_of_group(const nuts_penalties_desc* d, int64_t groups, int64_t least)
 {
-    return std::max<int64_t>(1, std::min(std::max(ceil_div(d->n_rows * ceil_div(d->n_classes, kSlice), kGroups), least), d->n_rows));
+    return std::max<int64_t>(1, std::min(std::max(ceil_div(d->n_rows * ceil_div(d->n_classes, kSlice), groups), least), d->n_rows));
 }
-// Rows go together where they have one history, whose counts are carried on.
-int64_t rows_of_group_sharing(const nuts_penalties_desc* d) { return d->history_len > 0 && d->history_stride == 0 ? rows_of_group(d, 1) : 1; }
-constexpr int64_t kBiasRows = 4;  // that are added up: their sums are stored
+// Rows go together where they have one history, whose counts are carried on, and where their gradients are added up.
+bool shares(const nuts_penalties_desc* d) { return d->history_len == 0 || d->history_stride == 0; }
+int64_t rows_each(const nuts_penalties_desc* d) { return shares(d) && d->n_bias == 0 ? rows_of_group(d, kGroups, 1) : 1; }
+int64_t grad_rows_each(const nuts_penalties_desc* d, bool bias)
+{
+    return bias ? rows_of_group(d, kGradGroups, kBiasRows) : shares(d) ? rows_of_group(d, kGradGroups, 1) : 1;
+}
 
 void launch(void (*kernel)(PenaltyArgs), PenaltyArgs a)
 {
@@ -461,8 +622,11 @@ int nuts_penalties(const nuts_penalties_desc* d, const void* logits, const void*
     a.bias_values = bias_values;
     a.allowed = allowed;
     a.out = out;
-    a.rows_each = (int)rows_of_group_sharing(d);
-    by_dtype(d->dtype, [&](auto t) { launch(penalties_kernel<decltype(t)>, a); });
+    a.rows_each = (int)rows_each(d);
+    by_dtype(d->dtype, [&](auto t) {
+        using T = decltype(t);
+        launch(d->n_bias > 0 ? penalties_kernel<T, false, true> : shares(d) ? penalties_kernel<T, true, false> : penalties_kernel<T, false, false>, a);
+    });
     NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
     return NUTS_OK;
 }
@@ -471,7 +635,7 @@ int nuts_penalties_grad_workspace(const nuts_penalties_desc* d, int64_t* bytes)
 {
     if (int rc = check_penalties(d, "nuts_penalties_grad_workspace")) return rc;
     if (!bytes) return api_fail(NUTS_E_INVALID_ARG, "nuts_penalties_grad_workspace: bytes must not be NULL");
-    *bytes = ceil_div(d->n_rows, rows_of_group(d, kBiasRows)) * d->n_classes * (int64_t)sizeof(float);
+    *bytes = ceil_div(d->n_rows, grad_rows_each(d, true)) * d->n_classes * (int64_t)sizeof(float);
     return NUTS_OK;
 }
 
@@ -490,7 +654,7 @@ int nuts_penalties_grad(const nuts_penalties_desc* d, const void* grad_out, int6
         if (grad_logits == grad_out && grad_stride != d->out_stride && d->n_rows > 1)
             return api_fail(NUTS_E_INVALID_ARG, "nuts_penalties_grad: in place grad_stride and out_stride must be the same");
     }
-    const int64_t rows_each = rows_of_group(d, kBiasRows), groups = ceil_div(d->n_rows, rows_each);
+    const int64_t groups = ceil_div(d->n_rows, grad_rows_each(d, true));
     if (grad_bias && groups > 0) {
         const int64_t bytes = groups * d->n_classes * (int64_t)sizeof(float);
         if (!workspace || workspace_bytes < bytes) return api_fail(NUTS_E_INVALID_ARG, "nuts_penalties_grad: needs a workspace of %lld bytes", (long long)bytes);
@@ -508,8 +672,11 @@ int nuts_penalties_grad(const nuts_penalties_desc* d, const void* grad_out, int6
     a.grad_stride = (long)grad_stride;
     a.out = grad_logits;
     a.grad_bias = grad_bias ? static_cast<float*>(workspace) : nullptr;
-    a.rows_each = grad_bias ? (int)rows_each : (int)rows_of_group_sharing(d);
-    by_dtype(d->dtype, [&](auto t) { launch(penalties_grad_kernel<decltype(t)>, a); });
+    a.rows_each = (int)grad_rows_each(d, grad_bias != nullptr);
+    by_dtype(d->dtype, [&](auto t) {
+        using T = decltype(t);
+        launch(shares(d) ? penalties_grad_kernel<T, true> : penalties_grad_kernel<T, false>, a);
+    });
     if (grad_bias) {
         constexpr long kMost = kMaxBlocks / (kJoinThreads / kThreads);
         for (long first = 0, blocks = (long)ceil_div(d->n_classes, kColumns); first < blocks; first += kMost)
