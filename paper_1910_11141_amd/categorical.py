@@ -290,7 +290,7 @@ def nuts_score_grad(x, weight, targets, lse, entropy=None, *, grad_logprob=None,
 
 def _factor(value, what, n, device):
     """(number of all rows, tensor of each row's) of a penalty's strength."""
-    if isinstance(value, torch.Tensor) and value.dim() > 0:
+    if type(value) is not float and isinstance(value, torch.Tensor) and value.dim() > 0:
         return 1.0, _per_row(value, what, n)
     return float(value), None
 
@@ -307,12 +307,20 @@ def _history(t, n):
     """(tensor, type, places in a row, from row to row) of the classes said before: [places] for all rows or [n, places]."""
     if t is None:
         return None, None, 0, 0
-    if t.dtype not in _ID_TYPES or t.dim() not in (1, 2) or (t.dim() == 2 and t.shape[0] not in (1, n)):
+    shape, id_type = t.shape, _ID_TYPES.get(t.dtype)
+    if len(shape) == 2 and shape[0] in (1, n):
+        rows, places = shape
+        apart, step = t.stride()
+    elif len(shape) == 1:
+        rows, places, apart, step = 1, shape[0], 0, t.stride(0)
+    else:
+        id_type = None
+    if id_type is None:
         raise ValueError(f"history must be int32 or int64 [places] or [{n}, places]")
-    one = t.dim() == 1 or t.shape[0] <= 1
-    if (t.shape[-1] > 1 and t.stride(-1) != 1) or (not one and 0 < t.stride(0) < t.shape[-1]):  # (rows that overlap, too)
+    if (places > 1 and step != 1) or (rows > 1 and 0 < apart < places):  # (rows that overlap, too)
         t = t.contiguous()
-    return t, _ID_TYPES[t.dtype], t.shape[-1], 0 if one else t.stride(0)
+        apart = places
+    return t, id_type, places, apart if rows > 1 else 0
 
 
 def _rows_like(logits):
@@ -321,8 +329,8 @@ def _rows_like(logits):
     n, classes = logits.shape
     line = 128 // logits.element_size()
     if n <= 1 or classes < 1024 or classes % line == 0:
-        return logits.new_empty((n, classes))
-    return logits.new_empty((n, (classes + line - 1) // line * line))[:, :classes]
+        return torch.empty((n, classes), dtype=logits.dtype, device=logits.device)
+    return torch.empty((n, (classes + line - 1) // line * line), dtype=logits.dtype, device=logits.device)[:, :classes]
 
 
 def nuts_penalties(logits, history=None, *, lengths=None, prompts=None, repetition=1.0, frequency=0.0, presence=0.0, bias=None,

@@ -12,9 +12,9 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kSlice = 4096;        // classes of a workgroup, with a counter each in LDS
-constexpr int kColumns = 64;        // of a workgroup that joins the biases' gradients
 constexpr int kJoinThreads = 1024;
-constexpr int64_t kBiasRows = 4;    // that are added up, at least: their sums are stored
+constexpr int kNarrow = 8192;       // classes: up to here 16 of them are joined by a workgroup, then 64
+constexpr int64_t kBiasRows = 2;    // that are added up, at least: their sums are stored
 constexpr int kGroups = 1024, kGradGroups = 768;  // workgroups that the chip has at a time
 
 // A class's counter: how often it was said behind the prompt; whether it has a bias of its own; whether it was in the prompt.
@@ -218,7 +218,7 @@ __device__ __forceinline__ void count(const PenaltyArgs& a, long row, int begin,
                                       Counters<T>& counters)
 {
     __syncthreads();
-    for (int i = (int)threadIdx.x * 4; i < kSlice; i += kThreads * 4) *reinterpret_cast<uint4*>(&shared[i]) = uint4{0, 0, 0, 0};
+    for (int i = (int)threadIdx.x * 4; i < (n + 7) / 8 * 8; i += kThreads * 4) *reinterpret_cast<uint4*>(&shared[i]) = uint4{0, 0, 0, 0};
     __syncthreads();
     look_through(a, row, done.length, now.length, begin, n, [&](int i, int v) {
         if (i >= now.prompt) atomicAdd(&shared[v], 1u);
@@ -505,7 +505,8 @@ __global__ __launch_bounds__(kThreads, 6) void penalties_grad_kernel(PenaltyArgs
     }
 }
 
-// Groups' sums as those of all rows: 64 classes a workgroup, the groups divided between its 16 waves.
+// Groups' sums as those of all rows: kColumns classes a workgroup, the groups divided between 1024 / kColumns rows of threads.
+template <int kColumns>
 __global__ __launch_bounds__(kJoinThreads) void join_bias_kernel(const float* part, float* grad_bias, long n_groups, int n_classes, long first_block)
 {
     constexpr int kParts = kJoinThreads / kColumns;
@@ -513,13 +514,17 @@ __global__ __launch_bounds__(kJoinThreads) void join_bias_kernel(const float* pa
     const long v = (first_block + blockIdx.x) * kColumns + threadIdx.x % kColumns;
     const int own = threadIdx.x / kColumns;
     float sum = 0.f;
-    if (v < n_classes)
+    if (v < n_classes) {
+#pragma unroll 4
         for (long k = own; k < n_groups; k += kParts) sum += part[k * n_classes + v];
+    }
     shared[own][threadIdx.x % kColumns] = sum;
     __syncthreads();
-    if (own != 0 || v >= n_classes) return;
-    for (int k = 1; k < kParts; ++k) sum += shared[k][threadIdx.x];
-    grad_bias[v] = sum;
+    for (int half = kParts / 2; half >= 1; half /= 2) {
+        if (own < half) shared[own][threadIdx.x % kColumns] += shared[own + half][threadIdx.x % kColumns];
+        __syncthreads();
+    }
+    if (own == 0 && v < n_classes) grad_bias[v] = shared[0][threadIdx.x];
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
@@ -678,9 +683,11 @@ int nuts_penalties_grad(const nuts_penalties_desc* d, const void* grad_out, int6
         launch(shares(d) ? penalties_grad_kernel<T, true> : penalties_grad_kernel<T, false>, a);
     });
     if (grad_bias) {
+        // few classes: more workgroups for them
+        const bool narrow = d->n_classes <= kNarrow;
         constexpr long kMost = kMaxBlocks / (kJoinThreads / kThreads);
-        for (long first = 0, blocks = (long)ceil_div(d->n_classes, kColumns); first < blocks; first += kMost)
-            hipLaunchKernelGGL(join_bias_kernel, dim3((unsigned)std::min(blocks - first, kMost)), dim3(kJoinThreads), 0, api_stream(),
+        for (long first = 0, blocks = (long)ceil_div(d->n_classes, narrow ? 16 : 64); first < blocks; first += kMost)
+            hipLaunchKernelGGL(narrow ? join_bias_kernel<16> : join_bias_kernel<64>, dim3((unsigned)std::min(blocks - first, kMost)), dim3(kJoinThreads), 0, api_stream(),
                                static_cast<const float*>(workspace), grad_bias, (long)groups, (int)d->n_classes, first);
     }
     NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);

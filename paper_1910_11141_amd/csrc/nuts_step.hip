@@ -277,23 +277,47 @@ __device__ __forceinline__ void random_words(unsigned c0, unsigned c1, unsigned 
 __device__ __forceinline__ float chance(unsigned bits) { return __builtin_fmaf((float)(bits & 1023u), 1.f / 1024.f, 0.5f / 1024.f); }
 
 // Codes of 8 bits.  x is what they stand for in units of the scale: 127^2, or 254^2, at a block's largest.  The code below x is the whole part of
-// its root, and where that comes out one too high or too low for a last place the comparison makes up for it: the
-// square roots need not be exact.
+// its root, and where that comes out one too high or too low for a last place the comparison makes up for it: these
+// square roots need not be exact.  All else is rounded as single operations are, so that a step has the same codes wherever it is made.
 __device__ __forceinline__ float m_value(float code, float scale) { return code * __builtin_fabsf(code) * scale; }
 __device__ __forceinline__ float root_value(float code, float scale) { return code * code * scale; }
-__device__ __forceinline__ float m_code(float m, float by_scale, unsigned word)
+struct Scale {
+    float of, by;  // by = 1 / of, 0 for 0
+};
+// x / scale, rounded once: a product that is at most a unit in the last place off, and its remainder (Markstein, 1990).
+__device__ __forceinline__ float in_units(float x, const Scale& s)
 {
-    const float x = __builtin_fabsf(m) * by_scale, c = fminf(floorf(__builtin_amdgcn_sqrtf(x)), 126.f);
+    const float q = x * s.by;
+    return __builtin_fmaf(__builtin_fmaf(-q, s.of, x), s.by, q);
+}
+__device__ __forceinline__ Scale scale_of(float top, float last)  // top / last^2
+{
+    // (a scale with fewer than 24 places is taken as 0)
+    const float of = top * (1.f / (last * last));
+    if (!(of >= 0x1p-126f)) return Scale{0.f, 0.f};
+    const float by = __builtin_amdgcn_rcpf(of);
+    return Scale{of, __builtin_fmaf(__builtin_fmaf(-of, by, 1.f), by, by)};
+}
+__device__ __forceinline__ float m_code(float m, const Scale& scale, unsigned word)
+{
+    const float x = in_units(__builtin_fabsf(m), scale), c = fminf(floorf(__builtin_amdgcn_sqrtf(x)), 126.f);
     const bool up = __builtin_fmaf(-c, c, x) > __builtin_fmaf(2.f, c, 1.f) * chance(word);
     return __builtin_copysignf(up ? c + 1.f : c, m);
 }
-__device__ __forceinline__ float v_code(float root, float by_scale, unsigned word)
+__device__ __forceinline__ float v_code(float root, const Scale& scale, unsigned word)
 {
-    const float x = root * by_scale, c = fminf(floorf(__builtin_amdgcn_sqrtf(x)), 253.f);
+    const float x = in_units(root, scale), c = fminf(floorf(__builtin_amdgcn_sqrtf(x)), 253.f);
     const float below = c * c, gap = __builtin_fmaf(2.f, c, 1.f);  // (c + 1)^2 - c^2
-    // x^2 - c^4 > ((c + 1)^4 - c^4) chance
-    const bool up = (x - below) * (x + below) > gap * __builtin_fmaf(2.f, below, gap) * chance(word >> 10);
+    // ((c + 1)^4 - c^4) chance
+    const bool up = x * x - below * below > gap * __builtin_fmaf(2.f, below, gap) * chance(word >> 10);
     return (int)up | ((int)(c == 0.f) & (int)(root > 0.f)) ? c + 1.f : c;
+}
+// The square root, rounded once: from one that is a unit or two in the last place off, and the remainder of its square.
+__device__ __forceinline__ float exact_root(float v)
+{
+    const float y = __builtin_amdgcn_rsqf(v), s = v * y;
+    const float root = __builtin_fmaf(__builtin_fmaf(-s, s, v), 0.5f * y, s);
+    return v >= 0x1p-126f && v < INFINITY ? root : __builtin_amdgcn_sqrtf(v);
 }
 
 constexpr unsigned kInfinite = 0x7f800000u;
@@ -365,7 +389,7 @@ __device__ __forceinline__ void decode(unsigned m_word, unsigned v_word, float m
     }
 }
 
-// A block's moments, four in each lane, as codes and scales.  A scale with fewer than 24 places is taken as 0.
+// A block's moments, four in each lane, as codes and scales.
 __device__ __forceinline__ void encode(const nuts_adamw_tensor& t, long block, long i, int n, float (&m)[4], float (&root)[4], const unsigned (&words)[4])
 {
     unsigned m_top = wave_max(max(max(size_of(m[0]), size_of(m[1])), max(size_of(m[2]), size_of(m[3]))));
@@ -386,22 +410,18 @@ __device__ __forceinline__ void encode(const nuts_adamw_tensor& t, long block, l
         m_top = wave_max(max(max(size_of(m[0]), size_of(m[1])), max(size_of(m[2]), size_of(m[3]))));
         v_top = wave_max(max(max(size_of(root[0]), size_of(root[1])), max(size_of(root[2]), size_of(root[3]))));
     }
-    constexpr float kLeast = 0x1p-126f;
-    float m_scale = __uint_as_float(m_top) * (1.f / (127.f * 127.f)), v_scale = __uint_as_float(v_top) * (1.f / (254.f * 254.f));
-    if (m_scale < kLeast) m_scale = 0.f;
-    if (v_scale < kLeast) v_scale = 0.f;
-    const float by_m = m_scale > 0.f ? __builtin_amdgcn_rcpf(m_scale) : 0.f, by_v = v_scale > 0.f ? __builtin_amdgcn_rcpf(v_scale) : 0.f;
+    const Scale m_scale = scale_of(__uint_as_float(m_top), 127.f), v_scale = scale_of(__uint_as_float(v_top), 254.f);
     unsigned m_word = 0, v_word = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        m_word |= ((unsigned)(int)m_code(m[e], by_m, words[e]) & 255u) << 8 * e;
-        v_word |= (unsigned)v_code(root[e], by_v, words[e]) << 8 * e;
+        m_word |= ((unsigned)(int)m_code(m[e], m_scale, words[e]) & 255u) << 8 * e;
+        v_word |= (unsigned)v_code(root[e], v_scale, words[e]) << 8 * e;
     }
     store_codes(t.m, i, n, (m_word & ~m_lost) | (m_lost & 0x80808080u));
     store_codes(t.v, i, n, v_word | v_lost);
     if (threadIdx.x % 64 == 0) {
-        t.m_scale[block] = m_scale;
-        t.v_scale[block] = v_scale;
+        t.m_scale[block] = m_scale.of;
+        t.v_scale[block] = v_scale.of;
     }
 }
 
@@ -429,7 +449,7 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const Factors& f, 
         const float x = g[e] * f.scale;
         m[e] = m[e] * a.beta1 + x * a.rest1;
         v[e] = v[e] * a.beta2 + x * x * a.rest2;
-        root[e] = __builtin_amdgcn_sqrtf(v[e]);  // (a unit in the last place off at most, as the reciprocal)
+        root[e] = kEight ? exact_root(v[e]) : __builtin_amdgcn_sqrtf(v[e]);  // (a unit in the last place off at most, as the reciprocal)
         p[e] = p[e] * f.keep - f.size * m[e] * __builtin_amdgcn_rcpf(root[e] * f.root_scale + a.eps);
         if (sizeof(P) == 2) p[e] = rounded_at_random(p[e], words[e]);
     }
