@@ -1,10 +1,12 @@
 """Builds the HIP library (libnuts_hip.so) for gfx950 with hipcc, in-tree."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import re
 import subprocess
 import sys
+import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
@@ -108,15 +110,27 @@ UBENCH_SRC = os.path.join(CSRC, "ubench", "issue_ubench.hip")
 UBENCH_LIB = os.path.join(HERE, "libnuts_ubench.so")
 
 
+# What reads PyTorch's tensors is host code, and the only code that knows PyTorch.
+TENSORS_SRC = os.path.join(CSRC, "binding", "tensors.cpp")
+TENSORS_LIB = os.path.join(HERE, "libnuts_tensors.so")
+
+
+def tensors_command():
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=1",
+            "-isystem", os.path.join(torch, "include"), "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+            "-I" + sysconfig.get_paths()["include"], TENSORS_SRC, "-o", TENSORS_LIB, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+
+
 def build(force: bool = True, verbose: bool = False) -> str:
-    """The sampler library, and the instruction-issue microbenchmark as a library of its own."""
-    if not force and not is_stale() and os.path.exists(UBENCH_LIB) and \
-            os.path.getmtime(UBENCH_LIB) >= os.path.getmtime(UBENCH_SRC):
+    """The library, the instruction-issue microbenchmark as a library of its own, and the reader of PyTorch's tensors as one."""
+    others = ((UBENCH_LIB, UBENCH_SRC), (TENSORS_LIB, TENSORS_SRC))
+    if not force and not is_stale() and all(os.path.exists(made) and os.path.getmtime(made) >= os.path.getmtime(source) for made, source in others):
         return LIB_PATH
     with tempfile.TemporaryDirectory() as tmp:
         objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in sources()]
         cmds = [[HIPCC] + flags_of(s) + ["--save-temps=obj", "-c", s, "-o", o] for s, o in zip(sources(), objects)]
-        cmds.append([HIPCC] + FLAGS + [UBENCH_SRC, "-o", UBENCH_LIB])
+        cmds += [[HIPCC] + FLAGS + [UBENCH_SRC, "-o", UBENCH_LIB], tensors_command()]
         for cmd in cmds if verbose else []:
             print(" ".join(cmd), file=sys.stderr)
         with ThreadPoolExecutor(max_workers=min(len(cmds), os.cpu_count() or 1)) as pool:  # one compiler per source

@@ -7,6 +7,7 @@ those of categorical.py go to, and autograd knows none of them, either: paramete
 from __future__ import annotations
 
 import ctypes as C
+import os
 from array import array
 from collections import namedtuple
 
@@ -21,25 +22,36 @@ Norm = namedtuple("Norm", "norm factor")
 
 _PARAM_DTYPES = {torch.float32: _b.NUTS_F32, torch.bfloat16: _b.NUTS_BF16}
 _COPY_DTYPES = {torch.bfloat16: _b.NUTS_BF16, torch.float16: _b.NUTS_F16}
+TENSORS_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libnuts_tensors.so")
 _PARAM, _GRAD, _COPY, _M, _V, _M_SCALE, _V_SCALE, _N = range(8)  # columns of a table of nuts_adamw_tensor
 assert C.sizeof(_b.nuts_adamw_tensor) == 64 and C.sizeof(_b.nuts_tensor) == 24
 
 
-def _of_one_device(tensors):
-    """The device of `tensors` (None where there are none), which must be the current one."""
-    device = tensors[0].device if tensors else None
-    if device is not None and any([t.get_device() != device.index for t in tensors] if device.type == "cuda" else [t.device != device for t in tensors]):
-        raise ValueError(f"tensors are on {' and '.join(sorted({str(t.device) for t in tensors}))}")
-    if device is not None and torch.cuda.is_available():
+_tensors = None
+_SEVERAL_TYPES, _SEVERAL_DEVICES, _GAPS, _OTHER_SHAPES, _MOVED = 1, 2, 4, 8, 16
+
+
+def _read(tensors, like, table, width, address, count=-1, type_=-1):
+    """Columns of `table`, rows of `width` numbers, from a list of tensors (or None); bits of what they have not in common."""
+    global _tensors
+    if _tensors is None:
+        if not os.path.exists(TENSORS_PATH):
+            raise ImportError(f"{TENSORS_PATH} is missing: run `python -c 'import __graft_entry__ as g; g.build()'`")
+        lib = C.PyDLL(TENSORS_PATH)
+        lib.nuts_tensor_table.argtypes = [C.py_object, C.py_object, C.c_void_p] + [C.c_int64] * 4
+        lib.nuts_tensor_table.restype = C.c_int
+        _tensors = lib.nuts_tensor_table
+    return _tensors(tensors, like, table.buffer_info()[0], width, address, count, type_)
+
+
+def _current(device):
+    """`device`, which must be the current one where there is one."""
+    if torch.cuda.is_available():
         if device.type != "cuda":
             raise ValueError(f"tensors must be on the GPU, not on {device}")
         if device.index != torch.cuda.current_device():
             raise ValueError(f"tensors are on {device}, the current device is {torch.cuda.current_device()}")
     return device
-
-
-def _places(tensors):
-    return array("q", [t.data_ptr() if t is not None else 0 for t in tensors])
 
 
 def _run(entry, args, tensors, device):
@@ -60,15 +72,20 @@ def _scalar(t, what, dtype, device):
 
 def nuts_norm(tensors, *, max_norm=1.0):
     """(norm, factor), float32 scalars on the device: the square root of the sum of all squares of `tensors`, and what all of them are to
-    be multiplied with so that it is no more than max_norm (NaN where the norm is not finite)."""
-    tensors = [t if t.is_contiguous() else t.contiguous() for t in tensors]
-    device = _of_one_device(tensors)
-    if device is None:
+    be multiplied with so that it is no more than max_norm (NaN where the norm is not finite).  None among them counts as nothing."""
+    tensors = [t for t in tensors if t is not None]
+    if not tensors:
         raise ValueError("nuts_norm needs a tensor")
-    try:
-        table = array("q", [x for t in tensors for x in (t.data_ptr(), t.numel(), _DTYPES[t.dtype])])  # (0 behind the type)
-    except KeyError as e:
-        raise ValueError(f"tensors must be {' or '.join(str(d) for d in _DTYPES)}, not {e.args[0]}") from None
+    table = array("q", bytes(24 * len(tensors)))
+    bits = _read(tensors, None, table, 3, 0, 1, 2)
+    if bits & _GAPS:
+        tensors = [t.contiguous() for t in tensors]
+        _read(tensors, None, table, 3, 0, 1, 2)
+    if bits & _SEVERAL_DEVICES:
+        raise ValueError("tensors must be on one device")
+    if bits & _SEVERAL_TYPES and -1 in table[2::3] or tensors[0].dtype not in _DTYPES:
+        raise ValueError(f"tensors must be {' or '.join(str(d) for d in _DTYPES)}")
+    device = _current(tensors[0].device)
     L, size, at = _b.lib(), C.c_int64(), table.buffer_info()[0]
     _b._check(L.nuts_norm_workspace(at, len(tensors), C.byref(size)))
     norm, factor = torch.empty(2, dtype=torch.float32, device=device).unbind(0)
@@ -118,7 +135,6 @@ class Moments:
                 if t is not None and (t.dtype != dtype or t.numel() != size or not t.is_contiguous()):
                     raise ValueError(f"{what} of parameter {i} must be {size} {dtype} without gaps")
         self._tensors = [t for each in zip(self.params, self.copies, *states) for t in each if t is not None]
-        self.device = _of_one_device(self._tensors)
         self._describe()
         # two of them in one place would be written by two workgroups at a time
         spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self._tensors if t.numel())
@@ -126,20 +142,26 @@ class Moments:
             raise ValueError("parameters, moments and copies must not overlap")
 
     def _describe(self):
-        self._sizes, self._shapes = [p.numel() for p in self.params], [p.shape for p in self.params]
+        self._sizes = [p.numel() for p in self.params]
         self._table = array("q", bytes(64 * len(self.params)))
-        for column, tensors in ((_PARAM, self.params), (_COPY, self.copies), (_M, self.m), (_V, self.v), (_M_SCALE, self.m_scales), (_V_SCALE, self.v_scales)):
-            self._table[column::8] = _places(tensors)
+        lists = ((_PARAM, self.params), (_COPY, self.copies), (_M, self.m), (_V, self.v), (_M_SCALE, self.m_scales), (_V_SCALE, self.v_scales))
+        for column, tensors in lists:
+            _read(tensors, None, self._table, 8, column)
         self._table[_N::8] = array("q", self._sizes)
-        self._at = self._table[_PARAM::8].tolist()
+        if any(t.device != self.params[0].device for t in self._tensors):
+            raise ValueError("parameters, moments and copies must be on one device")
+        self.device = _current(self.params[0].device)
 
-    def _check_places(self):
-        """A parameter may have been given another place (`.data`) since: then it must still be of its kind."""
-        if [p.data_ptr() for p in self.params] != self._at:
+    def _now(self):
+        """The table.  A parameter may have been given another place (`.data`) since: then it must still be of its kind."""
+        table = self._table[:]
+        if _read(self.params, None, table, 8, _PARAM) & _MOVED:
             if any(p.numel() != n or p.dtype != self.dtype or p.device != self.device or not p.is_contiguous() for p, n in zip(self.params, self._sizes)):
                 raise ValueError("a parameter has changed its size, type or device")
             self.__init__(self.params, bits=self.bits, copies=None if all(c is None for c in self.copies) else self.copies,
                           states=(self.m, self.v) if self.bits == 32 else (self.m, self.v, self.m_scales, self.v_scales))
+            table = self._table[:]
+        return table  # (calls on two threads have gradients of their own)
 
 
 def nuts_adamw(moments, grads, *, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, scale=1.0, factor=None, seed=0):
@@ -151,22 +173,17 @@ def nuts_adamw(moments, grads, *, step, lr, betas=(0.9, 0.999), eps=1e-8, weight
     grads = list(grads)
     if len(grads) != len(moments.params):
         raise ValueError(f"there are {len(moments.params)} parameters and {len(grads)} gradients")
-    moments._check_places()
-    device, used = moments.device, [g for g in grads if g is not None]
-    if not used:
+    first = next((g for g in grads if g is not None), None)
+    if first is None:
         return
-    dtype = used[0].dtype
-    if dtype not in _DTYPES:
-        raise ValueError(f"gradients must be {' or '.join(str(d) for d in _DTYPES)}")
-    at = used[0].get_device()
-    if used[0].device != device or any([g is not None and (g.shape != shape or g.dtype is not dtype or g.get_device() != at) for g, shape in zip(grads, moments._shapes)]):
-        raise ValueError(f"gradients must be {dtype} on {device}, each as its parameter")
-    if not all([g.is_contiguous() for g in used]):
+    table, dtype, device = moments._now(), first.dtype, _current(moments.device)
+    bits = _read(grads, moments.params, table, 8, _GRAD)
+    if bits & (_SEVERAL_TYPES | _SEVERAL_DEVICES | _OTHER_SHAPES) or dtype not in _DTYPES or first.device != device:
+        raise ValueError(f"gradients must be {' or '.join(str(d) for d in _DTYPES)}, all of one type, on {device}, each as its parameter")
+    if bits & _GAPS:
         grads = [g.contiguous() if g is not None else None for g in grads]
-        used = [g for g in grads if g is not None]
-    places = _places(grads)
-    if device.type == "cuda" and device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {device}, the current device is {torch.cuda.current_device()}")
+        _read(grads, moments.params, table, 8, _GRAD)
+    used = [g for g in grads if g is not None]
     step_at = lr_at = factor_at = None
     if isinstance(step, torch.Tensor):
         step_at, step = _scalar(step, "step", torch.int64, device), used.append(step) or 1
@@ -175,8 +192,6 @@ def nuts_adamw(moments, grads, *, step, lr, betas=(0.9, 0.999), eps=1e-8, weight
     if factor is not None:
         factor_at = _scalar(factor, "factor", torch.float32, device)
         used.append(factor)
-    table = moments._table[:]  # (calls on two threads have gradients of their own)
-    table[_GRAD::8] = places
     desc = _b.nuts_adamw_desc(_PARAM_DTYPES[moments.dtype], _DTYPES[dtype], _COPY_DTYPES[moments.copy_dtype], moments.bits, float(lr), float(betas[0]),
                               float(betas[1]), float(eps), float(weight_decay), float(scale), int(step), int(seed) & 0xFFFFFFFFFFFFFFFF)
     _run(_b.lib().nuts_adamw, [C.byref(desc), table.buffer_info()[0], len(grads), step_at, lr_at, factor_at], _Both(moments._tensors, used), device)
@@ -205,13 +220,9 @@ def nuts_adamw_values(moments, *, dtype=torch.float32, out=None):
     used = [t for t in (*m, *v) if t is not None]
     if not used:
         return m, v
-    dtype, at = used[0].dtype, used[0].get_device()
-    if dtype not in _DTYPES or used[0].device != moments.device or any(
-            [t is not None and (t.numel() != n or t.dtype is not dtype or t.get_device() != at or not t.is_contiguous()) for some in (m, v) for t, n in zip(some, moments._sizes)]):
-        raise ValueError(f"out must be {' or '.join(str(d) for d in _DTYPES)} without gaps on {moments.device}, each as its parameter")
-    if moments.device.type == "cuda" and moments.device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {moments.device}, the current device is {torch.cuda.current_device()}")
-    table = moments._table[:]
-    table[_PARAM::8], table[_COPY::8] = _places(m), _places(v)
-    _run(_b.lib().nuts_adamw_values, [table.buffer_info()[0], len(m), _DTYPES[dtype]], _Both(moments._tensors, used), moments.device)
+    table, device, dtype = moments._now(), _current(moments.device), used[0].dtype
+    bits = _read(m, moments.params, table, 8, _PARAM) | _read(v, moments.params, table, 8, _COPY)
+    if bits & (_SEVERAL_TYPES | _SEVERAL_DEVICES | _OTHER_SHAPES | _GAPS) or dtype not in _DTYPES or any(t.dtype != dtype or t.device != device for t in (used[0], used[-1])):
+        raise ValueError(f"out must be {' or '.join(str(d) for d in _DTYPES)}, all of one type, without gaps, on {device}, each as its parameter")
+    _run(_b.lib().nuts_adamw_values, [table.buffer_info()[0], len(m), _DTYPES[dtype]], _Both(moments._tensors, used), device)
     return m, v

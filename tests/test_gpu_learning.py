@@ -69,7 +69,7 @@ def test_norm_of_what_is_not_finite(x):
 
 
 def test_norm_of_nothing():
-    got = nuts.nuts_norm([torch.zeros(0, device="cuda"), torch.zeros(5, device="cuda")])
+    got = nuts.nuts_norm([torch.zeros(0, device="cuda"), None, torch.zeros(5, device="cuda")])
     assert float(got.norm) == 0.0 and float(got.factor) == 1.0
 
 

@@ -191,6 +191,33 @@ def test_tensors_that_do_not_fit():
         nuts.nuts_adamw(mo, [torch.zeros(3, 8), g[1]], step=1, lr=0.1)
 
 
+def test_lists_that_are_not_of_tensors():
+    x = torch.zeros(4, 8)
+    for call in (lambda: nuts.nuts_norm([x, 1.0]), lambda: nuts.nuts_norm([x.to_sparse()]), lambda: nuts.Moments([x], states=([3], [x.clone()])),
+                 lambda: nuts.nuts_adamw(nuts.Moments([x]), ["x"], step=1, lr=0.1)):
+        with pytest.raises((TypeError, AttributeError, ValueError)):
+            call()
+
+
+def test_tables_are_read_from_lists():
+    from array import array
+    from paper_1910_11141_amd import learning as G
+    x = [torch.zeros(4, 8), torch.zeros(5), None, torch.nn.Parameter(torch.zeros(2, 3))]
+    table = array("q", [-7] * 20)
+    assert G._read(x, None, table, 5, 1, 2, 4) == G._MOVED
+    at = [t.data_ptr() if t is not None else 0 for t in x]
+    assert table.tolist() == [-7, at[0], 32, -7, 0, -7, at[1], 5, -7, 0, -7, 0, 0, -7, -7, -7, at[3], 6, -7, 0]
+    assert G._read(x, None, table, 5, 1, 2, 4) == 0
+    assert G._read(x, [torch.zeros(4, 8), torch.zeros(5), torch.zeros(1), torch.zeros(6)], table, 5, 1) == G._OTHER_SHAPES
+    assert G._read([x[0], x[1].half()], None, table, 5, 3, -1, 4) == G._SEVERAL_TYPES | G._MOVED and table[4::5].tolist()[:2] == [0, 3]
+    assert G._read([x[0].t()], None, table, 5, 1) == G._GAPS
+    assert G._read([torch.zeros(3, dtype=torch.int8)], None, table, 5, -1, -1, 0) == 0 and table[0] == -1
+    assert G._read([], None, table, 5, 1) == 0
+    for bad in ((None, None), ((x[0],), None), ([x[0]], [])):
+        with pytest.raises(TypeError):
+            G._read(*bad, table, 5, 1)
+
+
 def test_numbers_that_the_library_refuses():
     x = torch.zeros(4, 8)
     for call in (lambda: nuts.nuts_penalties(x, repetition=0.0), lambda: nuts.nuts_penalties(x, frequency=NAN),
