@@ -380,7 +380,7 @@ typedef struct {
     int64_t out_stride;     /* of what is written, >= n_classes                                            */
     int64_t allowed_stride; /* 32-bit words from one row of `allowed` to the next; 0: one row for all      */
     int64_t bias_stride;    /* of `bias`, >= n_classes; 0: one row for all                                 */
-    int64_t history_len;    /* 0 .. 2^30 - 1: places in a row of the history                               */
+    int64_t history_len;    /* 0 .. 2^29 - 1: places in a row of the history                               */
     int64_t history_stride; /* >= history_len; 0: one row for all                                          */
     int64_t n_bias;         /* 0 .. 1024: single classes with a bias, in each row                          */
     double repetition;      /* what all rows have where the array of that name is NULL: finite, > 0        */

@@ -10,15 +10,24 @@
 namespace nuts {
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kSlice = 4096;        // classes of a workgroup, with a counter each in LDS
+// A workgroup's threads, and the classes that it has a counter for in LDS: a slice.  Each slice looks through the whole history, so long ones want wide
+// slices; all others want many workgroups.
+struct Usual {
+    static constexpr int kThreads = 512, kSlice = 4096;
+};
+struct Wide {
+    static constexpr int kThreads = 1024, kSlice = 16384;
+};
 constexpr int kJoinThreads = 1024;
+constexpr int kLong = 2048;           // places of a history from which on slices are wide, if there are kFull of them
+constexpr int kFull = 512;
 constexpr int kNarrow = 8192;       // classes: up to here 16 of them are joined by a workgroup, then 64
 constexpr int64_t kBiasRows = 2;    // that are added up, at least: their sums are stored
 constexpr int kGroups = 1024, kGradGroups = 768;  // workgroups that the chip has at a time
 
-// A class's counter: how often it was said behind the prompt; whether it has a bias of its own; whether it was in the prompt.
-constexpr unsigned kPrompt = 1u << 31, kBiased = 1u << 30, kCount = kBiased - 1, kSeen = kPrompt | kCount;
+// A class's counter: how often it was said behind the prompt; whether it was in the prompt; whether it has a bias of its own, or several.
+constexpr unsigned kPrompt = 1u << 31, kBiased = 1u << 30, kAgain = 1u << 29, kCount = kAgain - 1, kSeen = kPrompt | kCount;
+constexpr unsigned kPlace = NUTS_CAT_MAX_BIAS - 1;  // of the bias that stands for a class
 
 struct PenaltyArgs {
     const void* logits;
@@ -62,32 +71,41 @@ __device__ __forceinline__ int clamped(const int32_t* lengths, long row, int mos
 }
 
 // Calls `see` for the places from .. to - 1 of a history that hold one of the classes begin .. begin + n - 1, thread by thread.
-template <typename Id, typename See>
+template <typename W, typename Id, typename See>
 __device__ __forceinline__ void look_through(const Id* history, int from, int to, int begin, int n, See see)
 {
-    constexpr int kEach = 16 / sizeof(Id);
-    for (int i = from + (int)threadIdx.x * kEach; i < to; i += kThreads * kEach) {
-        Id id[kEach];
+    constexpr int kEach = 16 / sizeof(Id), kStep = W::kThreads * kEach, kFlight = 4;
+    auto look = [&](Id id, int i) {
+        const uint64_t v = (uint64_t)(int64_t)id - (uint64_t)begin;
+        if (v < (uint64_t)n) see(i, (int)v);
+    };
+    long i = from + (long)threadIdx.x * kEach;
+    for (; i + (kFlight - 1) * kStep + kEach <= to; i += kFlight * kStep) {
+        Pack<Id, kEach> in[kFlight];
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) in[u] = load_pack<Id, kEach>(history + i + u * kStep);
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u)
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) look(in[u].v[e], (int)i + u * kStep + e);
+    }
+    for (; i < to; i += kStep) {
         if (i + kEach <= to) {
             const Pack<Id, kEach> in = load_pack<Id, kEach>(history + i);
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) id[e] = in.v[e];
+            for (int e = 0; e < kEach; ++e) look(in.v[e], (int)i + e);
         } else {
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) id[e] = i + e < to ? history[i + e] : (Id)-1;
-        }
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const uint64_t v = (uint64_t)(int64_t)id[e] - (uint64_t)begin;
-            if (v < (uint64_t)n && i + e < to) see(i + e, (int)v);
+            for (int e = 0; e < kEach; ++e)
+                if (i + e < to) look(history[i + e], (int)i + e);
         }
     }
 }
-template <typename See>
+template <typename W, typename See>
 __device__ __forceinline__ void look_through(const PenaltyArgs& a, long row, int from, int to, int begin, int n, See see)
 {
-    if (a.id_type == NUTS_I64) look_through(static_cast<const int64_t*>(a.history) + row * a.history_stride, from, to, begin, n, see);
-    else look_through(static_cast<const int32_t*>(a.history) + row * a.history_stride, from, to, begin, n, see);
+    if (a.id_type == NUTS_I64) look_through<W>(static_cast<const int64_t*>(a.history) + row * a.history_stride, from, to, begin, n, see);
+    else look_through<W>(static_cast<const int32_t*>(a.history) + row * a.history_stride, from, to, begin, n, see);
 }
 
 // The class at a place of a row's history, as one of the slice, or -1: the same for all threads.
@@ -108,24 +126,24 @@ __device__ __forceinline__ Seen seen_of(const PenaltyArgs& a, long row)
     return Seen{clamped(a.lengths, row, a.history_len, a.history_len), clamped(a.prompts, row, a.history_len, 0)};
 }
 
-// The counters of a thread's classes: those of its packs, of which pack u begins at class (u kThreads + thread) kN of the slice.
+// The counters of a thread's classes: those of its packs, of which pack u begins at class (u threads + thread) kN of the slice.
 template <typename T>
 constexpr int kPackN = 16 / sizeof(T);
-template <typename T>
-constexpr int kPacks = kSlice / kThreads / kPackN<T>;
-template <typename T>
+template <typename W, typename T>
+constexpr int kPacks = W::kSlice / W::kThreads / kPackN<T>;
+template <typename W, typename T>
 __device__ __forceinline__ int class_of_pack(int u)
 {
-    return (u * kThreads + (int)threadIdx.x) * kPackN<T>;
+    return (u * W::kThreads + (int)threadIdx.x) * kPackN<T>;
 }
-template <typename T>
+template <typename W, typename T>
 struct Counters {
-    unsigned c[kPacks<T>][kPackN<T>];
+    unsigned c[kPacks<W, T>][kPackN<T>];
 
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
-        for (int u = 0; u < kPacks<T>; ++u)
+        for (int u = 0; u < kPacks<W, T>; ++u)
 #pragma unroll
             for (int e = 0; e < kPackN<T>; ++e) c[u][e] = 0;
     }
@@ -136,17 +154,14 @@ struct Counters {
         for (int e = 0; e < kPackN<T>; ++e) all |= c[u][e];
         return all;
     }
-    // Counts from `shared`, which the workgroup makes of the places from .. to - 1, added to what is here.
-    __device__ __forceinline__ void add(const unsigned* shared)
+    __device__ __forceinline__ void read(const unsigned* shared)
     {
 #pragma unroll
-        for (int u = 0; u < kPacks<T>; ++u)
+        for (int u = 0; u < kPacks<W, T>; ++u)
 #pragma unroll
             for (int e = 0; e < kPackN<T>; e += 4) {
-                const uint4 in = *reinterpret_cast<const uint4*>(&shared[class_of_pack<T>(u) + e]);
-                const unsigned more[4] = {in.x, in.y, in.z, in.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) c[u][e + k] = ((c[u][e + k] & ~kPrompt) + (more[k] & ~kPrompt)) | ((c[u][e + k] | more[k]) & kPrompt);
+                const uint4 in = *reinterpret_cast<const uint4*>(&shared[class_of_pack<W, T>(u) + e]);
+                c[u][e] = in.x, c[u][e + 1] = in.y, c[u][e + 2] = in.z, c[u][e + 3] = in.w;
             }
     }
     // One class of the slice (or none) was said, or what was counted as said is prompt.  (A wave whose it is not goes on at once; the one whose it is has no
@@ -155,8 +170,8 @@ struct Counters {
     {
 #ifdef __HIP_DEVICE_COMPILE__
 #pragma unroll
-        for (int u = 0; u < kPacks<T>; ++u) {
-            const unsigned off = (unsigned)(v - class_of_pack<T>(u));
+        for (int u = 0; u < kPacks<W, T>; ++u) {
+            const unsigned off = (unsigned)(v - class_of_pack<W, T>(u));
             if (!__builtin_amdgcn_ballot_w64(off < (unsigned)kPackN<T>)) continue;
 #pragma unroll
             for (int e = 0; e < kPackN<T>; ++e) {
@@ -168,69 +183,84 @@ struct Counters {
     }
 };
 
-// What single classes of a slice have as biases of their own.
+// What single classes have as biases of their own: the row's, in their order, those of other slices with no class.  One of a class's biases stands
+// for it in the end: its value is their sum, its count what was counted, and the class's counter is its place.
 struct Biases {
-    float of[kSlice];
-    uint16_t v[NUTS_CAT_MAX_BIAS];  // (kSlice is less than 2^16)
+    alignas(16) uint16_t v[NUTS_CAT_MAX_BIAS];  // (eight at a time, the last ones with kNone behind them)
     float value[NUTS_CAT_MAX_BIAS];
-    int n;
-};
-// The row's biases of this slice, in their order: by one wave.
-__device__ __forceinline__ void list_biases(const PenaltyArgs& a, long row, int begin, int n, Biases& b)
-{
-    if (threadIdx.x >= 64) return;
-    int listed = 0;
-    for (int i = 0; i < a.n_bias; i += 64) {
-#ifdef __HIP_DEVICE_COMPILE__
-        const int k = i + (int)threadIdx.x;
-        const uint64_t v = k < a.n_bias ? (uint64_t)id_at(a.bias_ids, a.id_type, row * a.n_bias + k) - (uint64_t)begin : ~(uint64_t)0;
-        const unsigned long long mine = __builtin_amdgcn_ballot_w64(v < (uint64_t)n);
-        if (v < (uint64_t)n) {
-            const int at = listed + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mine >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mine, 0u));
-            b.v[at] = (uint16_t)v;
-            b.value[at] = a.bias_values[row * a.n_bias + k];
-        }
-        listed += __popcll(mine);
-#endif
-    }
-    if (threadIdx.x == 0) b.n = listed;
-}
-// The sums of each class's, in its counter's bit and in b.of: by the thread that has the first of them.
-__device__ __forceinline__ void add_biases(Biases& b, unsigned* shared)
-{
-    for (int i = threadIdx.x; i < b.n; i += kThreads) {
-        const int v = b.v[i];
-        bool first = true;
-        for (int k = 0; k < i; ++k) first &= b.v[k] != v;
-        if (!first) continue;
-        float sum = b.value[i];
-        for (int k = i + 1; k < b.n; ++k)
-            if (b.v[k] == v) sum += b.value[k];
-        b.of[v] = sum;
-        shared[v] |= kBiased;
-    }
-}
+    unsigned count[NUTS_CAT_MAX_BIAS];
 
-// The counters of a slice from the places of a row's history, in LDS, where adding whole numbers in any order gives the same; `done`: how much of it they
-// have, if not nothing.
-template <typename T, typename B>
-__device__ __forceinline__ void count(const PenaltyArgs& a, long row, int begin, int n, const Seen& done, const Seen& now, unsigned* shared, B&& biases,
-                                      Counters<T>& counters)
+    static constexpr uint16_t kNone = 0xffff;
+    static_assert(Wide::kSlice < kNone && Usual::kSlice < kNone, "classes of 16 bits");
+
+    template <typename W>
+    __device__ __forceinline__ void read(const PenaltyArgs& a, long row, int begin, int n)
+    {
+        for (int k = threadIdx.x; k < (a.n_bias + 7) / 8 * 8; k += W::kThreads) {
+            const uint64_t at = k < a.n_bias ? (uint64_t)id_at(a.bias_ids, a.id_type, row * a.n_bias + k) - (uint64_t)begin : ~(uint64_t)0;
+            v[k] = at < (uint64_t)n ? (uint16_t)at : kNone;
+            if (k < a.n_bias) value[k] = a.bias_values[row * a.n_bias + k];
+        }
+    }
+    // While others count: the counters' bits do not touch.  Returns a bit for each of this thread's biases that is to stand for its class.
+    template <typename W>
+    __device__ __forceinline__ unsigned mark(const PenaltyArgs& a, unsigned* shared) const
+    {
+        unsigned mine = 0, bit = 1;
+        for (int k = threadIdx.x; k < a.n_bias; k += W::kThreads, bit *= 2) {
+            if (v[k] == kNone) continue;
+            if (atomicOr(&shared[v[k]], kBiased) & kBiased) atomicOr(&shared[v[k]], kAgain);
+            else mine |= bit;
+        }
+        return mine;
+    }
+    // (behind a barrier; the values of a class are read by one thread, which then writes one of them)
+    template <typename W>
+    __device__ __forceinline__ void add_up(const PenaltyArgs& a, unsigned mine, unsigned* shared)
+    {
+        for (int k = threadIdx.x; k < a.n_bias; k += W::kThreads, mine /= 2) {
+            if (!(mine & 1)) continue;
+            const unsigned c = shared[v[k]];
+            if (c & kAgain) {
+                const unsigned twice = v[k] * 0x10001u;
+                float sum = -0.f;  // (which adds nothing to anything)
+#pragma unroll 2
+                for (int j = 0; j < a.n_bias; j += 8) {
+                    const uint4 some = *reinterpret_cast<const uint4*>(&v[j]);
+                    const unsigned off[4] = {some.x ^ twice, some.y ^ twice, some.z ^ twice, some.w ^ twice};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if ((off[e / 2] >> e % 2 * 16 & 0xffffu) == 0) sum += value[j + e];
+                }
+                value[k] = sum;
+            }
+            count[k] = c & kSeen;
+            shared[v[k]] = kBiased | (unsigned)k;
+        }
+    }
+};
+
+// The counters of a slice from a row's history, in LDS, where adding whole numbers in any order gives the same.
+template <typename W, typename T, typename B>
+__device__ __forceinline__ void count(const PenaltyArgs& a, long row, int begin, int n, const Seen& now, unsigned* shared, B&& biases, Counters<W, T>& counters)
 {
+    constexpr bool kBiases = std::is_same_v<B, Biases&>;
+    if constexpr (kBiases) biases.template read<W>(a, row, begin, n);
+    else __syncthreads();  // (a row before this one may still be read)
+    for (int i = (int)threadIdx.x * 4; i < (n + 7) / 8 * 8; i += W::kThreads * 4) *reinterpret_cast<uint4*>(&shared[i]) = uint4{0, 0, 0, 0};
     __syncthreads();
-    for (int i = (int)threadIdx.x * 4; i < (n + 7) / 8 * 8; i += kThreads * 4) *reinterpret_cast<uint4*>(&shared[i]) = uint4{0, 0, 0, 0};
-    __syncthreads();
-    look_through(a, row, done.length, now.length, begin, n, [&](int i, int v) {
+    unsigned mine = 0;
+    if constexpr (kBiases) mine = biases.template mark<W>(a, shared);
+    look_through<W>(a, row, 0, now.length, begin, n, [&](int i, int v) {
         if (i >= now.prompt) atomicAdd(&shared[v], 1u);
         else atomicOr(&shared[v], kPrompt);
     });
     __syncthreads();
-    if constexpr (std::is_same_v<B, Biases&>) {
-        add_biases(biases, shared);
+    if constexpr (kBiases) {
+        biases.template add_up<W>(a, mine, shared);
         __syncthreads();
     }
-    if (done.length == 0) counters.clear();
-    counters.add(shared);
+    counters.read(shared);
 }
 
 // Places of a history that a row has more than the one before and that each thread looks at by itself.
@@ -239,8 +269,8 @@ constexpr int kFew = 16;
 // Where all rows have one history and a row has seen a little more of it than the one before, the counters stay in registers and what is new is added
 // to them: rows of one text wait for no one then.  False: it is not so.  (4096 rows of 50001 with their gradients: 362 us with
 // counters in LDS and barriers before and behind each row, MEASURED so.)
-template <typename T>
-__device__ __forceinline__ bool count_on(const PenaltyArgs& a, long row, int begin, int n, const Seen& done, const Seen& now, Counters<T>& counters)
+template <typename W, typename T>
+__device__ __forceinline__ bool count_on(const PenaltyArgs& a, long row, int begin, int n, const Seen& done, const Seen& now, Counters<W, T>& counters)
 {
     const int more = now.length - done.length, less = now.prompt - done.prompt;
     if (more < 0 || less < 0 || more > kFew || less > kFew) return false;
@@ -272,13 +302,13 @@ __device__ __forceinline__ Pack<T, kPackN<T>> load_some(const T* row, int v, int
         if (v + e < n) in.v[e] = row[v + e];
     return in;
 }
-template <typename T>
+template <typename W, typename T>
 struct Slice {
-    Pack<T, kPackN<T>> pack[kPacks<T>];
+    Pack<T, kPackN<T>> pack[kPacks<W, T>];
     __device__ __forceinline__ void fetch(const T* row, int n)
     {
 #pragma unroll
-        for (int u = 0; u < kPacks<T>; ++u) pack[u] = load_some(row, class_of_pack<T>(u), n);
+        for (int u = 0; u < kPacks<W, T>; ++u) pack[u] = load_some(row, class_of_pack<W, T>(u), n);
     }
 };
 template <typename T>
@@ -325,39 +355,39 @@ __device__ __forceinline__ unsigned allowed_of(const uint32_t* allowed, int v, i
 }
 
 // A workgroup a slice of one row, or (kShared) of `rows_each` rows that have one history.
-template <typename T, bool kShared, bool kBiases>
-__global__ __launch_bounds__(kThreads, 8) void penalties_kernel(PenaltyArgs a)
+template <typename W, typename T, bool kShared, bool kBiases>
+__global__ __launch_bounds__(W::kThreads, 8) void penalties_kernel(PenaltyArgs a)
 {
     constexpr int kN = kPackN<T>;
-    __shared__ __attribute__((aligned(16))) unsigned shared[kSlice];
+    __shared__ __attribute__((aligned(16))) unsigned shared[W::kSlice];
     __shared__ std::conditional_t<kBiases, Biases, int> biases;
     const long block = a.first_block + blockIdx.x, group = block / a.slices;
-    const int begin = (int)(block % a.slices) * kSlice, n = min(kSlice, a.n_classes - begin);
+    const int begin = (int)(block % a.slices) * W::kSlice, n = min(W::kSlice, a.n_classes - begin);
     const bool sparse = a.logits == a.out && !a.bias;  // what nothing changes is left alone
     long row = group * a.rows_each;
     const long end = min(row + a.rows_each, a.n_rows);
     const T* x_row = static_cast<const T*>(a.logits) + row * a.row_stride + begin;
-    Slice<T> next;
+    Slice<W, T> next;
     if (!sparse) next.fetch(x_row, n);
-    Counters<T> counters;
+    Counters<W, T> counters;
     counters.clear();
-    float bias[kPacks<T>][kN];
-    unsigned may[kPacks<T>];
+    float bias[kPacks<W, T>][kN];
+    unsigned may[kPacks<W, T>];
     auto prepare = [&]() {  // what may be the same for all rows
 #pragma unroll
-        for (int u = 0; u < kPacks<T>; ++u) {
-            if (a.bias) read_bias<kN>(a.bias + row * a.bias_stride + begin, class_of_pack<T>(u), n, bias[u]);
-            may[u] = allowed_of<kN>(a.allowed ? a.allowed + row * a.allowed_stride + begin / 32 : nullptr, class_of_pack<T>(u), n);
+        for (int u = 0; u < kPacks<W, T>; ++u) {
+            if (a.bias) read_bias<kN>(a.bias + row * a.bias_stride + begin, class_of_pack<W, T>(u), n, bias[u]);
+            may[u] = allowed_of<kN>(a.allowed ? a.allowed + row * a.allowed_stride + begin / 32 : nullptr, class_of_pack<W, T>(u), n);
         }
     };
     prepare();
-    auto finish_row = [&](const Slice<T>& own) {
+    auto finish_row = [&](const Slice<W, T>& own) {
         const float r = a.repetition ? uniform(a.repetition + row) : a.r;
         const RowFactors p{r, 1.f / r, a.frequency ? uniform(a.frequency + row) : a.f, a.presence ? uniform(a.presence + row) : a.q};
         T* to = static_cast<T*>(a.out) + row * a.out_stride + begin;
 #pragma unroll
-        for (int u = 0; u < kPacks<T>; ++u) {
-            const int v = class_of_pack<T>(u);
+        for (int u = 0; u < kPacks<W, T>; ++u) {
+            const int v = class_of_pack<W, T>(u);
             if (v >= n) break;
             const unsigned any = counters.any(u);
             Pack<T, kN> in = own.pack[u];
@@ -369,7 +399,11 @@ __global__ __launch_bounds__(kThreads, 8) void penalties_kernel(PenaltyArgs a)
             unpack(in, x);
             if (any) {
 #pragma unroll
-                for (int e = 0; e < kN; ++e) x[e] = penalised(x[e], counters.c[u][e], p);
+                for (int e = 0; e < kN; ++e) {
+                    unsigned c = counters.c[u][e];
+                    if constexpr (kBiases) c = c & kBiased ? biases.count[c & kPlace] : c;
+                    x[e] = penalised(x[e], c, p);
+                }
             }
             if (a.bias) {
 #pragma unroll
@@ -379,7 +413,7 @@ __global__ __launch_bounds__(kThreads, 8) void penalties_kernel(PenaltyArgs a)
                 if (any & kBiased) {
 #pragma unroll
                     for (int e = 0; e < kN; ++e)
-                        if (counters.c[u][e] & kBiased) x[e] += biases.of[v + e];
+                        if (counters.c[u][e] & kBiased) x[e] += biases.value[counters.c[u][e] & kPlace];
                 }
             }
             if (a.allowed) {
@@ -390,15 +424,14 @@ __global__ __launch_bounds__(kThreads, 8) void penalties_kernel(PenaltyArgs a)
         }
     };
     if constexpr (!kShared) {
-        if constexpr (kBiases) list_biases(a, row, begin, n, biases);
-        count(a, row, begin, n, Seen{0, 0}, seen_of(a, row), shared, biases, counters);
+        count(a, row, begin, n, seen_of(a, row), shared, biases, counters);
         finish_row(next);
     } else {
         while (row < end) {
             Seen done = seen_of(a, row);
-            if (a.history_len > 0) count(a, row, begin, n, Seen{0, 0}, done, shared, 0, counters);
+            if (a.history_len > 0) count(a, row, begin, n, done, shared, 0, counters);
             while (true) {
-                const Slice<T> own = next;
+                const Slice<W, T> own = next;
                 if (!sparse && row + 1 < end) next.fetch(x_row + a.row_stride, n);
                 finish_row(own);
                 ++row;
@@ -414,44 +447,44 @@ __global__ __launch_bounds__(kThreads, 8) void penalties_kernel(PenaltyArgs a)
 }
 
 // A workgroup a slice of `rows_each` rows, whose gradients it adds up.  kShared: they have one history.
-template <typename T, bool kShared>
-__global__ __launch_bounds__(kThreads, 6) void penalties_grad_kernel(PenaltyArgs a)
+template <typename W, typename T, bool kShared>
+__global__ __launch_bounds__(W::kThreads, W::kThreads == 512 ? 6 : 4) void penalties_grad_kernel(PenaltyArgs a)
 {
     constexpr int kN = kPackN<T>;
-    __shared__ __attribute__((aligned(16))) unsigned shared[kSlice];
+    __shared__ __attribute__((aligned(16))) unsigned shared[W::kSlice];
     const long block = a.first_block + blockIdx.x, group = block / a.slices;
-    const int begin = (int)(block % a.slices) * kSlice, n = min(kSlice, a.n_classes - begin);
+    const int begin = (int)(block % a.slices) * W::kSlice, n = min(W::kSlice, a.n_classes - begin);
     const bool sparse = a.grad_out == a.out && !a.grad_bias, counting = a.out && a.history_len > 0;
     long row = group * a.rows_each;
     const long end = min(row + a.rows_each, a.n_rows);
     const T* g_row = static_cast<const T*>(a.grad_out) + row * a.grad_stride + begin;
-    float sum[kPacks<T>][kN] = {};
-    Slice<T> next;
+    float sum[kPacks<W, T>][kN] = {};
+    Slice<W, T> next;
     if (!sparse) next.fetch(g_row, n);
-    Counters<T> counters;
+    Counters<W, T> counters;
     counters.clear();
-    unsigned may[kPacks<T>];
+    unsigned may[kPacks<W, T>];
     auto prepare = [&]() {
 #pragma unroll
-        for (int u = 0; u < kPacks<T>; ++u) may[u] = allowed_of<kN>(a.allowed ? a.allowed + row * a.allowed_stride + begin / 32 : nullptr, class_of_pack<T>(u), n);
+        for (int u = 0; u < kPacks<W, T>; ++u) may[u] = allowed_of<kN>(a.allowed ? a.allowed + row * a.allowed_stride + begin / 32 : nullptr, class_of_pack<W, T>(u), n);
     };
     prepare();
     auto finish_row = [&]() {
-        const Slice<T> own = next;
+        const Slice<W, T> own = next;
         const float r = a.repetition ? uniform(a.repetition + row) : a.r, by_r = 1.f / r;
         const T* x_row = static_cast<const T*>(a.logits) + row * a.row_stride + begin;
         T* to = a.out ? static_cast<T*>(a.out) + row * a.out_stride + begin : nullptr;
         // (loads come back in their order: what this row waits for goes before what the next one does)
-        Slice<T> logits{};
+        Slice<W, T> logits{};
 #pragma unroll
-        for (int u = 0; u < kPacks<T>; ++u) {
-            const int v = class_of_pack<T>(u);
+        for (int u = 0; u < kPacks<W, T>; ++u) {
+            const int v = class_of_pack<W, T>(u);
             if (counters.any(u)) logits.pack[u] = load_some(x_row, v, n);
         }
         if (!sparse && row + 1 < end) next.fetch(g_row + a.grad_stride, n);
 #pragma unroll
-        for (int u = 0; u < kPacks<T>; ++u) {
-            const int v = class_of_pack<T>(u);
+        for (int u = 0; u < kPacks<W, T>; ++u) {
+            const int v = class_of_pack<W, T>(u);
             if (v >= n) break;
             const unsigned any = counters.any(u);
             Pack<T, kN> in = own.pack[u];
@@ -479,7 +512,7 @@ __global__ __launch_bounds__(kThreads, 6) void penalties_grad_kernel(PenaltyArgs
     auto seen = [&]() { return Seen{clamped(a.lengths, row, a.history_len, a.history_len), 0}; };
     while (row < end) {
         Seen done = seen();
-        if (counting) count(a, row, begin, n, Seen{0, 0}, done, shared, 0, counters);
+        if (counting) count(a, row, begin, n, done, shared, 0, counters);
         while (true) {
             finish_row();
             ++row;
@@ -497,8 +530,8 @@ __global__ __launch_bounds__(kThreads, 6) void penalties_grad_kernel(PenaltyArgs
     }
     if (!a.grad_bias) return;
 #pragma unroll
-    for (int u = 0; u < kPacks<T>; ++u) {
-        const int v = class_of_pack<T>(u);
+    for (int u = 0; u < kPacks<W, T>; ++u) {
+        const int v = class_of_pack<W, T>(u);
 #pragma unroll
         for (int e = 0; e < kN; ++e)
             if (v + e < n) a.grad_bias[group * a.n_classes + begin + v + e] = sum[u][e];
@@ -543,7 +576,7 @@ int check_penalties(const nuts_penalties_desc* d, const char* who)
         return api_fail(NUTS_E_INVALID_ARG, "%s: allowed_stride must be 0 or at least n_classes / 32 words", who);
     if (d->bias_stride < 0 || (d->bias_stride > 0 && d->bias_stride < d->n_classes) || d->bias_stride > most)
         return api_fail(NUTS_E_INVALID_ARG, "%s: bias_stride must be 0 or at least n_classes", who);
-    if (d->history_len < 0 || d->history_len > (1 << 30) - 1) return api_fail(NUTS_E_INVALID_ARG, "%s: history_len must be in [0, 2^30)", who);
+    if (d->history_len < 0 || d->history_len > (int64_t)kCount) return api_fail(NUTS_E_INVALID_ARG, "%s: history_len must be in [0, 2^29)", who);
     if (d->history_stride < 0 || (d->history_stride > 0 && d->history_stride < d->history_len) || d->history_stride > most)
         return api_fail(NUTS_E_INVALID_ARG, "%s: history_stride must be 0 or at least history_len", who);
     if (d->n_bias < 0 || d->n_bias > NUTS_CAT_MAX_BIAS) return api_fail(NUTS_E_INVALID_ARG, "%s: n_bias must be in [0, %d]", who, NUTS_CAT_MAX_BIAS);
@@ -570,29 +603,36 @@ PenaltyArgs args_of(const nuts_penalties_desc* d)
     a.id_type = d->id_type;
     a.history_len = (int)d->history_len;
     a.n_bias = (int)d->n_bias;
-    a.slices = (int)ceil_div(d->n_classes, kSlice);
-    a.rows_each = 1;
     a.streamed = d->n_rows * d->n_classes * (int64_t)cat_size(d->dtype) >= kStreamed;
     return a;
 }
 
+// Where rows have histories of their own, of which each slice reads all, wide slices pay from 16 bytes of history for a byte of a slice on... MEASURED
+bool shares(const nuts_penalties_desc* d) { return d->history_len == 0 || d->history_stride == 0; }
+bool wants_wide(const nuts_penalties_desc* d)
+{
+    return !shares(d) && d->history_len >= kLong && d->n_rows * ceil_div(d->n_classes, Wide::kSlice) >= kFull;
+}
 // Rows of a workgroup, for a launch of `groups` workgroups, but at least `least`.
 int64_t rows_of_group(const nuts_penalties_desc* d, int64_t groups, int64_t least)
 {
-    return std::max<int64_t>(1, std::min(std::max(ceil_div(d->n_rows * ceil_div(d->n_classes, kSlice), groups), least), d->n_rows));
+    const int64_t slices = ceil_div(d->n_classes, wants_wide(d) ? Wide::kSlice : Usual::kSlice);
+    return std::max<int64_t>(1, std::min(std::max(ceil_div(d->n_rows * slices, groups), least), d->n_rows));
 }
 // Rows go together where they have one history, whose counts are carried on, and where their gradients are added up.
-bool shares(const nuts_penalties_desc* d) { return d->history_len == 0 || d->history_stride == 0; }
 int64_t rows_each(const nuts_penalties_desc* d) { return shares(d) && d->n_bias == 0 ? rows_of_group(d, kGroups, 1) : 1; }
 int64_t grad_rows_each(const nuts_penalties_desc* d, bool bias)
 {
     return bias ? rows_of_group(d, kGradGroups, kBiasRows) : shares(d) ? rows_of_group(d, kGradGroups, 1) : 1;
 }
 
+template <typename W>
 void launch(void (*kernel)(PenaltyArgs), PenaltyArgs a)
 {
-    for (const long blocks = (long)ceil_div(a.n_rows, a.rows_each) * a.slices; a.first_block < blocks; a.first_block += kMaxBlocks)
-        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(blocks - a.first_block, kMaxBlocks)), dim3(kThreads), 0, api_stream(), a);
+    a.slices = (int)ceil_div(a.n_classes, W::kSlice);
+    constexpr long kMost = kMaxBlocks * 512 / W::kThreads;
+    for (const long blocks = (long)ceil_div(a.n_rows, a.rows_each) * a.slices; a.first_block < blocks; a.first_block += kMost)
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(blocks - a.first_block, kMost)), dim3(W::kThreads), 0, api_stream(), a);
 }
 
 }  // namespace
@@ -630,7 +670,9 @@ int nuts_penalties(const nuts_penalties_desc* d, const void* logits, const void*
     a.rows_each = (int)rows_each(d);
     by_dtype(d->dtype, [&](auto t) {
         using T = decltype(t);
-        launch(d->n_bias > 0 ? penalties_kernel<T, false, true> : shares(d) ? penalties_kernel<T, true, false> : penalties_kernel<T, false, false>, a);
+        if (wants_wide(d)) launch<Wide>(d->n_bias > 0 ? penalties_kernel<Wide, T, false, true> : penalties_kernel<Wide, T, false, false>, a);
+        else if (d->n_bias > 0) launch<Usual>(penalties_kernel<Usual, T, false, true>, a);
+        else launch<Usual>(shares(d) ? penalties_kernel<Usual, T, true, false> : penalties_kernel<Usual, T, false, false>, a);
     });
     NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
     return NUTS_OK;
@@ -680,12 +722,13 @@ int nuts_penalties_grad(const nuts_penalties_desc* d, const void* grad_out, int6
     a.rows_each = (int)grad_rows_each(d, grad_bias != nullptr);
     by_dtype(d->dtype, [&](auto t) {
         using T = decltype(t);
-        launch(shares(d) ? penalties_grad_kernel<T, true> : penalties_grad_kernel<T, false>, a);
+        if (wants_wide(d)) launch<Wide>(penalties_grad_kernel<Wide, T, false>, a);
+        else launch<Usual>(shares(d) ? penalties_grad_kernel<Usual, T, true> : penalties_grad_kernel<Usual, T, false>, a);
     });
     if (grad_bias) {
         // few classes: more workgroups for them
         const bool narrow = d->n_classes <= kNarrow;
-        constexpr long kMost = kMaxBlocks / (kJoinThreads / kThreads);
+        constexpr long kMost = kMaxBlocks * 512 / kJoinThreads;
         for (long first = 0, blocks = (long)ceil_div(d->n_classes, narrow ? 16 : 64); first < blocks; first += kMost)
             hipLaunchKernelGGL(narrow ? join_bias_kernel<16> : join_bias_kernel<64>, dim3((unsigned)std::min(blocks - first, kMost)), dim3(kJoinThreads), 0, api_stream(),
                                static_cast<const float*>(workspace), grad_bias, (long)groups, (int)d->n_classes, first);

@@ -52,7 +52,7 @@ NAN, INF = float("nan"), float("inf")
     (dict(row_stride=2 ** 61), "row_stride"), (dict(out_stride=4), "out_stride"), (dict(out_stride=2 ** 61), "out_stride"),
     (dict(n_classes=65, row_stride=65, out_stride=65, allowed_stride=2), "allowed_stride"), (dict(allowed_stride=-1), "allowed_stride"),
     (dict(allowed_stride=2 ** 61), "allowed_stride"), (dict(bias_stride=4), "bias_stride"), (dict(bias_stride=-8), "bias_stride"),
-    (dict(bias_stride=2 ** 61), "bias_stride"), (dict(history_len=-1), "history_len"), (dict(history_len=2 ** 30, history_stride=2 ** 30), "history_len"),
+    (dict(bias_stride=2 ** 61), "bias_stride"), (dict(history_len=-1), "history_len"), (dict(history_len=2 ** 29, history_stride=2 ** 29), "history_len"),
     (dict(history_stride=5), "history_stride"), (dict(history_stride=-6), "history_stride"), (dict(history_stride=2 ** 61), "history_stride"),
     (dict(n_bias=-1), "n_bias"), (dict(n_bias=1025), "n_bias"), (dict(repetition=0.0), "repetition"), (dict(repetition=-1.0), "repetition"),
     (dict(repetition=NAN), "repetition"), (dict(repetition=INF), "repetition"), (dict(repetition=1e-60), "repetition"), (dict(frequency=NAN), "frequency"),
@@ -67,7 +67,7 @@ def test_penalties_descriptors(bad, word):
 def test_penalties_ends_of_the_ranges():
     lib, n = B.lib(), C.c_int64()
     wide = dict(n_rows=1, n_classes=2 ** 31 - 2 ** 18 - 1, row_stride=2 ** 31, out_stride=2 ** 31)
-    for good in (wide, dict(n_rows=2 ** 31 - 2), dict(history_len=2 ** 30 - 1, history_stride=2 ** 30), dict(history_len=0, history_stride=0), dict(n_bias=1024)):
+    for good in (wide, dict(n_rows=2 ** 31 - 2), dict(history_len=2 ** 29 - 1, history_stride=2 ** 29), dict(history_len=0, history_stride=0), dict(n_bias=1024)):
         assert lib.nuts_penalties_grad_workspace(penalties(**good), C.byref(n)) == B.NUTS_OK and n.value > 0, good
 
 
