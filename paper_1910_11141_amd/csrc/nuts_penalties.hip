@@ -10,8 +10,7 @@
 namespace nuts {
 namespace {
 
-// A workgroup's threads, and the classes that it has a counter for in LDS: a slice.  Each slice looks through the whole history, so long ones want wide
-// slices; all others want many workgroups.
+// A workgroup's threads, and the classes that it has a counter for in LDS: a slice.  Each slice looks through the whole history.
 struct Usual {
     static constexpr int kThreads = 512, kSlice = 4096;
 };
@@ -19,8 +18,7 @@ struct Wide {
     static constexpr int kThreads = 1024, kSlice = 16384;
 };
 constexpr int kJoinThreads = 1024;
-constexpr int kLong = 2048;           // places of a history from which on slices are wide, if there are kFull of them
-constexpr int kFull = 512;
+constexpr int kLong = 2048, kFull = 256;  // of wide slices: places of a history (binary32), workgroups
 constexpr int kNarrow = 8192;       // classes: up to here 16 of them are joined by a workgroup, then 64
 constexpr int64_t kBiasRows = 2;    // that are added up, at least: their sums are stored
 constexpr int kGroups = 1024, kGradGroups = 768;  // workgroups that the chip has at a time
@@ -448,7 +446,7 @@ __global__ __launch_bounds__(W::kThreads, 8) void penalties_kernel(PenaltyArgs a
 
 // A workgroup a slice of `rows_each` rows, whose gradients it adds up.  kShared: they have one history.
 template <typename W, typename T, bool kShared>
-__global__ __launch_bounds__(W::kThreads, W::kThreads == 512 ? 6 : 4) void penalties_grad_kernel(PenaltyArgs a)
+__global__ __launch_bounds__(W::kThreads, 6) void penalties_grad_kernel(PenaltyArgs a)
 {
     constexpr int kN = kPackN<T>;
     __shared__ __attribute__((aligned(16))) unsigned shared[W::kSlice];
@@ -607,17 +605,20 @@ PenaltyArgs args_of(const nuts_penalties_desc* d)
     return a;
 }
 
-// Where rows have histories of their own, of which each slice reads all, wide slices pay from 16 bytes of history for a byte of a slice on... MEASURED
 bool shares(const nuts_penalties_desc* d) { return d->history_len == 0 || d->history_stride == 0; }
+// Where rows have histories of their own wide slices look through them less often, and their threads have more on their way: 500 rows of 128000 bfloat16
+// with histories of 256 56 us (usual ones 66), of 8000 73 (100); binary32 45 (43) and 53 (58).  Not where a wide slice would be half empty
+// (3000 rows of 5000: 29, 24) and for too few workgroups, and not for gradients, whose rows keep their sums in registers (500 rows of
+// 50001: 98, 54).
 bool wants_wide(const nuts_penalties_desc* d)
 {
-    return !shares(d) && d->history_len >= kLong && d->n_rows * ceil_div(d->n_classes, Wide::kSlice) >= kFull;
+    return !shares(d) && d->n_classes >= Wide::kSlice / 2 && (d->dtype != NUTS_F32 || d->history_len >= kLong) &&
+           d->n_rows * ceil_div(d->n_classes, Wide::kSlice) >= kFull;
 }
 // Rows of a workgroup, for a launch of `groups` workgroups, but at least `least`.
 int64_t rows_of_group(const nuts_penalties_desc* d, int64_t groups, int64_t least)
 {
-    const int64_t slices = ceil_div(d->n_classes, wants_wide(d) ? Wide::kSlice : Usual::kSlice);
-    return std::max<int64_t>(1, std::min(std::max(ceil_div(d->n_rows * slices, groups), least), d->n_rows));
+    return std::max<int64_t>(1, std::min(std::max(ceil_div(d->n_rows * ceil_div(d->n_classes, Usual::kSlice), groups), least), d->n_rows));
 }
 // Rows go together where they have one history, whose counts are carried on, and where their gradients are added up.
 int64_t rows_each(const nuts_penalties_desc* d) { return shares(d) && d->n_bias == 0 ? rows_of_group(d, kGroups, 1) : 1; }
@@ -722,8 +723,7 @@ int nuts_penalties_grad(const nuts_penalties_desc* d, const void* grad_out, int6
     a.rows_each = (int)grad_rows_each(d, grad_bias != nullptr);
     by_dtype(d->dtype, [&](auto t) {
         using T = decltype(t);
-        if (wants_wide(d)) launch<Wide>(penalties_grad_kernel<Wide, T, false>, a);
-        else launch<Usual>(shares(d) ? penalties_grad_kernel<Usual, T, true> : penalties_grad_kernel<Usual, T, false>, a);
+        launch<Usual>(shares(d) ? penalties_grad_kernel<Usual, T, true> : penalties_grad_kernel<Usual, T, false>, a);
     });
     if (grad_bias) {
         // few classes: more workgroups for them
