@@ -390,11 +390,11 @@ typedef struct {
 /* A row's history is the first lengths[row] of its places (all of them where `lengths` is NULL; a length is taken as
  * the nearest in [0, history_len]), the first prompts[row] of which are not the model's own (NULL: none).  With seen_v = class v comes in it
  * and count_v = how often it comes behind the prompt, and z = logits_v,
- *   z = z > 0 ? z / repetition : z * repetition   where seen_v;     z = z - (frequency count_v + presence [count_v > 0]);
+ *   z = z > 0 ? z (1 / repetition) : z repetition   where seen_v;     z = z - (frequency count_v + presence [count_v > 0]);
  *   z = z + bias_v, then + the sum of the row's bias_values whose bias_ids are v, in their order;     z = -infinity where v is not allowed,
  * whatever was there (NaN, too).  The arrays repetition, frequency and presence are [n_rows], bias [n_classes] or rows of it, bias_ids and
  * bias_values [n_rows][n_bias]; each may be NULL, and `allowed` is that of nuts_logprobs.  All of it is binary32 and rounded once.
- * `out` may be `logits` itself, with the same stride: then classes that nothing changes are neither read nor written. */
+ * `out` may be `logits` itself, with the same stride: then 16 bytes in which nothing changes are neither read nor written. */
 int nuts_penalties(const nuts_penalties_desc* desc, const void* logits, const void* history, const int32_t* lengths,
                    const int32_t* prompts, const float* repetition, const float* frequency, const float* presence,
                    const float* bias, const void* bias_ids, const float* bias_values, const uint32_t* allowed, void* out);
@@ -456,7 +456,7 @@ typedef struct {
  *
  * Arithmetic is binary32.  Moments of 8 bits stand for powers of their codes, m = sign(c) c^2 m_scale (c = -127 .. 127), v = (c^2 v_scale)^2
  * (c = 0 .. 254); a block's largest has the last code.  What stands between two codes becomes one of them, at random so that
- * the mean is kept, but a v above 0 does not become 0.  c = -128 and c = 255 are what is not finite and count as NaN.
+ * the mean is kept, but a v above 0 does not become 0, and a block of m whose largest is below 2^-126 127^2 is zeros.  c = -128 and c = 255 are what is not finite and count as NaN.
  * Parameters of bfloat16 are rounded at random, too (a step is mostly less than half a unit in their last place, and to the nearest they would stay where they
  * are); the parameters' copies are rounded to the nearest.  The random bits of the four numbers from 4 q of tensor t on are the four words of
  * Philox4x32-10 with the key `seed` and the counter (q mod 2^32, 6 + 256 (q / 2^32), step mod 2^32, t): bits 0-9 of a word are m's, 10-19 v's,

@@ -339,7 +339,7 @@ def nuts_penalties(logits, history=None, *, lengths=None, prompts=None, repetiti
     come are -infinity.  history: [places] for all rows or [rows, places], of which the first lengths[row] are there, and the
     first prompts[row] are not the model's own.  repetition, frequency, presence: numbers, or a float32 vector of each row's.
     bias: float32 [classes] or [rows, classes]; bias_ids, bias_values: [rows, some], biases of single classes.  allowed: bits, as in
-    nuts_logprobs.  out: where to write, which may be `logits`."""
+    nuts_logprobs.  out: where to write, which may be `logits`; a new one's rows may lie further apart than they are long."""
     _matrix(logits, "logits")
     n, classes = logits.shape
     history, id_type, places, history_stride = _history(history, n)
@@ -358,8 +358,9 @@ def nuts_penalties(logits, history=None, *, lengths=None, prompts=None, repetiti
             raise ValueError(f"bias_values must be float32 {list(bias_ids.shape)}")
         if id_type is None:
             id_type = _ID_TYPES[bias_ids.dtype]
-        elif id_type != _ID_TYPES[bias_ids.dtype]:
-            bias_ids = bias_ids.to(history.dtype)
+        elif id_type != _ID_TYPES[bias_ids.dtype]:  # (to the wider type: the other could make a class of what is none)
+            history, bias_ids, id_type = history.long(), bias_ids.long(), _b.NUTS_I64
+            history_stride = places if history_stride else 0
         bias_ids, bias_values, n_bias = bias_ids.contiguous(), bias_values.contiguous(), bias_ids.shape[1]
     bias_stride = 0
     if bias is not None:

@@ -207,6 +207,40 @@ def test_histories_of_other_orders():
     assert nuts.nuts_penalties(logits[:0], history[:0]).shape == (0, 500)
 
 
+@pytest.mark.parametrize("dtype,length", [(BF16, 40), (F16, 20000), (F32, 2048), (F32, 17001)])
+@pytest.mark.parametrize("n_bias", [0, 5, 1024])
+def test_wide_slices(dtype, length, n_bias):
+    """Histories of their own of enough rows of enough classes: three slices of 16384, the last of which is nearly empty."""
+    n, classes, g = 90, 32771, gen(22)
+    kw = {}
+    if n_bias:
+        kw = dict(bias_ids=torch.randint(-2, classes + 2, (n, n_bias), generator=g, device="cuda"), bias_values=torch.randn(n, n_bias, generator=g, device="cuda"))
+        kw["bias_ids"][:, n_bias // 2] = kw["bias_ids"][:, 0]
+        kw["bias_ids"][3] = 32770
+    check(matrix(n, classes, dtype, g, pad=1), history_of(n, length, classes, g), lengths=places(n, length, g), prompts=places(n, length, g),
+          repetition=rows(n, 0.5, 2.0, g), frequency=rows(n, 0.0, 0.25, g), presence=0.5, bias=torch.randn(classes, generator=g, device="cuda"),
+          allowed=masks(n, classes, g), **kw)
+    check(matrix(n, classes, dtype, g), history_of(n, length, classes, g, torch.int32), repetition=1.5, presence=1.0, **kw)
+
+
+def test_outputs_past_the_caches():
+    n, classes, g = 2100, 32003, gen(23)
+    logits = matrix(n, classes, BF16, g)
+    text = history_of(1, n, classes, g, torch.int32)[0]
+    check(logits, text, lengths=torch.arange(n, device="cuda").int(), repetition=1.5, frequency=0.25)
+    check_grad(logits, logits.flip(0), text, lengths=torch.arange(n, device="cuda").int(), repetition=1.5)
+
+
+def test_ids_of_two_types():
+    """A bias of a class that only 64 bits tell from one of the table's."""
+    g = gen(24)
+    logits, history = matrix(2, 100, F32, g), history_of(2, 30, 100, g, torch.int32)
+    ids = torch.tensor([[5, 2 ** 32 + 7, -2 ** 32 + 9], [2 ** 31 + 3, 11, 11]], device="cuda")
+    check(logits, history, repetition=1.5, bias_ids=ids, bias_values=torch.ones(2, 3, device="cuda"))
+    check(logits, history[0], repetition=1.5, bias_ids=ids, bias_values=torch.ones(2, 3, device="cuda"))
+    check(logits, history.long() + 2 ** 33 * (history.long() % 3), presence=1.5, bias_ids=ids.int().clamp(0, 50), bias_values=torch.ones(2, 3, device="cuda"))
+
+
 # ---- gradient -----------------------------------------------------------------------------------------------------------
 
 def check_grad(grad, logits, history, **kw):
