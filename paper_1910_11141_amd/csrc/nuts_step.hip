@@ -179,7 +179,7 @@ int64_t norm_blocks(const nuts_tensor* tensors, int64_t n)
 
 // ---- AdamW ----------------------------------------------------------------------------------------------------------
 
-constexpr int kStepTensors = 48;
+constexpr int kStepTensors = 56;
 // Numbers of a workgroup: 256 a wave at a time, eight times in large calls; in small ones as few times as kStepBlocks workgroups allow (16000
 // numbers: the kernel takes 8.4 us with eight times, 5.3 with one).
 constexpr int64_t kChunkLeast = 1024, kChunkMost = 8192, kStepBlocks = 1024;

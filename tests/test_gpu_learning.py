@@ -155,7 +155,7 @@ class Step:
             assert bool(((code >= L.v_codes(low.sqrt(), u)) & (code <= L.v_codes(high.sqrt(), u))).all()), i
 
 
-SIZES = [[1], [2, 3], [255, 256, 257], [8191, 8192, 8193, 4], [100003], [31] * 47, [260] * 48, [77] * 49 + [9000], [5, 0, 300, 0]]
+SIZES = [[1], [2, 3], [255, 256, 257], [8191, 8192, 8193, 4], [100003], [31] * 55, [260] * 56, [77] * 57 + [9000], [5, 0, 300, 0]]
 
 
 @pytest.mark.parametrize("sizes", SIZES, ids=lambda s: f"{len(s)}x{s[0]}")
