@@ -373,8 +373,9 @@ __device__ __forceinline__ unsigned allowed_of(const uint32_t* allowed, int v, i
 }
 
 // A workgroup a slice of one row, or (kShared) of `rows_each` rows that have one history.  Bound by its reads and writes: 4096 rows of 32001 bfloat16
-// with one history and biases 105 us, 5.0 TB/s (8 % more with loads that the caches keep, and 4 % with stores past them, as the gradient has), 500 rows of 128000
-// with histories of their own 56 us, 4.6 TB/s.  64 such rows take 8 us: a length, a history and a row, waited for one behind the other.
+// with one history and biases 112 us, 4.7 TB/s (120 with stores that the caches keep, 119 with loads that they do), 500 rows of 128000 with histories
+// of their own 56 us (68 with loads that the caches keep), 4.6 TB/s.  64 such rows take 8 us: a length, a history and a row, waited for one
+// behind the other.
 template <typename W, typename T, bool kShared, bool kBiases>
 __global__ __launch_bounds__(W::kThreads, 8) void penalties_kernel(PenaltyArgs a)
 {
@@ -440,7 +441,7 @@ __global__ __launch_bounds__(W::kThreads, 8) void penalties_kernel(PenaltyArgs a
 #pragma unroll
                 for (int e = 0; e < kN; ++e) x[e] = may[u] >> e & 1 ? x[e] : -INFINITY;
             }
-            write_pack(to, x, v, n, false);
+            write_pack(to, x, v, n, a.streamed);
         }
     };
     if constexpr (!kShared) {
