@@ -31,11 +31,15 @@ __device__ __forceinline__ int tensor_of(const int (&first)[kTensors], int block
 
 // ---- norm -----------------------------------------------------------------------------------------------------------
 
+// A pass over all numbers, bound by its reads: 200 million bfloat16 in 150 tensors 72 us, 5.6 TB/s, and 2 for joining the workgroups' sums.  The sums are binary64,
+// which hold the squares of all types and cost nothing here: two instructions a number.
 constexpr int kNormTensors = 190;
 constexpr int kNormBlocks = 2048;   // about so many workgroups in all
 constexpr int kNormLeast = 8192;    // numbers of a workgroup, at least
 constexpr int kNormThreads = 1024;  // of the workgroup that joins theirs
-constexpr int kNormSmall = 32768;   // numbers that it does alone, of kNormFew tensors at most, which it takes one after the other
+// Numbers that it does alone, of kNormFew tensors at most, which it takes one after the other: 32768 take it 4.7 us, where two launches take 3.8, 1.9
+// and the host's way to another one.
+constexpr int kNormSmall = 32768;
 constexpr int kNormFew = 4;
 
 struct NormArgs {
@@ -181,7 +185,7 @@ int64_t norm_blocks(const nuts_tensor* tensors, int64_t n)
 
 constexpr int kStepTensors = 56;
 // Numbers of a workgroup: 256 a wave at a time, eight times in large calls; in small ones as few times as kStepBlocks workgroups allow (16000
-// numbers: the kernel takes 8.4 us with eight times, 5.3 with one).
+// numbers: 8.4 us with eight times, 3.8 with one).
 constexpr int64_t kChunkLeast = 1024, kChunkMost = 8192, kStepBlocks = 1024;
 
 struct StepArgs {
@@ -248,6 +252,23 @@ __device__ __forceinline__ void store4(T* p, int n, const float (&x)[4])
     }
 }
 
+template <typename T, int kN>
+__device__ __forceinline__ void store_some(T* p, int n, const Pack<T, kN>& out)
+{
+    if (n == kN) {
+#pragma unroll
+        for (int e = 0; e < kN; e += 16 / sizeof(T)) {
+            Pack<T, 16 / sizeof(T)> part;
+            __builtin_memcpy(&part, &out.v[e], 16);
+            store_pack(p + e, part);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < kN; ++e)
+            if (e < n) p[e] = out.v[e];
+    }
+}
+
 // To bfloat16, up with the probability of what is cut off: 12 random bits and a half.
 __device__ __forceinline__ float rounded_at_random(float x, unsigned word)
 {
@@ -274,10 +295,11 @@ __device__ __forceinline__ void random_words(unsigned c0, unsigned c1, unsigned 
     words[0] = c0, words[1] = c1, words[2] = c2, words[3] = c3;
 }
 
-__device__ __forceinline__ float chance(unsigned bits) { return __builtin_fmaf((float)(bits & 1023u), 1.f / 1024.f, 0.5f / 1024.f); }
+// 1024 times a chance of 10 bits and a half: (2^23 + bits) - (2^23 - 1/2).
+__device__ __forceinline__ float chance(unsigned bits) { return __uint_as_float((bits & 1023u) | 0x4b000000u) - 8388607.5f; }
 
 // Codes of 8 bits.  x is what they stand for in units of the scale: 127^2, or 254^2, at a block's largest.  The code below x is the whole part of
-// its root, and where that comes out one too high or too low for a last place the comparison makes up for it: these
+// its root, and where that comes out one too high or too low for a last place (or is the last code) the comparison makes up for it: these
 // square roots need not be exact.  All else is rounded as single operations are, so that a step has the same codes wherever it is made.
 __device__ __forceinline__ float m_value(float code, float scale) { return code * __builtin_fabsf(code) * scale; }
 __device__ __forceinline__ float root_value(float code, float scale) { return code * code * scale; }
@@ -300,32 +322,30 @@ __device__ __forceinline__ Scale scale_of(float top, float last)  // top / last^
 }
 __device__ __forceinline__ float m_code(float m, const Scale& scale, unsigned word)
 {
-    const float x = in_units(__builtin_fabsf(m), scale), c = fminf(floorf(__builtin_amdgcn_sqrtf(x)), 126.f);
-    const bool up = __builtin_fmaf(-c, c, x) > __builtin_fmaf(2.f, c, 1.f) * chance(word);
+    const float x = in_units(__builtin_fabsf(m), scale), c = floorf(__builtin_amdgcn_sqrtf(x));
+    const float gap = __builtin_fmaf(c, 2.f / 1024.f, 1.f / 1024.f);  // ((c + 1)^2 - c^2) / 1024
+    const bool up = __builtin_fmaf(-c, c, x) > gap * chance(word);
     return __builtin_copysignf(up ? c + 1.f : c, m);
 }
 __device__ __forceinline__ float v_code(float root, const Scale& scale, unsigned word)
 {
-    const float x = in_units(root, scale), c = fminf(floorf(__builtin_amdgcn_sqrtf(x)), 253.f);
+    const float x = in_units(root, scale), c = floorf(__builtin_amdgcn_sqrtf(x));
     const float below = c * c, gap = __builtin_fmaf(2.f, c, 1.f);  // (c + 1)^2 - c^2
-    // ((c + 1)^4 - c^4) chance
-    const bool up = x * x - below * below > gap * __builtin_fmaf(2.f, below, gap) * chance(word >> 10);
-    return (int)up | ((int)(c == 0.f) & (int)(root > 0.f)) ? c + 1.f : c;
+    // ((c + 1)^4 - c^4) / 1024
+    const bool up = x * x - below * below > gap * __builtin_fmaf(2.f / 1024.f, below, gap * (1.f / 1024.f)) * chance(word >> 10);
+    return fmaxf(up ? c + 1.f : c, fminf(x * 0x1p126f, 1.f));  // (1 at least, where there is anything)
 }
-// The square root, rounded once: from one that is a unit or two in the last place off, and the remainder of its square.
+// The square root of a number of 24 places, rounded once: from one that is a unit or two in the last place off, and the remainder of its square.
 __device__ __forceinline__ float exact_root(float v)
 {
     const float y = __builtin_amdgcn_rsqf(v), s = v * y;
-    const float root = __builtin_fmaf(__builtin_fmaf(-s, s, v), 0.5f * y, s);
-    return v >= 0x1p-126f && v < INFINITY ? root : __builtin_amdgcn_sqrtf(v);
+    return __builtin_fmaf(__builtin_fmaf(-s, s, v), 0.5f * y, s);
 }
 
-constexpr unsigned kInfinite = 0x7f800000u;
-__device__ __forceinline__ unsigned size_of(float x) { return __float_as_uint(x) & 0x7fffffffu; }  // rises with |x|; NaN is above infinity
-
-// The largest of a wave's, in all of its lanes.
-__device__ __forceinline__ unsigned wave_max(unsigned v)
+// The largest of a wave's numbers that are 0 or more, in all of its lanes.
+__device__ __forceinline__ float wave_max(float x)
 {
+    unsigned v = __float_as_uint(x);  // (which rises as they do)
 #ifdef __HIP_DEVICE_COMPILE__
 #define NUTS_MAX_STEP(control, rows) v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, control, rows, 0xf, rows == 0xf))
     NUTS_MAX_STEP(0xb1, 0xf);   // quads: neighbours, then pairs
@@ -335,9 +355,21 @@ __device__ __forceinline__ unsigned wave_max(unsigned v)
     NUTS_MAX_STEP(0x142, 0xa);  // rows 1 and 3: the last lane of the row before
     NUTS_MAX_STEP(0x143, 0xc);  // the upper half: lane 31
 #undef NUTS_MAX_STEP
-    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+    v = (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+#endif
+    return __uint_as_float(v);
+}
+__device__ __forceinline__ float largest(const float (&x)[4])
+{
+    return wave_max(fmaxf(fmaxf(__builtin_fabsf(x[0]), __builtin_fabsf(x[1])), fmaxf(__builtin_fabsf(x[2]), __builtin_fabsf(x[3]))));
+}
+// Whether any lane says so.
+__device__ __forceinline__ bool any_lane(bool is)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    return __builtin_amdgcn_ballot_w64(is) != 0;
 #else
-    return v;
+    return is;
 #endif
 }
 
@@ -372,52 +404,53 @@ __device__ __forceinline__ void store_codes(void* codes, long i, int n, unsigned
 }
 __device__ __forceinline__ unsigned zero_bytes(unsigned word) { return (word - 0x01010101u) & ~word & 0x80808080u; }  // 0: there is none
 
-// What four codes stand for: m, and the root of v.
-__device__ __forceinline__ void decode(unsigned m_word, unsigned v_word, float m_scale, float v_scale, float (&m)[4], float (&root)[4])
+// What four codes stand for: m, and the root of v.  Returns whether a lane has one that counts as NaN.
+__device__ __forceinline__ bool decode(unsigned m_word, unsigned v_word, float m_scale, float v_scale, float (&m)[4], float (&root)[4])
 {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         m[e] = m_value((float)(int8_t)(m_word >> 8 * e), m_scale);
         root[e] = root_value((float)(uint8_t)(v_word >> 8 * e), v_scale);
     }
-    if (__builtin_amdgcn_ballot_w64((zero_bytes(m_word ^ 0x80808080u) | zero_bytes(~v_word)) != 0)) {
+    const bool lost = any_lane((zero_bytes(m_word ^ 0x80808080u) | zero_bytes(~v_word)) != 0);
+    if (lost) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if ((m_word >> 8 * e & 255u) == 128u) m[e] = NAN;
             if ((v_word >> 8 * e & 255u) == 255u) root[e] = NAN;
         }
     }
+    return lost;
 }
 
-// A block's moments, four in each lane, as codes and scales.
-__device__ __forceinline__ void encode(const nuts_adamw_tensor& t, long block, long i, int n, float (&m)[4], float (&root)[4], const unsigned (&words)[4])
+// A block's moments, four in each lane, as codes and scales.  lost: some may not be finite.
+__device__ __forceinline__ void encode(const nuts_adamw_tensor& t, long block, long i, int n, bool lost, float (&m)[4], float (&root)[4],
+                                       const unsigned (&words)[4])
 {
-    unsigned m_top = wave_max(max(max(size_of(m[0]), size_of(m[1])), max(size_of(m[2]), size_of(m[3]))));
-    unsigned v_top = wave_max(max(max(size_of(root[0]), size_of(root[1])), max(size_of(root[2]), size_of(root[3]))));
-    unsigned m_lost = 0, v_lost = 0;  // codes that are not finite
-    if (m_top >= kInfinite || v_top >= kInfinite) {
+    unsigned m_lost = 0, v_lost = 0;
+    if (lost) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (size_of(m[e]) >= kInfinite) {
+            if (!(__builtin_fabsf(m[e]) < INFINITY)) {
                 m[e] = 0.f;
                 m_lost |= 255u << 8 * e;
             }
-            if (size_of(root[e]) >= kInfinite) {
+            if (!(root[e] < INFINITY)) {
                 root[e] = 0.f;
                 v_lost |= 255u << 8 * e;
             }
         }
-        m_top = wave_max(max(max(size_of(m[0]), size_of(m[1])), max(size_of(m[2]), size_of(m[3]))));
-        v_top = wave_max(max(max(size_of(root[0]), size_of(root[1])), max(size_of(root[2]), size_of(root[3]))));
     }
-    const Scale m_scale = scale_of(__uint_as_float(m_top), 127.f), v_scale = scale_of(__uint_as_float(v_top), 254.f);
+    const Scale m_scale = scale_of(largest(m), 127.f), v_scale = scale_of(largest(root), 254.f);
     unsigned m_word = 0, v_word = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         m_word |= ((unsigned)(int)m_code(m[e], m_scale, words[e]) & 255u) << 8 * e;
-        v_word |= (unsigned)v_code(root[e], v_scale, words[e]) << 8 * e;
+#ifdef __HIP_DEVICE_COMPILE__
+        v_word = __builtin_amdgcn_cvt_pk_u8_f32(v_code(root[e], v_scale, words[e]), e, v_word);
+#endif
     }
-    store_codes(t.m, i, n, (m_word & ~m_lost) | (m_lost & 0x80808080u));
+    store_codes(t.m, i, n, lost ? (m_word & ~m_lost) | (m_lost & 0x80808080u) : m_word);
     store_codes(t.v, i, n, v_word | v_lost);
     if (threadIdx.x % 64 == 0) {
         t.m_scale[block] = m_scale.of;
@@ -432,10 +465,11 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const Factors& f, 
     const long i = at + threadIdx.x % 64 * 4, block = at / 256;
     const int n = kWhole ? 4 : (int)max(min(end - i, 4l), 0l);
     float p[4], g[4], m[4], v[4], root[4];
+    bool lost = false;
     load4(static_cast<const P*>(t.param) + i, n, p);
     load4(static_cast<const G*>(t.grad) + i, n, g);
     if (kEight) {
-        decode(load_codes(t.m, i, n), load_codes(t.v, i, n), t.m_scale[block], t.v_scale[block], m, root);
+        lost = decode(load_codes(t.m, i, n), load_codes(t.v, i, n), t.m_scale[block], t.v_scale[block], m, root);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = root[e] * root[e];
     } else {
@@ -443,27 +477,49 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const Factors& f, 
         load4(static_cast<const float*>(t.v) + i, n, v);
     }
     unsigned words[4] = {};
-    if (kEight || sizeof(P) == 2) random_words((unsigned)(i / 4), 6u | (unsigned)(at / 4 >> 32) << 8, f.t, tensor, a.k0, a.k1, words);
+    if (kEight || sizeof(P) == 2) random_words((unsigned)((uint64_t)at >> 2) + threadIdx.x % 64, 6u | (unsigned)((uint64_t)at >> 34) << 8, f.t, tensor, a.k0, a.k1, words);
+    bool usual = true;  // (neither 0 nor infinity nor NaN: what the root wants)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const float x = g[e] * f.scale;
         m[e] = m[e] * a.beta1 + x * a.rest1;
         v[e] = v[e] * a.beta2 + x * x * a.rest2;
-        root[e] = kEight ? exact_root(v[e]) : __builtin_amdgcn_sqrtf(v[e]);  // (a unit in the last place off at most, as the reciprocal)
-        p[e] = p[e] * f.keep - f.size * m[e] * __builtin_amdgcn_rcpf(root[e] * f.root_scale + a.eps);
+        usual &= __builtin_isnormal(v[e]);
+    }
+    if (!kEight || any_lane(!usual)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            root[e] = __builtin_amdgcn_sqrtf(v[e]);  // (a unit in the last place off at most, as the reciprocal)
+            if (kEight && __builtin_isnormal(v[e])) root[e] = exact_root(v[e]);
+            if (kEight) lost |= !(v[e] < INFINITY);
+        }
+        if (kEight) lost = any_lane(lost);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) root[e] = exact_root(v[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        p[e] = __builtin_fmaf(-f.size * m[e], __builtin_amdgcn_rcpf(__builtin_fmaf(root[e], f.root_scale, a.eps)), p[e] * f.keep);
         if (sizeof(P) == 2) p[e] = rounded_at_random(p[e], words[e]);
     }
     store4(static_cast<P*>(t.param) + i, n, p);
     if (t.copy) a.copy_dtype == NUTS_BF16 ? store4(static_cast<bf16*>(t.copy) + i, n, p) : store4(static_cast<f16*>(t.copy) + i, n, p);
     if (kEight) {
-        encode(t, block, i, n, m, root, words);
+        encode(t, block, i, n, lost, m, root, words);
     } else {
         store4(static_cast<float*>(t.m) + i, n, m);
         store4(static_cast<float*>(t.v) + i, n, v);
     }
 }
 
-// A workgroup `chunk` numbers of a tensor, a wave 256 of them at a time: a block of the moments of 8 bits.
+// A workgroup `chunk` numbers of a tensor, a wave 256 of them at a time: a block of the moments of 8 bits.  One pass, each number read and written once.
+//
+// 32 bits: bound by memory.  102 million numbers, all binary32: 548 us, 5.2 TB/s; 120 million with gradients and copies of 16 bits in 150 tensors, three
+// launches, 640 us, 4.9 TB/s.
+// 8 bits: 200 million binary32 parameters with gradients and copies of 16 bits 646 us, 5.0 TB/s.  Instructions are as near: some 98 a number, of which
+// the ten rounds of Philox are 10 and the two codes 42 (with a table of c^4 and its steps in LDS they are 36, and the time 642).  With library roots and quotients,
+// lanes checked one by one and codes by bytes the same took 1290 us.
 template <typename P, typename G, bool kEight>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a)
 {
@@ -479,20 +535,43 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a)
     if (at < end) step_block<P, G, kEight, false>(a, f, t, a.first_tensor + k, at, end);
 }
 
+// Eight numbers a thread.  Bound by memory: 200 million to bfloat16 234 us, 5.1 TB/s (285 with four numbers a thread).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void values_kernel(StepArgs a)
 {
+    constexpr int kEach = 8;
     const int k = tensor_of(a.first, (int)blockIdx.x);
     const nuts_adamw_tensor& t = a.tensor[k];
     const long begin = (a.first_block + (long)((int)blockIdx.x - a.first[k])) * a.chunk, end = min(begin + a.chunk, (long)t.n);
-    for (long i = begin + (long)threadIdx.x * 4; i < end; i += kThreads * 4) {
-        const int n = (int)min(end - i, 4l);
-        float m[4], v[4];
-        decode(load_codes(t.m, i, n), load_codes(t.v, i, n), t.m_scale[i / 256], t.v_scale[i / 256], m, v);
+    for (long at = begin; at < end; at += kThreads * kEach) {  // (whole waves)
+        const long i = at + (long)threadIdx.x * kEach;
+        const int n = (int)max(min(end - i, (long)kEach), 0l);
+        unsigned m_word[2] = {}, v_word[2] = {};
+        if (n == kEach) {
+            const Pack<uint8_t, kEach> m_in = load_pack<uint8_t, kEach>(static_cast<const uint8_t*>(t.m) + i), v_in = load_pack<uint8_t, kEach>(static_cast<const uint8_t*>(t.v) + i);
+            __builtin_memcpy(m_word, &m_in, kEach);
+            __builtin_memcpy(v_word, &v_in, kEach);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] *= v[e];
-        if (t.param) store4(static_cast<T*>(t.param) + i, n, m);
-        if (t.copy) store4(static_cast<T*>(t.copy) + i, n, v);
+            for (int q = 0; q < 2; ++q) {
+                m_word[q] = load_codes(t.m, i + 4 * q, max(min(n - 4 * q, 4), 0));
+                v_word[q] = load_codes(t.v, i + 4 * q, max(min(n - 4 * q, 4), 0));
+            }
+        }
+        const float m_scale = n > 0 ? t.m_scale[i / 256] : 0.f, v_scale = n > 0 ? t.v_scale[i / 256] : 0.f;
+        Pack<T, kEach> m_out, v_out;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            float m[4], root[4];
+            decode(m_word[q], v_word[q], m_scale, v_scale, m, root);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                m_out.v[4 * q + e] = rounded<T>(m[e]);
+                v_out.v[4 * q + e] = rounded<T>(root[e] * root[e]);
+            }
+        }
+        if (t.param) store_some(static_cast<T*>(t.param) + i, n, m_out);
+        if (t.copy) store_some(static_cast<T*>(t.copy) + i, n, v_out);
     }
 }
 
