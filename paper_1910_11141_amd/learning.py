@@ -99,7 +99,8 @@ class Moments:
     """What AdamW keeps of a list of parameters (all float32, or all bfloat16): their moments, zeros at first, in 32 bits
     (`m`, `v`: float32, as the parameters) or in 8 (`m` int8, `v` uint8, as the parameters; `m_scales`, `v_scales`: float32, one for each 256 of a
     parameter's numbers).  copies: a tensor of bfloat16 or float16 for each parameter (or None), which receives what the
-    parameter becomes.  states: (m, v) or (m, v, m_scales, v_scales), lists of tensors to be used for the moments."""
+    parameter becomes.  states: (m, v) or (m, v, m_scales, v_scales), lists of tensors to be used for the moments.  Parameters and
+    copies may be given other places later (`.data`); moments stay in the memory that they had here."""
 
     def __init__(self, params, *, bits=32, copies=None, states=None):
         if bits not in (32, 8):
@@ -121,8 +122,8 @@ class Moments:
         states = [list(s) for s in states]
         if len(states) != (2 if bits == 32 else 4) or any(len(s) != n for s in states) or len(self.copies) != n:
             raise ValueError(f"states must be {'(m, v)' if bits == 32 else '(m, v, m_scales, v_scales)'}, and they and copies must have {n} tensors each")
-        self.m, self.v = states[:2]
-        self.m_scales, self.v_scales = states[2:] if bits == 8 else ([None] * n, [None] * n)
+        self.m, self.v = map(tuple, states[:2])
+        self.m_scales, self.v_scales = map(tuple, states[2:]) if bits == 8 else ((None,) * n, (None,) * n)
         given = [c for c in self.copies if c is not None]
         self.copy_dtype = given[0].dtype if given else torch.bfloat16
         if self.copy_dtype not in _COPY_DTYPES:
@@ -132,35 +133,41 @@ class Moments:
             for t, what, dtype, size in ((p, "a parameter", self.dtype, p.numel()), (self.m[i], "m", want[0], p.numel()), (self.v[i], "v", want[1], p.numel()),
                                          (self.m_scales[i], "m_scales", torch.float32, blocks[i]), (self.v_scales[i], "v_scales", torch.float32, blocks[i]),
                                          (self.copies[i], "a copy", self.copy_dtype, p.numel())):
+                if t is None and what not in ("a copy", "m_scales", "v_scales") or t is None and bits == 8 and what != "a copy":
+                    raise ValueError(f"{what} of parameter {i} is missing")
                 if t is not None and (t.dtype != dtype or t.numel() != size or not t.is_contiguous()):
                     raise ValueError(f"{what} of parameter {i} must be {size} {dtype} without gaps")
-        self._tensors = [t for each in zip(self.params, self.copies, *states) for t in each if t is not None]
-        self._describe()
-        # two of them in one place would be written by two workgroups at a time
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self._tensors if t.numel())
-        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
-            raise ValueError("parameters, moments and copies must not overlap")
-
-    def _describe(self):
         self._sizes = [p.numel() for p in self.params]
-        self._table = array("q", bytes(64 * len(self.params)))
-        lists = ((_PARAM, self.params), (_COPY, self.copies), (_M, self.m), (_V, self.v), (_M_SCALE, self.m_scales), (_V_SCALE, self.v_scales))
-        for column, tensors in lists:
-            _read(tensors, None, self._table, 8, column)
+        self._has_copies = bool(given)
+        self._states = [[t.detach() for t in some] for some in states]  # (their memory)
+        self._table = array("q", bytes(64 * n))
         self._table[_N::8] = array("q", self._sizes)
-        if any(t.device != self.params[0].device for t in self._tensors):
+        for column, tensors in zip((_M, _V, _M_SCALE, _V_SCALE), self._states):
+            _read(tensors, None, self._table, 8, column)
+        self._settle()
+
+    def _settle(self):
+        """Parameters and copies where they are now."""
+        tensors = [t.detach() for some in (self.params, self.copies, *self._states) for t in some if t is not None]
+        if any(t.device != self.params[0].device for t in tensors):
             raise ValueError("parameters, moments and copies must be on one device")
         self.device = _current(self.params[0].device)
+        # two of them in one place would be written by two workgroups at a time
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors if t.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("parameters, moments and copies must not overlap")
+        self._tensors = tensors
+        _read(self.params, None, self._table, 8, _PARAM)
+        _read(self.copies, None, self._table, 8, _COPY)
 
     def _now(self):
-        """The table.  A parameter may have been given another place (`.data`) since: then it must still be of its kind."""
+        """The table.  A parameter or a copy may have been given another place (`.data`) since: then it must still be of its kind."""
         table = self._table[:]
-        if _read(self.params, None, table, 8, _PARAM) & _MOVED:
-            if any(p.numel() != n or p.dtype != self.dtype or p.device != self.device or not p.is_contiguous() for p, n in zip(self.params, self._sizes)):
-                raise ValueError("a parameter has changed its size, type or device")
-            self.__init__(self.params, bits=self.bits, copies=None if all(c is None for c in self.copies) else self.copies,
-                          states=(self.m, self.v) if self.bits == 32 else (self.m, self.v, self.m_scales, self.v_scales))
-            table = self._table[:]
+        if (_read(self.params, None, table, 8, _PARAM) | (self._has_copies and _read(self.copies, None, table, 8, _COPY))) & _MOVED:
+            for tensors, dtype in ((self.params, self.dtype), (self.copies, self.copy_dtype)):
+                if any(t is not None and (t.numel() != n or t.dtype != dtype or t.device != self.device or not t.is_contiguous()) for t, n in zip(tensors, self._sizes)):
+                    raise ValueError("a parameter or a copy has changed its size, type or device")
+            self._settle()
         return table  # (calls on two threads have gradients of their own)
 
 

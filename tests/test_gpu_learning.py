@@ -237,8 +237,9 @@ def test_step_and_rate_on_the_device():
         s.check(call=lambda mo, g, **kw: nuts.nuts_adamw(mo, g, **(kw | {"lr": lr})))
 
 
-def test_values():
-    s = Step([700, 1, 256, 8193], F32, F32, 8)
+@pytest.mark.parametrize("offset", [0, 3])
+def test_values(offset):
+    s = Step([700, 1, 256, 8193], F32, F32, 8, offset=offset)
     for dtype in (F32, BF16, F16):
         m, v = nuts.nuts_adamw_values(s.moments, dtype=dtype)
         for i in range(4):
@@ -353,3 +354,15 @@ def test_other_streams_graphs_and_parameters_that_move():
     leaf.data = kept.clone()
     nuts.nuts_adamw(mo, [torch.ones_like(kept)], step=1, lr=0.5, weight_decay=0.0)
     assert float((leaf.detach() - (kept - 0.5)).abs().max()) <= 1e-6
+    # a copy in another place; moments whose tensors have been given others go on in the memory that they had
+    copy = torch.zeros(5000, dtype=BF16, device="cuda")
+    p = kept.clone()
+    mo = nuts.Moments([p], copies=[copy])
+    m = mo.m[0].detach()
+    copy.data = torch.zeros(5000, dtype=BF16, device="cuda")
+    mo.m[0].data = torch.zeros(7, device="cuda")
+    nuts.nuts_adamw(mo, [torch.ones_like(kept)], step=1, lr=0.5, weight_decay=0.0)
+    assert torch.equal(copy, p.bfloat16()) and float((m - 0.1).abs().max()) <= 1e-7
+    copy.data = torch.zeros(4999, dtype=BF16, device="cuda")
+    with pytest.raises(ValueError):
+        nuts.nuts_adamw(mo, [torch.ones_like(kept)], step=2, lr=0.5)

@@ -170,7 +170,8 @@ def test_tensors_that_do_not_fit():
                  lambda: nuts.Moments([]), lambda: nuts.Moments([x], bits=16), lambda: nuts.Moments([x.half()]), lambda: nuts.Moments([x, x.bfloat16()]),
                  lambda: nuts.Moments([x.t()]), lambda: nuts.Moments([x], copies=[]), lambda: nuts.Moments([x], copies=[x.clone()]),
                  lambda: nuts.Moments([x], copies=[x.half()[:3]]), lambda: nuts.Moments([x, x]), lambda: nuts.Moments([x[:3], x[2:]]),
-                 lambda: nuts.Moments([x], states=([x.clone()], [x])), lambda: nuts.Moments([x], states=([x.clone()],)),
+                 lambda: nuts.Moments([x], states=([x.clone()], [x])), lambda: nuts.Moments([x], states=([x.clone()],)), lambda: nuts.Moments([x], states=([None], [x.clone()])),
+                 lambda: nuts.Moments([x], bits=8, states=([x.char()], [x.byte()], [None], [torch.zeros(1)])),
                  lambda: nuts.Moments([x], states=([x.clone()], [x.clone().half()])), lambda: nuts.Moments([x], bits=8, states=([x.clone()], [x.clone()])),
                  lambda: nuts.Moments([x], bits=8, states=([x.clone().char()], [x.clone().byte()], [torch.zeros(2)], [torch.zeros(1)])),
                  lambda: nuts.nuts_adamw_values(nuts.Moments([x])), lambda: nuts.nuts_adamw_values(nuts.Moments([x], bits=8), out=([x], [])),
