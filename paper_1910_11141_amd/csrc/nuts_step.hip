@@ -327,13 +327,20 @@ __device__ __forceinline__ float m_code(float m, const Scale& scale, unsigned wo
     const bool up = __builtin_fmaf(-c, c, x) > gap * chance(word);
     return __builtin_copysignf(up ? c + 1.f : c, m);
 }
-__device__ __forceinline__ float v_code(float root, const Scale& scale, unsigned word)
+// For a code c of v: c^4, and ((c + 1)^4 - c^4) / 1024.  A table in LDS, for the vector units have the most to do here.
+constexpr int kSteps = 256;
+__device__ __forceinline__ float2 v_step(float c)
 {
-    const float x = in_units(root, scale), c = floorf(__builtin_amdgcn_sqrtf(x));
     const float below = c * c, gap = __builtin_fmaf(2.f, c, 1.f);  // (c + 1)^2 - c^2
-    // ((c + 1)^4 - c^4) / 1024
-    const bool up = x * x - below * below > gap * __builtin_fmaf(2.f / 1024.f, below, gap * (1.f / 1024.f)) * chance(word >> 10);
-    return fmaxf(up ? c + 1.f : c, fminf(x * 0x1p126f, 1.f));  // (1 at least, where there is anything)
+    return float2{below * below, gap * __builtin_fmaf(2.f / 1024.f, below, gap * (1.f / 1024.f))};
+}
+__device__ __forceinline__ unsigned v_code(float root, const Scale& scale, unsigned word, const float2* steps)
+{
+    const float x = in_units(root, scale);
+    const unsigned c = (unsigned)__builtin_amdgcn_sqrtf(x);  // 254 at most: x is 254^2 and a unit in its last place at most
+    const float2 step = steps[c];
+    const unsigned code = c + (x * x - step.x > step.y * chance(word >> 10));
+    return max(code, (unsigned)(x > 0.f));  // (1 at least, where there is anything)
 }
 // The square root of a number of 24 places, rounded once: from one that is a unit or two in the last place off, and the remainder of its square.
 __device__ __forceinline__ float exact_root(float v)
@@ -425,7 +432,7 @@ __device__ __forceinline__ bool decode(unsigned m_word, unsigned v_word, float m
 
 // A block's moments, four in each lane, as codes and scales.  lost: some may not be finite.
 __device__ __forceinline__ void encode(const nuts_adamw_tensor& t, long block, long i, int n, bool lost, float (&m)[4], float (&root)[4],
-                                       const unsigned (&words)[4])
+                                       const unsigned (&words)[4], const float2* steps)
 {
     unsigned m_lost = 0, v_lost = 0;
     if (lost) {
@@ -446,9 +453,7 @@ __device__ __forceinline__ void encode(const nuts_adamw_tensor& t, long block, l
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         m_word |= ((unsigned)(int)m_code(m[e], m_scale, words[e]) & 255u) << 8 * e;
-#ifdef __HIP_DEVICE_COMPILE__
-        v_word = __builtin_amdgcn_cvt_pk_u8_f32(v_code(root[e], v_scale, words[e]), e, v_word);
-#endif
+        v_word |= v_code(root[e], v_scale, words[e], steps) << 8 * e;
     }
     store_codes(t.m, i, n, lost ? (m_word & ~m_lost) | (m_lost & 0x80808080u) : m_word);
     store_codes(t.v, i, n, v_word | v_lost);
@@ -460,7 +465,7 @@ __device__ __forceinline__ void encode(const nuts_adamw_tensor& t, long block, l
 
 // Four numbers of each lane, from i on; kWhole: every lane has four.
 template <typename P, typename G, bool kEight, bool kWhole>
-__device__ __forceinline__ void step_block(const StepArgs& a, const Factors& f, const nuts_adamw_tensor& t, unsigned tensor, long at, long end)
+__device__ __forceinline__ void step_block(const StepArgs& a, const Factors& f, const nuts_adamw_tensor& t, unsigned tensor, long at, long end, const float2* steps)
 {
     const long i = at + threadIdx.x % 64 * 4, block = at / 256;
     const int n = kWhole ? 4 : (int)max(min(end - i, 4l), 0l);
@@ -506,7 +511,7 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const Factors& f, 
     store4(static_cast<P*>(t.param) + i, n, p);
     if (t.copy) a.copy_dtype == NUTS_BF16 ? store4(static_cast<bf16*>(t.copy) + i, n, p) : store4(static_cast<f16*>(t.copy) + i, n, p);
     if (kEight) {
-        encode(t, block, i, n, lost, m, root, words);
+        encode(t, block, i, n, lost, m, root, words, steps);
     } else {
         store4(static_cast<float*>(t.m) + i, n, m);
         store4(static_cast<float*>(t.v) + i, n, v);
@@ -517,12 +522,19 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const Factors& f, 
 //
 // 32 bits: bound by memory.  102 million numbers, all binary32: 548 us, 5.2 TB/s; 120 million with gradients and copies of 16 bits in 150 tensors, three
 // launches, 640 us, 4.9 TB/s.
-// 8 bits: 200 million binary32 parameters with gradients and copies of 16 bits 646 us, 5.0 TB/s.  Instructions are as near: some 98 a number, of which
-// the ten rounds of Philox are 10 and the two codes 42 (with a table of c^4 and its steps in LDS they are 36, and the time 642).  With library roots and quotients,
-// lanes checked one by one and codes by bytes the same took 1290 us.
+// 8 bits: 200 million binary32 parameters with gradients and copies of 16 bits 643 us, 5.0 TB/s.  Instructions are as near: some 92 a number, of which
+// the ten rounds of Philox are 10 and the two codes 36 (42 without the table of the codes' steps); 67 million bfloat16 parameters and gradients, 10 bytes a
+// number, 177 us, 3.8 TB/s, are bound by them (183 without the table).  With library roots and quotients, lanes checked one by one and
+// codes by bytes 200 million took 1290 us.
 template <typename P, typename G, bool kEight>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a)
 {
+    __shared__ float2 steps[kEight ? kSteps : 1];
+    if (kEight) {
+        static_assert(kThreads == kSteps, "a thread a step");
+        steps[threadIdx.x] = v_step((float)threadIdx.x);
+        __syncthreads();
+    }
     const float factor = a.factor ? *a.factor : 1.f;
     if (factor != factor) return;
     const Factors f = factors_of(a, factor);
@@ -531,8 +543,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a)
     const long begin = (a.first_block + (long)((int)blockIdx.x - a.first[k])) * a.chunk, end = min(begin + a.chunk, (long)t.n);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     long at = begin + wave * 256;
-    for (; at + 256 <= end; at += kThreads * 4) step_block<P, G, kEight, true>(a, f, t, a.first_tensor + k, at, end);
-    if (at < end) step_block<P, G, kEight, false>(a, f, t, a.first_tensor + k, at, end);
+    for (; at + 256 <= end; at += kThreads * 4) step_block<P, G, kEight, true>(a, f, t, a.first_tensor + k, at, end, steps);
+    if (at < end) step_block<P, G, kEight, false>(a, f, t, a.first_tensor + k, at, end, steps);
 }
 
 // Eight numbers a thread.  Bound by memory: 200 million to bfloat16 234 us, 5.1 TB/s (285 with four numbers a thread).
