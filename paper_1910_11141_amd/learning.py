@@ -100,18 +100,19 @@ class Moments:
     (`m`, `v`: float32, as the parameters) or in 8 (`m` int8, `v` uint8, as the parameters; `m_scales`, `v_scales`: float32, one for each 256 of a
     parameter's numbers).  copies: a tensor of bfloat16 or float16 for each parameter (or None), which receives what the
     parameter becomes.  states: (m, v) or (m, v, m_scales, v_scales), lists of tensors to be used for the moments.  Parameters and
-    copies may be given other places later (`.data`); moments stay in the memory that they had here."""
+    copies may be given other places later (`.data`); moments stay in the memory that they had here.  Can be copied (deeply: together with the
+    parameters) and pickled."""
 
     def __init__(self, params, *, bits=32, copies=None, states=None):
         if bits not in (32, 8):
             raise ValueError("bits must be 32 or 8")
-        self.params, self.bits = list(params), bits
+        self.params, self.bits = tuple(params), bits
         if not self.params:
             raise ValueError("Moments needs a parameter")
         self.dtype = self.params[0].dtype
         if self.dtype not in _PARAM_DTYPES:
             raise ValueError(f"parameters must be {' or '.join(str(d) for d in _PARAM_DTYPES)}")
-        self.copies = list(copies) if copies is not None else [None] * len(self.params)
+        self.copies = tuple(copies) if copies is not None else (None,) * len(self.params)
         n = len(self.params)
         blocks = [-(-p.numel() // _b.NUTS_STATE_BLOCK) for p in self.params]
         if states is None:
@@ -137,6 +138,7 @@ class Moments:
                     raise ValueError(f"{what} of parameter {i} is missing")
                 if t is not None and (t.dtype != dtype or t.numel() != size or not t.is_contiguous()):
                     raise ValueError(f"{what} of parameter {i} must be {size} {dtype} without gaps")
+        self._params, self._copies = list(self.params), list(self.copies)  # (as _read wants them)
         self._sizes = [p.numel() for p in self.params]
         self._has_copies = bool(given)
         self._states = [[t.detach() for t in some] for some in states]  # (their memory)
@@ -145,6 +147,10 @@ class Moments:
         for column, tensors in zip((_M, _V, _M_SCALE, _V_SCALE), self._states):
             _read(tensors, None, self._table, 8, column)
         self._settle()
+
+    def __reduce__(self):
+        """Copies, and what comes back from a file, have tables of their own tensors' addresses."""
+        return _moments, (self.params, self.bits, self.copies if self._has_copies else None, self._states)
 
     def _settle(self):
         """Parameters and copies where they are now."""
@@ -157,18 +163,22 @@ class Moments:
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("parameters, moments and copies must not overlap")
         self._tensors = tensors
-        _read(self.params, None, self._table, 8, _PARAM)
-        _read(self.copies, None, self._table, 8, _COPY)
+        _read(self._params, None, self._table, 8, _PARAM)
+        _read(self._copies, None, self._table, 8, _COPY)
 
     def _now(self):
         """The table.  A parameter or a copy may have been given another place (`.data`) since: then it must still be of its kind."""
         table = self._table[:]
-        if (_read(self.params, None, table, 8, _PARAM) | (self._has_copies and _read(self.copies, None, table, 8, _COPY))) & _MOVED:
+        if (_read(self._params, None, table, 8, _PARAM) | (self._has_copies and _read(self._copies, None, table, 8, _COPY))) & _MOVED:
             for tensors, dtype in ((self.params, self.dtype), (self.copies, self.copy_dtype)):
                 if any(t is not None and (t.numel() != n or t.dtype != dtype or t.device != self.device or not t.is_contiguous()) for t, n in zip(tensors, self._sizes)):
                     raise ValueError("a parameter or a copy has changed its size, type or device")
             self._settle()
         return table  # (calls on two threads have gradients of their own)
+
+
+def _moments(params, bits, copies, states):
+    return Moments(params, bits=bits, copies=copies, states=states)
 
 
 def nuts_adamw(moments, grads, *, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, scale=1.0, factor=None, seed=0):
@@ -184,12 +194,12 @@ def nuts_adamw(moments, grads, *, step, lr, betas=(0.9, 0.999), eps=1e-8, weight
     if first is None:
         return
     table, dtype, device = moments._now(), first.dtype, _current(moments.device)
-    bits = _read(grads, moments.params, table, 8, _GRAD)
+    bits = _read(grads, moments._params, table, 8, _GRAD)
     if bits & (_SEVERAL_TYPES | _SEVERAL_DEVICES | _OTHER_SHAPES) or dtype not in _DTYPES or first.device != device:
         raise ValueError(f"gradients must be {' or '.join(str(d) for d in _DTYPES)}, all of one type, on {device}, each as its parameter")
     if bits & _GAPS:
         grads = [g.contiguous() if g is not None else None for g in grads]
-        _read(grads, moments.params, table, 8, _GRAD)
+        _read(grads, moments._params, table, 8, _GRAD)
     used = [g for g in grads if g is not None]
     step_at = lr_at = factor_at = None
     if isinstance(step, torch.Tensor):
@@ -228,7 +238,7 @@ def nuts_adamw_values(moments, *, dtype=torch.float32, out=None):
     if not used:
         return m, v
     table, device, dtype = moments._now(), _current(moments.device), used[0].dtype
-    bits = _read(m, moments.params, table, 8, _PARAM) | _read(v, moments.params, table, 8, _COPY)
+    bits = _read(m, moments._params, table, 8, _PARAM) | _read(v, moments._params, table, 8, _COPY)
     if bits & (_SEVERAL_TYPES | _SEVERAL_DEVICES | _OTHER_SHAPES | _GAPS) or dtype not in _DTYPES or any(t.dtype != dtype or t.device != device for t in (used[0], used[-1])):
         raise ValueError(f"out must be {' or '.join(str(d) for d in _DTYPES)}, all of one type, without gaps, on {device}, each as its parameter")
     _run(_b.lib().nuts_adamw_values, [table.buffer_info()[0], len(m), _DTYPES[dtype]], _Both(moments._tensors, used), device)

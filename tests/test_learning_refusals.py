@@ -1,4 +1,5 @@
 """Penalties, norms and AdamW steps refuse what they cannot do, on the host and before anything is written."""
+import copy
 import ctypes as C
 import subprocess
 import sys
@@ -257,3 +258,28 @@ def test_random_bits_are_the_oracles():
     assert [int(x[0]) for x in w] == [0x6627e8d5, 0xe169c58d, 0xbc57ac4c, 0x9b00dbd8]
     w = L.philox(*[torch.tensor([0xffffffff])] * 4, 0xffffffffffffffff)
     assert [int(x[0]) for x in w] == [0x408f276d, 0x41c83b0e, 0xa20bc7c6, 0x6d5451fd]
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="parameters on the CPU")
+@pytest.mark.parametrize("bits", [32, 8])
+def test_copies_of_moments_have_memory_of_their_own(bits, tmp_path):
+    p = torch.nn.Parameter(torch.ones(300))
+    mo = nuts.Moments([p, torch.zeros(5)], bits=bits, copies=[torch.zeros(300, dtype=torch.bfloat16), None])
+    mo.v[0][:3] = 3
+    torch.save(mo, tmp_path / "moments")
+    model, twin = copy.deepcopy((p, mo))
+    for other in (twin, torch.load(tmp_path / "moments", weights_only=False), copy.copy(mo)):
+        addresses = other._now()[:]
+        for i in range(2):
+            tensors = (other.params[i], None, other.copies[i], other.m[i], other.v[i], other.m_scales[i], other.v_scales[i])
+            assert [t.data_ptr() if t is not None else 0 for t in tensors] == list(addresses[8 * i:8 * i + 7])
+            assert addresses[8 * i + 7] == (300, 5)[i]
+        assert other.bits == bits and torch.equal(other.v[0], mo.v[0]) and torch.equal(other.params[0], p)
+    assert twin.params[0] is model and twin.m[0].data_ptr() != mo.m[0].data_ptr()
+
+
+def test_parameters_of_moments_stay_in_number():
+    if torch.cuda.is_available():
+        pytest.skip("parameters on the CPU")
+    mo = nuts.Moments([torch.zeros(3)])
+    assert all(isinstance(some, tuple) for some in (mo.params, mo.copies, mo.m, mo.v, mo.m_scales, mo.v_scales))
