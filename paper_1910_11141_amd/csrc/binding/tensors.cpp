@@ -23,7 +23,7 @@ int64_t type_of(const at::Tensor& t)
 
 // For each item i of `list` (of a tensor, or None), of its address, count and type those into rows[i * width + column] whose column is not negative (0 and
 // nothing for None).  Returns bits: 1 tensors of several types, 2 on several devices, 4 with gaps, 8 of another shape than the item of `like` (a list, or
-// None) in the same place, 16 an address is not what was in its place.  -1 with an exception: an item is neither.
+// None) in the same place, 16 an address or a count is not what was in its place.  -1 with an exception: an item is neither.
 extern "C" __attribute__((visibility("default"))) int nuts_tensor_table(PyObject* list, PyObject* like, int64_t* rows, int64_t width, int64_t address, int64_t count,
                                                                         int64_t type)
 try {
@@ -39,6 +39,7 @@ try {
         if (item == Py_None) {
             if (address >= 0 && row[address] != 0) bits |= 16;
             if (address >= 0) row[address] = 0;
+            if (count >= 0 && row[count] != 0) bits |= 16;
             if (count >= 0) row[count] = 0;
             continue;
         }
@@ -64,7 +65,10 @@ try {
             if (row[address] != at) bits |= 16;
             row[address] = at;
         }
-        if (count >= 0) row[count] = t.numel();
+        if (count >= 0) {
+            if (row[count] != t.numel()) bits |= 16;
+            row[count] = t.numel();
+        }
         if (type >= 0) row[type] = type_of(t);
     }
     return bits;

@@ -141,6 +141,7 @@ class Moments:
         self._params, self._copies = list(self.params), list(self.copies)  # (as _read wants them)
         self._sizes = [p.numel() for p in self.params]
         self._has_copies = bool(given)
+        self._copy_sizes = array("q", [c.numel() if c is not None else 0 for c in self.copies])
         self._states = [[t.detach() for t in some] for some in states]  # (their memory)
         self._table = array("q", bytes(64 * n))
         self._table[_N::8] = array("q", self._sizes)
@@ -169,7 +170,10 @@ class Moments:
     def _now(self):
         """The table.  A parameter or a copy may have been given another place (`.data`) since: then it must still be of its kind."""
         table = self._table[:]
-        if (_read(self._params, None, table, 8, _PARAM) | (self._has_copies and _read(self._copies, None, table, 8, _COPY))) & _MOVED:
+        bits = _read(self._params, None, table, 8, _PARAM, _N)
+        if self._has_copies:
+            bits |= _read(self._copies, None, table, 8, _COPY) | _read(self._copies, None, self._copy_sizes[:], 1, -1, 0)
+        if bits & (_MOVED | _GAPS | _SEVERAL_TYPES):
             for tensors, dtype in ((self.params, self.dtype), (self.copies, self.copy_dtype)):
                 if any(t is not None and (t.numel() != n or t.dtype != dtype or t.device != self.device or not t.is_contiguous()) for t, n in zip(tensors, self._sizes)):
                     raise ValueError("a parameter or a copy has changed its size, type or device")

@@ -1,4 +1,5 @@
 """The norm of many tensors and AdamW steps over them, with moments of 32 and of 8 bits, against 64 bits."""
+import copy
 import math
 
 import pytest
@@ -366,3 +367,18 @@ def test_other_streams_graphs_and_parameters_that_move():
     copy.data = torch.zeros(4999, dtype=BF16, device="cuda")
     with pytest.raises(ValueError):
         nuts.nuts_adamw(mo, [torch.ones_like(kept)], step=2, lr=0.5)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_copies_of_moments_step_by_themselves(bits, tmp_path):
+    s = Step([300, 1000], F32, BF16, bits, copies=BF16)
+    torch.save(s.moments, tmp_path / "moments")
+    twins = [copy.deepcopy(s.moments), torch.load(tmp_path / "moments", weights_only=False)]
+    before = [t.clone() for t in s.moments._tensors]
+    for twin in twins:
+        nuts.nuts_adamw(twin, s.grads, step=7, lr=0.1, seed=5)
+    assert all(torch.equal(a, b) for a, b in zip(before, s.moments._tensors))
+    nuts.nuts_adamw(s.moments, s.grads, step=7, lr=0.1, seed=5)
+    for twin in twins:
+        assert all(torch.equal(a, b) for a, b in zip(twin._tensors, s.moments._tensors))
+    assert not torch.equal(before[0], s.params[0])

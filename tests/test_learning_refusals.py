@@ -283,3 +283,16 @@ def test_parameters_of_moments_stay_in_number():
         pytest.skip("parameters on the CPU")
     mo = nuts.Moments([torch.zeros(3)])
     assert all(isinstance(some, tuple) for some in (mo.params, mo.copies, mo.m, mo.v, mo.m_scales, mo.v_scales))
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="parameters on the CPU")
+@pytest.mark.parametrize("part", [lambda p: p[:2], lambda p: p.t(), lambda p: p.view(torch.int8)])
+@pytest.mark.parametrize("what", ["parameter", "copy"])
+def test_parameters_and_copies_that_are_another_part_of_their_memory(part, what):
+    p, c = torch.zeros(4, 4), torch.zeros(4, 4, dtype=torch.bfloat16)
+    mo = nuts.Moments([p, torch.zeros(3)], copies=[c, None], bits=8)
+    x = p if what == "parameter" else c
+    x.data = part(x.data)
+    for call in (lambda: nuts.nuts_adamw(mo, [torch.zeros(p.shape), torch.zeros(3)], step=1, lr=0.1), lambda: nuts.nuts_adamw_values(mo)):
+        with pytest.raises(ValueError, match="changed its size, type or device"):
+            call()
