@@ -188,7 +188,7 @@ struct Counters {
 // What single classes have as biases of their own: the row's, in their order, those of other slices with no class.  One of a class's biases stands
 // for it in the end: its value is their sum, its count what was counted, and the class's counter is its place.
 struct Biases {
-    alignas(16) uint16_t v[NUTS_CAT_MAX_BIAS];  // (eight at a time, the last ones with kNone behind them)
+    uint16_t v[NUTS_CAT_MAX_BIAS];
     float value[NUTS_CAT_MAX_BIAS];
     unsigned count[NUTS_CAT_MAX_BIAS];
 
@@ -198,10 +198,10 @@ struct Biases {
     template <typename W>
     __device__ __forceinline__ void read(const PenaltyArgs& a, long row, int begin, int n)
     {
-        for (int k = threadIdx.x; k < (a.n_bias + 7) / 8 * 8; k += W::kThreads) {
-            const uint64_t at = k < a.n_bias ? (uint64_t)id_at(a.bias_ids, a.id_type, row * a.n_bias + k) - (uint64_t)begin : ~(uint64_t)0;
+        for (int k = threadIdx.x; k < a.n_bias; k += W::kThreads) {
+            const uint64_t at = (uint64_t)id_at(a.bias_ids, a.id_type, row * a.n_bias + k) - (uint64_t)begin;
             v[k] = at < (uint64_t)n ? (uint16_t)at : kNone;
-            if (k < a.n_bias) value[k] = a.bias_values[row * a.n_bias + k];
+            value[k] = a.bias_values[row * a.n_bias + k];
         }
     }
     // While others count: the counters' bits do not touch.  Returns a bit for each of this thread's biases that is to stand for its class.
@@ -216,29 +216,41 @@ struct Biases {
         }
         return mine;
     }
-    // (behind a barrier; the values of a class are read by one thread, which then writes one of them)
+    // Behind a barrier.  Classes of several values are added up by whole waves, one class after the other: the values of a class are read by one wave,
+    // which then writes one of them.  (1000 rows of 8000 with 1000 biases each at random: 41 us, 178 with a thread for each class that looks through all;
+    // 64 rows of 128000 with 300: 11.5, 19.9; 4096 rows of 1000 with 300: 68, 73.)
     template <typename W>
     __device__ __forceinline__ void add_up(const PenaltyArgs& a, unsigned mine, unsigned* shared)
     {
-        for (int k = threadIdx.x; k < a.n_bias; k += W::kThreads, mine /= 2) {
-            if (!(mine & 1)) continue;
-            const unsigned c = shared[v[k]];
-            if (c & kAgain) {
-                const unsigned twice = v[k] * 0x10001u;
+#ifdef __HIP_DEVICE_COMPILE__
+        constexpr int kFlight = 4;
+        static_assert(NUTS_CAT_MAX_BIAS % (kFlight * 64) == 0, "what is read and not a bias is not behind the arrays");
+        const int lane = (int)threadIdx.x % 64;
+        for (int first = __builtin_amdgcn_readfirstlane((int)threadIdx.x - lane); first < a.n_bias; first += W::kThreads, mine /= 2) {
+            const int k = first + lane;
+            const bool stands = mine & 1;
+            const int own = stands ? v[k] : kNone;
+            const unsigned c = stands ? shared[own] : 0;
+            for (uint64_t several = __builtin_amdgcn_ballot_w64(c & kAgain); several; several &= several - 1) {
+                const int leader = __builtin_ctzll(several), its = __builtin_amdgcn_readlane(own, leader);
                 float sum = -0.f;  // (which adds nothing to anything)
-#pragma unroll 2
-                for (int j = 0; j < a.n_bias; j += 8) {
-                    const uint4 some = *reinterpret_cast<const uint4*>(&v[j]);
-                    const unsigned off[4] = {some.x ^ twice, some.y ^ twice, some.z ^ twice, some.w ^ twice};
+                for (int from = 0; from < a.n_bias; from += kFlight * 64) {
+                    int at[kFlight], x[kFlight];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if ((off[e / 2] >> e % 2 * 16 & 0xffffu) == 0) sum += value[j + e];
+                    for (int u = 0; u < kFlight; ++u) at[u] = v[from + u * 64 + lane], x[u] = __float_as_int(value[from + u * 64 + lane]);
+#pragma unroll
+                    for (int u = 0; u < kFlight; ++u)
+                        for (uint64_t hits = __builtin_amdgcn_ballot_w64(at[u] == its && from + u * 64 + lane < a.n_bias); hits; hits &= hits - 1)
+                            sum += __int_as_float(__builtin_amdgcn_readlane(x[u], __builtin_ctzll(hits)));
                 }
-                value[k] = sum;
+                if (lane == leader) value[k] = sum;
             }
-            count[k] = c & kSeen;
-            shared[v[k]] = kBiased | (unsigned)k;
+            if (stands) {
+                count[k] = c & kSeen;
+                shared[own] = kBiased | (unsigned)k;
+            }
         }
+#endif
     }
 };
 
