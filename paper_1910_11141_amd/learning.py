@@ -73,19 +73,20 @@ def _scalar(t, what, dtype, device):
 def nuts_norm(tensors, *, max_norm=1.0):
     """(norm, factor), float32 scalars on the device: the square root of the sum of all squares of `tensors`, and what all of them are to
     be multiplied with so that it is no more than max_norm (NaN where the norm is not finite).  None among them counts as nothing."""
-    tensors = [t for t in tensors if t is not None]
-    if not tensors:
+    tensors = list(tensors)
+    first = next((t for t in tensors if t is not None), None)
+    if first is None:
         raise ValueError("nuts_norm needs a tensor")
     table = array("q", bytes(24 * len(tensors)))
     bits = _read(tensors, None, table, 3, 0, 1, 2)
     if bits & _GAPS:
-        tensors = [t.contiguous() for t in tensors]
+        tensors = [t.contiguous() if t is not None else None for t in tensors]
         _read(tensors, None, table, 3, 0, 1, 2)
     if bits & _SEVERAL_DEVICES:
         raise ValueError("tensors must be on one device")
-    if bits & _SEVERAL_TYPES and -1 in table[2::3] or tensors[0].dtype not in _DTYPES:
+    if bits & _SEVERAL_TYPES and -1 in table[2::3] or first.dtype not in _DTYPES:
         raise ValueError(f"tensors must be {' or '.join(str(d) for d in _DTYPES)}")
-    device = _current(tensors[0].device)
+    device = _current(first.device)
     L, size, at = _b.lib(), C.c_int64(), table.buffer_info()[0]
     _b._check(L.nuts_norm_workspace(at, len(tensors), C.byref(size)))
     norm, factor = torch.empty(2, dtype=torch.float32, device=device).unbind(0)
@@ -172,7 +173,9 @@ class Moments:
         table = self._table[:]
         bits = _read(self._params, None, table, 8, _PARAM, _N)
         if self._has_copies:
-            bits |= _read(self._copies, None, table, 8, _COPY) | _read(self._copies, None, self._copy_sizes[:], 1, -1, 0)
+            bits |= _read(self._copies, self._params, table, 8, _COPY)
+            if bits & _OTHER_SHAPES:  # (or the same number in another shape)
+                bits |= _read(self._copies, None, self._copy_sizes[:], 1, -1, 0)
         if bits & (_MOVED | _GAPS | _SEVERAL_TYPES):
             for tensors, dtype in ((self.params, self.dtype), (self.copies, self.copy_dtype)):
                 if any(t is not None and (t.numel() != n or t.dtype != dtype or t.device != self.device or not t.is_contiguous()) for t, n in zip(tensors, self._sizes)):
@@ -204,22 +207,21 @@ def nuts_adamw(moments, grads, *, step, lr, betas=(0.9, 0.999), eps=1e-8, weight
     if bits & _GAPS:
         grads = [g.contiguous() if g is not None else None for g in grads]
         _read(grads, moments._params, table, 8, _GRAD)
-    used = [g for g in grads if g is not None]
+    scalars = [t for t in (step, lr, factor) if isinstance(t, torch.Tensor)]
     step_at = lr_at = factor_at = None
     if isinstance(step, torch.Tensor):
-        step_at, step = _scalar(step, "step", torch.int64, device), used.append(step) or 1
+        step_at, step = _scalar(step, "step", torch.int64, device), 1
     if isinstance(lr, torch.Tensor):
-        lr_at, lr = _scalar(lr, "lr", torch.float32, device), used.append(lr) or 0.0
+        lr_at, lr = _scalar(lr, "lr", torch.float32, device), 0.0
     if factor is not None:
         factor_at = _scalar(factor, "factor", torch.float32, device)
-        used.append(factor)
     desc = _b.nuts_adamw_desc(_PARAM_DTYPES[moments.dtype], _DTYPES[dtype], _COPY_DTYPES[moments.copy_dtype], moments.bits, float(lr), float(betas[0]),
                               float(betas[1]), float(eps), float(weight_decay), float(scale), int(step), int(seed) & 0xFFFFFFFFFFFFFFFF)
-    _run(_b.lib().nuts_adamw, [C.byref(desc), table.buffer_info()[0], len(grads), step_at, lr_at, factor_at], _Both(moments._tensors, used), device)
+    _run(_b.lib().nuts_adamw, [C.byref(desc), table.buffer_info()[0], len(grads), step_at, lr_at, factor_at], _Chain(moments._tensors, grads, scalars), device)
 
 
-class _Both:
-    """Two lists, one behind the other, that are gone through only where a stream has to be told of them."""
+class _Chain:
+    """Lists, one behind the other, that are gone through only where a stream has to be told of them."""
 
     def __init__(self, *lists):
         self.lists = lists
@@ -245,5 +247,5 @@ def nuts_adamw_values(moments, *, dtype=torch.float32, out=None):
     bits = _read(m, moments._params, table, 8, _PARAM) | _read(v, moments._params, table, 8, _COPY)
     if bits & (_SEVERAL_TYPES | _SEVERAL_DEVICES | _OTHER_SHAPES | _GAPS) or dtype not in _DTYPES or any(t.dtype != dtype or t.device != device for t in (used[0], used[-1])):
         raise ValueError(f"out must be {' or '.join(str(d) for d in _DTYPES)}, all of one type, without gaps, on {device}, each as its parameter")
-    _run(_b.lib().nuts_adamw_values, [table.buffer_info()[0], len(m), _DTYPES[dtype]], _Both(moments._tensors, used), device)
+    _run(_b.lib().nuts_adamw_values, [table.buffer_info()[0], len(m), _DTYPES[dtype]], _Chain(moments._tensors, used), device)
     return m, v
