@@ -183,34 +183,80 @@ int64_t norm_blocks(const nuts_tensor* tensors, int64_t n)
 
 // ---- AdamW ----------------------------------------------------------------------------------------------------------
 
-constexpr int kStepTensors = 56;
 // Numbers of a workgroup: 256 a wave at a time, eight times in large calls; in small ones as few times as kStepBlocks workgroups allow (16000
 // numbers: 8.4 us with eight times, 3.8 with one).
 constexpr int64_t kChunkLeast = 1024, kChunkMost = 8192, kStepBlocks = 1024;
 
+// What a launch knows of its tensors.  Addresses and counts of 48 bits, so that there are more tensors: 300 of 100 numbers 26 us, 37 with 56 tensors a launch.
+template <bool kEight>
 struct StepArgs {
-    nuts_adamw_tensor tensor[kStepTensors];
-    int first[kStepTensors];
+    static constexpr int kPlaces = kEight ? 8 : 6, kTensors = kEight ? 75 : 98;
+    unsigned tensor[kTensors][kPlaces * 3 / 2];
+    int first[kTensors];
+    unsigned t, k0, k1, first_tensor;
     const int64_t* step;
     const float* lr_at;
     const float* factor;
     double log_beta1, log_beta2, lr, decay;
     float beta1, rest1, beta2, rest2, eps, scale;
     float keep, size, root_scale;  // 1 - lr d, lr / (1 - b1^t), 1 / sqrt(1 - b2^t), where neither t nor lr is on the device
-    unsigned t, k0, k1, first_tensor;
     int chunk;
     long first_block;
     int64_t host_step;
     int copy_dtype;
 };
-static_assert(sizeof(StepArgs) <= 4096, "the arguments of a launch");
+static_assert(sizeof(StepArgs<false>) <= 4096 && sizeof(StepArgs<true>) <= 4096, "the arguments of a launch");
+
+// A tensor's addresses and count, two in three words.
+template <bool kEight>
+void pack_tensor(const nuts_adamw_tensor& t, unsigned* words)
+{
+    const uint64_t place[8] = {(uint64_t)t.n,          (uint64_t)(uintptr_t)t.param, (uint64_t)(uintptr_t)t.grad,    (uint64_t)(uintptr_t)t.copy,
+                               (uint64_t)(uintptr_t)t.m, (uint64_t)(uintptr_t)t.v,     (uint64_t)(uintptr_t)t.m_scale, (uint64_t)(uintptr_t)t.v_scale};
+    for (int k = 0; k < StepArgs<kEight>::kPlaces; k += 2, words += 3) {
+        words[0] = (unsigned)place[k];
+        words[1] = (unsigned)(place[k] >> 32 & 0xffff) | (unsigned)place[k + 1] << 16;
+        words[2] = (unsigned)(place[k + 1] >> 16);
+    }
+}
+// (of the device's memory, which an address alone does not say)
+__device__ __forceinline__ void* global(uint64_t address)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    return (void*)(__attribute__((address_space(1))) void*)address;
+#else
+    return reinterpret_cast<void*>(address);
+#endif
+}
+template <bool kEight>
+__device__ __forceinline__ nuts_adamw_tensor unpack_tensor(const unsigned* words)
+{
+    uint64_t place[8] = {};
+#pragma unroll
+    for (int k = 0; k < StepArgs<kEight>::kPlaces; k += 2) {
+        const unsigned *w = words + k * 3 / 2, middle = w[1];
+        place[k] = (uint64_t)(middle & 0xffffu) << 32 | w[0];
+        place[k + 1] = (uint64_t)w[2] << 16 | middle >> 16;
+    }
+    nuts_adamw_tensor t;
+    t.n = (int64_t)place[0];
+    t.param = global(place[1]);
+    t.grad = global(place[2]);
+    t.copy = global(place[3]);
+    t.m = global(place[4]);
+    t.v = global(place[5]);
+    t.m_scale = static_cast<float*>(global(place[6]));
+    t.v_scale = static_cast<float*>(global(place[7]));
+    return t;
+}
 
 struct Factors {
     float scale, keep, size, root_scale;
     unsigned t;
 };
 
-__device__ __forceinline__ Factors factors_of(const StepArgs& a, float factor)
+template <bool kEight>
+__device__ __forceinline__ Factors factors_of(const StepArgs<kEight>& a, float factor)
 {
     Factors f{a.scale * factor, a.keep, a.size, a.root_scale, a.t};
     if (a.step || a.lr_at) {
@@ -465,7 +511,7 @@ __device__ __forceinline__ void encode(const nuts_adamw_tensor& t, long block, l
 
 // Four numbers of each lane, from i on; kWhole: every lane has four.
 template <typename P, typename G, bool kEight, bool kWhole>
-__device__ __forceinline__ void step_block(const StepArgs& a, const Factors& f, const nuts_adamw_tensor& t, unsigned tensor, long at, long end, const float2* steps)
+__device__ __forceinline__ void step_block(const StepArgs<kEight>& a, const Factors& f, const nuts_adamw_tensor& t, unsigned tensor, long at, long end, const float2* steps)
 {
     const long i = at + threadIdx.x % 64 * 4, block = at / 256;
     const int n = kWhole ? 4 : (int)max(min(end - i, 4l), 0l);
@@ -520,14 +566,14 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const Factors& f, 
 
 // A workgroup `chunk` numbers of a tensor, a wave 256 of them at a time: a block of the moments of 8 bits.  One pass, each number read and written once.
 //
-// 32 bits: bound by memory.  102 million numbers, all binary32: 548 us, 5.2 TB/s; 120 million with gradients and copies of 16 bits in 150 tensors, three
-// launches, 640 us, 4.9 TB/s.
-// 8 bits: 200 million binary32 parameters with gradients and copies of 16 bits 643 us, 5.0 TB/s.  Instructions are as near: some 92 a number, of which
+// 32 bits: bound by memory.  102 million numbers, all binary32: 548 us, 5.2 TB/s; 120 million with gradients and copies of 16 bits in 150 tensors, two
+// launches, 632 us, 5.3 TB/s.
+// 8 bits: 200 million binary32 parameters with gradients and copies of 16 bits 657 us, 4.9 TB/s.  Instructions are as near: some 92 a number, of which
 // the ten rounds of Philox are 10 and the two codes 36 (42 without the table of the codes' steps); 67 million bfloat16 parameters and gradients, 10 bytes a
 // number, 177 us, 3.8 TB/s, are bound by them (183 without the table).  With library roots and quotients, lanes checked one by one and
 // codes by bytes 200 million took 1290 us.
 template <typename P, typename G, bool kEight>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a)
+__global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs<kEight> a)
 {
     __shared__ float2 steps[kEight ? kSteps : 1];
     if (kEight) {
@@ -539,7 +585,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a)
     if (factor != factor) return;
     const Factors f = factors_of(a, factor);
     const int k = tensor_of(a.first, (int)blockIdx.x);
-    const nuts_adamw_tensor& t = a.tensor[k];
+    const nuts_adamw_tensor t = unpack_tensor<kEight>(a.tensor[k]);
     const long begin = (a.first_block + (long)((int)blockIdx.x - a.first[k])) * a.chunk, end = min(begin + a.chunk, (long)t.n);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     long at = begin + wave * 256;
@@ -549,11 +595,11 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a)
 
 // Eight numbers a thread.  Bound by memory: 200 million to bfloat16 234 us, 5.1 TB/s (285 with four numbers a thread).
 template <typename T>
-__global__ __launch_bounds__(kThreads) void values_kernel(StepArgs a)
+__global__ __launch_bounds__(kThreads) void values_kernel(StepArgs<true> a)
 {
     constexpr int kEach = 8;
     const int k = tensor_of(a.first, (int)blockIdx.x);
-    const nuts_adamw_tensor& t = a.tensor[k];
+    const nuts_adamw_tensor t = unpack_tensor<true>(a.tensor[k]);
     const long begin = (a.first_block + (long)((int)blockIdx.x - a.first[k])) * a.chunk, end = min(begin + a.chunk, (long)t.n);
     for (long at = begin; at < end; at += kThreads * kEach) {  // (whole waves)
         const long i = at + (long)threadIdx.x * kEach;
@@ -588,9 +634,10 @@ __global__ __launch_bounds__(kThreads) void values_kernel(StepArgs a)
 }
 
 // Calls `go` for as many tensors at a time as a launch takes, and as many workgroups as it takes.
-template <typename Wanted, typename Go>
-void by_tables(StepArgs& a, const nuts_adamw_tensor* tensors, int64_t n, Wanted wanted, Go go)
+template <bool kEight, typename Wanted, typename Go>
+void by_tables(StepArgs<kEight>& a, const nuts_adamw_tensor* tensors, int64_t n, Wanted wanted, Go go)
 {
+    constexpr int kTensors = StepArgs<kEight>::kTensors;
     int64_t at = 0, total = 0;
     for (int64_t i = 0; i < n; ++i) total += wanted(tensors[i]) ? tensors[i].n : 0;
     a.chunk = (int)std::clamp(ceil_div(ceil_div(total, kStepBlocks), kChunkLeast) * kChunkLeast, kChunkLeast, kChunkMost);
@@ -599,13 +646,13 @@ void by_tables(StepArgs& a, const nuts_adamw_tensor* tensors, int64_t n, Wanted 
         int used = 0;
         a.first_tensor = (unsigned)at;
         a.first_block = 0;
-        for (; used < kStepTensors && at < n; ++used, ++at) {
+        for (; used < kTensors && at < n; ++used, ++at) {
             const int64_t own = wanted(tensors[at]) ? ceil_div(tensors[at].n, a.chunk) : 0;
             if (blocks + own > kMaxBlocks) {
                 if (used > 0) break;
                 // a tensor of more workgroups than a launch has: alone, in several
-                a.tensor[0] = tensors[at];
-                for (int k = 0; k < kStepTensors; ++k) a.first[k] = k ? INT32_MAX : 0;
+                pack_tensor<kEight>(tensors[at], a.tensor[0]);
+                for (int k = 0; k < kTensors; ++k) a.first[k] = k ? INT32_MAX : 0;
                 for (int64_t done = 0; done < own; done += kMaxBlocks) {
                     a.first_block = (long)done;
                     go((unsigned)std::min<int64_t>(own - done, kMaxBlocks));
@@ -615,29 +662,66 @@ void by_tables(StepArgs& a, const nuts_adamw_tensor* tensors, int64_t n, Wanted 
                 ++at;
                 break;
             }
-            a.tensor[used] = tensors[at];
+            pack_tensor<kEight>(tensors[at], a.tensor[used]);
             a.first[used] = (int)blocks;
             blocks += own;
         }
         if (blocks == 0) continue;
-        for (int k = used; k < kStepTensors; ++k) a.first[k] = INT32_MAX;
+        for (int k = used; k < kTensors; ++k) a.first[k] = INT32_MAX;
         go((unsigned)blocks);
     }
 }
 
-int check_tensors(const nuts_adamw_tensor* tensors, int64_t n, const char* who)
+// grads, scales: whether the call has to do with them.
+int check_tensors(const nuts_adamw_tensor* tensors, int64_t n, bool grads, bool scales, const char* who)
 {
     if (n < 0 || n > (1 << 20)) return api_fail(NUTS_E_INVALID_ARG, "%s: n_tensors must be in [0, 2^20]", who);
     if (n > 0 && !tensors) return api_fail(NUTS_E_INVALID_ARG, "%s: tensors must not be NULL", who);
-    for (int64_t i = 0; i < n; ++i)
-        if (tensors[i].n < 0 || tensors[i].n > kLongest) return api_fail(NUTS_E_INVALID_ARG, "%s: n of tensor %lld must be in [0, 2^40]", who, (long long)i);
+    for (int64_t i = 0; i < n; ++i) {
+        const nuts_adamw_tensor& t = tensors[i];
+        if (t.n < 0 || t.n > kLongest) return api_fail(NUTS_E_INVALID_ARG, "%s: n of tensor %lld must be in [0, 2^40]", who, (long long)i);
+        // (a launch has 48 bits of an address, which all of the device's have)
+        uint64_t any = (uintptr_t)t.param | (uintptr_t)t.copy | (uintptr_t)t.m | (uintptr_t)t.v;
+        if (grads) any |= (uintptr_t)t.grad;
+        if (scales) any |= (uintptr_t)t.m_scale | (uintptr_t)t.v_scale;
+        if (any >> 48) return api_fail(NUTS_E_INVALID_ARG, "%s: tensor %lld has an address that is none of the device's", who, (long long)i);
+    }
     return NUTS_OK;
 }
 
-template <typename P, typename G>
-void (*step_kernel(int bits))(StepArgs)
+// The workgroups' step for all tensors.
+template <bool kEight>
+void step_all(const nuts_adamw_desc* d, const nuts_adamw_tensor* tensors, int64_t n_tensors, const int64_t* step, const float* lr, const float* factor)
 {
-    return bits == 8 ? adamw_kernel<P, G, true> : adamw_kernel<P, G, false>;
+    StepArgs<kEight> a{};
+    a.step = step;
+    a.lr_at = lr;
+    a.factor = factor;
+    a.log_beta1 = std::log(d->beta1);
+    a.log_beta2 = std::log(d->beta2);
+    a.lr = d->lr;
+    a.decay = d->weight_decay;
+    a.beta1 = (float)d->beta1;
+    a.rest1 = (float)(1.0 - d->beta1);
+    a.beta2 = (float)d->beta2;
+    a.rest2 = (float)(1.0 - d->beta2);
+    a.eps = (float)d->eps;
+    a.scale = (float)d->scale;
+    a.keep = (float)(1.0 - d->lr * d->weight_decay);
+    a.size = (float)(d->lr / -std::expm1((double)d->step * a.log_beta1));
+    a.root_scale = (float)(1.0 / std::sqrt(-std::expm1((double)d->step * a.log_beta2)));
+    a.t = (unsigned)d->step;
+    a.host_step = d->step;
+    a.k0 = (unsigned)d->seed;
+    a.k1 = (unsigned)(d->seed >> 32);
+    a.copy_dtype = d->copy_dtype;
+    void (*kernel)(StepArgs<kEight>) = nullptr;
+    by_dtype(d->grad_dtype, [&](auto g) {
+        using G = decltype(g);
+        kernel = d->param_dtype == NUTS_F32 ? adamw_kernel<float, G, kEight> : adamw_kernel<bf16, G, kEight>;
+    });
+    by_tables(a, tensors, n_tensors, [](const nuts_adamw_tensor& t) { return t.grad != nullptr; },
+              [&](unsigned blocks) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, api_stream(), a); });
 }
 
 }  // namespace
@@ -713,7 +797,7 @@ int nuts_adamw(const nuts_adamw_desc* d, const nuts_adamw_tensor* tensors, int64
     if (!std::isfinite((float)d->weight_decay)) return api_fail(NUTS_E_INVALID_ARG, "nuts_adamw: weight_decay must be finite");
     if (!std::isfinite((float)d->scale)) return api_fail(NUTS_E_INVALID_ARG, "nuts_adamw: scale must be finite");
     if (d->step < 1) return api_fail(NUTS_E_INVALID_ARG, "nuts_adamw: step must be at least 1");
-    if (int rc = check_tensors(tensors, n_tensors, "nuts_adamw")) return rc;
+    if (int rc = check_tensors(tensors, n_tensors, true, d->state_bits == 8, "nuts_adamw")) return rc;
     int64_t total = 0;
     for (int64_t i = 0; i < n_tensors; ++i) {
         const nuts_adamw_tensor& t = tensors[i];
@@ -724,35 +808,7 @@ int nuts_adamw(const nuts_adamw_desc* d, const nuts_adamw_tensor* tensors, int64
     }
     if (total == 0) return NUTS_OK;
     if (int rc = api_have_device()) return rc;
-    StepArgs a{};
-    a.step = step;
-    a.lr_at = lr;
-    a.factor = factor;
-    a.log_beta1 = std::log(d->beta1);
-    a.log_beta2 = std::log(d->beta2);
-    a.lr = d->lr;
-    a.decay = d->weight_decay;
-    a.beta1 = (float)d->beta1;
-    a.rest1 = (float)(1.0 - d->beta1);
-    a.beta2 = (float)d->beta2;
-    a.rest2 = (float)(1.0 - d->beta2);
-    a.eps = (float)d->eps;
-    a.scale = (float)d->scale;
-    a.keep = (float)(1.0 - d->lr * d->weight_decay);
-    a.size = (float)(d->lr / -std::expm1((double)d->step * a.log_beta1));
-    a.root_scale = (float)(1.0 / std::sqrt(-std::expm1((double)d->step * a.log_beta2)));
-    a.t = (unsigned)d->step;
-    a.host_step = d->step;
-    a.k0 = (unsigned)d->seed;
-    a.k1 = (unsigned)(d->seed >> 32);
-    a.copy_dtype = d->copy_dtype;
-    void (*kernel)(StepArgs) = nullptr;
-    by_dtype(d->grad_dtype, [&](auto g) {
-        using G = decltype(g);
-        kernel = d->param_dtype == NUTS_F32 ? step_kernel<float, G>(d->state_bits) : step_kernel<bf16, G>(d->state_bits);
-    });
-    by_tables(a, tensors, n_tensors, [](const nuts_adamw_tensor& t) { return t.grad != nullptr; },
-              [&](unsigned blocks) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, api_stream(), a); });
+    d->state_bits == 8 ? step_all<true>(d, tensors, n_tensors, step, lr, factor) : step_all<false>(d, tensors, n_tensors, step, lr, factor);
     NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
     return NUTS_OK;
 }
@@ -760,7 +816,7 @@ int nuts_adamw(const nuts_adamw_desc* d, const nuts_adamw_tensor* tensors, int64
 int nuts_adamw_values(const nuts_adamw_tensor* tensors, int64_t n_tensors, int32_t dtype)
 {
     if (!cat_dtype_known(dtype)) return api_fail(NUTS_E_INVALID_ARG, "nuts_adamw_values: dtype must be NUTS_F32, NUTS_BF16 or NUTS_F16");
-    if (int rc = check_tensors(tensors, n_tensors, "nuts_adamw_values")) return rc;
+    if (int rc = check_tensors(tensors, n_tensors, false, true, "nuts_adamw_values")) return rc;
     int64_t total = 0;
     for (int64_t i = 0; i < n_tensors; ++i) {
         const nuts_adamw_tensor& t = tensors[i];
@@ -770,7 +826,7 @@ int nuts_adamw_values(const nuts_adamw_tensor* tensors, int64_t n_tensors, int32
     }
     if (total == 0) return NUTS_OK;
     if (int rc = api_have_device()) return rc;
-    StepArgs a{};
+    StepArgs<true> a{};
     by_dtype(dtype, [&](auto t) {
         by_tables(a, tensors, n_tensors, [](const nuts_adamw_tensor& x) { return x.param || x.copy; },
                   [&](unsigned blocks) { hipLaunchKernelGGL(values_kernel<decltype(t)>, dim3(blocks), dim3(kThreads), 0, api_stream(), a); });

@@ -382,3 +382,15 @@ def test_copies_of_moments_step_by_themselves(bits, tmp_path):
     for twin in twins:
         assert all(torch.equal(a, b) for a, b in zip(twin._tensors, s.moments._tensors))
     assert not torch.equal(before[0], s.params[0])
+
+
+@pytest.mark.parametrize("params,grads", [(F32, F32), (BF16, BF16)])
+@pytest.mark.parametrize("bits,n", [(32, 97), (32, 98), (32, 99), (8, 74), (8, 75), (8, 76), (32, 200), (8, 230)])
+def test_tables_that_a_launch_just_holds(bits, n, params, grads):
+    s = Step([20 + 3 * i for i in range(n)], params, grads, bits, copies=F16 if params == F32 else None)
+    s.check(seed=7, eps=1e-8, weight_decay=0.1)
+    if bits == 8:
+        m, v = nuts.nuts_adamw_values(s.moments, dtype=F32)
+        for i in range(n):
+            assert torch.equal(m[i].double(), L.m_values(s.moments.m[i], s.moments.m_scales[i]).float().double())
+            assert L.close(v[i], L.v_values(s.moments.v[i], s.moments.v_scales[i]), 4 * U * v[i].double().abs() + 2.0 ** -149)

@@ -296,3 +296,13 @@ def test_parameters_and_copies_that_are_another_part_of_their_memory(part, what)
     for call in (lambda: nuts.nuts_adamw(mo, [torch.zeros(p.shape), torch.zeros(3)], step=1, lr=0.1), lambda: nuts.nuts_adamw_values(mo)):
         with pytest.raises(ValueError, match="changed its size, type or device"):
             call()
+
+
+@pytest.mark.parametrize("field", ["param", "grad", "copy", "m", "v", "m_scale", "v_scale"])
+def test_addresses_that_no_device_has(field):
+    lib, bad = B.lib(), table(B.nuts_adamw_tensor, tensor(), tensor(**{field: 1 << 48 | 4096}))
+    refused(lib.nuts_adamw(adamw(state_bits=8), bad, 2, None, None, None), "address")
+    if field not in ("m_scale", "v_scale"):
+        refused(lib.nuts_adamw(adamw(), bad, 2, None, None, None), "address")
+    if field != "grad":
+        refused(lib.nuts_adamw_values(bad, 2, B.NUTS_F32), "address")
