@@ -37,10 +37,10 @@ constexpr int kNormTensors = 190;
 constexpr int kNormBlocks = 2048;   // about so many workgroups in all
 constexpr int kNormLeast = 8192;    // numbers of a workgroup, at least
 constexpr int kNormThreads = 1024;  // of the workgroup that joins theirs
-// Numbers that it does alone, of kNormFew tensors at most, which it takes one after the other: 32768 take it 4.7 us, where two launches take 3.8, 1.9
-// and the host's way to another one.
-constexpr int kNormSmall = 32768;
-constexpr int kNormFew = 4;
+// Numbers of a part of a tensor, which a wave of one workgroup takes at a time, and parts up to which that workgroup does all of it alone.  48 parts take it
+// 4.1 to 5.9 us and two launches 4.6, for which the host has 14.8 us to do where one needs 10.6 (16 parts: 3.3 us, 64: 6.9).
+constexpr int kNormPart = 2048;
+constexpr int kNormSmall = 48;
 
 struct NormArgs {
     const void* data[kNormTensors];
@@ -63,13 +63,13 @@ __device__ __forceinline__ double block_sum(double v, double* shared, int n_wave
     return v;
 }
 
-// The squares of n numbers that lie next to each other, by kCount threads.
+// The squares of n numbers that lie next to each other, by kCount threads, of which this is one.
 template <typename T, int kCount>
-__device__ __forceinline__ double squares(const T* x, long n)
+__device__ __forceinline__ double squares(const T* x, long n, int thread)
 {
     constexpr int kN = 16 / sizeof(T), kFlight = 4;
     double sum[kFlight] = {};
-    long i = (long)threadIdx.x * kN;
+    long i = (long)thread * kN;
     for (; i + (kFlight - 1) * kCount * kN + kN <= n; i += kFlight * kCount * kN) {
         Pack<T, kN> in[kFlight];
 #pragma unroll
@@ -100,11 +100,11 @@ __device__ __forceinline__ double squares(const T* x, long n)
     return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 template <int kCount>
-__device__ __forceinline__ double squares(const void* data, int dtype, long begin, long n)
+__device__ __forceinline__ double squares(const void* data, int dtype, long begin, long n, int thread)
 {
-    if (dtype == NUTS_F32) return squares<float, kCount>(static_cast<const float*>(data) + begin, n);
-    if (dtype == NUTS_BF16) return squares<bf16, kCount>(static_cast<const bf16*>(data) + begin, n);
-    return squares<f16, kCount>(static_cast<const f16*>(data) + begin, n);
+    if (dtype == NUTS_F32) return squares<float, kCount>(static_cast<const float*>(data) + begin, n, thread);
+    if (dtype == NUTS_BF16) return squares<bf16, kCount>(static_cast<const bf16*>(data) + begin, n, thread);
+    return squares<f16, kCount>(static_cast<const f16*>(data) + begin, n, thread);
 }
 
 __device__ __forceinline__ void write_norm(double sum, double max_norm, float* norm, float* factor)
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a)
     __shared__ double shared[kThreads / 64];
     const int t = tensor_of(a.first, (int)blockIdx.x);
     const long begin = (long)((int)blockIdx.x - a.first[t]) * a.each, n = min(a.each, a.n[t] - begin);
-    const double sum = block_sum(squares<kThreads>(a.data[t], a.dtype[t], begin, n), shared, kThreads / 64);
+    const double sum = block_sum(squares<kThreads>(a.data[t], a.dtype[t], begin, n, (int)threadIdx.x), shared, kThreads / 64);
     if (threadIdx.x == 0) a.part[blockIdx.x] = sum;
 }
 
@@ -133,12 +133,16 @@ __global__ __launch_bounds__(kNormThreads) void join_norm_kernel(const double* p
     write_norm(block_sum(sum, shared, kNormThreads / 64), max_norm, norm, factor);
 }
 
-// All of it by one workgroup, where there is little: one launch in place of two.
-__global__ __launch_bounds__(kNormThreads) void small_norm_kernel(NormArgs a, int n_tensors, double max_norm, float* norm, float* factor)
+// All of it by one workgroup, where there is little: one launch in place of two.  Each wave its parts, one after the other.
+__global__ __launch_bounds__(kNormThreads) void small_norm_kernel(NormArgs a, int n_parts, double max_norm, float* norm, float* factor)
 {
     __shared__ double shared[kNormThreads / 64];
     double sum = 0;
-    for (int t = 0; t < n_tensors; ++t) sum += squares<kNormThreads>(a.data[t], a.dtype[t], 0, a.n[t]);
+    for (int part = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64); part < n_parts; part += kNormThreads / 64) {
+        const int t = tensor_of(a.first, part);
+        const long begin = (long)(part - a.first[t]) * kNormPart, n = min((long)kNormPart, a.n[t] - begin);
+        sum += squares<64>(a.data[t], a.dtype[t], begin, n, (int)threadIdx.x % 64);
+    }
     write_norm(block_sum(sum, shared, kNormThreads / 64), max_norm, norm, factor);
 }
 
@@ -167,9 +171,9 @@ int check_norm(const nuts_tensor* tensors, int64_t n, const char* who)
 
 bool norm_is_small(const nuts_tensor* tensors, int64_t n)
 {
-    int64_t total = 0;
-    for (int64_t i = 0; i < n && n <= kNormFew; ++i) total += tensors[i].n;
-    return n <= kNormFew && total <= kNormSmall;
+    int64_t parts = 0;
+    for (int64_t i = 0; i < n && parts <= kNormSmall; ++i) parts += ceil_div(tensors[i].n, kNormPart);
+    return n <= kNormTensors && parts <= kNormSmall;
 }
 
 int64_t norm_blocks(const nuts_tensor* tensors, int64_t n)
@@ -750,29 +754,31 @@ int nuts_norm(const nuts_tensor* tensors, int64_t n_tensors, double max_norm, fl
     if (bytes > 0 && reinterpret_cast<uintptr_t>(workspace) % 256) return api_fail(NUTS_E_INVALID_ARG, "nuts_norm: workspace must be aligned to 256 bytes");
     if (int rc = api_have_device()) return rc;
     NormArgs a{};
-    if (norm_is_small(tensors, n_tensors)) {
-        for (int i = 0; i < (int)n_tensors; ++i) {
-            a.data[i] = tensors[i].data;
-            a.n[i] = (long)tensors[i].n;
-            a.dtype[i] = (unsigned char)tensors[i].dtype;
-        }
-        hipLaunchKernelGGL(small_norm_kernel, dim3(1), dim3(kNormThreads), 0, api_stream(), a, (int)n_tensors, max_norm, norm, factor);
-        NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
-        return NUTS_OK;
-    }
-    a.each = (long)norm_each(tensors, n_tensors);
-    double* part = static_cast<double*>(workspace);
-    for (int64_t at = 0; at < n_tensors;) {
-        int64_t own = 0;
+    // A table from tensor `at` on, of parts of `each` numbers; returns how many they are.
+    int64_t at = 0;
+    auto next_table = [&](int64_t each) {
+        int64_t parts = 0;
         int used = 0;
         for (; used < kNormTensors && at < n_tensors; ++used, ++at) {
             a.data[used] = tensors[at].data;
             a.n[used] = (long)tensors[at].n;
             a.dtype[used] = (unsigned char)tensors[at].dtype;
-            a.first[used] = (int)own;
-            own += ceil_div(tensors[at].n, a.each);
+            a.first[used] = (int)parts;
+            parts += ceil_div(tensors[at].n, each);
         }
         for (; used < kNormTensors; ++used) a.first[used] = INT32_MAX;
+        return parts;
+    };
+    if (norm_is_small(tensors, n_tensors)) {
+        const int parts = (int)next_table(kNormPart);
+        hipLaunchKernelGGL(small_norm_kernel, dim3(1), dim3(kNormThreads), 0, api_stream(), a, parts, max_norm, norm, factor);
+        NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
+        return NUTS_OK;
+    }
+    a.each = (long)norm_each(tensors, n_tensors);
+    double* part = static_cast<double*>(workspace);
+    while (at < n_tensors) {
+        const int64_t own = next_table(a.each);
         a.part = part;
         if (own > 0) hipLaunchKernelGGL(norm_kernel, dim3((unsigned)own), dim3(kThreads), 0, api_stream(), a);
         part += own;

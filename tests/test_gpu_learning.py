@@ -394,3 +394,13 @@ def test_tables_that_a_launch_just_holds(bits, n, params, grads):
         for i in range(n):
             assert torch.equal(m[i].double(), L.m_values(s.moments.m[i], s.moments.m_scales[i]).float().double())
             assert L.close(v[i], L.v_values(s.moments.v[i], s.moments.v_scales[i]), 4 * U * v[i].double().abs() + 2.0 ** -149)
+
+
+@pytest.mark.parametrize("sizes", [[2048] * 48, [2049] * 24, [100] * 48, [100] * 49, [0] * 100 + [5], [5] + [0] * 189, [5] + [0] * 190, [98304], [98305], [3] * 17 + [4097, 0, 2047, 1]])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_norm_of_parts(sizes, dtype):
+    g = gen(len(sizes) + 7)
+    tensors = [tensor(n, dtype, g, offset=i % 4) for i, n in enumerate(sizes)]
+    for t in tensors[:50:7]:
+        t[-1:] = 40.0   # (a last number that is left out shows)
+    check_norm(tensors + [tensor(77, F32, g)], max_norm=0.5)
