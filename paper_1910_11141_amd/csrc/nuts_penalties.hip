@@ -389,7 +389,7 @@ __device__ __forceinline__ unsigned allowed_of(const uint32_t* allowed, int v, i
 }
 
 // A workgroup a slice of one row, or (kShared) of `rows_each` rows that have one history.  Bound by its reads and writes: 4096 rows of 32001 bfloat16
-// with one history and biases 112 us, 4.7 TB/s (120 with stores that the caches keep, 119 with loads that they do), 500 rows of 128000 with histories
+// with one history and biases 112 us, 4.7 TB/s (120 with stores that the caches keep, 119 with loads that they do, 135 with registers enough for all of it and fewer waves), 500 rows of 128000 with histories
 // of their own 56 us (68 with loads that the caches keep), 4.6 TB/s.  64 such rows take 8 us: a length, a history and a row, waited for one
 // behind the other.
 template <typename W, typename T, bool kShared, bool kBiases>
