@@ -452,7 +452,7 @@ typedef struct {
  *   g = scale factor grad;   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2;
  *   param = param (1 - lr weight_decay) - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps).
  * `step`, `lr` and `factor` are DEVICE scalars or NULL; the first two take the descriptor's place (a captured step that is replayed needs
- * them there; a step below 1 counts as 1), and where factor is NaN the call changes nothing.  No two things that are written may overlap.
+ * them there; a step below 1 counts as 1), and where factor is NaN the call changes nothing.  No two things that are written may overlap, nor a gradient with them.
  *
  * Arithmetic is binary32.  Moments of 8 bits stand for powers of their codes, m = sign(c) c^2 m_scale (c = -127 .. 127), v = (c^2 v_scale)^2
  * (c = 0 .. 254); a block's largest has the last code.  What stands between two codes becomes one of them, at random so that

@@ -189,8 +189,8 @@ def _moments(params, bits, copies, states):
 
 
 def nuts_adamw(moments, grads, *, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, scale=1.0, factor=None, seed=0):
-    """One step of AdamW for the parameters of `moments`, which change where they are.  grads: a tensor for each, all of one type (None: that
-    parameter is left alone).  step: the step's number, from 1 on, and lr: numbers, or tensors on the device (one int64, one
+    """One step of AdamW for the parameters of `moments`, which change where they are.  grads: a tensor for each, all of one type, none of them in memory that
+    the step writes (None: that parameter is left alone).  step: the step's number, from 1 on, and lr: numbers, or tensors on the device (one int64, one
     float32), which a captured step that is replayed needs.  Gradients are multiplied with scale (-1: uphill) and with factor, a float32 scalar on
     the device, of nuts_norm; where that is NaN nothing changes.  seed: of what is rounded at random (moments of 8 bits, parameters of
     bfloat16)."""
