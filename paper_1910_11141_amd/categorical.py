@@ -359,8 +359,8 @@ def nuts_penalties(logits, history=None, *, lengths=None, prompts=None, repetiti
         if id_type is None:
             id_type = _ID_TYPES[bias_ids.dtype]
         elif id_type != _ID_TYPES[bias_ids.dtype]:  # (to the wider type: the other could make a class of what is none)
-            history, bias_ids, id_type = history.long(), bias_ids.long(), _b.NUTS_I64
-            history_stride = places if history_stride else 0
+            history, id_type, places, history_stride = _history(history.long(), n)  # (which may be another tensor, or the same)
+            bias_ids = bias_ids.long()
         bias_ids, bias_values, n_bias = bias_ids.contiguous(), bias_values.contiguous(), bias_ids.shape[1]
     bias_stride = 0
     if bias is not None:
