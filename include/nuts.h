@@ -456,7 +456,8 @@ typedef struct {
  *
  * Arithmetic is binary32.  Moments of 8 bits stand for powers of their codes, m = sign(c) c^2 m_scale (c = -127 .. 127), v = (c^2 v_scale)^2
  * (c = 0 .. 254); a block's largest has the last code.  What stands between two codes becomes one of them, at random so that
- * the mean is kept, but a v above 0 does not become 0, and a block of m whose largest is below 2^-126 127^2 is zeros.  c = -128 and c = 255 are what is not finite and count as NaN.
+ * the mean is kept, but a v above 0 does not get the code 0 (in a block whose largest v is below 2^-118 the smallest codes stand for what binary32 has as 0), and a
+ * block of m whose largest is below 2^-126 127^2 is zeros.  c = -128 and c = 255 are what is not finite and count as NaN.
  * Parameters of bfloat16 are rounded at random, too (a step is mostly less than half a unit in their last place, and to the nearest they would stay where they
  * are); the parameters' copies are rounded to the nearest.  The random bits of the four numbers from 4 q of tensor t on are the four words of
  * Philox4x32-10 with the key `seed` and the counter (q mod 2^32, 6 + 256 (q / 2^32), step mod 2^32, t): bits 0-9 of a word are m's, 10-19 v's,

@@ -393,10 +393,20 @@ __device__ __forceinline__ unsigned v_code(float root, const Scale& scale, unsig
     return max(code, (unsigned)(x > 0.f));  // (1 at least, where there is anything)
 }
 // The square root of a number of 24 places, rounded once: from one that is a unit or two in the last place off, and the remainder of its square.
+// (Of a v below 2^-100 the remainder has fewer places: a unit off then.)
 __device__ __forceinline__ float exact_root(float v)
 {
     const float y = __builtin_amdgcn_rsqf(v), s = v * y;
     return __builtin_fmaf(__builtin_fmaf(-s, s, v), 0.5f * y, s);
+}
+
+// The root that a step divides by: of moments of 32 bits the instruction's, a unit in the last place off at most; of 8 bits, whose codes follow
+// from it, rounded once.
+template <bool kExact>
+__device__ __forceinline__ float root_of(float v)
+{
+    const float s = __builtin_amdgcn_sqrtf(v);
+    return kExact && __builtin_isnormal(v) ? exact_root(v) : s;
 }
 
 // The largest of a wave's numbers that are 0 or more, in all of its lanes.
@@ -533,7 +543,7 @@ __device__ __forceinline__ void step_block(const StepArgs<kEight>& a, const Fact
     }
     unsigned words[4] = {};
     if (kEight || sizeof(P) == 2) random_words((unsigned)((uint64_t)at >> 2) + threadIdx.x % 64, 6u | (unsigned)((uint64_t)at >> 34) << 8, f.t, tensor, a.k0, a.k1, words);
-    bool usual = true;  // (neither 0 nor infinity nor NaN: what the root wants)
+    bool usual = true;  // (not below 2^-126, not infinity, not NaN)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const float x = g[e] * f.scale;
@@ -541,21 +551,22 @@ __device__ __forceinline__ void step_block(const StepArgs<kEight>& a, const Fact
         v[e] = v[e] * a.beta2 + x * x * a.rest2;
         usual &= __builtin_isnormal(v[e]);
     }
-    if (!kEight || any_lane(!usual)) {
+    if (any_lane(!usual)) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            root[e] = __builtin_amdgcn_sqrtf(v[e]);  // (a unit in the last place off at most, as the reciprocal)
-            if (kEight && __builtin_isnormal(v[e])) root[e] = exact_root(v[e]);
+            const bool low = v[e] < 0x1p-126f;  // (of which the root's instruction makes 0)
+            root[e] = root_of<kEight>(low ? v[e] * 0x1p64f : v[e]);
+            if (low) root[e] *= 0x1p-32f;
             if (kEight) lost |= !(v[e] < INFINITY);
         }
         if (kEight) lost = any_lane(lost);
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) root[e] = exact_root(v[e]);
+        for (int e = 0; e < 4; ++e) root[e] = kEight ? exact_root(v[e]) : __builtin_amdgcn_sqrtf(v[e]);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        p[e] = __builtin_fmaf(-f.size * m[e], __builtin_amdgcn_rcpf(__builtin_fmaf(root[e], f.root_scale, a.eps)), p[e] * f.keep);
+        p[e] = __builtin_fmaf(-f.size * m[e], __builtin_amdgcn_rcpf(__builtin_fmaf(root[e], f.root_scale, a.eps)), p[e] * f.keep);  // (a reciprocal a unit off at most)
         if (sizeof(P) == 2) p[e] = rounded_at_random(p[e], words[e]);
     }
     store4(static_cast<P*>(t.param) + i, n, p);
