@@ -454,7 +454,8 @@ typedef struct {
  * `step`, `lr` and `factor` are DEVICE scalars or NULL; the first two take the descriptor's place (a captured step that is replayed needs
  * them there; a step below 1 counts as 1), and where factor is NaN the call changes nothing.  No two things that are written may overlap, nor a gradient with them.
  *
- * Arithmetic is binary32.  Moments of 8 bits stand for powers of their codes, m = sign(c) c^2 m_scale (c = -127 .. 127), v = (c^2 v_scale)^2
+ * Arithmetic is binary32 (the quotient, and with moments of 32 bits the root, are a unit or two in the last place off); where v is 0 in it and eps is 0, the
+ * quotient is infinite or NaN.  Moments of 8 bits stand for powers of their codes, m = sign(c) c^2 m_scale (c = -127 .. 127), v = (c^2 v_scale)^2
  * (c = 0 .. 254); a block's largest has the last code.  What stands between two codes becomes one of them, at random so that
  * the mean is kept, but a v above 0 does not get the code 0 (in a block whose largest v is below 2^-118 the smallest codes stand for what binary32 has as 0), and a
  * block of m whose largest is below 2^-126 127^2 is zeros.  c = -128 and c = 255 are what is not finite and count as NaN.

@@ -208,6 +208,9 @@ struct StepArgs {
     long first_block;
     int64_t host_step;
     int copy_dtype;
+    // What the reciprocal takes is below 2^-126 (and counts as 0), or it gives such a number (and 0), only for an eps that is not in [2^-100, 2^100]: sqrt(v) times its
+    // factor is 2^77 at most.  Then m and the denominator are moved by 2^64.
+    int usual_eps;
 };
 static_assert(sizeof(StepArgs<false>) <= 4096 && sizeof(StepArgs<true>) <= 4096, "the arguments of a launch");
 
@@ -564,10 +567,21 @@ __device__ __forceinline__ void step_block(const StepArgs<kEight>& a, const Fact
 #pragma unroll
         for (int e = 0; e < 4; ++e) root[e] = kEight ? exact_root(v[e]) : __builtin_amdgcn_sqrtf(v[e]);
     }
+    if (a.usual_eps) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        p[e] = __builtin_fmaf(-f.size * m[e], __builtin_amdgcn_rcpf(__builtin_fmaf(root[e], f.root_scale, a.eps)), p[e] * f.keep);  // (a reciprocal a unit off at most)
-        if (sizeof(P) == 2) p[e] = rounded_at_random(p[e], words[e]);
+        for (int e = 0; e < 4; ++e)
+            // (a reciprocal a unit in the last place off at most)
+            p[e] = __builtin_fmaf(-f.size * m[e], __builtin_amdgcn_rcpf(__builtin_fmaf(root[e], f.root_scale, a.eps)), p[e] * f.keep);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float under = __builtin_fmaf(root[e], f.root_scale, a.eps), move = under < 0x1p-60f ? 0x1p64f : under > 0x1p100f ? 0x1p-64f : 1.f;
+            p[e] = __builtin_fmaf(-f.size * (m[e] * move), __builtin_amdgcn_rcpf(under * move), p[e] * f.keep);
+        }
+    }
+    if (sizeof(P) == 2) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = rounded_at_random(p[e], words[e]);
     }
     store4(static_cast<P*>(t.param) + i, n, p);
     if (t.copy) a.copy_dtype == NUTS_BF16 ? store4(static_cast<bf16*>(t.copy) + i, n, p) : store4(static_cast<f16*>(t.copy) + i, n, p);
@@ -721,6 +735,7 @@ void step_all(const nuts_adamw_desc* d, const nuts_adamw_tensor* tensors, int64_
     a.beta2 = (float)d->beta2;
     a.rest2 = (float)(1.0 - d->beta2);
     a.eps = (float)d->eps;
+    a.usual_eps = a.eps >= 0x1p-100f && a.eps <= 0x1p100f;
     a.scale = (float)d->scale;
     a.keep = (float)(1.0 - d->lr * d->weight_decay);
     a.size = (float)(d->lr / -std::expm1((double)d->step * a.log_beta1));

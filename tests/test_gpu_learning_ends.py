@@ -1,4 +1,7 @@
-"""AdamW at the ends of binary32's range: a v whose root has to be found though v is below 2^-126.  Gradients are 0 and the moments shrink by a half (which is exact), so that what the update divides is known to the last bit."""
+"""AdamW at the ends of binary32's range: a v whose root has to be found though v is below 2^-126, denominators of which the reciprocal is not a usual
+number.  Gradients are 0 and the moments shrink by a half (which is exact), so that what the update divides is known to the last bit."""
+import math
+
 import pytest
 import torch
 
@@ -36,6 +39,35 @@ def test_roots_of_what_is_below_the_usual_numbers(n, eps, largest):
     m = (torch.rand(n, generator=g, device="cuda") + 1) * torch.where(torch.rand(n, generator=g, device="cuda") < 0.5, -1.0, 1.0) * 2.0 ** -70
     got, want = updates(m, v, 2.0 ** -9, eps)
     assert bool(((got.double() - want).abs() <= 10 * U * want.abs()).all())
+
+
+@pytest.mark.parametrize("eps,m,v,lr", [
+    (2.0 ** -133, 2.0 ** -140, 0.0, 2.0 ** -9),          # the denominator is eps, which is below the usual numbers, and so is m
+    (2.0 ** -127, 2.0 ** -100, 0.0, 2.0 ** -9),
+    (2.0 ** -149, -2.0 ** -149, 0.0, 2.0 ** -9),
+    (1.5 * 2.0 ** 126, 2.0 ** 60, 1.0, 2.0 ** 60),       # the reciprocal is below them
+    (1.5 * 2.0 ** 127, -2.0 ** 61, 2.0 ** 100, 2.0 ** 60),
+    (2.0 ** -99, 2.0 ** -50, 2.0 ** -126, 2.0 ** -9), (2.0 ** -101, 2.0 ** -50, 2.0 ** -126, 2.0 ** -9),   # either way to divide
+    (2.0 ** 99, 2.0 ** 50, 2.0 ** 126, 2.0 ** 9), (2.0 ** 101, 2.0 ** 50, 2.0 ** 126, 2.0 ** 9),
+    (0.0, 2.0 ** -30, 2.0 ** 126, 2.0 ** -9), (0.0, 2.0 ** 40, 2.0 ** 90, 2.0 ** -9), (0.0, 2.0 ** -75, 2.0 ** -149, 2.0 ** -9),
+])
+@pytest.mark.parametrize("n", [1, 700])
+def test_denominators_beyond_the_usual_numbers(eps, m, v, lr, n):
+    got, want = updates(torch.full((n,), m, device="cuda"), torch.full((n,), v, device="cuda"), lr, eps)
+    assert bool((want != 0).all()) and bool(((got.double() - want).abs() <= 10 * U * want.abs()).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("params", [torch.float32, torch.bfloat16])
+def test_moments_of_zero_and_a_denominator_below_the_usual_numbers(bits, params):
+    """0 / eps is 0; 0 / 0 is not a number."""
+    p = torch.ones(600, dtype=params, device="cuda")
+    moments = nuts.Moments([p], bits=bits)
+    for eps in (2.0 ** -149, 2.0 ** -133, 2.0 ** -127):
+        nuts.nuts_adamw(moments, [torch.zeros_like(p)], step=1, lr=0.1, eps=eps, weight_decay=0.0)
+        assert bool((p == 1).all())
+    nuts.nuts_adamw(moments, [torch.zeros_like(p)], step=1, lr=0.1, eps=0.0, weight_decay=0.0)
+    assert bool(p.isnan().all())
 
 
 def test_a_first_step_with_gradients_whose_squares_are_below_the_usual_numbers():
