@@ -127,6 +127,7 @@ class Moments:
         self.m, self.v = map(tuple, states[:2])
         self.m_scales, self.v_scales = map(tuple, states[2:]) if bits == 8 else ((None,) * n, (None,) * n)
         given = [c for c in self.copies if c is not None]
+        self._first_copy = given[0] if given else None
         self.copy_dtype = given[0].dtype if given else torch.bfloat16
         if self.copy_dtype not in _COPY_DTYPES:
             raise ValueError(f"copies must be {' or '.join(str(d) for d in _COPY_DTYPES)}")
@@ -176,7 +177,8 @@ class Moments:
             bits |= _read(self._copies, self._params, table, 8, _COPY)
             if bits & _OTHER_SHAPES:  # (or the same number in another shape)
                 bits |= _read(self._copies, None, self._copy_sizes[:], 1, -1, 0)
-        if bits & (_MOVED | _GAPS | _SEVERAL_TYPES):
+        # (one type for all, but is it the one?)
+        if bits & (_MOVED | _GAPS | _SEVERAL_TYPES) or self.params[0].dtype is not self.dtype or self._has_copies and self._first_copy.dtype is not self.copy_dtype:
             for tensors, dtype in ((self.params, self.dtype), (self.copies, self.copy_dtype)):
                 if any(t is not None and (t.numel() != n or t.dtype != dtype or t.device != self.device or not t.is_contiguous()) for t, n in zip(tensors, self._sizes)):
                     raise ValueError("a parameter or a copy has changed its size, type or device")
