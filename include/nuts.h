@@ -467,7 +467,7 @@ int nuts_adamw(const nuts_adamw_desc* desc, const nuts_adamw_tensor* tensors, in
                const float* lr, const float* factor);
 
 /* The moments of 8 bits as numbers: `param` receives m and `copy` v, in dtype (NUTS_F32, NUTS_BF16, NUTS_F16); either may
- * be NULL.  grad is not looked at. */
+ * be NULL.  grad is not looked at.  What is written may not overlap, nor the moments. */
 int nuts_adamw_values(const nuts_adamw_tensor* tensors, int64_t n_tensors, int32_t dtype);
 
 #ifdef __cplusplus

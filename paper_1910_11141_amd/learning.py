@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from array import array
+from bisect import bisect_left
 from collections import namedtuple
 
 import torch
@@ -27,21 +28,35 @@ _PARAM, _GRAD, _COPY, _M, _V, _M_SCALE, _V_SCALE, _N = range(8)  # columns of a 
 assert C.sizeof(_b.nuts_adamw_tensor) == 64 and C.sizeof(_b.nuts_tensor) == 24
 
 
-_tensors = None
-_SEVERAL_TYPES, _SEVERAL_DEVICES, _GAPS, _OTHER_SHAPES, _MOVED = 1, 2, 4, 8, 16
+_tensors = _compare = None
+_SEVERAL_TYPES, _SEVERAL_DEVICES, _GAPS, _OTHER_SHAPES, _MOVED, _MEETS, _OVERLAP = 1, 2, 4, 8, 16, 32, 64
 
 
-def _read(tensors, like, table, width, address, count=-1, type_=-1):
-    """Columns of `table`, rows of `width` numbers, from a list of tensors (or None); bits of what they have not in common."""
-    global _tensors
+def _read(tensors, like, table, width, address, count=-1, type_=-1, kept=0):
+    """Columns of `table`, rows of `width` numbers, from a list of tensors (or None); bits of what they have not in common, and of whether one lies
+    in memory of `kept`."""
+    global _tensors, _compare
     if _tensors is None:
         if not os.path.exists(TENSORS_PATH):
             raise ImportError(f"{TENSORS_PATH} is missing: run `python -c 'import __graft_entry__ as g; g.build()'`")
         lib = C.PyDLL(TENSORS_PATH)
-        lib.nuts_tensor_table.argtypes = [C.py_object, C.py_object, C.c_void_p] + [C.c_int64] * 4
-        lib.nuts_tensor_table.restype = C.c_int
-        _tensors = lib.nuts_tensor_table
-    return _tensors(tensors, like, table.buffer_info()[0], width, address, count, type_)
+        lib.nuts_tensor_table.argtypes = [C.py_object, C.py_object, C.c_void_p] + [C.c_int64] * 4 + [C.c_void_p]
+        lib.nuts_tensors_compare.argtypes = [C.py_object, C.py_object]
+        lib.nuts_tensor_table.restype = lib.nuts_tensors_compare.restype = C.c_int
+        _tensors, _compare = lib.nuts_tensor_table, lib.nuts_tensors_compare
+    return _tensors(tensors, like, table.buffer_info()[0], width, address, count, type_, kept)
+
+
+def _spans(tensors):
+    """Where tensors lie, in order."""
+    return sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors if t is not None and t.numel())
+
+
+def _meet(spans, others):
+    """Whether one of `spans` has memory of one of `others`, which lie apart and in order."""
+    begins = [begin for begin, _ in others]
+    last = [bisect_left(begins, end) - 1 for _, end in spans]  # of the others that begin before its end
+    return any(k >= 0 and others[k][1] > begin for k, (begin, _) in zip(last, spans))
 
 
 def _current(device):
@@ -162,10 +177,11 @@ class Moments:
             raise ValueError("parameters, moments and copies must be on one device")
         self.device = _current(self.params[0].device)
         # two of them in one place would be written by two workgroups at a time
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors if t.numel())
+        spans = _spans(tensors)
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("parameters, moments and copies must not overlap")
         self._tensors = tensors
+        self._written = array("q", [len(spans), *(at for span in spans for at in span)])
         _read(self._params, None, self._table, 8, _PARAM)
         _read(self._copies, None, self._table, 8, _COPY)
 
@@ -199,23 +215,30 @@ def nuts_adamw(moments, grads, *, step, lr, betas=(0.9, 0.999), eps=1e-8, weight
     grads = list(grads)
     if len(grads) != len(moments.params):
         raise ValueError(f"there are {len(moments.params)} parameters and {len(grads)} gradients")
-    first = next((g for g in grads if g is not None), None)
+    first = grads[0] if grads[0] is not None else next((g for g in grads if g is not None), None)
     if first is None:
         return
     table, dtype, device = moments._now(), first.dtype, _current(moments.device)
-    bits = _read(grads, moments._params, table, 8, _GRAD)
+    written = moments._written
+    bits = _read(grads, moments._params, table, 8, _GRAD, kept=written.buffer_info()[0])
     if bits & (_SEVERAL_TYPES | _SEVERAL_DEVICES | _OTHER_SHAPES) or dtype not in _DTYPES or first.device != device:
         raise ValueError(f"gradients must be {' or '.join(str(d) for d in _DTYPES)}, all of one type, on {device}, each as its parameter")
     if bits & _GAPS:
         grads = [g.contiguous() if g is not None else None for g in grads]
-        _read(grads, moments._params, table, 8, _GRAD)
-    scalars = [t for t in (step, lr, factor) if isinstance(t, torch.Tensor)]
-    step_at = lr_at = factor_at = None
+        bits = _read(grads, moments._params, table, 8, _GRAD, kept=written.buffer_info()[0])
+    if bits & _MEETS:  # (what belongs to parameters without a gradient is not written)
+        changed = [t for i, g in enumerate(grads) if g is not None for t in (moments.params[i], moments.copies[i], *(some[i] for some in moments._states))]
+        if _meet(_spans(grads), _spans(changed)):
+            raise ValueError("gradients must not lie in memory that the step writes")
+    scalars, step_at, lr_at, factor_at = [], None, None, None
     if isinstance(step, torch.Tensor):
+        scalars.append(step)
         step_at, step = _scalar(step, "step", torch.int64, device), 1
     if isinstance(lr, torch.Tensor):
+        scalars.append(lr)
         lr_at, lr = _scalar(lr, "lr", torch.float32, device), 0.0
     if factor is not None:
+        scalars.append(factor)
         factor_at = _scalar(factor, "factor", torch.float32, device)
     desc = _b.nuts_adamw_desc(_PARAM_DTYPES[moments.dtype], _DTYPES[dtype], _COPY_DTYPES[moments.copy_dtype], moments.bits, float(lr), float(betas[0]),
                               float(betas[1]), float(eps), float(weight_decay), float(scale), int(step), int(seed) & 0xFFFFFFFFFFFFFFFF)
@@ -234,20 +257,25 @@ class _Chain:
 
 def nuts_adamw_values(moments, *, dtype=torch.float32, out=None):
     """The moments of 8 bits as numbers: two lists of tensors (m, v), each as its parameter.  out: such lists to write to, all of one type (None for
-    a tensor that is not wanted)."""
+    a tensor that is not wanted), none in memory of another or of the moments."""
     if moments.bits != 8:
         raise ValueError("moments of 32 bits are numbers: m and v")
-    if out is None:
-        out = tuple([torch.empty(p.shape, dtype=dtype, device=p.device) for p in moments.params] for _ in range(2))
-    m, v = (list(some) for some in out)
+    given = out is not None
+    m, v = (list(some) for some in out) if given else ([torch.empty(p.shape, dtype=dtype, device=p.device) for p in moments.params] for _ in range(2))
     if len(m) != len(moments.params) or len(v) != len(moments.params):
         raise ValueError(f"out must be two lists of {len(moments.params)} tensors")
-    used = [t for t in (*m, *v) if t is not None]
-    if not used:
+    first = m[0] if m[0] is not None else next((t for t in (*m, *v) if t is not None), None)
+    if first is None:
         return m, v
-    table, device, dtype = moments._now(), _current(moments.device), used[0].dtype
-    bits = _read(m, moments._params, table, 8, _PARAM) | _read(v, moments._params, table, 8, _COPY)
-    if bits & (_SEVERAL_TYPES | _SEVERAL_DEVICES | _OTHER_SHAPES | _GAPS) or dtype not in _DTYPES or any(t.dtype != dtype or t.device != device for t in (used[0], used[-1])):
+    table, device, dtype = moments._now(), _current(moments.device), first.dtype
+    written = moments._written
+    kept = written.buffer_info()[0]
+    bits = _read(m, moments._params, table, 8, _PARAM, kept=kept) | _read(v, moments._params, table, 8, _COPY, kept=kept)
+    if given:
+        bits |= _compare(m, v)
+    if bits & (_SEVERAL_TYPES | _SEVERAL_DEVICES | _OTHER_SHAPES | _GAPS) or dtype not in _DTYPES or first.device != device:
         raise ValueError(f"out must be {' or '.join(str(d) for d in _DTYPES)}, all of one type, without gaps, on {device}, each as its parameter")
-    _run(_b.lib().nuts_adamw_values, [table.buffer_info()[0], len(m), _DTYPES[dtype]], _Chain(moments._tensors, used), device)
+    if bits & _OVERLAP or bits & _MEETS and _meet(_spans([*m, *v]), _spans([t for some in moments._states for t in some])):
+        raise ValueError("out must not overlap the moments, nor one of its tensors another")
+    _run(_b.lib().nuts_adamw_values, [table.buffer_info()[0], len(m), _DTYPES[dtype]], _Chain(moments._tensors, m, v), device)
     return m, v

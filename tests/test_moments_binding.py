@@ -1,8 +1,13 @@
-"""What AdamW's moments notice of tensors that have become others since they were given."""
+"""What AdamW's moments notice of tensors that have become others since they were given, and of others that lie in their memory."""
+import random
+from array import array
+
 import pytest
 import torch
 
 import paper_1910_11141_amd as nuts
+from paper_1910_11141_amd import binding as B
+from paper_1910_11141_amd import learning as G
 
 pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="parameters on the CPU")
 
@@ -25,3 +30,110 @@ def test_types_that_change_where_the_numbers_lie(bits, n, which, other):
     for call in calls:
         with pytest.raises(ValueError, match="changed its size, type or device"):
             call()
+
+
+def goes_to_the_library(call):
+    with pytest.raises(B.NutsError) as e:   # (there is no device)
+        call()
+    return e.value.code == B.NUTS_E_DEVICE
+
+
+def model(bits, n=3):
+    """A buffer of floats, the parameters and moments of n tensors of 40 in it, 10 apart, and what is behind them."""
+    flat = torch.zeros(n * 50 * 4 + 100)
+    parts = [flat[50 * i:50 * i + 40] for i in range(4 * n)]
+    states = (parts[n:2 * n], parts[2 * n:3 * n])
+    if bits == 8:
+        states = ([t[:10].view(torch.int8) for t in parts[n:2 * n]], [t[:10].view(torch.uint8) for t in parts[2 * n:3 * n]], [t[10:11] for t in parts[n:2 * n]],
+                  [t[10:11] for t in parts[2 * n:3 * n]])
+    copies = [t[:20].view(torch.bfloat16) for t in parts[3 * n:]]
+    return flat, nuts.Moments(parts[:n], bits=bits, states=states, copies=copies)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("at", [0, 7, -39, 39])
+def test_gradients_in_memory_that_a_step_writes(bits, at):
+    flat, moments = model(bits)
+    free = lambda: [torch.zeros(40) for _ in range(3)]  # noqa: E731
+    step = lambda grads: nuts.nuts_adamw(moments, grads, step=1, lr=0.1)  # noqa: E731
+    assert goes_to_the_library(lambda: step(free()))
+    for columns in (moments.params, moments.copies, *moments._states):
+        for i, t in enumerate(columns):
+            first = (t.data_ptr() - flat.data_ptr()) // 4 + min(at, t.numel() * t.element_size() // 4 - 1)   # (39: its last)
+            if first < 0:
+                continue
+            for k in range(3):
+                grads = free()
+                grads[k] = flat[first:first + 40]
+                with pytest.raises(ValueError, match="memory that the step writes"):
+                    step(grads)
+    with pytest.raises(ValueError, match="memory that the step writes"):
+        step([torch.zeros(40), None, moments.params[2]])
+
+
+def test_gradients_beside_what_a_step_writes():
+    flat, moments = model(32)
+    step = lambda grads: nuts.nuts_adamw(moments, grads, step=1, lr=0.1)  # noqa: E731
+    end = flat[-40:]
+    assert goes_to_the_library(lambda: step([end, end, end]))              # one gradient of all
+    assert goes_to_the_library(lambda: step([moments.params[1], None, moments.m[1]]))   # of a parameter that stays
+    with pytest.raises(ValueError, match="memory that the step writes"):
+        step([moments.params[1], torch.zeros(40), None])
+    whole = torch.zeros(120)
+    moments = nuts.Moments([whole[40:80]])
+    for g in (whole[:40], whole[80:]):
+        assert goes_to_the_library(lambda: nuts.nuts_adamw(moments, [g], step=1, lr=0.1))
+    for g in (whole[1:41], whole[79:119], whole[40:80]):
+        with pytest.raises(ValueError, match="memory that the step writes"):
+            nuts.nuts_adamw(moments, [g], step=1, lr=0.1)
+    # what is turned is copied first; parameters that have moved are where they are now
+    p = torch.zeros(4, 4)
+    moments = nuts.Moments([p])
+    assert goes_to_the_library(lambda: nuts.nuts_adamw(moments, [p.t()], step=1, lr=0.1))
+    old = p.data
+    p.data = torch.zeros(4, 4)
+    assert goes_to_the_library(lambda: nuts.nuts_adamw(moments, [old], step=1, lr=0.1))
+    with pytest.raises(ValueError, match="memory that the step writes"):
+        nuts.nuts_adamw(moments, [p.data], step=1, lr=0.1)
+
+
+def test_values_that_overlap():
+    flat, moments = model(8)
+    free = lambda: [torch.zeros(40) for _ in range(3)]  # noqa: E731
+    values = lambda m, v: nuts.nuts_adamw_values(moments, out=(m, v))  # noqa: E731
+    assert goes_to_the_library(lambda: values(free(), free()))
+    assert goes_to_the_library(lambda: nuts.nuts_adamw_values(moments))
+    assert goes_to_the_library(lambda: values([None, None, None], list(moments.params)))   # (no moments, if anyone wants that)
+    both, one = free(), torch.zeros(79)
+    for m, v in ((both, both), ([one[:40], None, None], [None, one[39:], None]), ([one[:40], one[39:], None], free()), (free(), [None, one[39:], one[:40]]),
+                 ([flat[150:190], None, None], free()), ([None] * 3, [flat[311:351], None, None])):
+        with pytest.raises(ValueError, match="overlap"):
+            values(m, v)
+    assert goes_to_the_library(lambda: values([one[39:], None, None], [one[:39].new_zeros(40), None, None]))
+
+
+def test_stretches_of_memory_in_any_order():
+    """Against every pair."""
+    rng = random.Random(4)
+    flat = torch.zeros(4000, dtype=torch.int8)
+    base = flat.data_ptr()
+    for _ in range(300):
+        ends = sorted(rng.sample(range(4001), 2 * rng.randrange(0, 30)))
+        kept = list(zip(ends[::2], ends[1::2]))
+        table = array("q", [len(kept), *(base + at for span in kept for at in span)])
+        tensors = []
+        for _ in range(rng.randrange(1, 12)):
+            a = rng.choice(ends) if ends and rng.random() < 0.5 else rng.randrange(4001)
+            tensors.append(flat[a:a + rng.choice([0, 1, 5, 60])])
+        if rng.random() < 0.5:
+            tensors.sort(key=lambda t: t.data_ptr())
+        spans = [(t.data_ptr() - base, t.data_ptr() - base + len(t)) for t in tensors]
+        want = any(max(a, c) < min(b, d) for a, b in spans for c, d in kept)
+        got = G._read(tensors, None, array("q", bytes(8 * len(tensors))), 1, 0, kept=table.buffer_info()[0]) & G._MEETS
+        assert bool(got) == want == G._meet(G._spans(tensors), [(base + a, base + b) for a, b in kept])
+        among = any(max(a, c) < min(b, d) for i, (a, b) in enumerate(spans) for c, d in spans[:i])
+        k = rng.randrange(len(tensors) + 1)
+        assert G._compare(tensors[:k] + [None], tensors[k:]) == (G._OVERLAP if among else 0)
+    for bad in (([1], []), (None, [])):
+        with pytest.raises(TypeError):
+            G._compare(*bad)
