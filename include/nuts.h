@@ -394,7 +394,8 @@ typedef struct {
  *   z = z + bias_v, then + the sum of the row's bias_values whose bias_ids are v, in their order;     z = -infinity where v is not allowed,
  * whatever was there (NaN, too).  The arrays repetition, frequency and presence are [n_rows], bias [n_classes] or rows of it, bias_ids and
  * bias_values [n_rows][n_bias]; each may be NULL, and `allowed` is that of nuts_logprobs.  All of it is binary32 and rounded once.
- * `out` may be `logits` itself, with the same stride: then 16 bytes in which nothing changes are neither read nor written. */
+ * `out` may be `logits` itself, with the same stride: then 16 bytes (from a row's beginning on) in which nothing changes are neither read nor written, but a
+ * row's last classes, where they are fewer than 16 bytes and there is a mask, are read and written as they were, NaNs as quiet ones. */
 int nuts_penalties(const nuts_penalties_desc* desc, const void* logits, const void* history, const int32_t* lengths,
                    const int32_t* prompts, const float* repetition, const float* frequency, const float* presence,
                    const float* bias, const void* bias_ids, const float* bias_values, const uint32_t* allowed, void* out);
