@@ -24,6 +24,10 @@ constexpr int kLong = 2048, kFull = 256;  // of wide slices: places of a history
 constexpr int kGroups = 1024, kGradGroups = 768;
 // Rows whose gradients are added up, at least: 1000 of 1000 binary32, joins included, 15.5 us with 2, 16.1 with 1 and with 4.
 constexpr int64_t kBiasRows = 2;
+// Rows that a workgroup adds up one behind the other, at most: sums of some thousands in binary32 lose three places (4 million rows on 768 workgroups: 7e-5 of a
+// sum, which becomes 2e-6 with 128).  There are more workgroups then, for as many whole rounds of them as it takes (200000 rows of 1000 bfloat16 545 us, 633 with 768
+// workgroups; binary32 717 and 709); and groups that are joined at a time, where there are more in two launches.
+constexpr int64_t kBiasRun = 128, kJoined = 1024;
 // Classes up to which 16 of them are joined by a workgroup, and not 64: 1000 classes 4.0 us and 5.7, 4000 3.5 and 3.7, 16384 5.7 and 4.1.
 constexpr int kNarrow = 4096;
 
@@ -577,18 +581,19 @@ __global__ __launch_bounds__(W::kThreads, 6) void penalties_grad_kernel(PenaltyA
     }
 }
 
-// Groups' sums as those of all rows: kColumns classes a workgroup, the groups divided between 1024 / kColumns rows of threads.
+// Groups' sums as those of all rows, or of each `each` groups: kColumns classes a workgroup, the groups divided between 1024 / kColumns rows of threads.
 template <int kColumns>
-__global__ __launch_bounds__(kJoinThreads) void join_bias_kernel(const float* part, float* grad_bias, long n_groups, int n_classes, long first_block)
+__global__ __launch_bounds__(kJoinThreads) void join_bias_kernel(const float* part, float* grad_bias, long n_groups, long each, int n_classes, long first_block)
 {
     constexpr int kParts = kJoinThreads / kColumns;
     __shared__ float shared[kParts][kColumns];
     const long v = (first_block + blockIdx.x) * kColumns + threadIdx.x % kColumns;
     const int own = threadIdx.x / kColumns;
+    const long begin = blockIdx.y * each, end = min(begin + each, n_groups);
     float sum = 0.f;
     if (v < n_classes) {
 #pragma unroll 4
-        for (long k = own; k < n_groups; k += kParts) sum += part[k * n_classes + v];
+        for (long k = begin + own; k < end; k += kParts) sum += part[k * n_classes + v];
     }
     shared[own][threadIdx.x % kColumns] = sum;
     __syncthreads();
@@ -596,7 +601,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_bias_kernel(const float* pa
         if (own < half) shared[own][threadIdx.x % kColumns] += shared[own + half][threadIdx.x % kColumns];
         __syncthreads();
     }
-    if (own == 0 && v < n_classes) grad_bias[v] = shared[0][threadIdx.x];
+    if (own == 0 && v < n_classes) grad_bias[(long)blockIdx.y * n_classes + v] = shared[0][threadIdx.x];
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
@@ -665,7 +670,24 @@ int64_t rows_of_group(const nuts_penalties_desc* d, int64_t groups, int64_t leas
 int64_t rows_each(const nuts_penalties_desc* d) { return shares(d) && d->n_bias == 0 ? rows_of_group(d, kGroups, 1) : 1; }
 int64_t grad_rows_each(const nuts_penalties_desc* d, bool bias)
 {
-    return bias ? rows_of_group(d, kGradGroups, kBiasRows) : shares(d) ? rows_of_group(d, kGradGroups, 1) : 1;
+    if (!bias) return shares(d) ? rows_of_group(d, kGradGroups, 1) : 1;
+    const int64_t rounds = ceil_div(rows_of_group(d, kGradGroups, kBiasRows), kBiasRun);
+    return std::min(rows_of_group(d, kGradGroups * rounds, kBiasRows), kBiasRun);
+}
+// Rows of the workspace: groups' sums, and where there are many those of each kJoined of them.
+int64_t grad_groups(const nuts_penalties_desc* d) { return ceil_div(d->n_rows, grad_rows_each(d, true)); }
+int64_t grad_joined(const nuts_penalties_desc* d) { return grad_groups(d) > kJoined ? ceil_div(grad_groups(d), kJoined) : 0; }
+int64_t grad_bytes(const nuts_penalties_desc* d) { return (grad_groups(d) + grad_joined(d)) * d->n_classes * (int64_t)sizeof(float); }
+
+// The sums of each `each` of n_groups rows of `part`, as rows of `to`.
+void join_groups(const float* part, float* to, int64_t n_groups, int64_t each, int n_classes)
+{
+    const bool narrow = n_classes <= kNarrow;  // (few classes: more workgroups for them)
+    const int64_t rows = std::max<int64_t>(1, ceil_div(n_groups, each));
+    const long most = std::max<long>(1, kMaxBlocks * 512 / kJoinThreads / rows);
+    for (long first = 0, blocks = (long)ceil_div(n_classes, narrow ? 16 : 64); first < blocks; first += most)
+        hipLaunchKernelGGL(narrow ? join_bias_kernel<16> : join_bias_kernel<64>, dim3((unsigned)std::min(blocks - first, most), (unsigned)rows), dim3(kJoinThreads), 0,
+                           api_stream(), part, to, (long)n_groups, (long)each, n_classes, first);
 }
 
 template <typename W>
@@ -724,7 +746,7 @@ int nuts_penalties_grad_workspace(const nuts_penalties_desc* d, int64_t* bytes)
 {
     if (int rc = check_penalties(d, "nuts_penalties_grad_workspace")) return rc;
     if (!bytes) return api_fail(NUTS_E_INVALID_ARG, "nuts_penalties_grad_workspace: bytes must not be NULL");
-    *bytes = ceil_div(d->n_rows, grad_rows_each(d, true)) * d->n_classes * (int64_t)sizeof(float);
+    *bytes = grad_bytes(d);
     return NUTS_OK;
 }
 
@@ -743,9 +765,9 @@ int nuts_penalties_grad(const nuts_penalties_desc* d, const void* grad_out, int6
         if (grad_logits == grad_out && grad_stride != d->out_stride && d->n_rows > 1)
             return api_fail(NUTS_E_INVALID_ARG, "nuts_penalties_grad: in place grad_stride and out_stride must be the same");
     }
-    const int64_t groups = ceil_div(d->n_rows, grad_rows_each(d, true));
+    const int64_t groups = grad_groups(d), joined = grad_joined(d);
     if (grad_bias && groups > 0) {
-        const int64_t bytes = groups * d->n_classes * (int64_t)sizeof(float);
+        const int64_t bytes = grad_bytes(d);
         if (!workspace || workspace_bytes < bytes) return api_fail(NUTS_E_INVALID_ARG, "nuts_penalties_grad: needs a workspace of %lld bytes", (long long)bytes);
         if (reinterpret_cast<uintptr_t>(workspace) % 256) return api_fail(NUTS_E_INVALID_ARG, "nuts_penalties_grad: workspace must be aligned to 256 bytes");
     }
@@ -767,12 +789,14 @@ int nuts_penalties_grad(const nuts_penalties_desc* d, const void* grad_out, int6
         launch<Usual>(shares(d) ? penalties_grad_kernel<Usual, T, true> : penalties_grad_kernel<Usual, T, false>, a);
     });
     if (grad_bias) {
-        // few classes: more workgroups for them
-        const bool narrow = d->n_classes <= kNarrow;
-        constexpr long kMost = kMaxBlocks * 512 / kJoinThreads;
-        for (long first = 0, blocks = (long)ceil_div(d->n_classes, narrow ? 16 : 64); first < blocks; first += kMost)
-            hipLaunchKernelGGL(narrow ? join_bias_kernel<16> : join_bias_kernel<64>, dim3((unsigned)std::min(blocks - first, kMost)), dim3(kJoinThreads), 0, api_stream(),
-                               static_cast<const float*>(workspace), grad_bias, (long)groups, (int)d->n_classes, first);
+        const float* part = static_cast<const float*>(workspace);
+        if (joined > 0) {
+            float* to = static_cast<float*>(workspace) + groups * d->n_classes;
+            join_groups(part, to, groups, kJoined, (int)d->n_classes);
+            part = to;
+        }
+        const int64_t left = joined > 0 ? joined : groups;
+        join_groups(part, grad_bias, left, std::max<int64_t>(1, left), (int)d->n_classes);
     }
     NUTS_CAT_TRY(hipGetLastError(), NUTS_E_DEVICE);
     return NUTS_OK;
