@@ -110,13 +110,19 @@ UBENCH_SRC = os.path.join(CSRC, "ubench", "issue_ubench.hip")
 UBENCH_LIB = os.path.join(HERE, "libnuts_ubench.so")
 
 
-# What reads PyTorch's tensors is host code, and the only code that knows PyTorch.
+# What reads PyTorch's tensors is host code, and the only code that knows PyTorch: it is built where PyTorch is.
 TENSORS_SRC = os.path.join(CSRC, "binding", "tensors.cpp")
 TENSORS_LIB = os.path.join(HERE, "libnuts_tensors.so")
 
 
+def torch_folder():
+    """Where PyTorch is installed, or None."""
+    spec = importlib.util.find_spec("torch")
+    return spec.submodule_search_locations[0] if spec else None
+
+
 def tensors_command():
-    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    torch = torch_folder()
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=1",
             "-isystem", os.path.join(torch, "include"), "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
             "-I" + sysconfig.get_paths()["include"], TENSORS_SRC, "-o", TENSORS_LIB, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
@@ -124,16 +130,18 @@ def tensors_command():
 
 def build(force: bool = True, verbose: bool = False) -> str:
     """The library, the instruction-issue microbenchmark as a library of its own, and the reader of PyTorch's tensors as one."""
-    others = ((UBENCH_LIB, UBENCH_SRC), (TENSORS_LIB, TENSORS_SRC))
+    others = [(UBENCH_LIB, UBENCH_SRC)] + ([(TENSORS_LIB, TENSORS_SRC)] if torch_folder() else [])
     if not force and not is_stale() and all(os.path.exists(made) and os.path.getmtime(made) >= os.path.getmtime(source) for made, source in others):
         return LIB_PATH
     with tempfile.TemporaryDirectory() as tmp:
         objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in sources()]
         cmds = [[HIPCC] + flags_of(s) + ["--save-temps=obj", "-c", s, "-o", o] for s, o in zip(sources(), objects)]
-        cmds += [[HIPCC] + FLAGS + [UBENCH_SRC, "-o", UBENCH_LIB], tensors_command()]
-        for cmd in cmds if verbose else []:
+        cmds.append([HIPCC] + FLAGS + [UBENCH_SRC, "-o", UBENCH_LIB])
+        reader = tensors_command() if torch_folder() else None
+        for cmd in cmds + [reader or []] if verbose else []:
             print(" ".join(cmd), file=sys.stderr)
         with ThreadPoolExecutor(max_workers=min(len(cmds), os.cpu_count() or 1)) as pool:  # one compiler per source
+            read = pool.submit(subprocess.run, reader, check=True) if reader else None
             list(pool.map(lambda cmd: subprocess.run(cmd, check=True), cmds))
         for o in objects:
             with open(re.sub(r"\.hip\.o$", "-hip-amdgcn-amd-amdhsa-gfx950.s", o)) as listing:
@@ -141,6 +149,8 @@ def build(force: bool = True, verbose: bool = False) -> str:
             if faults:
                 raise RuntimeError("\n".join(faults))
         subprocess.run([HIPCC] + FLAGS + objects + ["-o", LIB_PATH], check=True)
+        if read:
+            read.result()  # (what it lacks, a compiler or a header, the library does not)
     return LIB_PATH
 
 
