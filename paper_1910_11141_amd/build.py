@@ -121,9 +121,31 @@ def torch_folder():
     return spec.submodule_search_locations[0] if spec else None
 
 
+PYTHON = sys.implementation.cache_tag
+
+
+def torch_version():
+    """PyTorch's version (it is not imported for that), or None."""
+    if not torch_folder():
+        return None
+    with open(os.path.join(torch_folder(), "version.py")) as source:
+        return re.search(r"^__version__ = '([^']*)'", source.read(), re.M).group(1)
+
+
+def reader_mark():
+    """What the reader carries of what it was built for."""
+    return f"reader of the tensors of PyTorch {torch_version()} in {PYTHON}"
+
+
+def reader_fits():
+    """Whether the reader was built for the PyTorch and the Python that are here, without loading it."""
+    with open(TENSORS_LIB, "rb") as made:
+        return (reader_mark() + "\0").encode() in made.read()
+
+
 def tensors_command():
     torch = torch_folder()
-    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=1",
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=1", f'-DNUTS_READER_MARK="{reader_mark()}"',
             "-isystem", os.path.join(torch, "include"), "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
             "-I" + sysconfig.get_paths()["include"], TENSORS_SRC, "-o", TENSORS_LIB, "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
@@ -131,7 +153,8 @@ def tensors_command():
 def build(force: bool = True, verbose: bool = False) -> str:
     """The library, the instruction-issue microbenchmark as a library of its own, and the reader of PyTorch's tensors as one."""
     others = [(UBENCH_LIB, UBENCH_SRC)] + ([(TENSORS_LIB, TENSORS_SRC)] if torch_folder() else [])
-    if not force and not is_stale() and all(os.path.exists(made) and os.path.getmtime(made) >= os.path.getmtime(source) for made, source in others):
+    if not force and not is_stale() and all(os.path.exists(made) and os.path.getmtime(made) >= os.path.getmtime(source) for made, source in others) and \
+            (not torch_folder() or reader_fits()):
         return LIB_PATH
     with tempfile.TemporaryDirectory() as tmp:
         objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in sources()]

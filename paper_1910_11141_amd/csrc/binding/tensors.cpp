@@ -48,6 +48,9 @@ struct Kept {
 
 }  // namespace
 
+// Tensors are read as this PyTorch's headers lay them out: who loads this library looks for the mark first.
+extern "C" __attribute__((visibility("default"), used)) const char nuts_reader_mark[] = NUTS_READER_MARK;
+
 // For each item i of `list` (of a tensor, or None), of its address, count and type those into rows[i * width + column] whose column is not negative (0 and
 // nothing for None).  Returns bits: 1 tensors of several types, 2 on several devices, 4 with gaps, 8 of another shape than the item of `like` (a list, or
 // None) in the same place, 16 an address or a count is not what was in its place, 32 memory of what `kept` (see Kept, or NULL) says.  -1 with an exception: an

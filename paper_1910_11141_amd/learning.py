@@ -15,6 +15,7 @@ from collections import namedtuple
 import torch
 
 from . import binding as _b
+from . import build as _build
 from .categorical import _DTYPES, _enqueue
 
 __all__ = ("nuts_norm", "nuts_adamw", "nuts_adamw_values", "Moments", "Norm")
@@ -23,7 +24,7 @@ Norm = namedtuple("Norm", "norm factor")
 
 _PARAM_DTYPES = {torch.float32: _b.NUTS_F32, torch.bfloat16: _b.NUTS_BF16}
 _COPY_DTYPES = {torch.bfloat16: _b.NUTS_BF16, torch.float16: _b.NUTS_F16}
-TENSORS_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libnuts_tensors.so")
+TENSORS_PATH = _build.TENSORS_LIB
 _PARAM, _GRAD, _COPY, _M, _V, _M_SCALE, _V_SCALE, _N = range(8)  # columns of a table of nuts_adamw_tensor
 assert C.sizeof(_b.nuts_adamw_tensor) == 64 and C.sizeof(_b.nuts_tensor) == 24
 
@@ -39,6 +40,8 @@ def _read(tensors, like, table, width, address, count=-1, type_=-1, kept=0):
     if _tensors is None:
         if not os.path.exists(TENSORS_PATH):
             raise ImportError(f"{TENSORS_PATH} is missing: run `python -c 'import __graft_entry__ as g; g.build()'`")
+        if not _build.reader_fits():
+            raise ImportError(f"{TENSORS_PATH} was built for another PyTorch or Python: run `python -c 'import __graft_entry__ as g; g.build()'`")
         lib = C.PyDLL(TENSORS_PATH)
         lib.nuts_tensor_table.argtypes = [C.py_object, C.py_object, C.c_void_p] + [C.c_int64] * 4 + [C.c_void_p]
         lib.nuts_tensors_compare.argtypes = [C.py_object, C.py_object]
