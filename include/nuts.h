@@ -418,7 +418,8 @@ typedef struct {
 } nuts_tensor;
 
 /* norm = square root of the sum of all squares, summed in binary64; factor = min(1, max_norm / norm), which times all
- * numbers keeps their norm to max_norm (finite, > 0), and NaN where the norm is not finite.  Either may be NULL; one number each. */
+ * numbers keeps their norm to max_norm (finite, > 0), and NaN where the norm is not finite in binary64 (beyond binary32's range the norm is infinite and the
+ * factor is not).  Either may be NULL; one number each. */
 int nuts_norm_workspace(const nuts_tensor* tensors, int64_t n_tensors, int64_t* bytes);
 int nuts_norm(const nuts_tensor* tensors, int64_t n_tensors, double max_norm, float* norm, float* factor, void* workspace,
               int64_t workspace_bytes);

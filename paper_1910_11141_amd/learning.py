@@ -90,7 +90,8 @@ def _scalar(t, what, dtype, device):
 
 def nuts_norm(tensors, *, max_norm=1.0):
     """(norm, factor), float32 scalars on the device: the square root of the sum of all squares of `tensors`, and what all of them are to
-    be multiplied with so that it is no more than max_norm (NaN where the norm is not finite).  None among them counts as nothing."""
+    be multiplied with so that it is no more than max_norm (NaN where the norm is not finite in 64 bits, in which it is summed; one that 32 bits do not hold
+    is infinite, and its factor is right).  None among them counts as nothing."""
     tensors = list(tensors)
     first = next((t for t in tensors if t is not None), None)
     if first is None:
