@@ -129,7 +129,7 @@ def torch_version():
     if not torch_folder():
         return None
     with open(os.path.join(torch_folder(), "version.py")) as source:
-        return re.search(r"^__version__ = '([^']*)'", source.read(), re.M).group(1)
+        return re.search(r"""^__version__ *= *['"]([^'"]*)""", source.read(), re.M).group(1)
 
 
 def reader_mark():

@@ -29,3 +29,15 @@ def test_rows_that_workgroups_just_hold(n, dtype):
     for kw in ({}, dict(history=history), dict(history=history[0])):
         again = [nuts.nuts_penalties_grad(grad, grad, want_bias=True, repetition=2.0, **kw)[1] for _ in range(2)]
         assert torch.equal(again[0].double(), want) and torch.equal(*again)
+
+
+@pytest.mark.parametrize("n,classes", [(150_000, 4100), (131_073, 4096), (130_000, 12300)])
+def test_many_groups_of_more_classes_than_a_slice(n, classes):
+    """As above, joined in two launches of which each has several workgroups beside each other, by 16 and by 64 classes."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    grad = torch.randint(-8, 9, (n, classes), generator=g, device="cuda", dtype=torch.int8).to(torch.bfloat16)
+    want = torch.zeros(classes, dtype=torch.float64, device="cuda")
+    for part in grad.split(10_000):
+        want += part.double().sum(0)
+    bias = nuts.nuts_penalties_grad(grad, grad, want_logits=False, want_bias=True)[1]
+    assert torch.equal(bias.double(), want)
